@@ -407,6 +407,139 @@ int fq_sched_step(void *state, const float *entropy, void *stream);
 int fq_sched_peek(const void *state, int *next_event, int *tokens, double *thre,
                   double *last_mean, void *stream);
 
+/*
+ * ---- Between the linears of a decoder, and after its output layer --------------------------------------------
+ *
+ * Eq. (1) of Sec. 2.1 over a cache that is not quantized (Sec. 5.2 measures the step with it): rotary positions and
+ * the append of keys and values, attention over the cache, and the draw of the next token from the logits.  (The
+ * paper takes the argmax and names no cache layout: the interfaces are this library's.)
+ */
+#define FQ_F16 0  /* 16-bit types of queries, keys, values and outputs */
+#define FQ_BF16 1
+
+#define FQ_ROPE_PLAIN 0      /* f_i = base^(-2 i / rot_dim), i = 0 .. rot_dim / 2 - 1 */
+#define FQ_ROPE_LINEAR 1     /* f_i / factor */
+#define FQ_ROPE_BASE 2       /* base * factor^(rot_dim / (rot_dim - 2)) in base's place (rot_dim >= 4) */
+#define FQ_ROPE_WAVELENGTH 3 /* f_i (a + (1 - a) / factor), a = (turns_i - low) / (high - low) held in 0 .. 1,
+                                turns_i = original * f_i / 2 pi: what turns more than `high` times over the original
+                                length stays, what turns less than `low` times is divided, a blend in between */
+#define FQ_ROPE_RAMP 4       /* the same with a falling linearly in i from the pair that turns `high` times (rounded down,
+                                at least 0) to the one that turns `low` times (rounded up, at most rot_dim - 1): pair(t) =
+                                rot_dim ln(original / (2 pi t)) / (2 ln base) */
+
+/*
+ * Rotary frequencies in radians per position, written to HOST memory (the caller copies them to the device once).
+ *   freqs  host, f64 [rot_dim / 2]
+ * rot_dim even and >= 2, base > 1; factor >= 1 for every kind but PLAIN; 0 < low < high and original > 0 for WAVELENGTH
+ * and RAMP (arguments that a kind does not name are not looked at).  Launches nothing.
+ */
+int fq_rope_freqs(int rot_dim, double base, int kind, double factor, double low, double high, double original,
+                  double *freqs);
+
+/*
+ * A paged cache of keys and values of one decoder layer: `n_pages` pages of `page_tokens` tokens (a power of two, at most
+ * 65536) for `kv_heads` heads of `head_dim` (a multiple of 8, at most FQ_MAX_HEAD_DIM) 16-bit values.  Element (page, head,
+ * token, d) of either tensor is at page * page_stride + head * head_stride + token * token_stride + d (strides in elements,
+ * multiples of 8, not negative), so pages may be laid out head by head or token by token.  The handle borrows
+ * the two tensors (16-byte aligned); creating and destroying it launches nothing.
+ */
+#define FQ_MAX_HEAD_DIM 256
+typedef struct fq_kv fq_kv;
+int fq_kv_create(fq_kv **out, int dtype, int kv_heads, int head_dim, int page_tokens, int n_pages, void *k, void *v,
+                 long long page_stride, long long head_stride, long long token_stride);
+int fq_kv_destroy(fq_kv *kv);
+
+/*
+ * The sequences of a batch, as tables in DEVICE memory that the kernels read at run time (a captured graph follows what a
+ * later token writes there).  With T the rows of a call's q:
+ *   q_start       int32 [seqs + 1]: sequence b owns the new tokens (rows) q_start[b] .. q_start[b + 1] - 1; never
+ *                 decreasing, from 0 (values outside 0 .. T are held inside; rows that no sequence owns are left alone)
+ *   kv_len        int32 [seqs]: tokens of the sequence in the cache, the new ones included; held inside 0 .. table_width *
+ *                 page_tokens.  With n = q_start[b + 1] - q_start[b], new token j has place kv_len[b] - n + j
+ *   table         int32 [seqs][table_width]: place t of the sequence lies in page table[b][t / page_tokens], token
+ *                 t % page_tokens of it.  A page number outside 0 .. n_pages - 1 is a hole: nothing is written there, and
+ *                 attention passes over its keys
+ *   prefix_table  int32 [ceil(prefix_len / page_tokens)]: pages of `prefix_len` tokens that stand before the places of
+ *                 every sequence of the batch; NULL with prefix_len = 0
+ * 1 <= seqs <= FQ_MAX_SEQS, table_width >= 1; (table_width + 1) * page_tokens + prefix_len < 2^31 for the cache it is used with.  The handle
+ * borrows the tables and launches nothing.
+ */
+#define FQ_MAX_SEQS 65535
+typedef struct fq_seqs fq_seqs;
+int fq_seqs_create(fq_seqs **out, int seqs, const int32_t *q_start, const int32_t *kv_len, const int32_t *table,
+                   int table_width, const int32_t *prefix_table, int prefix_len);
+int fq_seqs_destroy(fq_seqs *seqs);
+
+/*
+ * Turns the first rot_dim values of every head of q and k by the token's position, writes q to q_out, k and v to the
+ * token's place in the cache.  Pair i of a head -- elements i and i + rot_dim / 2, or 2 i and 2 i + 1 where `interleaved` --
+ * becomes (a c - b s, b c + a s), c, s = amplitude * cos, sin(position * freqs[i]): the angle in binary64, the product in
+ * binary32, one rounding to the tensors' type.  The rest of a head is copied.
+ *   q, k, v    device, [tokens][heads][head_dim], rows q_stride, k_stride, v_stride elements apart (q, k and v may be parts
+ *              of one row), 16-byte aligned, strides multiples of 8                              (read)
+ *   q_out      device, rows q_out_stride elements apart; may not overlap q                       (written)
+ *   freqs      device, f64 [rot_dim / 2]; NULL with rot_dim = 0: nothing is turned
+ *   positions  device, int32 [tokens], or NULL: prefix_len + the place in the sequence
+ * q and q_out may be NULL with q_heads = 0 (keys and values only).  0 <= rot_dim <= head_dim, even.  tokens >= 0 (0 launches
+ * nothing).  One launch.  Two tokens of a call may not share a place.
+ */
+int fq_kv_append(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q, long long q_stride, int q_heads,
+                 void *q_out, long long q_out_stride, const void *k, long long k_stride, const void *v,
+                 long long v_stride, const double *freqs, int rot_dim, int interleaved, float amplitude,
+                 const int32_t *positions, void *stream);
+
+/*
+ * Attention of the new tokens over prefix and cache (Sec. 2.1 Eq. (1)): with the keys that new token j of sequence b sees --
+ * the prefix and the places 0 .. kv_len[b] - n + j, holes left out --
+ *   out[t][h] = sum_i p_i v_i,  p = softmax(scale * q[t][h] . k_i),  lse[t][h] = ln sum_i exp(scale * q[t][h] . k_i)
+ * query head h reading key head h / (q_heads / kv_heads).  Scores, statistics and sums in binary32, p rounded to the tensors'
+ * type where it meets v.  A row that sees no key gives 0 and lse = -inf.  What lies in the cache beyond kv_len, in holes and in other pages is not looked
+ * at, whatever it holds.
+ *   q, out     device, [tokens][q_heads][head_dim], rows q_stride, out_stride elements apart, 16-byte aligned, strides
+ *              multiples of 8                                                                    (read / written)
+ *   lse        device, f32 [tokens][q_heads], or NULL                                            (written)
+ *   max_q      no sequence has more new tokens than this (rows beyond are left alone), 1 <= max_q <= tokens
+ *   max_kv     no kv_len is larger than this (keys beyond are not seen; table_width * page_tokens always does); >= 1.  The launch is
+ *              shaped by the two: close bounds are faster
+ *   workspace  device, fq_attend_workspace_bytes(...) bytes, 256-byte aligned; calls that may overlap in time need one each
+ * q_heads a multiple of kv_heads, at most FQ_MAX_Q_HEADS; scale finite.  tokens >= 0 (0 launches nothing).  Never waits for the
+ * stream: may be captured into a graph.  Equal calls give equal bits.
+ */
+#define FQ_MAX_Q_HEADS 4096
+size_t fq_attend_workspace_bytes(const fq_kv *kv, const fq_seqs *seqs, int tokens, int q_heads, int max_q, int max_kv);
+int fq_attend(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q, long long q_stride, int q_heads, float scale,
+              void *out, long long out_stride, float *lse, int max_q, int max_kv, void *workspace, size_t workspace_bytes,
+              void *stream);
+
+/*
+ * Draws a token from each of R rows of logits with given numbers u.  Row r, with w_i = exp((l_i - max l) / temperature):
+ *   1. temperature <= 0 (or NaN): the token is the largest logit's, the smallest index on ties; prob = 1
+ *   2. top_k > 0: the top_k largest logits are kept, the smaller index first on ties
+ *   3. top_p < 1: of these, in the same order, the fewest whose w add up to at least top_p times the sum of them all (one at least)
+ *   4. min_p > 0: of these, those with w_i >= min(min_p, 1)
+ *   5. token = the first kept i, by index, at which the running sum of the kept w exceeds u times their whole sum
+ *      (u >= 1: the last with any weight);  prob = w_token / that sum
+ * A NaN logit counts as -inf; -inf is never drawn, and a row of nothing else gives token -1 and prob 0.  With +inf in a row only
+ * the +inf entries have weight, 1 each.  w is computed in binary64 and held as a whole number of 2^-(62 - ceil(log2 V)): sums
+ * are exact, equal calls give equal bits, and a weight under half of that unit counts as nothing.
+ *   logits       device, f32 (or fp16: fq_sample_f16) [R][V], rows row_stride elements apart (row_stride >= V; any alignment that
+ *                the type has)                                                                   (read)
+ *   u            device, f32 [R], in [0, 1)
+ *   temperature, top_k, top_p, min_p   device, f32 / int32 / f32 / f32 [R], or NULL: 1, 0, 1, 0
+ *   token        device, int32 [R]                                                               (written)
+ *   prob         device, f32 [R], or NULL                                                        (written)
+ *   workspace    device, fq_sample_workspace_bytes(R, V) bytes, 256-byte aligned; calls that may overlap need one each
+ * R >= 0 (R = 0 launches nothing), 1 <= V <= FQ_MAX_SAMPLE_V.  Never waits for the stream.
+ */
+#define FQ_MAX_SAMPLE_V (1 << 24)
+size_t fq_sample_workspace_bytes(int R, int V);
+int fq_sample(const float *logits, int R, int V, long long row_stride, const float *u, const float *temperature,
+              const int32_t *top_k, const float *top_p, const float *min_p, int32_t *token, float *prob, void *workspace,
+              size_t workspace_bytes, void *stream);
+int fq_sample_f16(const void *logits, int R, int V, long long row_stride, const float *u, const float *temperature,
+                  const int32_t *top_k, const float *top_p, const float *min_p, int32_t *token, float *prob, void *workspace,
+                  size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,6 +11,10 @@ _EXPORTS = (
     "fq_quantize_sym", "fq_fake_quantize", "fq_lm_head_entropy", "FQ_MAX_LM_HEAD_M",
     "fq_linears_static", "fq_stream_read", "FQ_STATIC_MAX_ENTRIES", "FQ_SCRATCH_BANKS",
     "fq_rank_ascending", "fq_sched_init", "fq_sched_peek",
+    "FQ_F16", "FQ_BF16", "FQ_ROPE_PLAIN", "FQ_ROPE_LINEAR", "FQ_ROPE_BASE", "FQ_ROPE_WAVELENGTH", "FQ_ROPE_RAMP",
+    "FQ_MAX_HEAD_DIM", "FQ_MAX_Q_HEADS", "FQ_MAX_SEQS", "FQ_MAX_SAMPLE_V",
+    "KVCache", "Sequences", "fq_rope_freqs", "fq_kv_append", "fq_attend", "fq_attend_workspace_bytes",
+    "fq_sample", "fq_sample_f16", "fq_sample_workspace_bytes",
     "fq_sched_state_bytes", "fq_sched_step", "fq_sched_threshold_from_prefill", "lib", "lib_path",
 )
 

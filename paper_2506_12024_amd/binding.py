@@ -17,6 +17,12 @@ FQ_MAX_DECODE_M = 32
 FQ_MAX_LM_HEAD_M = 4
 FQ_STATIC_MAX_ENTRIES = 512
 FQ_SCRATCH_BANKS = 16
+FQ_F16, FQ_BF16 = 0, 1
+FQ_ROPE_PLAIN, FQ_ROPE_LINEAR, FQ_ROPE_BASE, FQ_ROPE_WAVELENGTH, FQ_ROPE_RAMP = 0, 1, 2, 3, 4
+FQ_MAX_HEAD_DIM = 256
+FQ_MAX_Q_HEADS = 4096
+FQ_MAX_SEQS = 65535
+FQ_MAX_SAMPLE_V = 1 << 24
 FQ_OK, FQ_ERR_NULL, FQ_ERR_BITS, FQ_ERR_SHAPE, FQ_ERR_NOT_ATTACHED, FQ_ERR_ALIGN, FQ_ERR_HIP = \
     0, -1, -2, -3, -4, -5, -6
 
@@ -29,6 +35,8 @@ EXPORTS = [
     "fq_quantize_sym", "fq_fake_quantize", "fq_lm_head_entropy", "fq_linears_static",
     "fq_plan_staged_workspace_bytes", "fq_plan_create_staged", "fq_plan_set_wait_limit", "fq_plan_status",
     "fq_stream_read",
+    "fq_rope_freqs", "fq_kv_create", "fq_kv_destroy", "fq_seqs_create", "fq_seqs_destroy", "fq_kv_append",
+    "fq_attend_workspace_bytes", "fq_attend", "fq_sample_workspace_bytes", "fq_sample", "fq_sample_f16",
 ]
 
 
@@ -118,6 +126,28 @@ def _load() -> ctypes.CDLL:
     L.fq_sched_peek.restype = ci
     L.fq_sched_peek.argtypes = [vp, ctypes.POINTER(ci), ctypes.POINTER(ci), ctypes.POINTER(ctypes.c_double),
                                 ctypes.POINTER(ctypes.c_double), vp]
+    ll, cd, cf = ctypes.c_longlong, ctypes.c_double, ctypes.c_float
+    L.fq_rope_freqs.restype = ci
+    L.fq_rope_freqs.argtypes = [ci, cd, ci, cd, cd, cd, cd, ctypes.POINTER(cd)]
+    L.fq_kv_create.restype = ci
+    L.fq_kv_create.argtypes = [ctypes.POINTER(vp), ci, ci, ci, ci, ci, vp, vp, ll, ll, ll]
+    L.fq_kv_destroy.restype = ci
+    L.fq_kv_destroy.argtypes = [vp]
+    L.fq_seqs_create.restype = ci
+    L.fq_seqs_create.argtypes = [ctypes.POINTER(vp), ci, vp, vp, vp, ci, vp, ci]
+    L.fq_seqs_destroy.restype = ci
+    L.fq_seqs_destroy.argtypes = [vp]
+    L.fq_kv_append.restype = ci
+    L.fq_kv_append.argtypes = [vp, vp, ci, vp, ll, ci, vp, ll, vp, ll, vp, ll, vp, ci, ci, cf, vp, vp]
+    L.fq_attend_workspace_bytes.restype = sz
+    L.fq_attend_workspace_bytes.argtypes = [vp, vp, ci, ci, ci, ci]
+    L.fq_attend.restype = ci
+    L.fq_attend.argtypes = [vp, vp, ci, vp, ll, ci, cf, vp, ll, vp, ci, ci, vp, sz, vp]
+    L.fq_sample_workspace_bytes.restype = sz
+    L.fq_sample_workspace_bytes.argtypes = [ci, ci]
+    for name in ("fq_sample", "fq_sample_f16"):
+        getattr(L, name).restype = ci
+        getattr(L, name).argtypes = [vp, ci, ci, ll, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     return L
 
 
@@ -343,3 +373,184 @@ def fq_sched_peek(state, stream=None):
     _check(lib.fq_sched_peek(_ptr(state), ctypes.byref(ne), ctypes.byref(tk), ctypes.byref(th),
                              ctypes.byref(lm), _stream(stream)))
     return ne.value, tk.value, th.value, lm.value
+
+
+def fq_rope_freqs(rot_dim: int, base: float, kind: int = FQ_ROPE_PLAIN, factor: float = 1.0, low: float = 0.0,
+                  high: float = 0.0, original: float = 0.0):
+    """The frequencies as a list of ``rot_dim // 2`` floats; a float64 tensor of them on the device is what
+    ``fq_kv_append`` takes."""
+    out = (ctypes.c_double * max(rot_dim // 2, 1))()
+    _check(lib.fq_rope_freqs(rot_dim, base, kind, factor, low, high, original, out))
+    return list(out)
+
+
+def _typed(t, dtype, name):
+    """Device pointer of a contiguous tensor whose element type the call will assume, an int, or None."""
+    if t is not None and not isinstance(t, int) and t.dtype is not dtype:
+        raise ValueError("%s must be %s (got %s)" % (name, dtype, t.dtype))
+    return _ptr(t)
+
+
+def _rows(t, name, dtype, heads, dim):
+    """(pointer, row stride) of a [tokens][heads][dim] tensor: a row is one piece, rows may lie apart."""
+    if t.dtype is not dtype or t.dim() != 3 or (heads and t.shape[1] != heads) or t.shape[2] != dim:
+        raise ValueError("%s must be [tokens][%s][%d] of %s (got %s of %s)" % (name, heads or "heads", dim, dtype, tuple(t.shape),
+                                                                              t.dtype))
+    stride = t.stride()
+    if stride[2] != 1 or (t.shape[1] > 1 and stride[1] != dim):
+        raise ValueError("the heads of a row of %s must lie side by side" % name)
+    return t.data_ptr(), stride[0] if t.shape[0] > 1 else max(stride[0], t.shape[1] * dim)
+
+
+class KVCache:
+    """Owns an ``fq_kv`` handle and keeps the tensors alive: ``k`` and ``v`` are [page][head][token][dim] views of
+    equal strides over fp16 or bf16 storage, values of a head side by side (a pool laid out token by token is
+    ``pool.permute(0, 2, 1, 3)``)."""
+
+    def __init__(self, k, v):
+        import torch
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
+            raise ValueError("k and v must be [page][head][token][dim] of one shape, layout and type")
+        if k.dtype not in (torch.float16, torch.bfloat16):
+            raise ValueError("k and v must be float16 or bfloat16 (got %s)" % k.dtype)
+        if k.stride(3) != 1:
+            raise ValueError("the values of a head must lie side by side")
+        self.handle = None
+        self._keep = (k, v)
+        self.dtype = k.dtype
+        self.n_pages, self.kv_heads, self.page_tokens, self.head_dim = k.shape
+        h = ctypes.c_void_p()
+        _check(lib.fq_kv_create(ctypes.byref(h), FQ_F16 if k.dtype == torch.float16 else FQ_BF16, self.kv_heads, self.head_dim,
+                                self.page_tokens, self.n_pages, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
+                                k.stride(2)))
+        self.handle = h
+
+    def destroy(self):
+        if self.handle is not None:
+            _check(lib.fq_kv_destroy(self.handle))
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+class Sequences:
+    """Owns an ``fq_seqs`` handle and keeps its int32 device tables alive: ``q_start`` [seqs + 1], ``kv_len`` [seqs],
+    ``table`` [seqs][pages], ``prefix_table`` [pages of the shared prefix] or None."""
+
+    def __init__(self, q_start, kv_len, table, prefix_table=None, prefix_len: int = 0):
+        import torch
+        self.handle = None
+        if table.dim() != 2 or q_start.numel() != table.shape[0] + 1 or kv_len.numel() != table.shape[0]:
+            raise ValueError("need q_start [seqs + 1], kv_len [seqs] and table [seqs][pages]")
+        self._keep = (q_start, kv_len, table, prefix_table)
+        self.prefix_len = prefix_len
+        h = ctypes.c_void_p()
+        _check(lib.fq_seqs_create(ctypes.byref(h), table.shape[0], _typed(q_start, torch.int32, "q_start"),
+                                  _typed(kv_len, torch.int32, "kv_len"), _typed(table, torch.int32, "table"), table.shape[1],
+                                  _typed(prefix_table, torch.int32, "prefix_table"), prefix_len))
+        self.handle = h
+
+    def covers(self, cache) -> None:
+        """The prefix's table must hold every page of the prefix."""
+        t = self._keep[3]
+        if t is not None and t.numel() * cache.page_tokens < self.prefix_len:
+            raise ValueError("prefix_table has %d pages of %d tokens, the prefix %d tokens" % (
+                t.numel(), cache.page_tokens, self.prefix_len))
+
+    def destroy(self):
+        if self.handle is not None:
+            _check(lib.fq_seqs_destroy(self.handle))
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def fq_kv_append(cache: KVCache, seqs: Sequences, q, k, v, q_out, freqs, interleaved: bool = False, amplitude: float = 1.0,
+                 positions=None, stream=None):
+    """q, k, v, q_out: [tokens][heads][dim] (rows may lie apart); q and q_out may be None.  ``freqs``: float64 on the device,
+    one for each rotating pair, or None: nothing is turned."""
+    import torch
+    kp, ks = _rows(k, "k", cache.dtype, cache.kv_heads, cache.head_dim)
+    vp, vs = _rows(v, "v", cache.dtype, cache.kv_heads, cache.head_dim)
+    T = k.shape[0]
+    qp = qs = op = os_ = None
+    heads = 0
+    if q is not None:
+        heads = q.shape[1]
+        qp, qs = _rows(q, "q", cache.dtype, 0, cache.head_dim)
+        op, os_ = _rows(q_out, "q_out", cache.dtype, heads, cache.head_dim)
+    if v.shape[0] != T or (q is not None and (q.shape[0] != T or q_out.shape[0] != T)) or (
+            positions is not None and positions.numel() != T):
+        raise ValueError("q, k, v, q_out and positions must have as many rows")
+    _check(lib.fq_kv_append(cache.handle, seqs.handle, T, qp, qs or 0, heads, op, os_ or 0, kp, ks, vp, vs,
+                            _typed(freqs, torch.float64, "freqs"), 0 if freqs is None else 2 * freqs.numel(),
+                            1 if interleaved else 0, amplitude, _typed(positions, torch.int32, "positions"),
+                            _stream(stream)))
+
+
+def fq_attend_workspace_bytes(cache: KVCache, seqs: Sequences, tokens: int, q_heads: int, max_q: int, max_kv: int) -> int:
+    n = int(lib.fq_attend_workspace_bytes(cache.handle, seqs.handle, tokens, q_heads, max_q, max_kv))
+    if n == 0:
+        raise FlexqError(FQ_ERR_SHAPE, fq_last_error())
+    return n
+
+
+def _bytes(workspace) -> int:
+    return workspace.numel() * workspace.element_size()
+
+
+def fq_attend(cache: KVCache, seqs: Sequences, q, out, scale: float, max_q: int, max_kv: int, workspace, lse=None, stream=None):
+    """q, out: [tokens][q_heads][dim] (rows may lie apart); lse: float32 [tokens][q_heads] or None."""
+    import torch
+    seqs.covers(cache)
+    T, heads = q.shape[0], q.shape[1]
+    qp, qs = _rows(q, "q", cache.dtype, 0, cache.head_dim)
+    op, os_ = _rows(out, "out", cache.dtype, heads, cache.head_dim)
+    if out.shape[0] != T or (lse is not None and lse.numel() != T * heads):
+        raise ValueError("q, out and lse must have as many rows")
+    _check(lib.fq_attend(cache.handle, seqs.handle, T, qp, qs, heads, scale, op, os_, _typed(lse, torch.float32, "lse"), max_q,
+                         max_kv, _ptr(workspace), _bytes(workspace), _stream(stream)))
+
+
+def fq_sample_workspace_bytes(R: int, V: int) -> int:
+    n = int(lib.fq_sample_workspace_bytes(R, V))
+    if n == 0:
+        raise FlexqError(FQ_ERR_SHAPE, fq_last_error())
+    return n
+
+
+def _sample(call, dtype, logits, R, V, u, token, workspace, temperature, top_k, top_p, min_p, prob, stream):
+    import torch
+    if logits.dtype is not dtype or logits.dim() != 2 or logits.shape[0] < R or logits.shape[1] != V or logits.stride(1) != 1:
+        raise ValueError("logits must be %s [R][V], the logits of a row side by side" % dtype)
+    f32 = torch.float32
+    for name, t in (("u", u), ("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p),
+                    ("token", token), ("prob", prob)):
+        if t is not None and t.numel() < R:
+            raise ValueError("%s has fewer than %d entries" % (name, R))
+    _check(call(logits.data_ptr(), R, V, logits.stride(0) if R > 1 else V, _typed(u, f32, "u"), _typed(temperature, f32, "temperature"),
+                _typed(top_k, torch.int32, "top_k"), _typed(top_p, f32, "top_p"), _typed(min_p, f32, "min_p"),
+                _typed(token, torch.int32, "token"), _typed(prob, f32, "prob"), _ptr(workspace), _bytes(workspace),
+                _stream(stream)))
+
+
+def fq_sample(logits, R: int, V: int, u, token, workspace, temperature=None, top_k=None, top_p=None, min_p=None, prob=None,
+              stream=None):
+    """logits: float32 [R][V], rows may lie apart."""
+    import torch
+    _sample(lib.fq_sample, torch.float32, logits, R, V, u, token, workspace, temperature, top_k, top_p, min_p, prob, stream)
+
+
+def fq_sample_f16(logits, R: int, V: int, u, token, workspace, temperature=None, top_k=None, top_p=None, min_p=None, prob=None,
+                  stream=None):
+    """logits: float16 [R][V], rows may lie apart."""
+    import torch
+    _sample(lib.fq_sample_f16, torch.float16, logits, R, V, u, token, workspace, temperature, top_k, top_p, min_p, prob, stream)

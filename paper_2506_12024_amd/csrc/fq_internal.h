@@ -209,4 +209,53 @@ hipError_t fq_launch_w8a8_prompt(const FqLinearDesc &d, const void *xq, const fl
 hipError_t fq_launch_lm_head_entropy(const void *x, const void *w, int M, int V, int K, float *logits, float *H,
                                      int32_t *argmax, hipStream_t stream);
 
+// A paged cache and the tables of a batch, as the kernels of fq_append.hip and fq_attend.hip take them (strides in
+// elements of 16 bits).
+struct FqKvView {
+    uint16_t *k, *v;
+    long long page_stride, head_stride, token_stride;
+    int n_pages, page_shift, kv_heads, dim, bf16;
+};
+struct FqSeqsView {
+    const int32_t *q_start, *kv_len, *table, *prefix_table;
+    int seqs, table_width, prefix_len, tokens;
+};
+struct FqAppendArgs {
+    FqKvView kv;
+    FqSeqsView seqs;
+    const uint16_t *q, *k, *v;
+    uint16_t *q_out;
+    long long q_stride, q_out_stride, k_stride, v_stride;
+    const double *freqs;
+    const int32_t *positions;
+    int q_heads, rot;
+    float amplitude;
+};
+hipError_t fq_launch_append(const FqAppendArgs &a, bool interleaved, hipStream_t stream);
+
+struct FqAttendArgs {
+    FqKvView kv;
+    FqSeqsView seqs;
+    const uint16_t *q;
+    uint16_t *out;
+    float *lse; // or null
+    long long q_stride, out_stride;
+    int q_heads, max_q, max_kv;
+    float scale;
+};
+size_t fq_attend_bytes(const FqAttendArgs &a, int cus);
+hipError_t fq_launch_attend(const FqAttendArgs &a, void *workspace, hipStream_t stream);
+
+struct FqSampleArgs {
+    const void *logits;
+    const float *u, *temperature, *top_p, *min_p;
+    const int32_t *top_k;
+    int32_t *token;
+    float *prob;
+    long long row_stride;
+    int R, V;
+};
+size_t fq_sample_bytes(int R, int V);
+hipError_t fq_launch_sample(const FqSampleArgs &a, bool half, void *workspace, hipStream_t stream);
+
 #endif

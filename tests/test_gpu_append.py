@@ -1,0 +1,149 @@
+"""fq_kv_append against a 64-bit reference: both layouts, parts of a head, strides, positions, bad pages, capture."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2506_12024_amd as fq
+from serve_util import EPS, TYPES, Batch, pool, turn
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def run(batch, q_heads, kv_heads, dim, rot, interleaved, dtype, token_major=False, fused=False, positions=None, amplitude=1.0,
+        freqs=None, with_q=True):
+    gen = torch.Generator().manual_seed(7)
+    T = batch.tokens
+    kc, vc = (pool(gen, batch.pages, kv_heads, batch.page, dim, dtype, token_major) for _ in range(2))
+    k0, v0 = f64(kc), f64(vc)
+    row = torch.randn((T, q_heads + 2 * kv_heads, dim), generator=gen).to(dtype).to(DEV)
+    q, k, v = row[:, :q_heads], row[:, q_heads:q_heads + kv_heads], row[:, q_heads + kv_heads:]
+    if not fused:
+        q, k, v = q.contiguous(), k.contiguous(), v.contiguous()
+    q_out = torch.full((T, q_heads, dim), 9.0, dtype=dtype, device=DEV)
+    if freqs is None:
+        freqs = fq.fq_rope_freqs(rot, 10000.0) if rot else []
+    pos = np.array([p + batch.prefix for _, p in batch.places()]) if positions is None else positions
+    fq.fq_kv_append(fq.KVCache(kc, vc), batch.sequences(), q if with_q else None, k, v, q_out if with_q else None,
+                    torch.tensor(freqs, dtype=torch.float64, device=DEV) if rot else None, interleaved, amplitude,
+                    None if positions is None else torch.from_numpy(positions).int().to(DEV))
+    torch.cuda.synchronize()
+    if rot:
+        want_q, size_q = turn(f64(q), pos, freqs, rot, interleaved, amplitude)
+        want_k, size_k = turn(f64(k), pos, freqs, rot, interleaved, amplitude)
+    else:
+        want_q, want_k, size_q, size_k = f64(q), f64(k), 0.0 * f64(q), 0.0 * f64(k)
+    want_kc, size_kc, want_vc = k0, np.zeros_like(k0), v0
+    for t, (b, p) in enumerate(batch.places()):
+        page = batch.table[b, p // batch.page] if p >= 0 else -1
+        if 0 <= page < batch.pages:
+            want_kc[page, :, p % batch.page] = want_k[t]
+            size_kc[page, :, p % batch.page] = size_k[t]
+            want_vc[page, :, p % batch.page] = f64(v)[t]
+
+    def close(got, want, size):
+        # one rounding to the type; sine and cosine of a binary32 fraction of a turn (2^-25 of it, 2 pi / turn) and a few
+        # binary32 roundings: under 2^-20 of what went in
+        err = np.abs(f64(got) - want)
+        assert np.all(err <= np.where(size > 0, EPS[dtype] / 2 * np.abs(want) + 2.0 ** -20 * size + 2.0 ** -25, 0.0))
+    if with_q:
+        close(q_out, want_q, size_q)
+    close(kc, want_kc, size_kc)
+    assert np.array_equal(f64(vc), want_vc)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,rot", [(128, 128), (64, 64), (64, 32), (80, 20), (8, 2), (96, 0), (256, 256), (40, 38)])
+def test_layouts_and_parts_of_a_head(dtype, interleaved, dim, rot):
+    run(Batch([3, 1, 5], [20, 1, 5], 4), 4, 2, dim, rot, interleaved, TYPES[dtype], fused=True, token_major=dim == 80)
+
+
+@pytest.mark.parametrize("heads", [(1, 1), (32, 32), (64, 8), (7, 1), (40, 40)])
+@pytest.mark.parametrize("new,kv,page", [([1], [1], 16), ([1], [1000], 16), ([2048], [2048], 64), ([1] * 70, list(range(1, 71)), 8),
+                                         ([0, 3, 0, 0, 2, 0], [5, 3, 0, 7, 9, 0], 1), ([33], [40], 65536)])
+def test_batches(heads, new, kv, page):
+    if page == 65536 and heads[1] > 8:
+        pytest.skip("large pages once are enough")
+    run(Batch(new, kv, page, spare=1), heads[0], heads[1], 64 if page == 65536 else 128, 64, False, torch.float16)
+
+
+def test_positions_of_their_own_and_far_ones():
+    batch = Batch([4, 4], [9, 4], 8)
+    run(batch, 4, 4, 128, 128, False, torch.float16, positions=np.array([0, 1, 131071, 1000003, -5, 2 ** 31 - 1, 77, 2 ** 30]))
+    run(batch, 4, 4, 128, 128, True, torch.bfloat16, positions=np.arange(8) + 10 ** 6, amplitude=1.2772588722239782)
+
+
+def test_the_prefix_counts_in_the_position():
+    run(Batch([2, 1], [9, 4], 8, prefix=37), 4, 2, 64, 64, False, torch.float16)
+
+
+def test_keys_and_values_only():
+    run(Batch([2, 1], [9, 4], 8), 4, 2, 64, 64, False, torch.float16, with_q=False)
+
+
+@pytest.mark.parametrize("bad", [-1, -2 ** 31, 2 ** 31 - 1, None])
+def test_bad_pages_are_not_written(bad):
+    batch = Batch([5, 6], [13, 6], 4)
+    batch.table[0, 2] = batch.pages if bad is None else bad
+    batch.table[1, 0] = batch.pages + 1 if bad is None else bad
+    run(batch, 4, 2, 64, 64, False, torch.float16)
+
+
+def test_more_new_tokens_than_length_have_no_place():
+    run(Batch([6], [4], 4), 4, 2, 64, 64, False, torch.float16)
+
+
+def test_starts_and_lengths_out_of_range():
+    """Rows that no sequence owns stay, lengths beyond the table have no place."""
+    dtype, gen = torch.float16, torch.Generator().manual_seed(1)
+    kc, vc = (pool(gen, 4, 2, 8, 64, dtype) for _ in range(2))
+    k0 = kc.clone()
+    k = torch.randn((6, 2, 64), generator=gen).to(dtype).to(DEV)
+    q_out = torch.full((6, 2, 64), 9.0, dtype=dtype, device=DEV)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    table = torch.tensor([[0, 1], [2, 3]], **i32)
+    freqs = torch.tensor(fq.fq_rope_freqs(64, 10000.0), dtype=torch.float64, device=DEV)
+    # rows 0 and 1 belong to nobody, the second sequence ends past the rows, its length past its pages
+    seqs = fq.Sequences(torch.tensor([2, 4, 99], **i32), torch.tensor([-7, 1000], **i32), table)
+    fq.fq_kv_append(fq.KVCache(kc, vc), seqs, k, k, k, q_out, freqs)
+    torch.cuda.synchronize()
+    assert torch.all(q_out[:2] == 9.0) and not torch.any(q_out[2:] == 9.0)
+    want, _ = turn(f64(k)[4:], np.array([14, 15]), freqs.cpu().numpy(), 64, False)
+    assert np.abs(f64(kc)[3, :, 6:].transpose(1, 0, 2) - want).max() < 2e-3 * np.abs(want).max()
+    assert torch.equal(kc[:3], k0[:3]) and torch.equal(kc[3, :, :6], k0[3, :, :6])
+
+
+def test_a_captured_step_follows_the_tables():
+    dtype, gen = torch.bfloat16, torch.Generator().manual_seed(2)
+    batch = Batch([1, 1], [20, 20], 4)
+    kc, vc = (pool(gen, batch.pages, 2, 4, 64, dtype) for _ in range(2))
+    cache = fq.KVCache(kc, vc)
+    q = torch.randn((2, 4, 64), generator=gen).to(dtype).to(DEV)
+    k = torch.randn((2, 2, 64), generator=gen).to(dtype).to(DEV)
+    freqs = torch.tensor(fq.fq_rope_freqs(64, 10000.0), dtype=torch.float64, device=DEV)
+    seqs = batch.sequences()
+    kv_len = seqs._keep[1]
+    out = torch.empty_like(q)
+    g = torch.cuda.CUDAGraph()
+    s = torch.cuda.Stream()
+    with torch.cuda.graph(g, stream=s):
+        fq.fq_kv_append(cache, seqs, q, k, k, out, freqs)
+    for step in range(1, 5):
+        kv_len.copy_(torch.tensor([3 * step, 5 * step - 4], dtype=torch.int32))
+        q.add_(0.25)
+        g.replay()
+        torch.cuda.synchronize()
+        got = [out.clone(), kc.clone(), vc.clone()]
+        kc.zero_(), vc.zero_(), out.zero_()
+        fq.fq_kv_append(cache, seqs, q, k, k, out, freqs)
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], out)
+        for t, (b, p) in enumerate(zip((0, 1), (3 * step - 1, 5 * step - 5))):
+            page = int(batch.table[b, p // 4])
+            assert torch.equal(got[1][page, :, p % 4], kc[page, :, p % 4]) and torch.any(kc[page, :, p % 4] != 0)
+            assert torch.equal(got[2][page, :, p % 4], k[t])
