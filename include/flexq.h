@@ -461,7 +461,7 @@ int fq_kv_destroy(fq_kv *kv);
  *                 attention passes over its keys
  *   prefix_table  int32 [ceil(prefix_len / page_tokens)]: pages of `prefix_len` tokens that stand before the places of
  *                 every sequence of the batch; NULL with prefix_len = 0
- * 1 <= seqs <= FQ_MAX_SEQS, table_width >= 1; (table_width + 1) * page_tokens + prefix_len < 2^31 for the cache it is used with.  The handle
+ * 1 <= seqs <= FQ_MAX_SEQS, table_width >= 1; (table_width + 1) * page_tokens + prefix_len <= 2^31 - 2^16 for the cache it is used with.  The handle
  * borrows the tables and launches nothing.
  */
 #define FQ_MAX_SEQS 65535

@@ -1,0 +1,154 @@
+// What the attention kernels share: which rows and keys a workgroup takes, how a key's row is found, the matrix
+// instructions of both types, and the end of a row of the softmax.
+//
+// A sequence's keys are numbered through prefix and cache: key 0 .. prefix_len - 1, then its places.  Rows are (new token,
+// query head of one key head), token by token.  Both kernels compute the scores transposed, S^T = K Q^T: a lane then holds
+// scores of ONE row, over keys that run through its registers, so the statistics of a row are a lane's own but for one or two
+// exchanges, and exp(S^T) is already the right-hand operand of O^T = V^T P^T.  The contraction over keys may run in any order,
+// so the keys a lane holds after the first product are the keys it takes V's elements of (read transposed from LDS), and P never
+// moves between lanes.
+#ifndef FQ_ATTEND_H
+#define FQ_ATTEND_H
+
+#include <hip/hip_runtime.h>
+
+#include "fq_kv.h"
+#include "fq_mfma.h"
+
+// One launch of a kernel: the rows it takes and how their keys are split.
+struct FqAttendWork {
+    int shared;     // 1: all tokens' rows over the prefix; 0: a sequence's rows over its keys from key0 on
+    int key0;
+    int chunk;      // keys of one part
+    int part0;      // this launch's parts are part0 + blockIdx.y
+    int row_blocks; // of a sequence (shared: of all tokens)
+    float *part_o;  // [part][token][q_head][dim] not yet divided, or null: one part, the result goes out
+    float2 *part_ml; // [part][token][q_head]: largest score (times log2 e), sum
+};
+
+constexpr float FQ_LOG2E = 1.4426950408889634f, FQ_LN2 = 0.6931471805599453f;
+// Rows are rescaled when a score passes their reference by more than this (in powers of two): p stays under 2^8, which
+// binary16 holds as exactly as 1, and most tiles rescale nothing.
+constexpr float FQ_ATTEND_SLACK = 8.0f;
+
+// The rows of one workgroup's sequence and what they see.
+struct FqAttendRows {
+    int q0, rows;   // first token, rows
+    int own, n;     // own keys before the first new token (may be negative)
+    int P, max_kv;
+    bool shared;
+    __device__ __forceinline__ int limit(int j) const // keys 0 .. limit - 1 are seen by token j
+    {
+        return shared ? P : P + min(max(own + j + 1, 0), max_kv);
+    }
+};
+
+__device__ __forceinline__ FqAttendRows fq_attend_rows(const FqAttendArgs &a, const FqAttendWork &w, int b, int group)
+{
+    FqAttendRows r;
+    r.P = a.seqs.prefix_len;
+    r.max_kv = a.max_kv;
+    r.shared = w.shared != 0;
+    if (r.shared) {
+        r.q0 = 0;
+        r.n = a.seqs.tokens;
+        r.own = 0;
+        r.rows = r.n * group;
+    } else {
+        const FqSeq s = fq_seq(a.seqs, a.kv.page_shift, b);
+        r.q0 = s.q0;
+        r.n = s.n;
+        r.own = s.len - s.n;
+        r.rows = min(s.n, a.max_q) * group;
+    }
+    return r;
+}
+
+// The page of a key, -1 for one that is not there (past `end`, or a hole).
+__device__ __forceinline__ int fq_key_page(const FqAttendArgs &a, const int32_t *table, int key, int end)
+{
+    if (key >= end)
+        return -1;
+    const int P = a.seqs.prefix_len;
+    return key < P ? a.seqs.prefix_table[key >> a.kv.page_shift] : table[(key - P) >> a.kv.page_shift];
+}
+
+// Where the row of a key's values begins, for a page that is there.
+__device__ __forceinline__ long long fq_key_offset(const FqAttendArgs &a, int page, int key, int head)
+{
+    const int P = a.seqs.prefix_len;
+    const int place = key < P ? key : key - P;
+    return page * a.kv.page_stride + head * a.kv.head_stride + (place & ((1 << a.kv.page_shift) - 1)) * a.kv.token_stride;
+}
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short short4_t __attribute__((ext_vector_type(4)));
+
+template <bool BF16>
+__device__ __forceinline__ float4_t fq_mfma16(u32x4 x, u32x4 y, float4_t c)
+{
+    if constexpr (BF16)
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, x), __builtin_bit_cast(half8_t, y), c, 0, 0, 0);
+}
+
+template <bool BF16>
+__device__ __forceinline__ float16_t fq_mfma32(u32x4 x, u32x4 y, float16_t c)
+{
+    if constexpr (BF16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, x), __builtin_bit_cast(half8_t, y), c, 0, 0, 0);
+}
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Two values to the 16-bit type, each rounded to nearest even.
+template <bool BF16>
+__device__ __forceinline__ uint32_t fq_pack2(float x, float y)
+{
+    if constexpr (BF16)
+        return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
+    else
+        return __builtin_bit_cast(uint32_t, half2_t{(_Float16)x, (_Float16)y});
+}
+
+// Four consecutive rows (keys) of a 16-column block of LDS, column by column: of 16 lanes, lane t names 8 bytes (row t / 4, columns
+// 4 (t % 4) ..) and gets column t of the four rows.
+__device__ __forceinline__ u32x2 fq_read_transposed(const char *at)
+{
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((FQ_LDS short4_t *)at));
+}
+
+// The larger of (the sum of) a value and that of the lane 32 on; of the lanes 16 on.
+template <bool SUM>
+__device__ __forceinline__ float fq_over32(float v)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const float x = __builtin_bit_cast(float, (uint32_t)r[0]), y = __builtin_bit_cast(float, (uint32_t)r[1]);
+    return SUM ? x + y : fmaxf(x, y);
+}
+template <bool SUM>
+__device__ __forceinline__ float fq_over16(float v)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const float x = __builtin_bit_cast(float, (uint32_t)r[0]), y = __builtin_bit_cast(float, (uint32_t)r[1]);
+    return SUM ? x + y : fmaxf(x, y);
+}
+
+// exp2(x - m) for a row whose reference may still be -inf (nothing seen yet: 0)
+__device__ __forceinline__ float fq_reference(float m) { return m == -INFINITY ? 0.0f : m; }
+
+// lse in natural logarithms of a row with reference m (times log2 e) and sum l
+__device__ __forceinline__ float fq_lse(float m, float l) { return l == 0.0f ? -INFINITY : fq_reference(m) * FQ_LN2 + logf(l); }
+__device__ __forceinline__ float fq_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
+
+hipError_t fq_launch_attend_few(const FqAttendArgs &a, const FqAttendWork &w, int row_tiles, dim3 grid, hipStream_t stream);
+hipError_t fq_launch_attend_many(const FqAttendArgs &a, const FqAttendWork &w, dim3 grid, hipStream_t stream);
+constexpr int FQ_FEW_WAVES = 4;   // wavefronts of a workgroup of the first, each with keys of its own
+constexpr int FQ_MANY_ROWS = 128; // rows of a workgroup of the second
+
+#endif

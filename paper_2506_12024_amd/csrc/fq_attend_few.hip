@@ -1,0 +1,318 @@
+// Attention of up to 64 rows to a sequence and key head: the single tokens of a decode step, and a few more.
+//
+// Bound by reading the cache once.  A wavefront takes 32 keys at a time, its own ones: the rows of K go from memory straight
+// into the registers of the first product's left operand (a lane holds 16 bytes of a key; any order of the head's
+// dimensions serves if Q has the same), the rows of V pass through a piece of LDS that belongs to the wavefront alone and
+// are read back transposed.  No barrier until the end, where the wavefronts' rows are added up; a lane asks for the next
+// 32 keys as soon as the registers of the last are free, and for the page numbers a step before that.
+#include "fq_attend.h"
+
+namespace {
+
+constexpr int WAVES = FQ_FEW_WAVES;
+constexpr int KEYS = 32; // to a wavefront and step
+
+// 16-byte pieces to a row of V in LDS, and where piece c of row r goes: 16 rows of one piece fall on 16 different bank
+// groups (the writes), and so do 8 rows of a pair of pieces (the transposed reads).
+template <int DP>
+struct Place {
+    static constexpr int PITCH = DP <= 64 ? 8 : DP <= 128 ? 16 : 32;
+    static __device__ __forceinline__ int at(int r, int c)
+    {
+        const int s = PITCH == 8 ? (((r >> 1) & 3) << 1) | ((r >> 3) & 1) : ((r & 7) << 1) | ((r >> 3) & 1);
+        return (r * PITCH + (c ^ s)) << 4;
+    }
+};
+
+// DP: dimensions computed; FULL: the head has all of them; RT: tiles of 16 rows.
+template <bool BF16, int DP, bool FULL, int RT>
+__global__ __launch_bounds__(WAVES * 64) void attend_few_kernel(FqAttendArgs a, FqAttendWork w)
+{
+    constexpr int NS = DP / 32, ND = DP / 16;
+    constexpr int WAVE_LDS = KEYS * Place<DP>::PITCH * 16;
+    static_assert(WAVE_LDS >= 16 * DP * 4, "the rows are added up in the same piece");
+    __shared__ alignas(16) char lds[WAVES * WAVE_LDS];
+    __shared__ float all_m[WAVES][RT * 16], all_l[WAVES][RT * 16];
+
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+    const int head = blockIdx.x % a.kv.kv_heads, row0 = blockIdx.x / a.kv.kv_heads * (16 * RT), b = blockIdx.z;
+    const int group = a.q_heads / a.kv.kv_heads, dim = FULL ? DP : a.kv.dim;
+    const FqAttendRows rs = fq_attend_rows(a, w, b, group);
+    if (row0 >= rs.rows)
+        return;
+    const int last = min(row0 + 16 * RT, rs.rows) - 1;
+    const long long begin64 = w.key0 + (long long)blockIdx.y * w.chunk;
+    const int most = rs.limit(last / group);
+    if (begin64 >= most && w.part_o)
+        return; // nobody reads this part
+    const int begin = begin64 < most ? (int)begin64 : most;
+    const int end = (int)(begin64 + w.chunk < most ? begin64 + w.chunk : most);
+    const int all_seen = rs.limit(row0 / group); // every row sees the keys before this one
+
+    // Q: row col of tile rt, dimensions 32 s + 8 quad ..
+    u32x4 q[RT][NS];
+    int lim[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) {
+        const int r = row0 + rt * 16 + col;
+        const bool real = r <= last;
+        const int j = (real ? r : row0) / group, h = head * group + (real ? r : row0) % group;
+        lim[rt] = min(rs.limit(j), end);
+        const uint16_t *from = a.q + (rs.q0 + j) * a.q_stride + h * dim;
+#pragma unroll
+        for (int s = 0; s < NS; s++) {
+            const int d = 32 * s + 8 * quad;
+            q[rt][s] = u32x4{0, 0, 0, 0};
+            if (real && (FULL || d < dim))
+                q[rt][s] = *(const u32x4 *)(from + d);
+        }
+    }
+
+    float4_t o[RT][ND];
+    float m[RT], l[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) {
+        m[rt] = -INFINITY;
+        l[rt] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < ND; d++)
+            o[rt][d] = float4_t{0, 0, 0, 0};
+    }
+    const float c = a.scale * FQ_LOG2E;
+    const int32_t *table = a.seqs.table + (rs.shared ? 0 : (long long)b * a.seqs.table_width);
+    char *mine = lds + wave * WAVE_LDS;
+
+    const uint16_t *kp[2], *vp[2]; // the lane's two keys (col, col + 16)
+    bool ok[2];
+    u32x4 k[2][NS], v[2][NS];
+    int page[2];
+    auto pages = [&](int key) {
+#pragma unroll
+        for (int t = 0; t < 2; t++)
+            page[t] = fq_key_page(a, table, key + 16 * t + col, end);
+    };
+    auto addresses = [&](int key) {
+#pragma unroll
+        for (int t = 0; t < 2; t++) {
+            ok[t] = page[t] >= 0 && page[t] < a.kv.n_pages;
+            const long long at = ok[t] ? fq_key_offset(a, page[t], key + 16 * t + col, head) : 0; // (any address of the pool)
+            kp[t] = a.kv.k + at;
+            vp[t] = a.kv.v + at;
+        }
+    };
+    auto load = [&](const uint16_t *const (&p)[2], u32x4 (&x)[2][NS]) {
+#pragma unroll
+        for (int t = 0; t < 2; t++)
+#pragma unroll
+            for (int s = 0; s < NS; s++) {
+                const int d = 32 * s + 8 * quad;
+                x[t][s] = *(const u32x4 *)(p[t] + (FULL || d < dim ? d : 0));
+            }
+    };
+
+    constexpr int STEP = WAVES * KEYS;
+    int key = begin + wave * KEYS;
+    if (key < end) {
+        pages(key);
+        addresses(key);
+        load(kp, k);
+        load(vp, v);
+        pages(key + STEP < end ? key + STEP : end);
+    }
+    for (; key < end; key += STEP) {
+        const bool more = key + STEP < end;
+        const uint64_t there0 = __ballot(ok[0]), there1 = __ballot(ok[1]);
+        const uint32_t there = (uint32_t)(there0 & 0xffff) | ((uint32_t)(there1 & 0xffff) << 16);
+        float4_t sc[RT][2];
+#pragma unroll
+        for (int t = 0; t < 2; t++) {
+            if (!FULL) {
+#pragma unroll
+                for (int s = 0; s < NS; s++)
+                    if (32 * s + 8 * quad >= dim)
+                        k[t][s] = u32x4{0, 0, 0, 0};
+            }
+#pragma unroll
+            for (int rt = 0; rt < RT; rt++) {
+                sc[rt][t] = float4_t{0, 0, 0, 0};
+#pragma unroll
+                for (int s = 0; s < NS; s++)
+                    sc[rt][t] = fq_mfma16<BF16>(k[t][s], q[rt][s], sc[rt][t]);
+            }
+        }
+        // V of a key that is not there must be 0, whatever lies at its address: 0 times NaN is NaN
+        if (there != 0xffffffffu) {
+#pragma unroll
+            for (int t = 0; t < 2; t++)
+                if (!ok[t])
+#pragma unroll
+                    for (int s = 0; s < NS; s++)
+                        v[t][s] = u32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int t = 0; t < 2; t++)
+#pragma unroll
+            for (int s = 0; s < NS; s++)
+                *(u32x4 *)(mine + Place<DP>::at(16 * t + col, 4 * s + quad)) = v[t][s];
+        if (more) {
+            addresses(key + STEP);
+            load(kp, k);
+            load(vp, v);
+            pages(key + 2 * STEP < end ? key + 2 * STEP : end);
+        }
+        const bool masked = there != 0xffffffffu || key + KEYS > all_seen;
+        u32x4 p[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; rt++) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++)
+                x[i] = sc[rt][i >> 2][i & 3] * c;
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const int at = 16 * (i >> 2) + 4 * quad + (i & 3);
+                    if (!((there >> at) & 1) || key + at >= lim[rt])
+                        x[i] = -INFINITY;
+                }
+            }
+            float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+            top = fq_over32<false>(fq_over16<false>(top));
+            if (__any(top > m[rt] + FQ_ATTEND_SLACK)) {
+                const float now = fmaxf(m[rt], top);
+                const float fall = __builtin_amdgcn_exp2f(m[rt] - fq_reference(now));
+                m[rt] = now;
+                l[rt] *= fall;
+#pragma unroll
+                for (int d = 0; d < ND; d++)
+                    o[rt][d] *= fall;
+            }
+            const float ref = fq_reference(m[rt]);
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                x[i] = __builtin_amdgcn_exp2f(x[i] - ref);
+                sum += x[i];
+            }
+            l[rt] += sum;
+            p[rt] = u32x4{fq_pack2<BF16>(x[0], x[1]), fq_pack2<BF16>(x[2], x[3]), fq_pack2<BF16>(x[4], x[5]),
+                          fq_pack2<BF16>(x[6], x[7])};
+        }
+        // the wavefront's own writes, read by other lanes of it: LDS serves a wavefront in order, the compiler is told so
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+        for (int d = 0; d < ND; d++) {
+            const int r = 4 * quad + (col >> 2), piece = 2 * d + ((col & 3) >> 1), half = (col & 1) * 8;
+            const u32x2 lo = fq_read_transposed(mine + Place<DP>::at(r, piece) + half);
+            const u32x2 hi = fq_read_transposed(mine + Place<DP>::at(16 + r, piece) + half);
+            const u32x4 vt = {lo[0], lo[1], hi[0], hi[1]};
+#pragma unroll
+            for (int rt = 0; rt < RT; rt++)
+                o[rt][d] = fq_mfma16<BF16>(vt, p[rt], o[rt][d]);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) {
+        l[rt] = fq_over32<true>(fq_over16<true>(l[rt]));
+        if (quad == 0) {
+            all_m[wave][rt * 16 + col] = m[rt];
+            all_l[wave][rt * 16 + col] = l[rt];
+        }
+    }
+    const long long rows_all = (long long)a.seqs.tokens * a.q_heads;
+#pragma unroll
+    for (int rt = 0; rt < RT; rt++) {
+        __syncthreads();
+        const int r16 = rt * 16 + col;
+        float top = all_m[0][r16];
+#pragma unroll
+        for (int i = 1; i < WAVES; i++)
+            top = fmaxf(top, all_m[i][r16]);
+        const float fall = __builtin_amdgcn_exp2f(m[rt] - fq_reference(top));
+#pragma unroll
+        for (int d = 0; d < ND; d++)
+            *(float4_t *)(mine + ((col * DP + 16 * d + 4 * quad) << 2)) = o[rt][d] * fall;
+        __syncthreads();
+        // thread: row tid / (DP / 8), 8 dimensions of it
+        for (int u = threadIdx.x; u < 16 * (DP / 8); u += WAVES * 64) {
+            const int rr = u / (DP / 8), d = u % (DP / 8) * 8, r = row0 + rt * 16 + rr;
+            if (r > last || d >= dim)
+                continue;
+            float sum[8];
+            float best = all_m[0][rt * 16 + rr], total = 0.0f;
+#pragma unroll
+            for (int i = 1; i < WAVES; i++)
+                best = fmaxf(best, all_m[i][rt * 16 + rr]);
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                sum[e] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < WAVES; i++) {
+                total += all_l[i][rt * 16 + rr] * __builtin_amdgcn_exp2f(all_m[i][rt * 16 + rr] - fq_reference(best));
+                const float4_t *from = (const float4_t *)(lds + i * WAVE_LDS + ((rr * DP + d) << 2));
+                const float4_t x = from[0], y = from[1];
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    sum[e] += x[e];
+                    sum[4 + e] += y[e];
+                }
+            }
+            const long long t = rs.q0 + r / group;
+            const int h = head * group + r % group;
+            if (w.part_o) {
+                const long long at = (w.part0 + (long long)blockIdx.y) * rows_all + t * a.q_heads + h;
+                *(float4_t *)(w.part_o + at * dim + d) = float4_t{sum[0], sum[1], sum[2], sum[3]};
+                *(float4_t *)(w.part_o + at * dim + d + 4) = float4_t{sum[4], sum[5], sum[6], sum[7]};
+                if (d == 0)
+                    w.part_ml[at] = float2{best, total};
+            } else {
+                const float inv = fq_inverse(total);
+                u32x4 y;
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    y[e] = fq_pack2<BF16>(sum[2 * e] * inv, sum[2 * e + 1] * inv);
+                *(u32x4 *)(a.out + t * a.out_stride + h * dim + d) = y;
+                if (d == 0 && a.lse)
+                    a.lse[t * a.q_heads + h] = fq_lse(best, total);
+            }
+        }
+    }
+}
+
+template <bool BF16, int DP, bool FULL>
+hipError_t launch(const FqAttendArgs &a, const FqAttendWork &w, int row_tiles, dim3 grid, hipStream_t stream)
+{
+    if (row_tiles == 1)
+        attend_few_kernel<BF16, DP, FULL, 1><<<grid, WAVES * 64, 0, stream>>>(a, w);
+    else if (row_tiles == 2 || DP > 128)
+        attend_few_kernel<BF16, DP, FULL, 2><<<grid, WAVES * 64, 0, stream>>>(a, w);
+    else if constexpr (DP <= 128)
+        attend_few_kernel<BF16, DP, FULL, 4><<<grid, WAVES * 64, 0, stream>>>(a, w);
+    return hipGetLastError();
+}
+
+template <bool BF16>
+hipError_t by_width(const FqAttendArgs &a, const FqAttendWork &w, int row_tiles, dim3 grid, hipStream_t stream)
+{
+    const int dim = a.kv.dim;
+    if (dim == 64)
+        return launch<BF16, 64, true>(a, w, row_tiles, grid, stream);
+    if (dim == 128)
+        return launch<BF16, 128, true>(a, w, row_tiles, grid, stream);
+    if (dim <= 96)
+        return launch<BF16, 96, false>(a, w, row_tiles, grid, stream);
+    return launch<BF16, 256, false>(a, w, row_tiles, grid, stream);
+}
+
+} // namespace
+
+hipError_t fq_launch_attend_few(const FqAttendArgs &a, const FqAttendWork &w, int row_tiles, dim3 grid, hipStream_t stream)
+{
+    return a.kv.bf16 ? by_width<true>(a, w, row_tiles, grid, stream) : by_width<false>(a, w, row_tiles, grid, stream);
+}

@@ -35,8 +35,8 @@ int check_handles(const char *who, const fq_kv *kv, const fq_seqs *seqs, int tok
     if (tokens < 0)
         return fq_fail(FQ_ERR_SHAPE, "%s: tokens must be >= 0 (got %d)", who, tokens);
     const long long places = ((long long)seqs->view.table_width + 1) << kv->view.page_shift;
-    if (places + seqs->view.prefix_len > 0x7fffffffLL)
-        return fq_fail(FQ_ERR_SHAPE, "%s: %d pages of %d tokens to a sequence and a prefix of %d pass 2^31 places", who,
+    if (places + seqs->view.prefix_len > 0x7fff0000LL) // (a step beyond the last key still counts in 32 bits)
+        return fq_fail(FQ_ERR_SHAPE, "%s: %d pages of %d tokens to a sequence and a prefix of %d pass 2^31 - 2^16 places", who,
                        seqs->view.table_width, 1 << kv->view.page_shift, seqs->view.prefix_len);
     return FQ_OK;
 }
