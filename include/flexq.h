@@ -520,7 +520,7 @@ int fq_attend(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q, l
  *   5. token = the first kept i, by index, at which the running sum of the kept w exceeds u times their whole sum
  *      (u >= 1: the last with any weight);  prob = w_token / that sum
  * A NaN logit counts as -inf; -inf is never drawn, and a row of nothing else gives token -1 and prob 0.  With +inf in a row only
- * the +inf entries have weight, 1 each.  w is computed in binary64 and held as a whole number of 2^-(62 - ceil(log2 V)): sums
+ * the +inf entries have weight, 1 each.  w is computed in binary64 and held as a whole number of 2^-min(51, 62 - ceil(log2 V)): sums
  * are exact, equal calls give equal bits, and a weight under half of that unit counts as nothing.
  *   logits       device, f32 (or fp16: fq_sample_f16) [R][V], rows row_stride elements apart (row_stride >= V; any alignment that
  *                the type has)                                                                   (read)

@@ -1,15 +1,15 @@
 // Drawing the next token from a row of logits: temperature, top-k, top-p, min-p and a given random number.
 //
 // Weights are whole numbers (exp in binary64, rounded to a unit under which V of them still fit 62 bits), so sums are exact in any
-// order and atomics give the same bits every time.  One workgroup takes a row:
-//   1. the largest logit (a row of up to 32768 entries stays in registers from here on, a longer one is read again)
+// order and atomics give the same bits every time.  One workgroup takes a row, each of its wavefronts four stretches of it:
+//   1. the largest logit
 //   2. top-k of at most 1024: the k-th largest of the 1024 threads' own largest is no larger than the k-th of all, so the few
 //      entries from it on go to a list in LDS, which takes the row's place
 //   3. a cut (the entry at which a running count or sum, from the largest logit down, reaches its target): a histogram over 2048
-//      steps of 1/64 nat from the top, the step that holds the target, and the entries of that step in order
-//   4. the draw: kept weights summed over segments of the vocabulary, the segment that holds the target, its entries in order
-// Bound by reading a long row two (top-k, temperature, min-p) or three times (top-p), the second and third from the caches;
-// by the chain of steps for a short one.
+//      steps of 1/32 octave from the top, the step that holds the target, and the entries of that step in order
+//   4. the draw: kept weights summed over the 64 stretches, the one that holds the target, its entries in order
+// Bound by reading a long row two (top-k, temperature, min-p) or three times (top-p), all but the first from the caches, and by
+// the exponentials of the entries that count; by the chain of steps for a short one.
 #include <hip/hip_runtime.h>
 
 #include "fq_internal.h"
@@ -18,18 +18,17 @@ namespace {
 
 constexpr int THREADS = 1024;
 constexpr int WAVES = THREADS / 64;
-constexpr int HELD = 32;    // entries of a row that a thread holds in registers
-constexpr int BINS = 2048;  // steps of 1/64 nat; the last one holds everything from 32 nats on
+constexpr int ROOTS = 64;    // steps of an octave
+constexpr int BINS = 2048;   // pairs of steps from the top, 64 octaves; the last one holds what lies further down (weight 0)
+constexpr int STRETCHES = 64;
 constexpr int LIST = 8192;  // entries of the list of step 2
 constexpr int CELL = 1024;  // entries of one step that are put in order there
-constexpr int SEGMENTS = 1024;
 typedef unsigned long long u64;
 
-// Binary32 values as unsigned numbers in the same order; -0 is 0, a NaN is -inf.
-__device__ __forceinline__ float clean(float f) { return f != f ? -INFINITY : f + 0.0f; }
+// Binary32 values as unsigned numbers in the same order, -0 as 0.  (NaNs are nowhere larger or equal and weigh nothing.)
 __device__ __forceinline__ uint32_t ordered(float f)
 {
-    const uint32_t b = __builtin_bit_cast(uint32_t, f);
+    const uint32_t b = __builtin_bit_cast(uint32_t, f + 0.0f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float unordered(uint32_t k)
@@ -48,75 +47,107 @@ __device__ __forceinline__ u64 share(float x, u64 w, bool &rest)
     return __umul64hi(f, w);
 }
 
-// exp(y) for y <= 0: y = n ln 2 + f, the series of exp(f) to f^13 (|f| <= 0.347: what is left out is under 2^-57)
-__device__ __forceinline__ double exp_down(double y)
+// 2^(j / 64): the series of exp to the 13th power on an argument of at most ln 2 / 2 (what is left out is under 2^-57)
+__device__ __forceinline__ double root_of_two(int j)
 {
-    if (!(y > -750.0))
-        return 0.0;
-    const double n = rint(y * 1.4426950408889634074);
-    // ln 2 as its first 32 bits, of which n times is exact, and the rest
-    double f = fma(n, -0x1.62e42fee00000p-1, y);
-    f = fma(n, -0x1.a39ef35793c76p-33, f);
-    double p = 1.0 / 6227020800.0;
-    p = fma(p, f, 1.0 / 479001600.0);
-    p = fma(p, f, 1.0 / 39916800.0);
-    p = fma(p, f, 1.0 / 3628800.0);
-    p = fma(p, f, 1.0 / 362880.0);
-    p = fma(p, f, 1.0 / 40320.0);
-    p = fma(p, f, 1.0 / 5040.0);
-    p = fma(p, f, 1.0 / 720.0);
-    p = fma(p, f, 1.0 / 120.0);
-    p = fma(p, f, 1.0 / 24.0);
-    p = fma(p, f, 1.0 / 6.0);
-    p = fma(p, f, 0.5);
-    p = fma(p, f, 1.0);
-    p = fma(p, f, 1.0);
-    return ldexp(p, (int)n);
+    const double x = (j > ROOTS / 2 ? j - ROOTS : j) * (0.69314718055994530942 / ROOTS);
+    double p = 1.0;
+    for (int i = 13; i >= 1; i--)
+        p = fma(p * x, 1.0 / i, 1.0);
+    return j > ROOTS / 2 ? 2.0 * p : p;
 }
 
-struct Weigh {
-    float top;
-    double inv_t; // 1 / temperature
-    double unit;
-    double least; // min_p, 0 for none
-    __device__ __forceinline__ double power(float l) const // l > -inf
-    {
-        return l == top ? 1.0 : exp_down(((double)l - (double)top) * inv_t);
-    }
-    __device__ __forceinline__ u64 whole(double e) const
-    {
-        const double v = rint(e * unit);
-        const uint32_t hi = (uint32_t)(v * 0x1p-32);
-        return ((u64)hi << 32) | (uint32_t)fma((double)hi, -0x1p32, v);
-    }
-    __device__ __forceinline__ u64 operator()(float l) const { return l == -INFINITY ? 0 : whole(power(l)); }
-    // the weight of an entry that is kept where its standing is not under the cut
-    __device__ __forceinline__ u64 kept(float l, int i, u64 cut) const
-    {
-        if (l == -INFINITY || standing(l, i) < cut)
-            return 0;
-        const double e = power(l);
-        return e >= least ? whole(e) : 0;
-    }
-    __device__ __forceinline__ int bin(float l) const
-    {
-        if (l == top)
-            return 0;
-        const double x = ((double)top - (double)l) * inv_t * 64.0;
-        return x < BINS - 1 ? (int)x : BINS - 1;
-    }
+// How far down a logit lies: n + f steps of 1/64 octave, n whole (and not above 0), |f| <= 1/2.
+struct Depth {
+    double f;
+    int n;
 };
 
+// The weight of a logit, 2^((n + f) / 64): table[n % 64] times a polynomial in f (the series to the fifth power, under 2^-54 left
+// out) times 2^(n / 64).  Whole numbers are taken from the low bits of a sum with a power of two, which rounds to nearest as it
+// is formed: no conversions between double and integer.  The coefficients stay in scalar registers (pinned: as literals each
+// took a move of its own).
+struct Weigh {
+    double top;   // the largest logit
+    double scale; // 64 / (temperature * ln 2)
+    double least; // min_p times the unit, 0 for none
+    const double *table;
+    double c1 = 0.69314718055994530942 / ROOTS, c2 = c1 * c1 / 2, c3 = c1 * c2 / 3, c4 = c1 * c3 / 4, c5 = c1 * c4 / 5;
+    __device__ __forceinline__ Weigh(float top_, double scale_, double least_, const double *table_)
+        : top(top_), scale(scale_), least(least_), table(table_)
+    {
+        asm volatile("" : "+s"(c1), "+s"(c2), "+s"(c3), "+s"(c4), "+s"(c5));
+    }
+    __device__ __forceinline__ Depth depth(float l) const
+    {
+        // 64 octaves down (and at -inf, and for a NaN) the weight rounds to 0
+        const double t = fmax(((double)l - top) * scale, -64.0 * ROOTS);
+        const double m = t + 0x1.8p52;
+        return Depth{t - (m - 0x1.8p52), (int)(uint32_t)__builtin_bit_cast(u64, m)};
+    }
+    // times the unit, not yet rounded
+    __device__ __forceinline__ double value(const Depth &d) const
+    {
+        double p = fma(d.f, c5, c4);
+        p = fma(d.f, p, c3);
+        p = fma(d.f, p, c2);
+        p = fma(d.f, p, c1);
+        p = fma(d.f, p, 1.0);
+        return __builtin_bit_cast(double, __builtin_bit_cast(u64, table[d.n & (ROOTS - 1)] * p) +
+                                              ((u64)(uint32_t)((d.n & ~(ROOTS - 1)) << 14) << 32));
+    }
+    static __device__ __forceinline__ u64 whole(double v) // v <= 2^51
+    {
+        return __builtin_bit_cast(u64, v + 0x1p52) & ((1ULL << 52) - 1);
+    }
+    __device__ __forceinline__ u64 kept(const Depth &d) const // what min-p leaves of it
+    {
+        const double v = value(d);
+        return v >= least ? whole(v) : 0;
+    }
+    static __device__ __forceinline__ int bin(const Depth &d) { return min(-d.n >> 1, BINS - 1); }
+};
+
+// The last entry that is kept, in the order of standing.
+struct Cut {
+    float l;
+    int i;
+    __device__ __forceinline__ bool keeps(float x, int at) const { return x > l || (x == l && at <= i); }
+};
+__device__ __forceinline__ Cut cut_of(u64 standing)
+{
+    return Cut{unordered((uint32_t)(standing >> 32)), (int)(0xffffffffu - (uint32_t)standing)};
+}
+constexpr Cut FQ_NO_CUT = {-INFINITY, 0x7fffffff};
+
+// What lane i of a wavefront holds plus what the lanes before it hold: within rows of 16 lanes, then the rows' sums.
+template <int DPP, int ROWS>
+__device__ __forceinline__ u64 add_from(u64 v)
+{
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)v, DPP, ROWS, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(v >> 32), DPP, ROWS, 0xf, false);
+    return v + (((u64)hi << 32) | lo);
+}
+__device__ __forceinline__ u64 wave_running(u64 v)
+{
+    v = add_from<0x111, 0xf>(v); // row_shr 1, 2, 4, 8
+    v = add_from<0x112, 0xf>(v);
+    v = add_from<0x114, 0xf>(v);
+    v = add_from<0x118, 0xf>(v);
+    v = add_from<0x142, 0xa>(v); // lane 15 of a row to the next row: rows 1 and 3
+    v = add_from<0x143, 0xc>(v); // lane 31 to rows 2 and 3
+    return v;
+}
 __device__ __forceinline__ u64 wave_sum(u64 v)
 {
-    for (int o = 32; o; o >>= 1)
-        v += __shfl_xor(v, o);
-    return v;
+    v = wave_running(v);
+    return ((u64)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(v >> 32), 63) << 32) | (uint32_t)__builtin_amdgcn_readlane((uint32_t)v, 63);
 }
 
 struct Shared {
     u64 bins[BINS];
-    u64 segments[SEGMENTS];
+    u64 stretch[STRETCHES];
+    double table[ROOTS];
     u64 cell_key[CELL], cell_w[CELL];
     float list_l[LIST];
     int list_i[LIST];
@@ -129,10 +160,7 @@ struct Shared {
 __device__ __forceinline__ u64 running(Shared &s, u64 v, u64 &all)
 {
     const int lane = threadIdx.x & 63;
-    for (int o = 1; o < 64; o <<= 1) {
-        const u64 w = __shfl_up(v, o);
-        v += lane >= o ? w : 0;
-    }
+    v = wave_running(v);
     __syncthreads();
     if (lane == 63)
         s.wave[threadIdx.x >> 6] = v;
@@ -148,81 +176,77 @@ __device__ __forceinline__ u64 running(Shared &s, u64 v, u64 &all)
     return before + v;
 }
 
-// The row: each(f) calls f(logit, index) for every entry once, all 64 lanes of a wavefront together (-inf where there is
-// no entry), blocks(f, g) besides g(first index of the lane's block) after a block of VEC entries.
-template <class T, int VEC, bool IN_REGISTERS>
+// The row.  each(f) calls f(logit, index) for every entry once, all 64 lanes of a wavefront together (-inf where there is no
+// entry); stretches(f, g) besides g(stretch) after each of the wavefront's stretches of `length` entries (a multiple of 64 VEC).
+template <class T, int VEC>
 struct Row {
     const T *x;
-    int V;
-    float held[IN_REGISTERS ? HELD : 1];
+    int V, length;
+    bool infinite; // +inf is the largest: such entries count as 0, all others as -inf
     typedef T Vec __attribute__((ext_vector_type(VEC)));
 
-    __device__ __forceinline__ void block(int at, float (&l)[VEC]) const
+    __device__ __forceinline__ void block(int at, int end, float (&l)[VEC]) const
     {
-        if (at + VEC <= V) {
+        if (at + VEC <= end) {
             if constexpr (VEC > 1) {
                 const Vec v = *(const Vec *)(x + at);
 #pragma unroll
                 for (int e = 0; e < VEC; e++)
-                    l[e] = clean((float)v[e]);
+                    l[e] = (float)v[e];
             } else {
-                l[0] = clean((float)x[at]);
+                l[0] = (float)x[at];
             }
         } else {
 #pragma unroll
             for (int e = 0; e < VEC; e++)
-                l[e] = at + e < V ? clean((float)x[at + e]) : -INFINITY;
+                l[e] = at + e < end ? (float)x[at + e] : -INFINITY;
         }
     }
-    __device__ __forceinline__ void fill()
-    {
-        if constexpr (IN_REGISTERS) {
-#pragma unroll
-            for (int b = 0; b < HELD / VEC; b++) {
-                float l[VEC];
-                block((b * THREADS + threadIdx.x) * VEC, l);
-#pragma unroll
-                for (int e = 0; e < VEC; e++)
-                    held[b * VEC + e] = l[e];
-            }
-        }
-    }
+    __device__ __forceinline__ float fold(float l) const { return l == INFINITY ? 0.0f : -INFINITY; }
     template <class F, class G>
-    __device__ __forceinline__ void blocks(const F &f, const G &g) const
+    __device__ __forceinline__ void stretches(const F &f, const G &g) const
     {
-        if constexpr (IN_REGISTERS) {
-#pragma unroll
-            for (int b = 0; b < HELD / VEC; b++) {
-                if (b * THREADS * VEC < V) {
-                    const int at = (b * THREADS + threadIdx.x) * VEC;
-#pragma unroll
-                    for (int e = 0; e < VEC; e++)
-                        f(held[b * VEC + e], at + e);
-                    g(at);
-                }
-            }
-        } else {
-            constexpr int AHEAD = 64 / (VEC * (int)sizeof(T)); // 64 bytes a thread in flight
-            for (int first = 0; first < V; first += AHEAD * THREADS * VEC) {
+        constexpr int AHEAD = 64 / (VEC * (int)sizeof(T)); // 64 bytes a thread in flight
+        const int lane = threadIdx.x & 63;
+        for (int part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); part < STRETCHES && part * length < V; part += WAVES) {
+            const int end = min((part + 1) * length, V);
+            for (int first = part * length; first < end; first += AHEAD * 64 * VEC) {
                 float l[AHEAD][VEC];
 #pragma unroll
                 for (int b = 0; b < AHEAD; b++)
-                    block(first + (b * THREADS + threadIdx.x) * VEC, l[b]);
+                    if (first + b * 64 * VEC < end)
+                        block(first + (b * 64 + lane) * VEC, end, l[b]);
 #pragma unroll
-                for (int b = 0; b < AHEAD; b++) {
-                    const int at = first + (b * THREADS + threadIdx.x) * VEC;
+                for (int b = 0; b < AHEAD; b++)
+                    if (first + b * 64 * VEC < end) {
+                        if (infinite)
 #pragma unroll
-                    for (int e = 0; e < VEC; e++)
-                        f(l[b][e], at + e);
-                    g(at);
-                }
+                            for (int e = 0; e < VEC; e++)
+                                l[b][e] = fold(l[b][e]);
+#pragma unroll
+                        for (int e = 0; e < VEC; e++)
+                            f(l[b][e], first + (b * 64 + lane) * VEC + e);
+                    }
             }
+            g(part);
         }
     }
     template <class F>
     __device__ __forceinline__ void each(const F &f) const
     {
-        blocks(f, [](int) {});
+        stretches(f, [](int) {});
+    }
+};
+
+// The row, with what is to be done at the end of a stretch.
+template <class R, class G>
+struct RowOf {
+    const R &row;
+    const G &end;
+    template <class F>
+    __device__ __forceinline__ void each(const F &f) const
+    {
+        row.stretches(f, end);
     }
 };
 
@@ -291,11 +315,15 @@ __device__ __forceinline__ u64 reach_cell(Shared &s, int n, u64 target)
             for (int i = threadIdx.x; i < n; i += THREADS)
                 visit(s.cell_key[i], s.cell_w[i]);
         }, target);
-    if ((int)threadIdx.x < n) {
-        const u64 key = s.cell_key[threadIdx.x], w = s.cell_w[threadIdx.x];
+    // four threads to an entry: what stands before it
+    const int mine = threadIdx.x >> 2;
+    if (mine < n) {
+        const u64 key = s.cell_key[mine], w = s.cell_w[mine];
         u64 before = 0;
-        for (int i = 0; i < n; i++)
+        for (int i = threadIdx.x & 3; i < n; i += 4)
             before += s.cell_key[i] > key ? s.cell_w[i] : 0;
+        before += __shfl_xor(before, 1);
+        before += __shfl_xor(before, 2);
         if (before < target && target <= before + w)
             s.word[0] = key;
     }
@@ -305,47 +333,49 @@ __device__ __forceinline__ u64 reach_cell(Shared &s, int n, u64 target)
     return found;
 }
 
-// The standing at which the running sum of weight(l, i), from the largest logit down, reaches its target (a function of the
-// whole sum); 0 where it never does.
-template <class Source, class Weight, class Target>
-__device__ __forceinline__ u64 cut_at(Shared &s, const Source &src, const Weigh &weigh, const Weight &weight, const Target &target_of)
+// The entry at which the running sum of weights, from the largest logit down, reaches its target (a function of the whole sum):
+// weight(l, i, depth) -> u64.  False where it never does, and `cut` stays; else it is that entry, and entries of the source were handed
+// to above(l, i, depth) if they stand before it for sure (a lower step), the others of its step are in the cell, `n` of them (-1: above
+// was not called for all of them).
+template <class Source, class Weight, class Target, class Above>
+__device__ __forceinline__ bool cut_at(Shared &s, const Source &src, const Weigh &weigh, const Weight &weight, const Target &target_of,
+                                       const Above &above, Cut &cut, int &n)
 {
     __syncthreads();
     s.bins[threadIdx.x] = s.bins[threadIdx.x + THREADS] = 0;
     if (threadIdx.x == 0)
         s.count = 0;
     __syncthreads();
-    u64 far = 0;
     src.each([&](float l, int i) {
-        const u64 w = weight(l, i);
-        const int b = w ? weigh.bin(l) : BINS - 1;
+        const Depth d = weigh.depth(l);
+        const int b = Weigh::bin(d);
+        if (__all(b == BINS - 1))
+            return;
+        const u64 w = weight(l, i, d);
         const int one = __builtin_amdgcn_readfirstlane(b);
         if (__all(b == one)) { // (a flat row: 64 additions to one place would wait for each other)
-            if (one == BINS - 1) {
-                far += w;
-            } else {
-                const u64 sum = wave_sum(w);
-                if ((threadIdx.x & 63) == 0)
-                    atomicAdd(&s.bins[one], sum);
-            }
-        } else if (b == BINS - 1) {
-            far += w;
-        } else {
+            const u64 sum = wave_sum(w);
+            if ((threadIdx.x & 63) == 0)
+                atomicAdd(&s.bins[one], sum);
+        } else if (w) {
             atomicAdd(&s.bins[b], w);
         }
     });
-    far = wave_sum(far);
-    if ((threadIdx.x & 63) == 0)
-        atomicAdd(&s.bins[BINS - 1], far);
     u64 target = 0;
     if (!find_bin<BINS>(s, [&](u64 all) { return target = target_of(all); }))
-        return 0;
+        return false;
     const int cell = (int)s.word[0];
     const u64 left = s.word[1];
     src.each([&](float l, int i) {
-        const u64 w = weight(l, i);
-        if (w && weigh.bin(l) == cell) {
-            const int at = atomicAdd(&s.count, 1);
+        const Depth d = weigh.depth(l);
+        const int b = Weigh::bin(d);
+        if (!__any(b <= cell))
+            return;
+        if (b < cell)
+            above(l, i, d);
+        if (b == cell) {
+            const u64 w = weight(l, i, d);
+            const int at = w ? atomicAdd(&s.count, 1) : CELL;
             if (at < CELL) {
                 s.cell_key[at] = standing(l, i);
                 s.cell_w[at] = w;
@@ -353,22 +383,26 @@ __device__ __forceinline__ u64 cut_at(Shared &s, const Source &src, const Weigh 
         }
     });
     __syncthreads();
-    const int n = s.count;
-    if (n > CELL)
-        return reach<64>(s, [&](const auto &visit) {
-            src.each([&](float l, int i) { visit(standing(l, i), weight(l, i)); });
-        }, target);
-    return reach_cell(s, n, left);
+    n = s.count;
+    if (n > CELL) {
+        n = -1;
+        cut = cut_of(reach<64>(s, [&](const auto &visit) {
+            src.each([&](float l, int i) { visit(standing(l, i), weight(l, i, weigh.depth(l))); });
+        }, target));
+    } else {
+        cut = cut_of(reach_cell(s, n, left));
+    }
+    return true;
 }
 
-// The draw among the kept entries: segments holds their sums, 2^shift entries each.
-template <class T, int VEC, bool R>
-__device__ __forceinline__ void draw(Shared &s, const Row<T, VEC, R> &row, const Weigh &weigh, u64 cut, int shift, float u, int32_t *token,
+// The draw among the kept entries, whose sums over the stretches are there.
+template <class T, int VEC>
+__device__ __forceinline__ void draw(Shared &s, const Row<T, VEC> &row, const Weigh &weigh, const Cut &cut, float u, int32_t *token,
                                      float *prob)
 {
     __syncthreads();
     u64 all;
-    const u64 mine = s.segments[threadIdx.x], to = running(s, mine, all);
+    const u64 mine = threadIdx.x < STRETCHES ? s.stretch[threadIdx.x] : 0, to = running(s, mine, all);
     bool rest;
     const u64 target = u >= 1.0f ? all - 1 : u > 0.0f ? share(u, all, rest) : 0; // the first running sum above it
     if (to - mine <= target && target < to) {
@@ -377,13 +411,16 @@ __device__ __forceinline__ void draw(Shared &s, const Row<T, VEC, R> &row, const
     }
     __syncthreads();
     u64 left = s.word[1];
-    const int first = (int)s.word[0] << shift;
-    for (int base = 0; base < 1 << shift; base += THREADS) {
-        const int i = first + base + threadIdx.x;
-        const u64 w = base + (int)threadIdx.x < 1 << shift && i < row.V ? weigh.kept(clean((float)row.x[i]), i, cut) : 0;
+    const int first = (int)s.word[0] * row.length, end = min(first + row.length, row.V);
+    for (int base = first; base < end; base += THREADS) {
+        const int i = base + threadIdx.x;
+        float l = i < end ? (float)row.x[i] : -INFINITY;
+        if (row.infinite)
+            l = row.fold(l);
+        const u64 w = cut.keeps(l, i) ? weigh.kept(weigh.depth(l)) : 0;
         u64 sum;
-        const u64 end = running(s, w, sum);
-        if (end - w <= left && left < end) {
+        const u64 to = running(s, w, sum);
+        if (to - w <= left && left < to) {
             *token = i;
             if (prob)
                 *prob = (float)((double)w / (double)all);
@@ -394,18 +431,19 @@ __device__ __forceinline__ void draw(Shared &s, const Row<T, VEC, R> &row, const
     }
 }
 
-template <class T, int VEC, bool IN_REGISTERS>
-__global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double unit, int shift)
+template <class T, int VEC>
+__global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double unit, int length)
 {
     __shared__ Shared s;
     const int r = blockIdx.x, V = a.V, tid = threadIdx.x, lane = tid & 63;
     const float temperature = a.temperature ? a.temperature[r] : 1.0f, p = a.top_p ? a.top_p[r] : 1.0f;
     const float min_p = a.min_p ? a.min_p[r] : 0.0f, u = a.u[r];
     const int k = a.top_k ? a.top_k[r] : 0;
-    Row<T, VEC, IN_REGISTERS> row;
-    row.x = (const T *)a.logits + r * a.row_stride;
-    row.V = V;
-    row.fill();
+    Row<T, VEC> row{(const T *)a.logits + r * a.row_stride, V, length, false};
+    if (tid < ROOTS)
+        s.table[tid] = root_of_two(tid) * unit;
+    if (tid < STRETCHES)
+        s.stretch[tid] = 0;
     float mine = -INFINITY;
     int at = 0;
     row.each([&](float l, int i) {
@@ -434,24 +472,29 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
         }
         return;
     }
-    // (with +inf in the row 1 / temperature is too, so that what is finite has no weight)
-    const Weigh weigh{top, top == INFINITY ? (double)INFINITY : 1.0 / (double)temperature, unit,
-                      min_p > 0.0f ? (double)fminf(min_p, 1.0f) : 0.0};
+    row.infinite = top == INFINITY;
+    const Weigh weigh(row.infinite ? 0.0f : top, ROOTS * 1.4426950408889634074 / (double)temperature,
+                      min_p > 0.0f ? (double)fminf(min_p, 1.0f) * unit : 0.0, s.table);
     auto nucleus = [&](u64 all) { // the sum that top-p asks for
         bool rest = false;
         u64 t = p > 0.0f ? share(p, all, rest) : 0;
         t += rest;
         return t ? t : 1;
     };
-    u64 cut = 0; // entries whose standing is below it are out
-    __syncthreads();
-    s.segments[tid] = 0;
-    if (k > 0 && k <= THREADS && k < V) {
-        // a bound: the k-th largest of the threads' own largest, its last 8 bits let go
+    Cut cut = FQ_NO_CUT;
+    // (an entry of the last step has no weight, a top-k that reaches it keeps all that has)
+    auto count = [](float, int, const Depth &d) -> u64 { return Weigh::bin(d) < BINS - 1; };
+    auto weight = [&](float l, int i, const Depth &d) -> u64 { return cut.keeps(l, i) ? Weigh::whole(weigh.value(d)) : 0; };
+    // no entry this far down passes min-p (a step to spare)
+    const int least_n = min_p > 0.0f ? (int)(ROOTS * log2f(fminf(min_p, 1.0f))) - 2 : -BINS;
+    auto nothing = [](float, int, const Depth &) {};
+    int in_cell;
+    if (k > 0 && k <= THREADS && k < V && !row.infinite) {
+        // a bound: the k-th largest of the threads' own largest, its last 16 bits let go
         const uint32_t key = ordered(mine);
         u64 left = k;
         uint32_t bound = 0;
-        for (int b = 24; b >= 8; b -= 8) {
+        for (int b = 24; b >= 16; b -= 8) {
             __syncthreads();
             if (tid < 256)
                 s.bins[tid] = 0;
@@ -462,11 +505,13 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
             bound |= (255 - (uint32_t)s.word[0]) << b;
             left = s.word[1];
         }
+        // (below the order of the finite values lie -inf and what the bits that were let go make of it)
+        const float least_l = bound < 0x00800000u ? -3.402823466e38f : unordered(bound);
         if (tid == 0)
             s.count = 0;
         __syncthreads();
         row.each([&](float l, int i) {
-            const bool in = l > -INFINITY && ordered(l) >= bound;
+            const bool in = l >= least_l;
             const u64 who = __ballot(in);
             if (who) {
                 int base = 0;
@@ -483,45 +528,63 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
         const int n = s.count;
         if (n <= LIST) {
             const Listed list{&s, n};
-            cut = cut_at(s, list, weigh, [&](float l, int) -> u64 { return l > -INFINITY; }, [&](u64) { return (u64)k; });
-            if (!(p >= 1.0f)) {
-                const u64 c = cut_at(s, list, weigh, [&](float l, int i) { return standing(l, i) >= cut ? weigh(l) : 0; }, nucleus);
-                cut = c > cut ? c : cut;
-            }
+            cut_at(s, list, weigh, count, [&](u64) { return (u64)k; }, nothing, cut, in_cell);
+            if (!(p >= 1.0f))
+                cut_at(s, list, weigh, weight, nucleus, nothing, cut, in_cell);
             list.each([&](float l, int i) {
-                const u64 w = weigh.kept(l, i, cut);
+                const u64 w = cut.keeps(l, i) ? weigh.kept(weigh.depth(l)) : 0;
                 if (w)
-                    atomicAdd(&s.segments[i >> shift], w);
+                    atomicAdd(&s.stretch[i / length], w);
             });
-            draw(s, row, weigh, cut, shift, u, a.token + r, a.prob ? a.prob + r : nullptr);
+            draw(s, row, weigh, cut, u, a.token + r, a.prob ? a.prob + r : nullptr);
             return;
         }
     }
     if (k > 0 && k < V)
-        cut = cut_at(s, row, weigh, [&](float l, int) -> u64 { return l > -INFINITY; }, [&](u64) { return (u64)k; });
-    if (!(p >= 1.0f)) {
-        const u64 c = cut_at(s, row, weigh, [&](float l, int i) { return standing(l, i) >= cut ? weigh(l) : 0; }, nucleus);
-        cut = c > cut ? c : cut;
-    }
-    __syncthreads();
+        cut_at(s, row, weigh, count, [&](u64) { return (u64)k; }, nothing, cut, in_cell);
     u64 sum = 0;
-    row.blocks([&](float l, int i) { sum += weigh.kept(l, i, cut); },
-               [&](int i) { // the wavefront's blocks lie in one segment
-                   sum = wave_sum(sum);
-                   if (lane == 0 && sum)
-                       atomicAdd(&s.segments[i >> shift], sum);
-                   sum = 0;
-               });
-    draw(s, row, weigh, cut, shift, u, a.token + r, a.prob ? a.prob + r : nullptr);
+    auto add_stretch = [&](int part) {
+        sum = wave_sum(sum);
+        if (lane == 0)
+            s.stretch[part] = sum;
+        sum = 0;
+    };
+    bool summed = false;
+    if (!(p >= 1.0f)) {
+        const RowOf<Row<T, VEC>, decltype(add_stretch)> adding{row, add_stretch};
+        const Cut k_cut = cut;
+        if (cut.l == -INFINITY)
+            summed = cut_at(s, adding, weigh, [&](float, int, const Depth &d) { return Weigh::whole(weigh.value(d)); }, nucleus,
+                            [&](float, int, const Depth &d) { sum += weigh.kept(d); }, cut, in_cell);
+        else
+            summed = cut_at(s, adding, weigh, weight, nucleus, [&](float l, int i, const Depth &d) {
+                if (k_cut.keeps(l, i))
+                    sum += weigh.kept(d);
+            }, cut, in_cell);
+        summed = summed && in_cell >= 0;
+        if (summed && tid < in_cell) {
+            const Cut c = cut_of(s.cell_key[tid]);
+            const u64 w = cut.keeps(c.l, c.i) ? weigh.kept(weigh.depth(c.l)) : 0;
+            if (w)
+                atomicAdd(&s.stretch[c.i / length], w);
+        }
+    }
+    if (!summed && cut.l == -INFINITY && weigh.least == 0.0)
+        row.stretches([&](float l, int) { sum += Weigh::whole(weigh.value(weigh.depth(l))); }, add_stretch);
+    else if (!summed)
+        row.stretches([&](float l, int i) {
+            const Depth d = weigh.depth(l);
+            if (__any(d.n >= least_n))
+                sum += cut.keeps(l, i) ? weigh.kept(d) : 0;
+        }, add_stretch);
+    draw(s, row, weigh, cut, u, a.token + r, a.prob ? a.prob + r : nullptr);
 }
 
 template <class T, int VEC>
-void launch(const FqSampleArgs &a, double unit, int shift, hipStream_t stream)
+void launch(const FqSampleArgs &a, double unit, hipStream_t stream)
 {
-    if (a.V <= HELD * THREADS)
-        sample_kernel<T, VEC, true><<<a.R, THREADS, 0, stream>>>(a, unit, shift);
-    else
-        sample_kernel<T, VEC, false><<<a.R, THREADS, 0, stream>>>(a, unit, shift);
+    const int blocks = (a.V + STRETCHES * 64 * VEC - 1) / (STRETCHES * 64 * VEC);
+    sample_kernel<T, VEC><<<a.R, THREADS, 0, stream>>>(a, unit, blocks * 64 * VEC);
 }
 
 } // namespace
@@ -531,17 +594,16 @@ size_t fq_sample_bytes(int, int) { return 256; }
 hipError_t fq_launch_sample(const FqSampleArgs &a, bool half, void *, hipStream_t stream)
 {
     const int log_v = a.V > 1 ? 32 - __builtin_clz((unsigned)a.V - 1) : 0;
-    const double unit = (double)(1ULL << (62 - log_v));
-    const int shift = log_v - 10 > 9 ? log_v - 10 : 9; // entries of a segment: no more than 1024 of them, 64 blocks of 8 at least
+    const double unit = (double)(1ULL << (log_v > 11 ? 62 - log_v : 51));
     const int vec = half ? 8 : 4;
     const bool wide = ((uintptr_t)a.logits & 15) == 0 && (a.R == 1 || a.row_stride % vec == 0);
     if (half && wide)
-        launch<_Float16, 8>(a, unit, shift, stream);
+        launch<_Float16, 8>(a, unit, stream);
     else if (half)
-        launch<_Float16, 1>(a, unit, shift, stream);
+        launch<_Float16, 1>(a, unit, stream);
     else if (wide)
-        launch<float, 4>(a, unit, shift, stream);
+        launch<float, 4>(a, unit, stream);
     else
-        launch<float, 1>(a, unit, shift, stream);
+        launch<float, 1>(a, unit, stream);
     return hipGetLastError();
 }

@@ -117,11 +117,11 @@ def lse_tolerance(lse, steep, dim, keys):
 
 
 def weights(logits, temperature):
-    """Whole weights of a row: multiples of 2^-(62 - ceil(log2 V)) of the largest."""
+    """Whole weights of a row: multiples of 2^-min(51, 62 - ceil(log2 V)) of the largest."""
     x = logits.astype(np.float64).copy()
     x[np.isnan(x)] = -np.inf
     x = x + 0.0
-    unit = 62 - max(0, (len(x) - 1).bit_length())
+    unit = min(51, 62 - (len(x) - 1).bit_length())
     top = x.max()
     if top == np.inf:
         w = np.where(x == np.inf, 1.0, 0.0)
