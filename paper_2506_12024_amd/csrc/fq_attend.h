@@ -15,13 +15,14 @@
 #include "fq_kv.h"
 #include "fq_mfma.h"
 
-// One launch of a kernel: the rows it takes and how their keys are split.
+// One piece of work: the rows it takes and how their keys are split.
 struct FqAttendWork {
     int shared;     // 1: all tokens' rows over the prefix; 0: a sequence's rows over its keys from key0 on
     int key0;
     int chunk;      // keys of one part
-    int part0;      // this launch's parts are part0 + blockIdx.y
+    int part0;      // its parts are part0 .. part0 + parts - 1
     int row_blocks; // of a sequence (shared: of all tokens)
+    uint32_t blocks_x, parts, blocks; // its grid: key heads times row blocks, parts, sequences; workgroups in all
     float *part_o;  // [part][token][q_head][dim] not yet divided, or null: one part, the result goes out
     float2 *part_ml; // [part][token][q_head]: largest score (times log2 e), sum
 };
@@ -114,6 +115,11 @@ __device__ __forceinline__ uint32_t fq_pack2(float x, float y)
         return __builtin_bit_cast(uint32_t, half2_t{(_Float16)x, (_Float16)y});
 }
 
+// The factor of the scores in powers of two.  It is never negative -- Q's signs are turned instead (exact), so that the largest
+// product is the largest score -- nor 0, so that a masked -inf stays one (2^-120 of any score is nothing).
+__device__ __forceinline__ float fq_score_factor(float scale) { return fmaxf(fabsf(scale) * FQ_LOG2E, 0x1p-120f); }
+__device__ __forceinline__ u32x4 fq_signed(u32x4 q, float scale) { return scale < 0.0f ? q ^ 0x80008000u : q; }
+
 // Four consecutive rows (keys) of a 16-column block of LDS, column by column: of 16 lanes, lane t names 8 bytes (row t / 4, columns
 // 4 (t % 4) ..) and gets column t of the four rows.
 __device__ __forceinline__ u32x2 fq_read_transposed(const char *at)
@@ -146,9 +152,12 @@ __device__ __forceinline__ float fq_reference(float m) { return m == -INFINITY ?
 __device__ __forceinline__ float fq_lse(float m, float l) { return l == 0.0f ? -INFINITY : fq_reference(m) * FQ_LN2 + logf(l); }
 __device__ __forceinline__ float fq_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 
-hipError_t fq_launch_attend_few(const FqAttendArgs &a, const FqAttendWork &w, int row_tiles, dim3 grid, hipStream_t stream);
-hipError_t fq_launch_attend_many(const FqAttendArgs &a, const FqAttendWork &w, dim3 grid, hipStream_t stream);
-constexpr int FQ_FEW_WAVES = 4;   // wavefronts of a workgroup of the first, each with keys of its own
-constexpr int FQ_MANY_ROWS = 128; // rows of a workgroup of the second
+// rt0, rt1: tiles of 16 rows of a workgroup of each piece, 0 for the kernel of many rows.  A launch of one piece has no workgroups in
+// the second and names rt1 = rt0; of two pieces for few rows rt0 = rt1.
+hipError_t fq_launch_attend_f16(const FqAttendArgs &a, const FqAttendWork &w0, const FqAttendWork &w1, int rt0, int rt1, hipStream_t stream);
+hipError_t fq_launch_attend_bf16(const FqAttendArgs &a, const FqAttendWork &w0, const FqAttendWork &w1, int rt0, int rt1, hipStream_t stream);
+constexpr int FQ_ATTEND_THREADS = 256;
+constexpr uint32_t FQ_ATTEND_BLOCKS = 1u << 24; // fewer workgroups than this to a launch
+constexpr int FQ_MANY_ROWS = 128; // rows of a workgroup of many rows
 
 #endif

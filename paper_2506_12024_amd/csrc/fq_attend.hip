@@ -4,58 +4,82 @@
 namespace {
 
 // What one call launches.  The rows of a sequence and a key head share its keys; where they are few, the rows of the whole
-// batch share the prefix besides, and the prefix is a launch of its own.
-struct Piece {
-    FqAttendWork work;
-    int row_tiles; // 0: the kernel for many rows
-    dim3 grid;
-};
+// batch share the prefix besides, and the prefix is a piece of its own.
 struct Plan {
     int n, parts;
-    Piece piece[2];
+    FqAttendWork work[2];
+    int row_tiles[2]; // 0: the kernel for many rows
 };
+
+constexpr int MAX_PARTS = 512; // of one launch
 
 int div_up(long long a, long long b) { return (int)((a + b - 1) / b); }
 
-Piece piece(const FqAttendArgs &a, bool shared, int key0, long long keys, int seqs, int tokens, int cus)
+int tiles_of(const FqAttendArgs &a, long long rows)
+{
+    const bool wide = a.kv.dim > 96 && a.kv.dim != 128; // (the registers of such a head hold one tile)
+    return rows > (wide ? 16 : 32) ? 0 : rows > 16 ? 2 : 1;
+}
+
+FqAttendWork work(const FqAttendArgs &a, bool shared, int key0, long long keys, int seqs, int tokens, int row_tiles, int cus)
 {
     const long long rows = (long long)tokens * (a.q_heads / a.kv.kv_heads);
-    Piece p{};
-    const int few = a.kv.dim <= 96 || a.kv.dim == 128 ? 64 : 32; // (the registers of a wider head hold 32 rows)
-    p.row_tiles = rows > few ? 0 : rows > 32 ? 4 : rows > 16 ? 2 : 1;
-    const int step = p.row_tiles ? 128 : 64; // keys that a workgroup takes at once
-    p.work.shared = shared;
-    p.work.key0 = key0;
-    p.work.row_blocks = div_up(rows, p.row_tiles ? 16 * p.row_tiles : FQ_MANY_ROWS);
-    const long long groups = (long long)p.work.row_blocks * a.kv.kv_heads * seqs;
-    // parts: enough workgroups to fill the chip several times over, of a few steps each at least
-    const long long want = (p.row_tiles ? 12LL : 4LL) * cus;
-    long long parts = div_up(want, groups);
-    const long long most = div_up(keys, 4 * step);
-    parts = parts < 1 ? 1 : parts > most ? (most < 1 ? 1 : most) : parts;
-    if (parts > 256)
-        parts = 256;
-    p.work.chunk = div_up(div_up(keys > 0 ? keys : 1, parts), step) * step;
-    const int chunks = div_up(keys > 0 ? keys : 1, p.work.chunk);
-    p.grid = dim3((unsigned)(p.work.row_blocks * a.kv.kv_heads), chunks, seqs);
-    return p;
+    const int step = row_tiles ? 128 : 64; // keys that a workgroup takes at once
+    FqAttendWork w{};
+    w.shared = shared;
+    w.key0 = key0;
+    w.row_blocks = div_up(rows, row_tiles ? 16 * row_tiles : FQ_MANY_ROWS);
+    const long long groups = (long long)w.row_blocks * a.kv.kv_heads * seqs;
+    const long long steps = div_up(keys > 0 ? keys : 1, step);
+    // Steps to a part.  Few rows: all workgroups at once where that takes one step each; else four rounds of them (sequences differ
+    // in length), of as many steps that a part's sums (8 bytes to a row and dimension, written and read) are a
+    // sixteenth of its keys and values at most.  Many rows write 64 KiB of sums a part: one round, of four steps at least, and no
+    // parts at all where the rows alone make a round.
+    const long long slots = (row_tiles ? 3LL : a.kv.dim > 96 && a.kv.dim != 128 ? 1LL : 2LL) * cus;
+    long long take;
+    if (row_tiles) {
+        const long long in_block = rows < 16 * row_tiles ? rows : 16 * row_tiles, least = in_block > 8 ? in_block / 4 : 2;
+        take = groups * steps <= slots ? 1 : div_up(groups * steps, 4 * slots);
+        take = take < least && groups * steps > slots ? least : take;
+    } else {
+        const long long parts = groups < slots ? slots / groups : 1;
+        take = div_up(steps, parts);
+        take = take < 4 ? 4 : take;
+    }
+    if (div_up(steps, take) > MAX_PARTS)
+        take = div_up(steps, MAX_PARTS);
+    w.chunk = (int)(take < steps ? take : steps) * step;
+    w.parts = div_up(keys > 0 ? keys : 1, w.chunk);
+    w.blocks_x = (uint32_t)(w.row_blocks * a.kv.kv_heads);
+    const long long blocks = (long long)w.blocks_x * w.parts * seqs;
+    w.blocks = blocks < FQ_ATTEND_BLOCKS ? (uint32_t)blocks : FQ_ATTEND_BLOCKS;
+    return w;
 }
 
 Plan plan(const FqAttendArgs &a, int cus)
 {
-    const int group = a.q_heads / a.kv.kv_heads, P = a.seqs.prefix_len;
+    const long long group = a.q_heads / a.kv.kv_heads;
+    const int P = a.seqs.prefix_len;
     Plan pl{};
-    if (P > 0 && a.seqs.seqs > 1 && (long long)a.max_q * group < 64) {
-        pl.piece[0] = piece(a, true, 0, P, 1, a.seqs.tokens, cus);
-        pl.piece[1] = piece(a, false, P, a.max_kv, a.seqs.seqs, a.max_q, cus);
+    if (P > 0 && a.seqs.seqs > 1 && a.max_q * group < 64) {
+        int &t0 = pl.row_tiles[0], &t1 = pl.row_tiles[1];
+        t0 = tiles_of(a, a.seqs.tokens * group);
+        t1 = tiles_of(a, a.max_q * group);
+        if (t0 && t1)
+            t0 = t1 = t0 > t1 ? t0 : t1;
+        else
+            t0 = 0; // (few rows of the batch, many of a sequence: no such batch)
+        pl.work[0] = work(a, true, 0, P, 1, a.seqs.tokens, t0, cus);
+        pl.work[1] = work(a, false, P, a.max_kv, a.seqs.seqs, a.max_q, t1, cus);
         pl.n = 2;
     } else {
-        pl.piece[0] = piece(a, false, 0, (long long)P + a.max_kv, a.seqs.seqs, a.max_q, cus);
+        pl.row_tiles[0] = pl.row_tiles[1] = tiles_of(a, a.max_q * group);
+        pl.work[0] = work(a, false, 0, (long long)P + a.max_kv, a.seqs.seqs, a.max_q, pl.row_tiles[0], cus);
         pl.n = 1;
     }
     for (int i = 0; i < pl.n; i++) {
-        pl.piece[i].work.part0 = pl.parts;
-        pl.parts += pl.piece[i].grid.y;
+        pl.work[i].part0 = pl.parts;
+        pl.parts += pl.work[i].parts;
     }
     return pl;
 }
@@ -68,45 +92,87 @@ size_t bytes(const FqAttendArgs &a, const Plan &pl)
     return (rows * pl.parts * (a.kv.dim * sizeof(float) + sizeof(float2)) + 255) & ~(size_t)255;
 }
 
-// The parts of a row, added up in their order: a thread takes 4 dimensions of a row, 256 / (dim / 4) rows to a workgroup.
-__global__ __launch_bounds__(256) void attend_join_kernel(FqAttendArgs a, FqAttendWork w0, FqAttendWork w1, int n, int parts0, int parts1)
+// The parts of a row, added up.  dim / 4 threads take 4 dimensions each of every `lanes`-th part, each with a reference of its own;
+// then the lanes are added up through LDS in their order.  (One thread walking all parts waited for each load in turn: 196
+// parts took 160 us of 186 for one token of the 70B shapes behind 100000.)
+__global__ __launch_bounds__(256) void attend_join_kernel(FqAttendArgs a, FqAttendWork w0, FqAttendWork w1, int n, int lanes)
 {
-    const int per = a.kv.dim >> 2, rows_wg = 256 / per;
-    const int mine = threadIdx.x / per, d = (threadIdx.x - mine * per) << 2, b = blockIdx.z;
+    __shared__ float4_t sums[256];
+    __shared__ float2 stats[256];
+    const int per = a.kv.dim >> 2, rows_wg = 256 / (per * lanes);
+    const int unit = threadIdx.x / per, mine = unit / lanes, lane = unit - mine * lanes;
+    const int d = (threadIdx.x - unit * per) << 2, b = blockIdx.z;
     const FqSeq s = fq_seq(a.seqs, a.kv.page_shift, b);
-    const long long r = (long long)blockIdx.x * rows_wg + mine;
-    if (mine >= rows_wg || r >= (long long)min(s.n, a.max_q) * a.q_heads)
+    const int rows = min(s.n, a.max_q) * a.q_heads;
+    const int r = blockIdx.x * rows_wg + mine;
+    if ((int)blockIdx.x * rows_wg >= rows)
         return;
-    const int j = (int)(r / a.q_heads);
-    const long long t = s.q0 + j, row = t * a.q_heads + r % a.q_heads, rows_all = (long long)a.seqs.tokens * a.q_heads;
-    const int P = a.seqs.prefix_len, lim = P + min(max(s.len - s.n + j + 1, 0), a.max_kv);
-    // parts that hold keys this row sees
-    int have[2];
-    have[0] = w0.shared ? parts0 : min(parts0, lim > w0.key0 ? (lim - w0.key0 - 1) / w0.chunk + 1 : 0);
-    have[1] = n > 1 ? min(parts1, lim > w1.key0 ? (lim - w1.key0 - 1) / w1.chunk + 1 : 0) : 0;
-    float m = -INFINITY;
-    for (int i = 0; i < 2; i++)
-        for (int p = 0; p < have[i]; p++)
-            m = fmaxf(m, w0.part_ml[((i ? parts0 : 0) + p) * rows_all + row].x);
-    const float ref = fq_reference(m);
-    float l = 0.0f;
+    const bool real = mine < rows_wg && r < rows;
+    const int j = real ? r / a.q_heads : 0, h = real ? r - j * a.q_heads : 0;
+    const long long t = s.q0 + j, row = t * a.q_heads + h, rows_all = (long long)a.seqs.tokens * a.q_heads;
+    float m = -INFINITY, l = 0.0f;
     float4_t o = {0, 0, 0, 0};
-    for (int i = 0; i < 2; i++)
-        for (int p = 0; p < have[i]; p++) {
-            const long long at = ((i ? parts0 : 0) + p) * rows_all + row;
-            const float2 ml = w0.part_ml[at];
-            const float f = __builtin_amdgcn_exp2f(ml.x - ref);
-            l += ml.y * f;
-            o += *(const float4_t *)(w0.part_o + at * a.kv.dim + d) * f;
+    if (real) {
+        const int P = a.seqs.prefix_len, lim = P + min(max(s.len - s.n + j + 1, 0), a.max_kv);
+        // parts that hold keys this row sees: the first `have0`, and `have1` from parts0 on
+        const int parts0 = w0.parts, parts1 = w1.parts;
+        const int have0 = w0.shared ? parts0 : min(parts0, lim > w0.key0 ? (lim - w0.key0 - 1) / w0.chunk + 1 : 0);
+        const int have1 = n > 1 ? min(parts1, lim > w1.key0 ? (lim - w1.key0 - 1) / w1.chunk + 1 : 0) : 0;
+        const int have = have0 + have1;
+        constexpr int AHEAD = 4;
+        for (int p0 = lane; p0 < have; p0 += AHEAD * lanes) {
+            float2 ml[AHEAD];
+            float4_t x[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; i++) {
+                const int p = p0 + i * lanes;
+                ml[i] = float2{-INFINITY, 0.0f};
+                x[i] = float4_t{0, 0, 0, 0};
+                if (p < have) {
+                    const long long at = (p < have0 ? p : parts0 + p - have0) * rows_all + row;
+                    ml[i] = w0.part_ml[at];
+                    x[i] = *(const float4_t *)(w0.part_o + at * a.kv.dim + d);
+                }
+            }
+            float top = m;
+#pragma unroll
+            for (int i = 0; i < AHEAD; i++)
+                top = fmaxf(top, ml[i].x);
+            const float ref = fq_reference(top), fall = __builtin_amdgcn_exp2f(m - ref);
+            m = top;
+            l *= fall;
+            o *= fall;
+#pragma unroll
+            for (int i = 0; i < AHEAD; i++) {
+                const float f = __builtin_amdgcn_exp2f(ml[i].x - ref);
+                l += ml[i].y * f;
+                o += x[i] * f;
+            }
         }
+    }
+    sums[threadIdx.x] = o;
+    stats[threadIdx.x] = float2{m, l};
+    __syncthreads();
+    if (!real || lane != 0)
+        return;
+    for (int i = 1; i < lanes; i++)
+        m = fmaxf(m, stats[threadIdx.x + i * per].x);
+    const float ref = fq_reference(m);
+    l = 0.0f;
+    o = float4_t{0, 0, 0, 0};
+    for (int i = 0; i < lanes; i++) {
+        const float2 ml = stats[threadIdx.x + i * per];
+        const float f = __builtin_amdgcn_exp2f(ml.x - ref);
+        l += ml.y * f;
+        o += sums[threadIdx.x + i * per] * f;
+    }
     const float inv = fq_inverse(l);
-    uint16_t *to = a.out + t * a.out_stride + r % a.q_heads * a.kv.dim + d;
     u32x2 y;
     if (a.kv.bf16)
         y = u32x2{fq_pack2<true>(o[0] * inv, o[1] * inv), fq_pack2<true>(o[2] * inv, o[3] * inv)};
     else
         y = u32x2{fq_pack2<false>(o[0] * inv, o[1] * inv), fq_pack2<false>(o[2] * inv, o[3] * inv)};
-    *(u32x2 *)to = y;
+    *(u32x2 *)(a.out + t * a.out_stride + h * a.kv.dim + d) = y;
     if (d == 0 && a.lse)
         a.lse[row] = fq_lse(m, l);
 }
@@ -118,23 +184,25 @@ size_t fq_attend_bytes(const FqAttendArgs &a, int cus) { return bytes(a, plan(a,
 hipError_t fq_launch_attend(const FqAttendArgs &a, void *workspace, hipStream_t stream)
 {
     Plan pl = plan(a, fq_device_cus());
+    if (pl.work[0].blocks + pl.work[1].blocks >= FQ_ATTEND_BLOCKS)
+        return hipErrorInvalidConfiguration; // a launch has 2^32 threads at most
     const size_t rows = (size_t)a.seqs.tokens * a.q_heads;
-    for (int i = 0; i < pl.n; i++) {
+    for (int i = 0; i < pl.n; i++)
         if (pl.parts > 1) {
-            pl.piece[i].work.part_o = (float *)workspace;
-            pl.piece[i].work.part_ml = (float2 *)((float *)workspace + rows * pl.parts * a.kv.dim);
+            pl.work[i].part_o = (float *)workspace;
+            pl.work[i].part_ml = (float2 *)((float *)workspace + rows * pl.parts * a.kv.dim);
         }
-        const Piece &p = pl.piece[i];
-        const hipError_t e = p.row_tiles ? fq_launch_attend_few(a, p.work, p.row_tiles, p.grid, stream)
-                                         : fq_launch_attend_many(a, p.work, p.grid, stream);
-        if (e != hipSuccess)
-            return e;
-    }
+    const hipError_t e = (a.kv.bf16 ? fq_launch_attend_bf16 : fq_launch_attend_f16)(a, pl.work[0], pl.work[1], pl.row_tiles[0], pl.row_tiles[1],
+                                                                                    stream);
+    if (e != hipSuccess)
+        return e;
     if (pl.parts == 1)
         return hipSuccess;
-    const int rows_wg = 256 / (a.kv.dim / 4);
-    const dim3 grid(div_up((long long)a.max_q * a.q_heads, rows_wg), 1, a.seqs.seqs);
-    attend_join_kernel<<<grid, 256, 0, stream>>>(a, pl.piece[0].work, pl.piece[1].work, pl.n, pl.piece[0].grid.y,
-                                                 pl.n > 1 ? pl.piece[1].grid.y : 0);
+    const int per = a.kv.dim / 4;
+    int lanes = 1; // of a row: as many as take four parts each at least, where a workgroup has them
+    while (lanes * 4 < pl.parts && per * lanes * 2 <= 256)
+        lanes *= 2;
+    const dim3 grid(div_up((long long)a.max_q * a.q_heads, 256 / (per * lanes)), 1, a.seqs.seqs);
+    attend_join_kernel<<<grid, 256, 0, stream>>>(a, pl.work[0], pl.work[1], pl.n, lanes);
     return hipGetLastError();
 }

@@ -1,15 +1,18 @@
-// Attention of up to 64 rows to a sequence and key head: the single tokens of a decode step, and a few more.
+// Attention of up to 32 rows to a sequence and key head: the single tokens of a decode step, and a few more.
 //
 // Bound by reading the cache once.  A wavefront takes 32 keys at a time, its own ones: the rows of K go from memory straight
 // into the registers of the first product's left operand (a lane holds 16 bytes of a key; any order of the head's
 // dimensions serves if Q has the same), the rows of V pass through a piece of LDS that belongs to the wavefront alone and
 // are read back transposed.  No barrier until the end, where the wavefronts' rows are added up; a lane asks for the next
 // 32 keys as soon as the registers of the last are free, and for the page numbers a step before that.
+#ifndef FQ_ATTEND_FEW_H
+#define FQ_ATTEND_FEW_H
+
 #include "fq_attend.h"
 
-namespace {
+namespace few {
 
-constexpr int WAVES = FQ_FEW_WAVES;
+constexpr int WAVES = FQ_ATTEND_THREADS / 64;
 constexpr int KEYS = 32; // to a wavefront and step
 
 // 16-byte pieces to a row of V in LDS, and where piece c of row r goes: 16 rows of one piece fall on 16 different bank
@@ -24,24 +27,33 @@ struct Place {
     }
 };
 
-// DP: dimensions computed; FULL: the head has all of them; RT: tiles of 16 rows.
+// LDS of a workgroup.
+template <int DP, int RT>
+struct Lds {
+    static constexpr int WAVE = KEYS * Place<DP>::PITCH * 16; // a wavefront's V, its part of the rows at the end
+    static_assert(WAVE >= 16 * DP * 4, "the rows are added up in the same piece");
+    alignas(16) char v[WAVES * WAVE];
+    float m[WAVES][RT * 16], l[WAVES][RT * 16];
+};
+
+// Workgroup `at` of the launch.  DP: dimensions computed; FULL: the head has all of them; RT: tiles of 16 rows.
 template <bool BF16, int DP, bool FULL, int RT>
-__global__ __launch_bounds__(WAVES * 64) void attend_few_kernel(FqAttendArgs a, FqAttendWork w)
+__device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork &w, dim3 at_block, Lds<DP, RT> &shared)
 {
     constexpr int NS = DP / 32, ND = DP / 16;
-    constexpr int WAVE_LDS = KEYS * Place<DP>::PITCH * 16;
-    static_assert(WAVE_LDS >= 16 * DP * 4, "the rows are added up in the same piece");
-    __shared__ alignas(16) char lds[WAVES * WAVE_LDS];
-    __shared__ float all_m[WAVES][RT * 16], all_l[WAVES][RT * 16];
+    constexpr int WAVE_LDS = Lds<DP, RT>::WAVE;
+    char *const lds = shared.v;
+    auto &all_m = shared.m;
+    auto &all_l = shared.l;
 
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
-    const int head = blockIdx.x % a.kv.kv_heads, row0 = blockIdx.x / a.kv.kv_heads * (16 * RT), b = blockIdx.z;
+    const int head = at_block.x % a.kv.kv_heads, row0 = at_block.x / a.kv.kv_heads * (16 * RT), b = at_block.z;
     const int group = a.q_heads / a.kv.kv_heads, dim = FULL ? DP : a.kv.dim;
     const FqAttendRows rs = fq_attend_rows(a, w, b, group);
     if (row0 >= rs.rows)
         return;
     const int last = min(row0 + 16 * RT, rs.rows) - 1;
-    const long long begin64 = w.key0 + (long long)blockIdx.y * w.chunk;
+    const long long begin64 = w.key0 + (long long)at_block.y * w.chunk;
     const int most = rs.limit(last / group);
     if (begin64 >= most && w.part_o)
         return; // nobody reads this part
@@ -64,7 +76,7 @@ __global__ __launch_bounds__(WAVES * 64) void attend_few_kernel(FqAttendArgs a, 
             const int d = 32 * s + 8 * quad;
             q[rt][s] = u32x4{0, 0, 0, 0};
             if (real && (FULL || d < dim))
-                q[rt][s] = *(const u32x4 *)(from + d);
+                q[rt][s] = fq_signed(*(const u32x4 *)(from + d), a.scale);
         }
     }
 
@@ -78,7 +90,7 @@ __global__ __launch_bounds__(WAVES * 64) void attend_few_kernel(FqAttendArgs a, 
         for (int d = 0; d < ND; d++)
             o[rt][d] = float4_t{0, 0, 0, 0};
     }
-    const float c = a.scale * FQ_LOG2E;
+    const float c = fq_score_factor(a.scale);
     const int32_t *table = a.seqs.table + (rs.shared ? 0 : (long long)b * a.seqs.table_width);
     char *mine = lds + wave * WAVE_LDS;
 
@@ -167,7 +179,7 @@ __global__ __launch_bounds__(WAVES * 64) void attend_few_kernel(FqAttendArgs a, 
             float x[8];
 #pragma unroll
             for (int i = 0; i < 8; i++)
-                x[i] = sc[rt][i >> 2][i & 3] * c;
+                x[i] = sc[rt][i >> 2][i & 3];
             if (masked) {
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
@@ -177,7 +189,7 @@ __global__ __launch_bounds__(WAVES * 64) void attend_few_kernel(FqAttendArgs a, 
                 }
             }
             float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-            top = fq_over32<false>(fq_over16<false>(top));
+            top = fq_over32<false>(fq_over16<false>(top)) * c;
             if (__any(top > m[rt] + FQ_ATTEND_SLACK)) {
                 const float now = fmaxf(m[rt], top);
                 const float fall = __builtin_amdgcn_exp2f(m[rt] - fq_reference(now));
@@ -191,7 +203,7 @@ __global__ __launch_bounds__(WAVES * 64) void attend_few_kernel(FqAttendArgs a, 
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                x[i] = __builtin_amdgcn_exp2f(x[i] - ref);
+                x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, -ref));
                 sum += x[i];
             }
             l[rt] += sum;
@@ -266,7 +278,7 @@ __global__ __launch_bounds__(WAVES * 64) void attend_few_kernel(FqAttendArgs a, 
             const long long t = rs.q0 + r / group;
             const int h = head * group + r % group;
             if (w.part_o) {
-                const long long at = (w.part0 + (long long)blockIdx.y) * rows_all + t * a.q_heads + h;
+                const long long at = (w.part0 + (long long)at_block.y) * rows_all + t * a.q_heads + h;
                 *(float4_t *)(w.part_o + at * dim + d) = float4_t{sum[0], sum[1], sum[2], sum[3]};
                 *(float4_t *)(w.part_o + at * dim + d + 4) = float4_t{sum[4], sum[5], sum[6], sum[7]};
                 if (d == 0)
@@ -285,34 +297,6 @@ __global__ __launch_bounds__(WAVES * 64) void attend_few_kernel(FqAttendArgs a, 
     }
 }
 
-template <bool BF16, int DP, bool FULL>
-hipError_t launch(const FqAttendArgs &a, const FqAttendWork &w, int row_tiles, dim3 grid, hipStream_t stream)
-{
-    if (row_tiles == 1)
-        attend_few_kernel<BF16, DP, FULL, 1><<<grid, WAVES * 64, 0, stream>>>(a, w);
-    else if (row_tiles == 2 || DP > 128)
-        attend_few_kernel<BF16, DP, FULL, 2><<<grid, WAVES * 64, 0, stream>>>(a, w);
-    else if constexpr (DP <= 128)
-        attend_few_kernel<BF16, DP, FULL, 4><<<grid, WAVES * 64, 0, stream>>>(a, w);
-    return hipGetLastError();
-}
+} // namespace few
 
-template <bool BF16>
-hipError_t by_width(const FqAttendArgs &a, const FqAttendWork &w, int row_tiles, dim3 grid, hipStream_t stream)
-{
-    const int dim = a.kv.dim;
-    if (dim == 64)
-        return launch<BF16, 64, true>(a, w, row_tiles, grid, stream);
-    if (dim == 128)
-        return launch<BF16, 128, true>(a, w, row_tiles, grid, stream);
-    if (dim <= 96)
-        return launch<BF16, 96, false>(a, w, row_tiles, grid, stream);
-    return launch<BF16, 256, false>(a, w, row_tiles, grid, stream);
-}
-
-} // namespace
-
-hipError_t fq_launch_attend_few(const FqAttendArgs &a, const FqAttendWork &w, int row_tiles, dim3 grid, hipStream_t stream)
-{
-    return a.kv.bf16 ? by_width<true>(a, w, row_tiles, grid, stream) : by_width<false>(a, w, row_tiles, grid, stream);
-}
+#endif

@@ -3,11 +3,13 @@
 // Bound by the matrix cores and by the exponentials between the two products.  Four wavefronts take 32 rows each and share
 // tiles of 64 keys in LDS, two of them in turn: while one is computed the next one's rows are in flight to registers, and go
 // to the other tile before the one barrier of a step.
+#ifndef FQ_ATTEND_MANY_H
+#define FQ_ATTEND_MANY_H
+
 #include "fq_attend.h"
 
-namespace {
+namespace many {
 
-constexpr int THREADS = 256;
 constexpr int KEYS = 64;
 
 // 16-byte pieces to a key in LDS, and where piece c of key r goes: 16 keys of one piece (the reads of K), 4 keys of four pieces
@@ -22,24 +24,33 @@ struct Place {
     }
 };
 
+// LDS of a workgroup.
+template <int DP>
+struct Lds {
+    static constexpr int TILE = KEYS * Place<DP>::PITCH * 16;
+    alignas(16) char tiles[4 * TILE]; // K, V; K, V
+    uint64_t missing[2][4];           // keys of a tile that are not there, by the wavefront that fetched them
+};
+
+// Workgroup `at` of the launch.  DP: dimensions computed; FULL: the head has all of them.
 template <bool BF16, int DP, bool FULL>
-__global__ __launch_bounds__(THREADS, DP <= 128 ? 2 : 1) void attend_many_kernel(FqAttendArgs a, FqAttendWork w)
+__device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork &w, dim3 at_block, Lds<DP> &shared)
 {
     constexpr int NQ = DP / 16, ND = DP / 32, NC = DP / 32; // steps of the first product, tiles of dimensions, pieces to a thread
-    constexpr int TILE = KEYS * Place<DP>::PITCH * 16;
-    __shared__ alignas(16) char lds[4 * TILE]; // K, V; K, V
-    __shared__ uint64_t missing[2][4];         // keys of a tile that are not there, by the wavefront that fetched them
+    constexpr int TILE = Lds<DP>::TILE;
+    char *const lds = shared.tiles;
+    auto &missing = shared.missing;
 
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
-    const int head = blockIdx.x % a.kv.kv_heads, b = blockIdx.z;
+    const int head = at_block.x % a.kv.kv_heads, b = at_block.z;
     // the last rows see most keys: they begin first
-    const int row0 = (w.row_blocks - 1 - (int)(blockIdx.x / a.kv.kv_heads)) * FQ_MANY_ROWS;
+    const int row0 = (w.row_blocks - 1 - (int)(at_block.x / a.kv.kv_heads)) * FQ_MANY_ROWS;
     const int group = a.q_heads / a.kv.kv_heads, dim = FULL ? DP : a.kv.dim;
     const FqAttendRows rs = fq_attend_rows(a, w, b, group);
     if (row0 >= rs.rows)
         return;
     const int last = min(row0 + FQ_MANY_ROWS, rs.rows) - 1;
-    const long long begin64 = w.key0 + (long long)blockIdx.y * w.chunk;
+    const long long begin64 = w.key0 + (long long)at_block.y * w.chunk;
     const int most = rs.limit(last / group);
     if (begin64 >= most && w.part_o)
         return; // nobody reads this part
@@ -62,7 +73,7 @@ __global__ __launch_bounds__(THREADS, DP <= 128 ? 2 : 1) void attend_many_kernel
             const int d = 16 * s + 8 * half;
             q[s] = u32x4{0, 0, 0, 0};
             if (real && (FULL || d < dim))
-                q[s] = *(const u32x4 *)(from + d);
+                q[s] = fq_signed(*(const u32x4 *)(from + d), a.scale);
         }
     }
     float16_t o[ND];
@@ -72,7 +83,7 @@ __global__ __launch_bounds__(THREADS, DP <= 128 ? 2 : 1) void attend_many_kernel
         for (int i = 0; i < 16; i++)
             o[d][i] = 0.0f;
     float m = -INFINITY, l = 0.0f;
-    const float c = a.scale * FQ_LOG2E;
+    const float c = fq_score_factor(a.scale);
     const int32_t *table = a.seqs.table + (rs.shared ? 0 : (long long)b * a.seqs.table_width);
 
     // fetching: thread -> key threadIdx.x / 4 of a tile, pieces threadIdx.x % 4 + 4 i of its rows of K and V
@@ -145,7 +156,6 @@ __global__ __launch_bounds__(THREADS, DP <= 128 ? 2 : 1) void attend_many_kernel
             for (int t = 0; t < 2; t++)
 #pragma unroll
                 for (int i = 0; i < 16; i++) {
-                    sc[t][i] *= c;
                     if (masked) {
                         const int at = 32 * t + 8 * (i >> 2) + 4 * half + (i & 3);
                         const uint64_t gone = t == 0 ? (i < 8 ? gone0 : gone1) : (i < 8 ? gone2 : gone3);
@@ -154,7 +164,7 @@ __global__ __launch_bounds__(THREADS, DP <= 128 ? 2 : 1) void attend_many_kernel
                     }
                     top = fmaxf(top, sc[t][i]);
                 }
-            top = fq_over32<false>(top);
+            top = fq_over32<false>(top) * c;
             if (__any(top > m + FQ_ATTEND_SLACK)) {
                 const float now = fmaxf(m, top);
                 const float fall = __builtin_amdgcn_exp2f(m - fq_reference(now));
@@ -171,7 +181,7 @@ __global__ __launch_bounds__(THREADS, DP <= 128 ? 2 : 1) void attend_many_kernel
             for (int t = 0; t < 2; t++)
 #pragma unroll
                 for (int i = 0; i < 16; i++) {
-                    sc[t][i] = __builtin_amdgcn_exp2f(sc[t][i] - ref);
+                    sc[t][i] = __builtin_amdgcn_exp2f(fmaf(sc[t][i], c, -ref));
                     l += sc[t][i];
                 }
 #pragma unroll
@@ -200,7 +210,7 @@ __global__ __launch_bounds__(THREADS, DP <= 128 ? 2 : 1) void attend_many_kernel
     const long long t = rs.q0 + j;
     // register i of tile d holds dimension 32 d + 8 (i / 4) + 4 half + i % 4
     if (w.part_o) {
-        const long long at = (w.part0 + (long long)blockIdx.y) * a.seqs.tokens * a.q_heads + t * a.q_heads + h;
+        const long long at = (w.part0 + (long long)at_block.y) * a.seqs.tokens * a.q_heads + t * a.q_heads + h;
 #pragma unroll
         for (int d = 0; d < ND; d++)
 #pragma unroll
@@ -228,24 +238,6 @@ __global__ __launch_bounds__(THREADS, DP <= 128 ? 2 : 1) void attend_many_kernel
     }
 }
 
-template <bool BF16>
-hipError_t by_width(const FqAttendArgs &a, const FqAttendWork &w, dim3 grid, hipStream_t stream)
-{
-    const int dim = a.kv.dim;
-    if (dim == 64)
-        attend_many_kernel<BF16, 64, true><<<grid, THREADS, 0, stream>>>(a, w);
-    else if (dim == 128)
-        attend_many_kernel<BF16, 128, true><<<grid, THREADS, 0, stream>>>(a, w);
-    else if (dim <= 96)
-        attend_many_kernel<BF16, 96, false><<<grid, THREADS, 0, stream>>>(a, w);
-    else
-        attend_many_kernel<BF16, 256, false><<<grid, THREADS, 0, stream>>>(a, w);
-    return hipGetLastError();
-}
+} // namespace many
 
-} // namespace
-
-hipError_t fq_launch_attend_many(const FqAttendArgs &a, const FqAttendWork &w, dim3 grid, hipStream_t stream)
-{
-    return a.kv.bf16 ? by_width<true>(a, w, grid, stream) : by_width<false>(a, w, grid, stream);
-}
+#endif

@@ -67,7 +67,7 @@ def test_layouts_and_parts_of_a_head(dtype, interleaved, dim, rot):
 @pytest.mark.parametrize("new,kv,page", [([1], [1], 16), ([1], [1000], 16), ([2048], [2048], 64), ([1] * 70, list(range(1, 71)), 8),
                                          ([0, 3, 0, 0, 2, 0], [5, 3, 0, 7, 9, 0], 1), ([33], [40], 65536)])
 def test_batches(heads, new, kv, page):
-    if page == 65536 and heads[1] > 8:
+    if page == 65536 and heads[1] > 1:
         pytest.skip("large pages once are enough")
     run(Batch(new, kv, page, spare=1), heads[0], heads[1], 64 if page == 65536 else 128, 64, False, torch.float16)
 
