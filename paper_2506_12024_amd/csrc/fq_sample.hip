@@ -22,6 +22,7 @@ constexpr int ROOTS = 64;    // steps of an octave
 constexpr int BINS = 2048;   // pairs of steps from the top, 64 octaves; the last one holds what lies further down (weight 0)
 constexpr int STRETCHES = 64;
 constexpr int LIST = 8192;  // entries of the list of step 2
+constexpr int FEW = 256;     // entries of a list that need no histogram
 constexpr int CELL = 1024;  // entries of one step that are put in order there
 typedef unsigned long long u64;
 
@@ -65,8 +66,8 @@ struct Depth {
 
 // The weight of a logit, 2^((n + f) / 64): table[n % 64] times a polynomial in f (the series to the fifth power, under 2^-54 left
 // out) times 2^(n / 64).  Whole numbers are taken from the low bits of a sum with a power of two, which rounds to nearest as it
-// is formed: no conversions between double and integer.  The coefficients stay in scalar registers (pinned: as literals each
-// took a move of its own).
+// is formed: no conversions between double and integer.  The coefficients stay in vector registers (pinned: as literals or in
+// scalar ones they took nine moves to a weight).
 struct Weigh {
     double top;   // the largest logit
     double scale; // 64 / (temperature * ln 2)
@@ -76,7 +77,7 @@ struct Weigh {
     __device__ __forceinline__ Weigh(float top_, double scale_, double least_, const double *table_)
         : top(top_), scale(scale_), least(least_), table(table_)
     {
-        asm volatile("" : "+s"(c1), "+s"(c2), "+s"(c3), "+s"(c4), "+s"(c5));
+        asm volatile("" : "+v"(c1), "+v"(c2), "+v"(c3), "+v"(c4), "+v"(c5));
     }
     __device__ __forceinline__ Depth depth(float l) const
     {
@@ -176,10 +177,12 @@ __device__ __forceinline__ u64 running(Shared &s, u64 v, u64 &all)
     return before + v;
 }
 
-// The row.  each(f) calls f(logit, index) for every entry once, all 64 lanes of a wavefront together (-inf where there is no
-// entry); stretches(f, g) besides g(stretch) after each of the wavefront's stretches of `length` entries (a multiple of 64 VEC).
-template <class T, int VEC>
+// The row.  each(f) calls f(logits, index of the first) for every VEC entries once, all 64 lanes of a wavefront together (-inf where
+// there is no entry); stretches(f, g) besides g(stretch) after each of the wavefront's stretches of `length` entries (a multiple of
+// 64 VEC).
+template <class T, int VEC_>
 struct Row {
+    static constexpr int VEC = VEC_;
     const T *x;
     int V, length;
     bool infinite; // +inf is the largest: such entries count as 0, all others as -inf
@@ -223,9 +226,7 @@ struct Row {
 #pragma unroll
                             for (int e = 0; e < VEC; e++)
                                 l[b][e] = fold(l[b][e]);
-#pragma unroll
-                        for (int e = 0; e < VEC; e++)
-                            f(l[b][e], first + (b * 64 + lane) * VEC + e);
+                        f(l[b], first + (b * 64 + lane) * VEC);
                     }
             }
             g(part);
@@ -241,6 +242,7 @@ struct Row {
 // The row, with what is to be done at the end of a stretch.
 template <class R, class G>
 struct RowOf {
+    static constexpr int VEC = R::VEC;
     const R &row;
     const G &end;
     template <class F>
@@ -251,13 +253,16 @@ struct RowOf {
 };
 
 struct Listed {
+    static constexpr int VEC = 1;
     const Shared *s;
     int n;
     template <class F>
     __device__ __forceinline__ void each(const F &f) const
     {
-        for (int at = threadIdx.x; at - (int)threadIdx.x < n; at += THREADS)
-            f(at < n ? s->list_l[at] : -INFINITY, at < n ? s->list_i[at] : 0);
+        for (int at = threadIdx.x; at - (int)threadIdx.x < n; at += THREADS) {
+            const float l[1] = {at < n ? s->list_l[at] : -INFINITY};
+            f(l, at < n ? s->list_i[at] : 0);
+        }
     }
 };
 
@@ -346,39 +351,65 @@ __device__ __forceinline__ bool cut_at(Shared &s, const Source &src, const Weigh
     if (threadIdx.x == 0)
         s.count = 0;
     __syncthreads();
-    src.each([&](float l, int i) {
-        const Depth d = weigh.depth(l);
-        const int b = Weigh::bin(d);
-        if (__all(b == BINS - 1))
+    constexpr int VEC = Source::VEC;
+    src.each([&](const float (&l)[VEC], int i) {
+        Depth d[VEC];
+        int nearest = BINS, farthest = 0;
+#pragma unroll
+        for (int e = 0; e < VEC; e++) {
+            d[e] = weigh.depth(l[e]);
+            nearest = min(nearest, Weigh::bin(d[e]));
+            farthest = max(farthest, Weigh::bin(d[e]));
+        }
+        if (__all(nearest == BINS - 1))
             return;
-        const u64 w = weight(l, i, d);
-        const int one = __builtin_amdgcn_readfirstlane(b);
-        if (__all(b == one)) { // (a flat row: 64 additions to one place would wait for each other)
-            const u64 sum = wave_sum(w);
+        const int one = __builtin_amdgcn_readfirstlane(nearest);
+        if (__all(nearest == one && farthest == one)) { // (a flat row: additions to one place would wait for each other)
+            u64 sum = 0;
+#pragma unroll
+            for (int e = 0; e < VEC; e++)
+                sum += weight(l[e], i + e, d[e]);
+            sum = wave_sum(sum);
             if ((threadIdx.x & 63) == 0)
                 atomicAdd(&s.bins[one], sum);
-        } else if (w) {
-            atomicAdd(&s.bins[b], w);
+            return;
         }
+        u64 w[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; e++)
+            w[e] = weight(l[e], i + e, d[e]);
+#pragma unroll
+        for (int e = 0; e < VEC; e++)
+            if (w[e])
+                atomicAdd(&s.bins[Weigh::bin(d[e])], w[e]);
     });
     u64 target = 0;
     if (!find_bin<BINS>(s, [&](u64 all) { return target = target_of(all); }))
         return false;
     const int cell = (int)s.word[0];
     const u64 left = s.word[1];
-    src.each([&](float l, int i) {
-        const Depth d = weigh.depth(l);
-        const int b = Weigh::bin(d);
-        if (!__any(b <= cell))
+    src.each([&](const float (&l)[VEC], int i) {
+        Depth d[VEC];
+        int nearest = BINS;
+#pragma unroll
+        for (int e = 0; e < VEC; e++) {
+            d[e] = weigh.depth(l[e]);
+            nearest = min(nearest, Weigh::bin(d[e]));
+        }
+        if (!__any(nearest <= cell))
             return;
-        if (b < cell)
-            above(l, i, d);
-        if (b == cell) {
-            const u64 w = weight(l, i, d);
-            const int at = w ? atomicAdd(&s.count, 1) : CELL;
-            if (at < CELL) {
-                s.cell_key[at] = standing(l, i);
-                s.cell_w[at] = w;
+#pragma unroll
+        for (int e = 0; e < VEC; e++) {
+            const int b = Weigh::bin(d[e]);
+            if (b < cell)
+                above(l[e], i + e, d[e]);
+            if (b == cell) {
+                const u64 w = weight(l[e], i + e, d[e]);
+                const int at = w ? atomicAdd(&s.count, 1) : CELL;
+                if (at < CELL) {
+                    s.cell_key[at] = standing(l[e], i + e);
+                    s.cell_w[at] = w;
+                }
             }
         }
     });
@@ -387,12 +418,23 @@ __device__ __forceinline__ bool cut_at(Shared &s, const Source &src, const Weigh
     if (n > CELL) {
         n = -1;
         cut = cut_of(reach<64>(s, [&](const auto &visit) {
-            src.each([&](float l, int i) { visit(standing(l, i), weight(l, i, weigh.depth(l))); });
+            src.each([&](const float (&l)[VEC], int i) {
+#pragma unroll
+                for (int e = 0; e < VEC; e++)
+                    visit(standing(l[e], i + e), weight(l[e], i + e, weigh.depth(l[e])));
+            });
         }, target));
     } else {
         cut = cut_of(reach_cell(s, n, left));
     }
     return true;
+}
+
+// The draw takes the first entry whose running sum is above this.
+__device__ __forceinline__ u64 target_of(float u, u64 all)
+{
+    bool rest;
+    return u >= 1.0f ? all - 1 : u > 0.0f ? share(u, all, rest) : 0;
 }
 
 // The draw among the kept entries, whose sums over the stretches are there.
@@ -403,8 +445,7 @@ __device__ __forceinline__ void draw(Shared &s, const Row<T, VEC> &row, const We
     __syncthreads();
     u64 all;
     const u64 mine = threadIdx.x < STRETCHES ? s.stretch[threadIdx.x] : 0, to = running(s, mine, all);
-    bool rest;
-    const u64 target = u >= 1.0f ? all - 1 : u > 0.0f ? share(u, all, rest) : 0; // the first running sum above it
+    const u64 target = target_of(u, all);
     if (to - mine <= target && target < to) {
         s.word[0] = threadIdx.x;
         s.word[1] = target - (to - mine);
@@ -431,6 +472,54 @@ __device__ __forceinline__ void draw(Shared &s, const Row<T, VEC> &row, const We
     }
 }
 
+// All of it for a list of at most FEW entries, four threads to each: its place among them and what stands before it, then
+// the running sum by index.
+template <class Nucleus>
+__device__ __forceinline__ void draw_few(Shared &s, int n, const Weigh &weigh, int k, float p, const Nucleus &nucleus, float u, int32_t *token,
+                                         float *prob)
+{
+    const int mine = threadIdx.x >> 2, part = threadIdx.x & 3;
+    const bool real = mine < n;
+    const float l = real ? s.list_l[mine] : -INFINITY;
+    const int at = real ? s.list_i[mine] : 0;
+    const Depth d = weigh.depth(l);
+    const u64 key = standing(l, at), w = real ? Weigh::whole(weigh.value(d)) : 0;
+    if (real && part == 0) {
+        s.cell_key[mine] = key;
+        s.cell_w[mine] = w;
+    }
+    __syncthreads();
+    int ahead = 0;
+    u64 before = 0;
+    for (int i = part; i < n; i += 4) {
+        const bool larger = s.cell_key[i] > key;
+        ahead += larger;
+        before += larger ? s.cell_w[i] : 0;
+    }
+    ahead += __shfl_xor(ahead, 1);
+    ahead += __shfl_xor(ahead, 2);
+    before += __shfl_xor(before, 1);
+    before += __shfl_xor(before, 2);
+    u64 all;
+    running(s, ahead < k && part == 0 ? w : 0, all); // (its barriers part the reads above from the writes below)
+    const u64 target = p >= 1.0f ? all : nucleus(all);
+    const u64 kept = ahead < k && before < target && real ? weigh.kept(d) : 0;
+    if (real && part == 0)
+        s.cell_w[mine] = kept;
+    running(s, part == 0 ? kept : 0, all);
+    const u64 to = target_of(u, all);
+    u64 sum = 0;
+    for (int i = part; i < n; i += 4)
+        sum += s.list_i[i] < at ? s.cell_w[i] : 0;
+    sum += __shfl_xor(sum, 1);
+    sum += __shfl_xor(sum, 2);
+    if (part == 0 && sum <= to && to < sum + kept) {
+        *token = at;
+        if (prob)
+            *prob = (float)((double)kept / (double)all);
+    }
+}
+
 template <class T, int VEC>
 __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double unit, int length)
 {
@@ -446,11 +535,13 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
         s.stretch[tid] = 0;
     float mine = -INFINITY;
     int at = 0;
-    row.each([&](float l, int i) {
-        if (l > mine) {
-            mine = l;
-            at = i;
-        }
+    row.each([&](const float (&l)[VEC], int i) {
+#pragma unroll
+        for (int e = 0; e < VEC; e++)
+            if (l[e] > mine) {
+                mine = l[e];
+                at = i + e;
+            }
     });
     u64 best = standing(mine, at);
     for (int o = 32; o; o >>= 1) {
@@ -510,29 +601,36 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
         if (tid == 0)
             s.count = 0;
         __syncthreads();
-        row.each([&](float l, int i) {
-            const bool in = l >= least_l;
-            const u64 who = __ballot(in);
-            if (who) {
-                int base = 0;
-                if (lane == 0)
-                    base = atomicAdd(&s.count, __popcll(who));
-                const int to = __builtin_amdgcn_readfirstlane(base) + __popcll(who & ((1ULL << lane) - 1));
-                if (in && to < LIST) {
-                    s.list_l[to] = l;
-                    s.list_i[to] = i;
+        row.each([&](const float (&l)[VEC], int i) {
+            float largest = l[0];
+#pragma unroll
+            for (int e = 1; e < VEC; e++)
+                largest = fmaxf(largest, l[e]);
+            if (!__any(largest >= least_l))
+                return;
+#pragma unroll
+            for (int e = 0; e < VEC; e++)
+                if (l[e] >= least_l) {
+                    const int to = atomicAdd(&s.count, 1);
+                    if (to < LIST) {
+                        s.list_l[to] = l[e];
+                        s.list_i[to] = i + e;
+                    }
                 }
-            }
         });
         __syncthreads();
         const int n = s.count;
+        if (n <= FEW) {
+            draw_few(s, n, weigh, k, p, nucleus, u, a.token + r, a.prob ? a.prob + r : nullptr);
+            return;
+        }
         if (n <= LIST) {
             const Listed list{&s, n};
             cut_at(s, list, weigh, count, [&](u64) { return (u64)k; }, nothing, cut, in_cell);
             if (!(p >= 1.0f))
                 cut_at(s, list, weigh, weight, nucleus, nothing, cut, in_cell);
-            list.each([&](float l, int i) {
-                const u64 w = cut.keeps(l, i) ? weigh.kept(weigh.depth(l)) : 0;
+            list.each([&](const float (&l)[1], int i) {
+                const u64 w = cut.keeps(l[0], i) ? weigh.kept(weigh.depth(l[0])) : 0;
                 if (w)
                     atomicAdd(&s.stretch[i / length], w);
             });
@@ -570,12 +668,24 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
         }
     }
     if (!summed && cut.l == -INFINITY && weigh.least == 0.0)
-        row.stretches([&](float l, int) { sum += Weigh::whole(weigh.value(weigh.depth(l))); }, add_stretch);
+        row.stretches([&](const float (&l)[VEC], int) {
+#pragma unroll
+            for (int e = 0; e < VEC; e++)
+                sum += Weigh::whole(weigh.value(weigh.depth(l[e])));
+        }, add_stretch);
     else if (!summed)
-        row.stretches([&](float l, int i) {
-            const Depth d = weigh.depth(l);
-            if (__any(d.n >= least_n))
-                sum += cut.keeps(l, i) ? weigh.kept(d) : 0;
+        row.stretches([&](const float (&l)[VEC], int i) {
+            Depth d[VEC];
+            int nearest = -BINS * 2;
+#pragma unroll
+            for (int e = 0; e < VEC; e++) {
+                d[e] = weigh.depth(l[e]);
+                nearest = max(nearest, d[e].n);
+            }
+            if (__any(nearest >= least_n))
+#pragma unroll
+                for (int e = 0; e < VEC; e++)
+                    sum += cut.keeps(l[e], i + e) ? weigh.kept(d[e]) : 0;
         }, add_stretch);
     draw(s, row, weigh, cut, u, a.token + r, a.prob ? a.prob + r : nullptr);
 }
