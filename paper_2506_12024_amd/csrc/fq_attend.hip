@@ -33,9 +33,10 @@ FqAttendWork work(const FqAttendArgs &a, bool shared, int key0, long long keys, 
     const long long steps = div_up(keys > 0 ? keys : 1, step);
     // Steps to a part.  Few rows: all workgroups at once where that takes one step each; else four rounds of them (sequences differ
     // in length), of as many steps that a part's sums (8 bytes to a row and dimension, written and read) are a
-    // sixteenth of its keys and values at most.  Many rows write 64 KiB of sums a part: one round, of four steps at least, and no
-    // parts at all where the rows alone make a round.
-    const long long slots = (row_tiles ? 3LL : a.kv.dim > 96 && a.kv.dim != 128 ? 1LL : 2LL) * cus;
+    // sixteenth of its keys and values at most.  Many rows write 64 KiB of sums a part: one workgroup to a compute unit (48
+    // sequences behind a prefix of 8197: 66 us with a quarter as many, 48, 52 with half as many again, 54 with twice), of
+    // four steps at least.
+    const long long slots = (row_tiles ? 3LL : 1LL) * cus;
     long long take;
     if (row_tiles) {
         const long long in_block = rows < 16 * row_tiles ? rows : 16 * row_tiles, least = in_block > 8 ? in_block / 4 : 2;
