@@ -1,10 +1,13 @@
 // Attention of many rows to a sequence and key head: prompts, chunks of them, and a prefix that a batch shares.
 //
 // Bound by the matrix cores and by the exponentials between the two products.  Four wavefronts take 32 rows each and share
-// tiles of 64 keys in LDS, two of them in turn: while one is computed the next one's rows are in flight to registers, and go
-// to the other tile before the one barrier of a step.
+// tiles of 64 keys in LDS, two of them in turn.  Rows come through registers, two tiles ahead: while one is computed, the next has
+// had the time of a whole tile to arrive, is written to the other half of LDS at the end and the one barrier of a step follows.
+// (One tile ahead a lone workgroup of a compute unit waited for memory.)
 #ifndef FQ_ATTEND_MANY_H
 #define FQ_ATTEND_MANY_H
+
+#include <type_traits>
 
 #include "fq_attend.h"
 
@@ -12,22 +15,19 @@ namespace many {
 
 constexpr int KEYS = 64;
 
-// 16-byte pieces to a key in LDS, and where piece c of key r goes: 16 keys of one piece (the reads of K), 4 keys of four pieces
-// in a row (the writes, and the transposed reads of V) fall on different bank groups.
+// Where 16-byte piece c of key r lies in a tile: blocks of 16 keys, in them pieces of four a key at a time (64 bytes) key by key, the
+// four turned by the key's number.  16 keys of one piece (the reads of K), 4 keys of four pieces in a row (the writes, and the
+// transposed reads of V) fall on different banks, and all but the lowest bits of a lane's address are constants.
 template <int DP>
-struct Place {
-    static constexpr int PITCH = DP <= 64 ? 8 : DP <= 128 ? 16 : 32;
-    static __device__ __forceinline__ int at(int r, int c)
-    {
-        const int s = PITCH == 8 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : ((r & 3) << 2) | ((r >> 2) & 3);
-        return (r * PITCH + (c ^ s)) << 4;
-    }
-};
+__device__ __forceinline__ constexpr int place(int r, int c)
+{
+    return (r >> 4) * (DP * 32) + (c >> 2) * 1024 + (r & 15) * 64 + (((c & 3) ^ ((r >> 2) & 3)) << 4);
+}
 
 // LDS of a workgroup.
 template <int DP>
 struct Lds {
-    static constexpr int TILE = KEYS * Place<DP>::PITCH * 16;
+    static constexpr int TILE = KEYS * DP * 2;
     alignas(16) char tiles[4 * TILE]; // K, V; K, V
     uint64_t missing[2][4];           // keys of a tile that are not there, by the wavefront that fetched them
 };
@@ -88,67 +88,91 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
 
     // fetching: thread -> key threadIdx.x / 4 of a tile, pieces threadIdx.x % 4 + 4 i of its rows of K and V
     const int my_key = threadIdx.x >> 2, my_piece = threadIdx.x & 3;
-    u32x4 ks[NC], vs[NC];
-    bool there = false;
-    int page = -1;
-    auto fetch = [&](int key) { // from the page found a step before
-        there = page >= 0 && page < a.kv.n_pages;
+    constexpr int DEEP = DP <= 96 ? 2 : 1; // tiles ahead (the registers of a wider head hold one)
+    u32x4 ks[DEEP][NC], vs[DEEP][NC];
+    bool there[DEEP];
+    int page = -1; // of the tile that is fetched next
+    auto find = [&](int key) { page = fq_key_page(a, table, (key < end ? key : end) + my_key, end); };
+    auto fetch = [&](auto P, int key) {
+        const int p = DEEP == 2 ? P.value : 0;
+        there[p] = page >= 0 && page < a.kv.n_pages;
         const u32x4 zero = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < NC; i++)
-            ks[i] = vs[i] = zero;
-        if (there) {
+            ks[p][i] = vs[p][i] = zero;
+        if (there[p]) {
             const long long at = fq_key_offset(a, page, key + my_key, head) + 8 * my_piece;
 #pragma unroll
             for (int i = 0; i < NC; i++) {
                 if (FULL || 32 * i + 8 * my_piece < dim) {
-                    ks[i] = *(const u32x4 *)(a.kv.k + at + 32 * i);
-                    vs[i] = *(const u32x4 *)(a.kv.v + at + 32 * i);
+                    ks[p][i] = *(const u32x4 *)(a.kv.k + at + 32 * i);
+                    vs[p][i] = *(const u32x4 *)(a.kv.v + at + 32 * i);
                 }
             }
         }
     };
-    auto put = [&](int buf) {
-        char *kt = lds + buf * 2 * TILE, *vt = kt + TILE;
+    auto put = [&](auto P) {
+        const int p = DEEP == 2 ? P.value : 0;
+        char *kt = lds + P.value * 2 * TILE + place<DP>(my_key, my_piece), *vt = kt + TILE;
 #pragma unroll
         for (int i = 0; i < NC; i++) {
-            *(u32x4 *)(kt + Place<DP>::at(my_key, my_piece + 4 * i)) = ks[i];
-            *(u32x4 *)(vt + Place<DP>::at(my_key, my_piece + 4 * i)) = vs[i];
+            *(u32x4 *)(kt + 1024 * i) = ks[p][i];
+            *(u32x4 *)(vt + 1024 * i) = vs[p][i];
         }
-        const uint64_t gone = __ballot(!there); // lane 4 k + piece: key 16 wave + k
+        const uint64_t gone = __ballot(!there[p]); // lane 4 k + piece: key 16 wave + k
         if (lane == 0)
-            missing[buf][wave] = gone;
+            missing[P.value][wave] = gone;
     };
+    // a lane's piece of K: key col, dimensions 8 half .. of 16 (even and odd steps); of V: key 4 half + t16 / 4 (and 8 on)
+    const int t16 = lane & 15;
+    const int k_at[2] = {place<DP>(col, half), place<DP>(col, 2 + half)};
+    const int v_key = 4 * half + (t16 >> 2), v_piece = 2 * ((lane >> 4) & 1) + ((t16 & 3) >> 1);
+    const int v_at[2] = {place<DP>(v_key, v_piece) + 8 * (t16 & 1), place<DP>(v_key + 8, v_piece) + 8 * (t16 & 1)};
 
-    if (begin < end) {
-        page = fq_key_page(a, table, begin + my_key, end);
-        fetch(begin);
-        page = fq_key_page(a, table, min(begin + KEYS, end) + my_key, end);
-        put(0);
-    }
-    int buf = 0;
-    for (int key = begin; key < end; key += KEYS, buf ^= 1) {
-        const bool more = key + KEYS < end;
+    constexpr int RING = NQ < 8 ? NQ : 8; // pieces of K and V that are read ahead of the products
+    auto step = [&](auto P, auto Q, int key) { // P, Q: the halves of LDS with this tile and for the next
+        const int p = P.value;
         __syncthreads();
-        if (more) {
-            fetch(key + KEYS);
-            page = fq_key_page(a, table, (key + 2 * KEYS < end ? key + 2 * KEYS : end) + my_key, end);
+        if (key + DEEP * KEYS < end) {
+            fetch(P, key + DEEP * KEYS);
+            find(key + (DEEP + 1) * KEYS);
         }
-        const char *kt = lds + buf * 2 * TILE, *vt = kt + TILE;
+        const char *kt = lds + p * 2 * TILE, *vt = kt + TILE;
         if (key < wave_end) {
             float16_t sc[2];
 #pragma unroll
-            for (int t = 0; t < 2; t++) {
+            for (int t = 0; t < 2; t++)
 #pragma unroll
                 for (int i = 0; i < 16; i++)
                     sc[t][i] = 0.0f;
+            // The compiler reads a piece just before its product and waits for it; here eight are under way.
+            auto piece_k = [&](int i) {
+                const int t = i / NQ, s = i % NQ;
+                return *(const u32x4 *)(kt + k_at[s & 1] + t * (DP * 64) + (s >> 1) * 1024);
+            };
+            auto piece_v = [&](int i) {
+                const int s = i / ND, d = i % ND;
+                const u32x2 lo = fq_read_transposed(vt + v_at[0] + s * (DP * 32) + d * 1024);
+                const u32x2 hi = fq_read_transposed(vt + v_at[1] + s * (DP * 32) + d * 1024);
+                return u32x4{lo[0], lo[1], hi[0], hi[1]};
+            };
+            u32x4 ring[RING];
 #pragma unroll
-                for (int s = 0; s < NQ; s++) {
-                    const u32x4 k = *(const u32x4 *)(kt + Place<DP>::at(32 * t + col, 2 * s + half));
-                    sc[t] = fq_mfma32<BF16>(k, q[s], sc[t]);
-                }
+            for (int i = 0; i < RING; i++)
+                ring[i] = piece_k(i);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 2 * NQ; i++) {
+                sc[i / NQ] = fq_mfma32<BF16>(ring[i % RING], q[i % NQ], sc[i / NQ]);
+                if (i + RING < 2 * NQ)
+                    ring[i % RING] = piece_k(i + RING);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            const uint64_t gone0 = missing[buf][0], gone1 = missing[buf][1], gone2 = missing[buf][2], gone3 = missing[buf][3];
+#pragma unroll
+            for (int i = 0; i < RING; i++)
+                ring[i] = piece_v(i);
+            __builtin_amdgcn_sched_barrier(0);
+            const uint64_t gone0 = missing[p][0], gone1 = missing[p][1], gone2 = missing[p][2], gone3 = missing[p][3];
             const bool masked = (gone0 | gone1 | gone2 | gone3) != 0 || key + KEYS > all_seen;
             // register i of tile t holds key 32 t + 8 (i / 4) + 4 half + i % 4
             float top = -INFINITY;
@@ -184,24 +208,48 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
                     sc[t][i] = __builtin_amdgcn_exp2f(fmaf(sc[t][i], c, -ref));
                     l += sc[t][i];
                 }
+            u32x4 pk[4]; // 16 keys each: 16 s + 4 half + 0 .. 3 and 8 on
 #pragma unroll
-            for (int s = 0; s < 4; s++) { // 16 keys: 16 s + 4 half + 0 .. 3 and 8 on
-                u32x4 p;
+            for (int s = 0; s < 4; s++)
 #pragma unroll
                 for (int e = 0; e < 4; e++)
-                    p[e] = fq_pack2<BF16>(sc[s >> 1][8 * (s & 1) + 2 * e], sc[s >> 1][8 * (s & 1) + 2 * e + 1]);
-                const int t16 = lane & 15, key_at = 16 * s + 4 * half + (t16 >> 2);
+                    pk[s][e] = fq_pack2<BF16>(sc[s >> 1][8 * (s & 1) + 2 * e], sc[s >> 1][8 * (s & 1) + 2 * e + 1]);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int d = 0; d < ND; d++) {
-                    const int piece = 4 * d + 2 * ((lane >> 4) & 1) + ((t16 & 3) >> 1);
-                    const u32x2 lo = fq_read_transposed(vt + Place<DP>::at(key_at, piece) + 8 * (t16 & 1));
-                    const u32x2 hi = fq_read_transposed(vt + Place<DP>::at(key_at + 8, piece) + 8 * (t16 & 1));
-                    o[d] = fq_mfma32<BF16>(u32x4{lo[0], lo[1], hi[0], hi[1]}, p, o[d]);
-                }
+            for (int i = 0; i < 4 * ND; i++) {
+                o[i % ND] = fq_mfma32<BF16>(ring[i % RING], pk[i / ND], o[i % ND]);
+                if (i + RING < 4 * ND)
+                    ring[i % RING] = piece_v(i + RING);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (more)
-            put(buf ^ 1);
+        if (key + KEYS < end)
+            put(Q);
+    };
+    constexpr std::integral_constant<int, 0> EVEN;
+    constexpr std::integral_constant<int, 1> ODD;
+    if (begin < end) {
+        find(begin);
+        fetch(EVEN, begin);
+        find(begin + KEYS);
+        if constexpr (DEEP == 2) {
+            fetch(ODD, begin + KEYS);
+            find(begin + 2 * KEYS);
+        }
+        put(EVEN);
+    }
+    if constexpr (DEEP == 2) {
+        for (int key = begin; key < end; key += 2 * KEYS) {
+            step(EVEN, ODD, key);
+            if (key + KEYS < end)
+                step(ODD, EVEN, key + KEYS);
+        }
+    } else {
+        struct Half {
+            int value;
+        } now{0};
+        for (int key = begin; key < end; key += KEYS, now.value ^= 1)
+            step(now, Half{now.value ^ 1}, key);
     }
 
     l = fq_over32<true>(l);
