@@ -1,13 +1,12 @@
 // Attention of many rows to a sequence and key head: prompts, chunks of them, and a prefix that a batch shares.
 //
 // Bound by the matrix cores and by the exponentials between the two products.  Four wavefronts take 32 rows each and share
-// tiles of 64 keys in LDS, two of them in turn.  Rows come through registers, two tiles ahead: while one is computed, the next has
-// had the time of a whole tile to arrive, is written to the other half of LDS at the end and the one barrier of a step follows.
-// (One tile ahead a lone workgroup of a compute unit waited for memory.)
+// tiles of 64 keys in LDS, two of them in turn; a tile's rows come through registers while the one before is computed.  A wavefront
+// works in steps of 32 keys, three of them under way at once: the matrix cores sum V of the last one and score the next one while the
+// vector units take the exponentials of this one.  (One after the other the two kinds of units waited for each other, two
+// wavefronts to a SIMD or not: 2700 cycles to 64 keys where the products take 1024 and the rest 1200.)
 #ifndef FQ_ATTEND_MANY_H
 #define FQ_ATTEND_MANY_H
-
-#include <type_traits>
 
 #include "fq_attend.h"
 
@@ -88,40 +87,39 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
 
     // fetching: thread -> key threadIdx.x / 4 of a tile, pieces threadIdx.x % 4 + 4 i of its rows of K and V
     const int my_key = threadIdx.x >> 2, my_piece = threadIdx.x & 3;
-    constexpr int DEEP = DP <= 96 ? 2 : 1; // tiles ahead (the registers of a wider head hold one)
-    u32x4 ks[DEEP][NC], vs[DEEP][NC];
-    bool there[DEEP];
+    u32x4 ks[NC], vs[NC];
+    bool there = false;
     int page = -1; // of the tile that is fetched next
     auto find = [&](int key) { page = fq_key_page(a, table, (key < end ? key : end) + my_key, end); };
-    auto fetch = [&](auto P, int key) {
-        const int p = DEEP == 2 ? P.value : 0;
-        there[p] = page >= 0 && page < a.kv.n_pages;
-        const u32x4 zero = {0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < NC; i++)
-            ks[p][i] = vs[p][i] = zero;
-        if (there[p]) {
-            const long long at = fq_key_offset(a, page, key + my_key, head) + 8 * my_piece;
-#pragma unroll
-            for (int i = 0; i < NC; i++) {
-                if (FULL || 32 * i + 8 * my_piece < dim) {
-                    ks[p][i] = *(const u32x4 *)(a.kv.k + at + 32 * i);
-                    vs[p][i] = *(const u32x4 *)(a.kv.v + at + 32 * i);
-                }
-            }
-        }
-    };
-    auto put = [&](auto P) {
-        const int p = DEEP == 2 ? P.value : 0;
-        char *kt = lds + P.value * 2 * TILE + place<DP>(my_key, my_piece), *vt = kt + TILE;
+    auto fetch = [&](int key) {
+        there = page >= 0 && page < a.kv.n_pages;
+        // (a key that is not there is read from the pool's begin, and zeroed when it is put)
+        const long long at = (there ? fq_key_offset(a, page, key + my_key, head) : 0) + 8 * my_piece;
 #pragma unroll
         for (int i = 0; i < NC; i++) {
-            *(u32x4 *)(kt + 1024 * i) = ks[p][i];
-            *(u32x4 *)(vt + 1024 * i) = vs[p][i];
+            const int d = FULL || 32 * i + 8 * my_piece < dim ? 32 * i : -8 * my_piece;
+            ks[i] = *(const u32x4 *)(a.kv.k + at + d);
+            vs[i] = *(const u32x4 *)(a.kv.v + at + d);
         }
-        const uint64_t gone = __ballot(!there[p]); // lane 4 k + piece: key 16 wave + k
+    };
+    auto put = [&](int half_of_lds) {
+        const uint64_t gone = __ballot(!there); // lane 4 k + piece: key 16 wave + k
+        if (gone) {
+            if (!there)
+#pragma unroll
+                for (int i = 0; i < NC; i++)
+                    ks[i] = vs[i] = u32x4{0, 0, 0, 0};
+        }
+        char *kt = lds + half_of_lds * 2 * TILE + place<DP>(my_key, my_piece), *vt = kt + TILE;
+#pragma unroll
+        for (int i = 0; i < NC; i++) {
+            const u32x4 zero = {0, 0, 0, 0};
+            const bool real = FULL || 32 * i + 8 * my_piece < dim;
+            *(u32x4 *)(kt + 1024 * i) = real ? ks[i] : zero;
+            *(u32x4 *)(vt + 1024 * i) = real ? vs[i] : zero;
+        }
         if (lane == 0)
-            missing[P.value][wave] = gone;
+            missing[half_of_lds][wave] = gone;
     };
     // a lane's piece of K: key col, dimensions 8 half .. of 16 (even and odd steps); of V: key 4 half + t16 / 4 (and 8 on)
     const int t16 = lane & 15;
@@ -129,127 +127,128 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
     const int v_key = 4 * half + (t16 >> 2), v_piece = 2 * ((lane >> 4) & 1) + ((t16 & 3) >> 1);
     const int v_at[2] = {place<DP>(v_key, v_piece) + 8 * (t16 & 1), place<DP>(v_key + 8, v_piece) + 8 * (t16 & 1)};
 
-    constexpr int RING = NQ < 8 ? NQ : 8; // pieces of K and V that are read ahead of the products
-    auto step = [&](auto P, auto Q, int key) { // P, Q: the halves of LDS with this tile and for the next
-        const int p = P.value;
-        __syncthreads();
-        if (key + DEEP * KEYS < end) {
-            fetch(P, key + DEEP * KEYS);
-            find(key + (DEEP + 1) * KEYS);
-        }
-        const char *kt = lds + p * 2 * TILE, *vt = kt + TILE;
-        if (key < wave_end) {
-            float16_t sc[2];
+    float16_t next; // scores of the step to come; register i holds key 8 (i / 4) + 4 half + i % 4 of its 32
+    u32x4 pk[2];    // weights of the last step, 16 keys each
+    pk[0] = pk[1] = u32x4{0, 0, 0, 0};
+    // The products of a step: 2 ND with V of the last one, NQ with K of the next one.
+    constexpr int PRODUCTS = 2 * ND + NQ, AHEAD = 4;
+    auto piece = [&](int i, const char *vt, const char *kt) {
+        if (i >= 2 * ND)
+            return *(const u32x4 *)(kt + k_at[i & 1] + ((i - 2 * ND) >> 1) * 1024);
+        const int at = i / ND * (DP * 32) + i % ND * 1024;
+        const u32x2 lo = fq_read_transposed(vt + v_at[0] + at), hi = fq_read_transposed(vt + v_at[1] + at);
+        return u32x4{lo[0], lo[1], hi[0], hi[1]};
+    };
+    auto product = [&](int i, u32x4 x) {
+        const float16_t zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+        if (i >= 2 * ND)
+            next = fq_mfma32<BF16>(x, q[i - 2 * ND], i == 2 * ND ? zero : next);
+        else
+            o[i % ND] = fq_mfma32<BF16>(x, pk[i / ND], o[i % ND]);
+    };
+    // One step: the keys from `key` on (half `t` of the tile in half `p` of LDS), whose scores are in `next`; V of the
+    // step before at `v_last`, K of the step after at `k_next` (after the last step: any tile, nobody looks at the scores).
+    // Between any two products stands a share of the exponentials (a fence each: left to itself the compiler puts all products
+    // first), and four pieces are on their way from LDS.
+    auto step = [&](int key, int p, int t, const char *v_last, const char *k_next) {
+        float16_t x = next;
+        const uint64_t gone0 = missing[p][2 * t], gone1 = missing[p][2 * t + 1];
+        u32x4 ring[AHEAD];
 #pragma unroll
-            for (int t = 0; t < 2; t++)
+        for (int i = 0; i < AHEAD; i++)
+            ring[i] = piece(i, v_last, k_next);
+        if ((gone0 | gone1) != 0 || key + 32 > all_seen) {
+#pragma unroll
+            for (int i = 0; i < 16; i++) {
+                const int at = 8 * (i >> 2) + 4 * half + (i & 3);
+                if ((((i < 8 ? gone0 : gone1) >> (4 * (at & 15))) & 1) || key + at >= lim)
+                    x[i] = -INFINITY;
+            }
+        }
+        float top = x[0];
+#pragma unroll
+        for (int i = 1; i < 16; i++)
+            top = fmaxf(top, x[i]);
+        top = fq_over32<false>(top) * c;
+        const bool raise = __any(top > m + FQ_ATTEND_SLACK);
+        const float now = raise ? fmaxf(m, top) : m, ref = fq_reference(now);
+        const float fall = __builtin_amdgcn_exp2f(m - ref);
+        l *= fall; // (1 where nothing is raised)
+        m = now;
+        u32x4 weights[2];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < PRODUCTS; i++) {
+            product(i, ring[i % AHEAD]);
+            if (i + AHEAD < PRODUCTS)
+                ring[i % AHEAD] = piece(i + AHEAD, v_last, k_next);
+#pragma unroll
+            for (int e = i * 16 / PRODUCTS; e < (i + 1) * 16 / PRODUCTS; e++) {
+                x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], c, -ref));
+                if (e > 0)
+                    l += x[e - 1]; // (one behind: the exponential takes a while)
+                if (e > 1 && e % 2 == 0)
+                    weights[(e - 2) >> 3][((e - 2) & 7) >> 1] = fq_pack2<BF16>(x[e - 2], x[e - 1]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        l += x[15];
+        weights[1][3] = fq_pack2<BF16>(x[14], x[15]);
+        pk[0] = weights[0];
+        pk[1] = weights[1];
+        int rescale = raise;
+        // (else the compiler moves the exponentials behind this branch)
+        asm volatile("" : "+v"(rescale), "+v"(pk[0]), "+v"(pk[1]), "+v"(l));
+        if (__builtin_amdgcn_readfirstlane(rescale)) {
+#pragma unroll
+            for (int d = 0; d < ND; d++)
 #pragma unroll
                 for (int i = 0; i < 16; i++)
-                    sc[t][i] = 0.0f;
-            // The compiler reads a piece just before its product and waits for it; here eight are under way.
-            auto piece_k = [&](int i) {
-                const int t = i / NQ, s = i % NQ;
-                return *(const u32x4 *)(kt + k_at[s & 1] + t * (DP * 64) + (s >> 1) * 1024);
-            };
-            auto piece_v = [&](int i) {
-                const int s = i / ND, d = i % ND;
-                const u32x2 lo = fq_read_transposed(vt + v_at[0] + s * (DP * 32) + d * 1024);
-                const u32x2 hi = fq_read_transposed(vt + v_at[1] + s * (DP * 32) + d * 1024);
-                return u32x4{lo[0], lo[1], hi[0], hi[1]};
-            };
-            u32x4 ring[RING];
-#pragma unroll
-            for (int i = 0; i < RING; i++)
-                ring[i] = piece_k(i);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < 2 * NQ; i++) {
-                sc[i / NQ] = fq_mfma32<BF16>(ring[i % RING], q[i % NQ], sc[i / NQ]);
-                if (i + RING < 2 * NQ)
-                    ring[i % RING] = piece_k(i + RING);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-#pragma unroll
-            for (int i = 0; i < RING; i++)
-                ring[i] = piece_v(i);
-            __builtin_amdgcn_sched_barrier(0);
-            const uint64_t gone0 = missing[p][0], gone1 = missing[p][1], gone2 = missing[p][2], gone3 = missing[p][3];
-            const bool masked = (gone0 | gone1 | gone2 | gone3) != 0 || key + KEYS > all_seen;
-            // register i of tile t holds key 32 t + 8 (i / 4) + 4 half + i % 4
-            float top = -INFINITY;
-#pragma unroll
-            for (int t = 0; t < 2; t++)
-#pragma unroll
-                for (int i = 0; i < 16; i++) {
-                    if (masked) {
-                        const int at = 32 * t + 8 * (i >> 2) + 4 * half + (i & 3);
-                        const uint64_t gone = t == 0 ? (i < 8 ? gone0 : gone1) : (i < 8 ? gone2 : gone3);
-                        if (((gone >> (4 * (at & 15))) & 1) || key + at >= lim)
-                            sc[t][i] = -INFINITY;
-                    }
-                    top = fmaxf(top, sc[t][i]);
-                }
-            top = fq_over32<false>(top) * c;
-            if (__any(top > m + FQ_ATTEND_SLACK)) {
-                const float now = fmaxf(m, top);
-                const float fall = __builtin_amdgcn_exp2f(m - fq_reference(now));
-                m = now;
-                l *= fall;
-#pragma unroll
-                for (int d = 0; d < ND; d++)
-#pragma unroll
-                    for (int i = 0; i < 16; i++)
-                        o[d][i] *= fall;
-            }
-            const float ref = fq_reference(m);
-#pragma unroll
-            for (int t = 0; t < 2; t++)
-#pragma unroll
-                for (int i = 0; i < 16; i++) {
-                    sc[t][i] = __builtin_amdgcn_exp2f(fmaf(sc[t][i], c, -ref));
-                    l += sc[t][i];
-                }
-            u32x4 pk[4]; // 16 keys each: 16 s + 4 half + 0 .. 3 and 8 on
-#pragma unroll
-            for (int s = 0; s < 4; s++)
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    pk[s][e] = fq_pack2<BF16>(sc[s >> 1][8 * (s & 1) + 2 * e], sc[s >> 1][8 * (s & 1) + 2 * e + 1]);
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int i = 0; i < 4 * ND; i++) {
-                o[i % ND] = fq_mfma32<BF16>(ring[i % RING], pk[i / ND], o[i % ND]);
-                if (i + RING < 4 * ND)
-                    ring[i % RING] = piece_v(i + RING);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+                    o[d][i] *= fall;
         }
-        if (key + KEYS < end)
-            put(Q);
     };
-    constexpr std::integral_constant<int, 0> EVEN;
-    constexpr std::integral_constant<int, 1> ODD;
+
     if (begin < end) {
         find(begin);
-        fetch(EVEN, begin);
+        fetch(begin);
         find(begin + KEYS);
-        if constexpr (DEEP == 2) {
-            fetch(ODD, begin + KEYS);
+        put(0);
+        if (begin + KEYS < end) {
+            fetch(begin + KEYS);
             find(begin + 2 * KEYS);
         }
-        put(EVEN);
     }
-    if constexpr (DEEP == 2) {
-        for (int key = begin; key < end; key += 2 * KEYS) {
-            step(EVEN, ODD, key);
-            if (key + KEYS < end)
-                step(ODD, EVEN, key + KEYS);
+    __syncthreads();
+    constexpr int HALF = DP * 64; // bytes of 32 keys
+    if (begin < wave_end)
+#pragma unroll
+        for (int i = 2 * ND; i < PRODUCTS; i++)
+            product(i, piece(i, lds, lds));
+    const char *v_last = lds + TILE; // (the first step's weights are 0: any V of the tile does)
+    int p = 0;
+    for (int key = begin; key < end; key += KEYS, p ^= 1) {
+        const char *kt = lds + p * 2 * TILE, *vt = kt + TILE, *kn = lds + (p ^ 1) * 2 * TILE;
+        const bool more = key + KEYS < end;
+        if (key < wave_end)
+            step(key, p, 0, v_last, kt + HALF);
+        if (more) {
+            __syncthreads(); // the other half of LDS is read no more
+            put(p ^ 1);
+            if (key + 2 * KEYS < end) {
+                fetch(key + 2 * KEYS);
+                find(key + 3 * KEYS);
+            }
+            __syncthreads();
         }
-    } else {
-        struct Half {
-            int value;
-        } now{0};
-        for (int key = begin; key < end; key += KEYS, now.value ^= 1)
-            step(now, Half{now.value ^ 1}, key);
+        v_last = vt;
+        if (key + 32 < wave_end) {
+            step(key + 32, p, 1, vt, kn);
+            v_last = vt + HALF;
+        }
+        if (key + KEYS >= wave_end && key < wave_end) // the last step's V
+#pragma unroll
+            for (int i = 0; i < 2 * ND; i++)
+                product(i, piece(i, v_last, lds));
     }
 
     l = fq_over32<true>(l);
