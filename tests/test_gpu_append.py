@@ -37,13 +37,13 @@ def run(batch, q_heads, kv_heads, dim, rot, interleaved, dtype, token_major=Fals
         want_k, size_k = turn(f64(k), pos, freqs, rot, interleaved, amplitude)
     else:
         want_q, want_k, size_q, size_k = f64(q), f64(k), 0.0 * f64(q), 0.0 * f64(k)
-    want_kc, size_kc, want_vc = k0, np.zeros_like(k0), v0
+    want_kc, size_kc, want_vc, v64 = k0, np.zeros_like(k0), v0, f64(v)
     for t, (b, p) in enumerate(batch.places()):
         page = batch.table[b, p // batch.page] if p >= 0 else -1
         if 0 <= page < batch.pages:
             want_kc[page, :, p % batch.page] = want_k[t]
             size_kc[page, :, p % batch.page] = size_k[t]
-            want_vc[page, :, p % batch.page] = f64(v)[t]
+            want_vc[page, :, p % batch.page] = v64[t]
 
     def close(got, want, size):
         # one rounding to the type; sine and cosine of a binary32 fraction of a turn (2^-25 of it, 2 pi / turn) and a few
