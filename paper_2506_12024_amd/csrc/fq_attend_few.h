@@ -34,6 +34,7 @@ struct Lds {
     static_assert(WAVE >= 16 * DP * 4, "the rows are added up in the same piece");
     alignas(16) char v[WAVES * WAVE];
     float m[WAVES][RT * 16], l[WAVES][RT * 16];
+    int odd; // some sum is not finite
 };
 
 // Workgroup `at` of the launch.  DP: dimensions computed; FULL: the head has all of them; RT: tiles of 16 rows.
@@ -122,6 +123,8 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
             }
     };
 
+    if (threadIdx.x == 0)
+        shared.odd = 0;
     constexpr int STEP = WAVES * KEYS;
     int key = begin + wave * KEYS;
     if (key < end) {
@@ -235,6 +238,24 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
         if (quad == 0) {
             all_m[wave][rt * 16 + col] = m[rt];
             all_l[wave][rt * 16 + col] = l[rt];
+        }
+    }
+    if (all_seen < end) { // (the same for all threads)
+        __syncthreads();
+        float z = 0.0f;
+#pragma unroll
+        for (int rt = 0; rt < RT; rt++)
+#pragma unroll
+            for (int d = 0; d < ND; d++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    z = fmaf(o[rt][d][i], 0.0f, z);
+        if (z != 0.0f) // (a NaN)
+            shared.odd = 1;
+        __syncthreads();
+        if (shared.odd) {
+            fq_attend_row_by_row<BF16>(a, w, rs, table, at_block.y, head, row0, last, begin, end);
+            return;
         }
     }
     const long long rows_all = (long long)a.seqs.tokens * a.q_heads;

@@ -29,6 +29,7 @@ struct Lds {
     static constexpr int TILE = KEYS * DP * 2;
     alignas(16) char tiles[4 * TILE]; // K, V; K, V
     uint64_t missing[2][4];           // keys of a tile that are not there, by the wavefront that fetched them
+    int odd;                          // some sum is not finite
 };
 
 // Workgroup `at` of the launch.  DP: dimensions computed; FULL: the head has all of them.
@@ -56,6 +57,9 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
     const int begin = begin64 < most ? (int)begin64 : most;
     const int end = (int)(begin64 + w.chunk < most ? begin64 + w.chunk : most);
 
+    if (threadIdx.x == 0)
+        shared.odd = 0;
+    const int block_sees = rs.limit(row0 / group); // every row of the workgroup sees the keys before this one
     const int r = row0 + wave * 32 + col;
     const bool real = r <= last;
     const int j = (real ? r : row0) / group, h = head * group + (real ? r : row0) % group;
@@ -218,13 +222,17 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
             find(begin + 2 * KEYS);
         }
     }
-    __syncthreads();
+    // the first step has none before it: its weights are 0, and so is what they meet, in the half of LDS that is not yet filled
     constexpr int HALF = DP * 64; // bytes of 32 keys
+    char *const none = lds + 3 * TILE;
+    for (int i = threadIdx.x * 16; i < HALF; i += FQ_ATTEND_THREADS * 16)
+        *(u32x4 *)(none + i) = u32x4{0, 0, 0, 0};
+    __syncthreads();
     if (begin < wave_end)
 #pragma unroll
         for (int i = 2 * ND; i < PRODUCTS; i++)
             product(i, piece(i, lds, lds));
-    const char *v_last = lds + TILE; // (the first step's weights are 0: any V of the tile does)
+    const char *v_last = none;
     int p = 0;
     for (int key = begin; key < end; key += KEYS, p ^= 1) {
         const char *kt = lds + p * 2 * TILE, *vt = kt + TILE, *kn = lds + (p ^ 1) * 2 * TILE;
@@ -251,6 +259,21 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
                 product(i, piece(i, v_last, lds));
     }
 
+    if (block_sees < end) { // (the same for all threads)
+        float z[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int d = 0; d < ND; d++)
+#pragma unroll
+            for (int i = 0; i < 16; i++)
+                z[i & 1] = fmaf(o[d][i], 0.0f, z[i & 1]);
+        if (z[0] + z[1] != 0.0f) // (a NaN)
+            shared.odd = 1;
+        __syncthreads();
+        if (shared.odd) {
+            fq_attend_row_by_row<BF16>(a, w, rs, table, at_block.y, head, row0, last, begin, end);
+            return;
+        }
+    }
     l = fq_over32<true>(l);
     if (!real)
         return;

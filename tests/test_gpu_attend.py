@@ -107,6 +107,49 @@ def test_shared_prefixes_of_chunks(new):
     run(Batch(new, new, 8, prefix=64), 8, 2, 64, torch.bfloat16)
 
 
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("heads,dim", [((4, 2), 64), ((8, 1), 128), ((2, 2), 80), ((2, 1), 256)])
+@pytest.mark.parametrize("new,kv", [([4], [200]), ([3, 1], [64, 9]), ([40], [40]), ([150], [390]), ([70, 5], [70, 300])])
+def test_new_tokens_that_are_not_finite_reach_no_earlier_row(dtype, heads, dim, new, kv):
+    """Infinities and NaNs in K and V of a chunk's later tokens: rows before them are as if they were not there, rows that see
+    a NaN are NaN."""
+    batch = Batch(new, kv, 8)
+    gen = torch.Generator().manual_seed(21)
+    kc, vc = (pool(gen, batch.pages, heads[1], 8, dim, TYPES[dtype]) for _ in range(2))
+    q = torch.randn((batch.tokens, heads[0], dim), generator=gen).to(TYPES[dtype]).to(DEV)
+    first_bad = [n - n // 2 for n in new]  # of the new tokens
+    for b, (n, m) in enumerate(zip(new, kv)):
+        for j in range(first_bad[b], n):
+            p = m - n + j
+            vc[int(batch.table[b, p // 8]), :, p % 8, j % dim] = [float("nan"), float("inf"), -float("inf")][j % 3]
+            if j % 2:
+                kc[int(batch.table[b, p // 8]), :, p % 8, 3] = float("nan")
+    out, lse, _ = call(batch, fq.KVCache(kc, vc), q, 0.1)
+    torch.cuda.synchronize()
+    keep = np.concatenate([np.arange(n) < f for n, f in zip(new, first_bad)])
+    want, want_lse, size, steep, mass = attend(batch, f64(q), f64(torch.nan_to_num(kc, 0, 0, 0)), f64(torch.nan_to_num(vc, 0, 0, 0)), 0.1)
+    got, tol = f64(out), attend_tolerance(q.dtype, want, size, steep, mass, dim)
+    assert np.all(np.abs(got[keep] - want[keep]) <= tol[keep])
+    assert np.all(np.abs(f64(lse)[keep] - want_lse[keep]) <= lse_tolerance(want_lse[keep], steep[keep], dim, max(kv)))
+    for b, (n, f) in enumerate(zip(new, first_bad)):
+        for j in range(f, n):  # every row from the first bad token on sees that one's V
+            assert not np.isfinite(got[batch.q_start[b] + j, :, f % dim]).any()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_an_infinite_value_that_is_seen_stays_one(new):
+    batch = Batch([new], [100 + new], 16)
+    gen = torch.Generator().manual_seed(22)
+    kc, vc = (pool(gen, batch.pages, 2, 16, 64, torch.float16) for _ in range(2))
+    vc[int(batch.table[0, 0]), 1, 5, 7] = float("inf")
+    q = torch.randn((new, 4, 64), generator=gen).half().to(DEV)
+    out, _, _ = call(batch, fq.KVCache(kc, vc), q, 0.1)
+    torch.cuda.synchronize()
+    assert torch.all(out[:, 2:, 7] == float("inf"))
+    out[:, 2:, 7] = 0
+    assert torch.all(torch.isfinite(out))
+
+
 def test_rows_that_see_nothing():
     """Lengths of zero, more new tokens than length, no own keys behind a prefix."""
     run(Batch([1, 1, 1], [0, 5, 0], 4), 4, 2, 64, torch.float16)
