@@ -18,12 +18,13 @@ namespace {
 
 constexpr int THREADS = 1024;
 constexpr int WAVES = THREADS / 64;
-constexpr int ROOTS = 64;    // steps of an octave
-constexpr int BINS = 2048;   // pairs of steps from the top, 64 octaves; the last one holds what lies further down (weight 0)
+constexpr int ROOTS = 128;   // steps of an octave
+constexpr int BINS = 2048;   // groups of four steps from the top, 64 octaves; the last one holds what lies further down (weight 0)
 constexpr int STRETCHES = 64;
 constexpr int LIST = 8192;  // entries of the list of step 2
 constexpr int FEW = 256;     // entries of a list that need no histogram
 constexpr int CELL = 1024;  // entries of one step that are put in order there
+constexpr int DEEPEST = -128 * ROOTS; // no entry lies as far down, in steps
 typedef unsigned long long u64;
 
 // Binary32 values as unsigned numbers in the same order, -0 as 0.  (NaNs are nowhere larger or equal and weigh nothing.)
@@ -48,7 +49,7 @@ __device__ __forceinline__ u64 share(float x, u64 w, bool &rest)
     return __umul64hi(f, w);
 }
 
-// 2^(j / 64): the series of exp to the 13th power on an argument of at most ln 2 / 2 (what is left out is under 2^-57)
+// 2^(j / 128): the series of exp to the 13th power on an argument of at most ln 2 / 2 (what is left out is under 2^-57)
 __device__ __forceinline__ double root_of_two(int j)
 {
     const double x = (j > ROOTS / 2 ? j - ROOTS : j) * (0.69314718055994530942 / ROOTS);
@@ -58,55 +59,76 @@ __device__ __forceinline__ double root_of_two(int j)
     return j > ROOTS / 2 ? 2.0 * p : p;
 }
 
-// How far down a logit lies: n + f steps of 1/64 octave, n whole (and not above 0), |f| <= 1/2.
+// How far down a logit lies: n + f steps of 1/128 octave, n whole, |f| <= 1/2.
 struct Depth {
     double f;
     int n;
 };
 
-// The weight of a logit, 2^((n + f) / 64): table[n % 64] times a polynomial in f (the series to the fifth power, under 2^-54 left
-// out) times 2^(n / 64).  Whole numbers are taken from the low bits of a sum with a power of two, which rounds to nearest as it
-// is formed: no conversions between double and integer.  The coefficients stay in vector registers (pinned: as literals or in
-// scalar ones they took nine moves to a weight).
+// The weight of a logit, 2^((n + f) / 128): table[n % 128] times a polynomial in f (the series to the fourth power, under 2^-49
+// left out) times 2^(n / 128).  Binary64 instructions bound the passes over a row, so there are ten of them: the distance from the
+// top is multiplied twice (once rounded to a whole number by a sum with 1.5 * 2^52, once less that number), the weight is rounded to a
+// whole number by the sum with 2^52 that its last product ends in, nothing is converted between double and integer, and what is too far
+// down is held up in binary32.  The coefficients stay in vector registers (pinned: as literals or in scalar ones they took nine
+// moves to a weight).
 struct Weigh {
-    double top;   // the largest logit
-    double scale; // 64 / (temperature * ln 2)
-    double least; // min_p times the unit, 0 for none
+    double top, scale; // the largest logit; 128 / (temperature * ln 2)
+    float lowest;      // 64 octaves down and more (-inf and NaNs too) the weight rounds to 0
+    bool careful;      // temperature or logits so large or small that the above does not hold in binary32, or an infinite top
+    double least;      // min_p times the unit, 0 for none
     const double *table;
-    double c1 = 0.69314718055994530942 / ROOTS, c2 = c1 * c1 / 2, c3 = c1 * c2 / 3, c4 = c1 * c3 / 4, c5 = c1 * c4 / 5;
-    __device__ __forceinline__ Weigh(float top_, double scale_, double least_, const double *table_)
-        : top(top_), scale(scale_), least(least_), table(table_)
+    double c1 = 0.69314718055994530942 / ROOTS, c2 = c1 * c1 / 2, c3 = c1 * c2 / 3, c4 = c1 * c3 / 4;
+    __device__ __forceinline__ Weigh(float top_, double temperature, double least_, const double *table_)
+        : top(top_), scale(ROOTS * 1.4426950408889634074 / temperature), least(least_), table(table_)
     {
-        asm volatile("" : "+v"(c1), "+v"(c2), "+v"(c3), "+v"(c4), "+v"(c5));
+        // one step of binary32 at the top is less than the 64 octaves, and they end above the lowest value
+        const double reach = 64.0 * ROOTS / scale;
+        careful = !(fabs(top) * 0x1p-23 < reach && reach > 1e-30 && fabs(top) + reach < 1e38);
+        if (top_ == INFINITY)
+            scale = INFINITY; // what is finite has no weight
+        lowest = careful ? 0.0f : __double2float_rd(top - 64.0 * ROOTS / scale);
+        asm volatile("" : "+v"(c1), "+v"(c2), "+v"(c3), "+v"(c4));
     }
     __device__ __forceinline__ Depth depth(float l) const
     {
-        // 64 octaves down (and at -inf, and for a NaN) the weight rounds to 0
-        const double t = fmax(((double)l - top) * scale, -64.0 * ROOTS);
-        const double m = t + 0x1.8p52;
-        return Depth{t - (m - 0x1.8p52), (int)(uint32_t)__builtin_bit_cast(u64, m)};
+        double x, s;
+        if (careful) { // (the same for the whole row)
+            x = l == (float)top ? 0.0 : fmax(((double)l - top) * scale, -64.0 * ROOTS);
+            s = 1.0;
+        } else {
+            x = (double)fmaxf(l, lowest) - top;
+            s = scale;
+        }
+        const double m = fma(x, s, 0x1.8p52);
+        return Depth{fma(x, s, 0x1.8p52 - m), (int)(uint32_t)__builtin_bit_cast(u64, m)};
     }
-    // times the unit, not yet rounded
-    __device__ __forceinline__ double value(const Depth &d) const
+    __device__ __forceinline__ double series(double f) const
     {
-        double p = fma(d.f, c5, c4);
-        p = fma(d.f, p, c3);
-        p = fma(d.f, p, c2);
-        p = fma(d.f, p, c1);
-        p = fma(d.f, p, 1.0);
-        return __builtin_bit_cast(double, __builtin_bit_cast(u64, table[d.n & (ROOTS - 1)] * p) +
-                                              ((u64)(uint32_t)((d.n & ~(ROOTS - 1)) << 14) << 32));
+        double p = fma(f, c4, c3);
+        p = fma(f, p, c2);
+        p = fma(f, p, c1);
+        return fma(f, p, 1.0);
     }
-    static __device__ __forceinline__ u64 whole(double v) // v <= 2^51
+    __device__ __forceinline__ double power(int n) const // times the unit
     {
-        return __builtin_bit_cast(u64, v + 0x1p52) & ((1ULL << 52) - 1);
+        return __builtin_bit_cast(double, __builtin_bit_cast(u64, table[n & (ROOTS - 1)]) + ((u64)(uint32_t)((n & ~(ROOTS - 1)) << 13) << 32));
+    }
+    static __device__ __forceinline__ u64 low_bits(double v) { return __builtin_bit_cast(u64, v) & ((1ULL << 52) - 1); }
+    __device__ __forceinline__ u64 whole(const Depth &d) const // at most 2^51
+    {
+        return low_bits(fma(power(d.n), series(d.f), 0x1p52));
     }
     __device__ __forceinline__ u64 kept(const Depth &d) const // what min-p leaves of it
     {
-        const double v = value(d);
-        return v >= least ? whole(v) : 0;
+        const double v = power(d.n) * series(d.f);
+        return v >= least ? low_bits(v + 0x1p52) : 0;
     }
-    static __device__ __forceinline__ int bin(const Depth &d) { return min(-d.n >> 1, BINS - 1); }
+    static __device__ __forceinline__ int bin(const Depth &d) { return min(max(-d.n, 0) >> 2, BINS - 1); }
+    // no entry of the first `bins` bins lies below this
+    __device__ __forceinline__ float floor_of(int bins) const
+    {
+        return careful ? -INFINITY : __double2float_rd(top - (4.0 * bins + 1.0) / scale);
+    }
 };
 
 // The last entry that is kept, in the order of standing.
@@ -183,9 +205,9 @@ __device__ __forceinline__ u64 running(Shared &s, u64 v, u64 &all)
 template <class T, int VEC_>
 struct Row {
     static constexpr int VEC = VEC_;
+    static constexpr bool LIST = false;
     const T *x;
     int V, length;
-    bool infinite; // +inf is the largest: such entries count as 0, all others as -inf
     typedef T Vec __attribute__((ext_vector_type(VEC)));
 
     __device__ __forceinline__ void block(int at, int end, float (&l)[VEC]) const
@@ -205,7 +227,6 @@ struct Row {
                 l[e] = at + e < end ? (float)x[at + e] : -INFINITY;
         }
     }
-    __device__ __forceinline__ float fold(float l) const { return l == INFINITY ? 0.0f : -INFINITY; }
     template <class F, class G>
     __device__ __forceinline__ void stretches(const F &f, const G &g) const
     {
@@ -221,13 +242,8 @@ struct Row {
                         block(first + (b * 64 + lane) * VEC, end, l[b]);
 #pragma unroll
                 for (int b = 0; b < AHEAD; b++)
-                    if (first + b * 64 * VEC < end) {
-                        if (infinite)
-#pragma unroll
-                            for (int e = 0; e < VEC; e++)
-                                l[b][e] = fold(l[b][e]);
+                    if (first + b * 64 * VEC < end)
                         f(l[b], first + (b * 64 + lane) * VEC);
-                    }
             }
             g(part);
         }
@@ -237,23 +253,38 @@ struct Row {
     {
         stretches(f, [](int) {});
     }
+    template <class F, class G>
+    __device__ __forceinline__ void each(const F &f, const G &flush) const // flush() after every stretch
+    {
+        stretches(f, [&](int) { flush(); });
+    }
 };
 
 // The row, with what is to be done at the end of a stretch.
-template <class R, class G>
+template <class R, class End>
 struct RowOf {
     static constexpr int VEC = R::VEC;
+    static constexpr bool LIST = false;
     const R &row;
-    const G &end;
+    const End &end;
     template <class F>
     __device__ __forceinline__ void each(const F &f) const
     {
         row.stretches(f, end);
     }
+    template <class F, class G>
+    __device__ __forceinline__ void each(const F &f, const G &flush) const
+    {
+        row.stretches(f, [&](int part) {
+            flush();
+            end(part);
+        });
+    }
 };
 
 struct Listed {
     static constexpr int VEC = 1;
+    static constexpr bool LIST = true;
     const Shared *s;
     int n;
     template <class F>
@@ -263,6 +294,11 @@ struct Listed {
             const float l[1] = {at < n ? s->list_l[at] : -INFINITY};
             f(l, at < n ? s->list_i[at] : 0);
         }
+    }
+    template <class F, class G>
+    __device__ __forceinline__ void each(const F &f, const G &) const
+    {
+        each(f);
     }
 };
 
@@ -388,31 +424,59 @@ __device__ __forceinline__ bool cut_at(Shared &s, const Source &src, const Weigh
         return false;
     const int cell = (int)s.word[0];
     const u64 left = s.word[1];
-    src.each([&](const float (&l)[VEC], int i) {
-        Depth d[VEC];
-        int nearest = BINS;
-#pragma unroll
-        for (int e = 0; e < VEC; e++) {
-            d[e] = weigh.depth(l[e]);
-            nearest = min(nearest, Weigh::bin(d[e]));
-        }
-        if (!__any(nearest <= cell))
-            return;
-#pragma unroll
-        for (int e = 0; e < VEC; e++) {
-            const int b = Weigh::bin(d[e]);
-            if (b < cell)
-                above(l[e], i + e, d[e]);
-            if (b == cell) {
-                const u64 w = weight(l[e], i + e, d[e]);
-                const int at = w ? atomicAdd(&s.count, 1) : CELL;
-                if (at < CELL) {
-                    s.cell_key[at] = standing(l[e], i + e);
-                    s.cell_w[at] = w;
-                }
+    auto sort_in = [&](float l, int i) {
+        const Depth d = weigh.depth(l);
+        const int b = Weigh::bin(d);
+        if (b < cell)
+            above(l, i, d);
+        if (b == cell) {
+            const u64 w = weight(l, i, d);
+            const int at = w ? atomicAdd(&s.count, 1) : CELL;
+            if (at < CELL) {
+                s.cell_key[at] = standing(l, i);
+                s.cell_w[at] = w;
             }
         }
-    });
+    };
+    const float floor = weigh.floor_of(cell + 1);
+    if constexpr (VEC == 1 && Source::LIST) {
+        src.each([&](const float (&l)[VEC], int i) { sort_in(l[0], i); });
+    } else {
+        // What lies above the floor is collected, 64 entries to a wavefront, before any exponential is taken: a nucleus is a small
+        // part of a row, and a wavefront with one such entry costs as much as one with 64.  (The list's place is free here.)
+        float *const near_l = s.list_l + (threadIdx.x >> 6) * 128;
+        int *const near_i = s.list_i + (threadIdx.x >> 6) * 128;
+        const int lane = threadIdx.x & 63;
+        int held = 0; // (the same in all lanes)
+        auto take = [&](int from, int most) {
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            sort_in(lane < most ? near_l[from + lane] : -INFINITY, lane < most ? near_i[from + lane] : 0);
+        };
+        src.each([&](const float (&l)[VEC], int i) {
+#pragma unroll
+            for (int e = 0; e < VEC; e++) {
+                const u64 who = __ballot(l[e] >= floor);
+                if (who) {
+                    if (l[e] >= floor) {
+                        const int at = held + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+                        near_l[at] = l[e];
+                        near_i[at] = i + e;
+                    }
+                    held += __popcll(who);
+                    if (held >= 64) {
+                        held -= 64;
+                        take(held, 64);
+                    }
+                }
+            }
+        }, [&] {
+            if (held)
+                take(0, held);
+            held = 0;
+        });
+    }
     __syncthreads();
     n = s.count;
     if (n > CELL) {
@@ -455,9 +519,7 @@ __device__ __forceinline__ void draw(Shared &s, const Row<T, VEC> &row, const We
     const int first = (int)s.word[0] * row.length, end = min(first + row.length, row.V);
     for (int base = first; base < end; base += THREADS) {
         const int i = base + threadIdx.x;
-        float l = i < end ? (float)row.x[i] : -INFINITY;
-        if (row.infinite)
-            l = row.fold(l);
+        const float l = i < end ? (float)row.x[i] : -INFINITY;
         const u64 w = cut.keeps(l, i) ? weigh.kept(weigh.depth(l)) : 0;
         u64 sum;
         const u64 to = running(s, w, sum);
@@ -483,7 +545,7 @@ __device__ __forceinline__ void draw_few(Shared &s, int n, const Weigh &weigh, i
     const float l = real ? s.list_l[mine] : -INFINITY;
     const int at = real ? s.list_i[mine] : 0;
     const Depth d = weigh.depth(l);
-    const u64 key = standing(l, at), w = real ? Weigh::whole(weigh.value(d)) : 0;
+    const u64 key = standing(l, at), w = real ? weigh.whole(d) : 0;
     if (real && part == 0) {
         s.cell_key[mine] = key;
         s.cell_w[mine] = w;
@@ -528,7 +590,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
     const float temperature = a.temperature ? a.temperature[r] : 1.0f, p = a.top_p ? a.top_p[r] : 1.0f;
     const float min_p = a.min_p ? a.min_p[r] : 0.0f, u = a.u[r];
     const int k = a.top_k ? a.top_k[r] : 0;
-    Row<T, VEC> row{(const T *)a.logits + r * a.row_stride, V, length, false};
+    const Row<T, VEC> row{(const T *)a.logits + r * a.row_stride, V, length};
     if (tid < ROOTS)
         s.table[tid] = root_of_two(tid) * unit;
     if (tid < STRETCHES)
@@ -563,9 +625,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
         }
         return;
     }
-    row.infinite = top == INFINITY;
-    const Weigh weigh(row.infinite ? 0.0f : top, ROOTS * 1.4426950408889634074 / (double)temperature,
-                      min_p > 0.0f ? (double)fminf(min_p, 1.0f) * unit : 0.0, s.table);
+    const Weigh weigh(top, (double)temperature, min_p > 0.0f ? (double)fminf(min_p, 1.0f) * unit : 0.0, s.table);
     auto nucleus = [&](u64 all) { // the sum that top-p asks for
         bool rest = false;
         u64 t = p > 0.0f ? share(p, all, rest) : 0;
@@ -575,12 +635,12 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
     Cut cut = FQ_NO_CUT;
     // (an entry of the last step has no weight, a top-k that reaches it keeps all that has)
     auto count = [](float, int, const Depth &d) -> u64 { return Weigh::bin(d) < BINS - 1; };
-    auto weight = [&](float l, int i, const Depth &d) -> u64 { return cut.keeps(l, i) ? Weigh::whole(weigh.value(d)) : 0; };
+    auto weight = [&](float l, int i, const Depth &d) -> u64 { return cut.keeps(l, i) ? weigh.whole(d) : 0; };
     // no entry this far down passes min-p (a step to spare)
-    const int least_n = min_p > 0.0f ? (int)(ROOTS * log2f(fminf(min_p, 1.0f))) - 2 : -BINS;
+    const int least_n = min_p > 0.0f ? (int)(ROOTS * log2f(fminf(min_p, 1.0f))) - 2 : DEEPEST;
     auto nothing = [](float, int, const Depth &) {};
     int in_cell;
-    if (k > 0 && k <= THREADS && k < V && !row.infinite) {
+    if (k > 0 && k <= THREADS && k < V && top < INFINITY) {
         // a bound: the k-th largest of the threads' own largest, its last 16 bits let go
         const uint32_t key = ordered(mine);
         u64 left = k;
@@ -652,7 +712,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
         const RowOf<Row<T, VEC>, decltype(add_stretch)> adding{row, add_stretch};
         const Cut k_cut = cut;
         if (cut.l == -INFINITY)
-            summed = cut_at(s, adding, weigh, [&](float, int, const Depth &d) { return Weigh::whole(weigh.value(d)); }, nucleus,
+            summed = cut_at(s, adding, weigh, [&](float, int, const Depth &d) { return weigh.whole(d); }, nucleus,
                             [&](float, int, const Depth &d) { sum += weigh.kept(d); }, cut, in_cell);
         else
             summed = cut_at(s, adding, weigh, weight, nucleus, [&](float l, int i, const Depth &d) {
@@ -671,12 +731,12 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
         row.stretches([&](const float (&l)[VEC], int) {
 #pragma unroll
             for (int e = 0; e < VEC; e++)
-                sum += Weigh::whole(weigh.value(weigh.depth(l[e])));
+                sum += weigh.whole(weigh.depth(l[e]));
         }, add_stretch);
     else if (!summed)
         row.stretches([&](const float (&l)[VEC], int i) {
             Depth d[VEC];
-            int nearest = -BINS * 2;
+            int nearest = DEEPEST;
 #pragma unroll
             for (int e = 0; e < VEC; e++) {
                 d[e] = weigh.depth(l[e]);

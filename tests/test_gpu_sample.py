@@ -104,6 +104,28 @@ def test_infinities_and_nan():
     run(x, u, temperature=[1e-40, 1e-38, 1e-30, 1e30, 1e38, 1e-20, 1.0, 1e-45])
 
 
+def test_temperatures_and_logits_of_any_size():
+    """Logits far from 0, steps of binary32 wider than the temperature, weights that are all 1 or all 0 but one."""
+    V = 2500
+    rng = np.random.default_rng(12)
+    u = rng.random(10, dtype=np.float32)
+    scale = np.array([1e-40, 1e-30, 1e-6, 1.0, 1e4, 1e8, 1e20, 1e30, 1e37, 5e37])[:, None]
+    x = (rng.normal(0, 1, (10, V)) * scale).astype(np.float32)
+    offset = x + np.float32(1e4)
+    for t in (1e-40, 1e-30, 1e-6, 0.01, 1.0, 1e6, 1e30, 1e38):
+        run(x, u, temperature=[t] * 10)
+        run(x, u, temperature=[t] * 10, top_p=[0.9] * 10)
+        run(x, u, temperature=[t] * 10, top_k=[40] * 10, min_p=[0.3] * 10)
+    for t in (0.01, 0.5, 1.0, 1e6, 1e30):
+        run(offset, u, temperature=[t] * 10)
+        run(offset, u, temperature=[t] * 10, top_p=[0.9] * 10)
+    x[:, ::3] = -np.inf
+    x[:, 5] = np.nan
+    run(x, u, temperature=[np.inf] * 10, top_k=[7] * 10)
+    run(x, u, temperature=[np.inf] * 10, top_p=[0.3] * 10)
+    run(x, u, temperature=[1e30] * 10, top_p=[0.3] * 10, min_p=[1e-3] * 10)
+
+
 def test_numbers_at_the_ends():
     rng = np.random.default_rng(3)
     x = rng.normal(0, 3, (6, 2000))
