@@ -227,36 +227,52 @@ struct Row {
                 l[e] = at + e < end ? (float)x[at + e] : -INFINITY;
         }
     }
-    template <class F, class G>
+    // LIGHT passes ask for 64 bytes a thread at once; the others (exponentials) for the next 32 while the last are worked on.
+    template <bool LIGHT, class F, class G>
     __device__ __forceinline__ void stretches(const F &f, const G &g) const
     {
-        constexpr int AHEAD = 64 / (VEC * (int)sizeof(T)); // 64 bytes a thread in flight
+        constexpr int AHEAD = (LIGHT ? 64 : 32) / (VEC * (int)sizeof(T)), STEP = AHEAD * 64 * VEC;
         const int lane = threadIdx.x & 63;
         for (int part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); part < STRETCHES && part * length < V; part += WAVES) {
             const int end = min((part + 1) * length, V);
-            for (int first = part * length; first < end; first += AHEAD * 64 * VEC) {
-                float l[AHEAD][VEC];
+            float l[AHEAD][VEC];
+            auto ask = [&](int first, float (&to)[AHEAD][VEC]) {
 #pragma unroll
                 for (int b = 0; b < AHEAD; b++)
                     if (first + b * 64 * VEC < end)
-                        block(first + (b * 64 + lane) * VEC, end, l[b]);
+                        block(first + (b * 64 + lane) * VEC, end, to[b]);
+            };
+            if (!LIGHT)
+                ask(part * length, l);
+            for (int first = part * length; first < end; first += STEP) {
+                float next[AHEAD][VEC];
+                if (LIGHT)
+                    ask(first, l);
+                else if (first + STEP < end)
+                    ask(first + STEP, next);
 #pragma unroll
                 for (int b = 0; b < AHEAD; b++)
                     if (first + b * 64 * VEC < end)
                         f(l[b], first + (b * 64 + lane) * VEC);
+                if (!LIGHT)
+#pragma unroll
+                    for (int b = 0; b < AHEAD; b++)
+#pragma unroll
+                        for (int e = 0; e < VEC; e++)
+                            l[b][e] = next[b][e];
             }
             g(part);
         }
     }
-    template <class F>
+    template <bool LIGHT, class F>
     __device__ __forceinline__ void each(const F &f) const
     {
-        stretches(f, [](int) {});
+        stretches<LIGHT>(f, [](int) {});
     }
-    template <class F, class G>
+    template <bool LIGHT, class F, class G>
     __device__ __forceinline__ void each(const F &f, const G &flush) const // flush() after every stretch
     {
-        stretches(f, [&](int) { flush(); });
+        stretches<LIGHT>(f, [&](int) { flush(); });
     }
 };
 
@@ -267,15 +283,15 @@ struct RowOf {
     static constexpr bool LIST = false;
     const R &row;
     const End &end;
-    template <class F>
+    template <bool LIGHT, class F>
     __device__ __forceinline__ void each(const F &f) const
     {
-        row.stretches(f, end);
+        row.template stretches<LIGHT>(f, end);
     }
-    template <class F, class G>
+    template <bool LIGHT, class F, class G>
     __device__ __forceinline__ void each(const F &f, const G &flush) const
     {
-        row.stretches(f, [&](int part) {
+        row.template stretches<LIGHT>(f, [&](int part) {
             flush();
             end(part);
         });
@@ -287,7 +303,7 @@ struct Listed {
     static constexpr bool LIST = true;
     const Shared *s;
     int n;
-    template <class F>
+    template <bool LIGHT, class F>
     __device__ __forceinline__ void each(const F &f) const
     {
         for (int at = threadIdx.x; at - (int)threadIdx.x < n; at += THREADS) {
@@ -295,10 +311,10 @@ struct Listed {
             f(l, at < n ? s->list_i[at] : 0);
         }
     }
-    template <class F, class G>
+    template <bool LIGHT, class F, class G>
     __device__ __forceinline__ void each(const F &f, const G &) const
     {
-        each(f);
+        each<LIGHT>(f);
     }
 };
 
@@ -388,7 +404,7 @@ __device__ __forceinline__ bool cut_at(Shared &s, const Source &src, const Weigh
         s.count = 0;
     __syncthreads();
     constexpr int VEC = Source::VEC;
-    src.each([&](const float (&l)[VEC], int i) {
+    src.template each<false>([&](const float (&l)[VEC], int i) {
         Depth d[VEC];
         int nearest = BINS, farthest = 0;
 #pragma unroll
@@ -440,7 +456,7 @@ __device__ __forceinline__ bool cut_at(Shared &s, const Source &src, const Weigh
     };
     const float floor = weigh.floor_of(cell + 1);
     if constexpr (VEC == 1 && Source::LIST) {
-        src.each([&](const float (&l)[VEC], int i) { sort_in(l[0], i); });
+        src.template each<true>([&](const float (&l)[VEC], int i) { sort_in(l[0], i); });
     } else {
         // What lies above the floor is collected, 64 entries to a wavefront, before any exponential is taken: a nucleus is a small
         // part of a row, and a wavefront with one such entry costs as much as one with 64.  (The list's place is free here.)
@@ -454,7 +470,7 @@ __device__ __forceinline__ bool cut_at(Shared &s, const Source &src, const Weigh
             __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
             sort_in(lane < most ? near_l[from + lane] : -INFINITY, lane < most ? near_i[from + lane] : 0);
         };
-        src.each([&](const float (&l)[VEC], int i) {
+        src.template each<true>([&](const float (&l)[VEC], int i) {
 #pragma unroll
             for (int e = 0; e < VEC; e++) {
                 const u64 who = __ballot(l[e] >= floor);
@@ -482,7 +498,7 @@ __device__ __forceinline__ bool cut_at(Shared &s, const Source &src, const Weigh
     if (n > CELL) {
         n = -1;
         cut = cut_of(reach<64>(s, [&](const auto &visit) {
-            src.each([&](const float (&l)[VEC], int i) {
+            src.template each<true>([&](const float (&l)[VEC], int i) {
 #pragma unroll
                 for (int e = 0; e < VEC; e++)
                     visit(standing(l[e], i + e), weight(l[e], i + e, weigh.depth(l[e])));
@@ -597,7 +613,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
         s.stretch[tid] = 0;
     float mine = -INFINITY;
     int at = 0;
-    row.each([&](const float (&l)[VEC], int i) {
+    row.template each<true>([&](const float (&l)[VEC], int i) {
 #pragma unroll
         for (int e = 0; e < VEC; e++)
             if (l[e] > mine) {
@@ -661,7 +677,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
         if (tid == 0)
             s.count = 0;
         __syncthreads();
-        row.each([&](const float (&l)[VEC], int i) {
+        row.template each<true>([&](const float (&l)[VEC], int i) {
             float largest = l[0];
 #pragma unroll
             for (int e = 1; e < VEC; e++)
@@ -689,7 +705,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
             cut_at(s, list, weigh, count, [&](u64) { return (u64)k; }, nothing, cut, in_cell);
             if (!(p >= 1.0f))
                 cut_at(s, list, weigh, weight, nucleus, nothing, cut, in_cell);
-            list.each([&](const float (&l)[1], int i) {
+            list.template each<true>([&](const float (&l)[1], int i) {
                 const u64 w = cut.keeps(l[0], i) ? weigh.kept(weigh.depth(l[0])) : 0;
                 if (w)
                     atomicAdd(&s.stretch[i / length], w);
@@ -728,13 +744,13 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
         }
     }
     if (!summed && cut.l == -INFINITY && weigh.least == 0.0)
-        row.stretches([&](const float (&l)[VEC], int) {
+        row.template stretches<false>([&](const float (&l)[VEC], int) {
 #pragma unroll
             for (int e = 0; e < VEC; e++)
                 sum += weigh.whole(weigh.depth(l[e]));
         }, add_stretch);
     else if (!summed)
-        row.stretches([&](const float (&l)[VEC], int i) {
+        row.template stretches<false>([&](const float (&l)[VEC], int i) {
             Depth d[VEC];
             int nearest = DEEPEST;
 #pragma unroll
