@@ -41,7 +41,8 @@ enum Layout { NEIGHBOURS, PIECES, ANYHOW };
 
 // A thread's unit is two pieces of a head, which a pair of pieces turns together: what is asked for before any of it is used.
 // (One piece at a time, the partners value by value: 27 us for 2048 tokens of the 70B shapes where this takes 14, 5.8 TB/s.)  Where
-// partners are fetched value by value the units that turn come first, so that other wavefronts do not pass through it.
+// partners are fetched value by value a unit is one piece, and those that turn come first, so that other wavefronts do not pass
+// through it.
 template <Layout LAYOUT>
 __global__ __launch_bounds__(THREADS) void append_kernel(FqAppendArgs a, int per_head, int turning)
 {
@@ -80,8 +81,8 @@ __global__ __launch_bounds__(THREADS) void append_kernel(FqAppendArgs a, int per
             n.c = i;
             n.c2 = i + (half >> 3);
         } else {
-            n.c = 2 * i; // (rot is a multiple of 16 where pieces pair up: past the rotation they go on at rot / 8 = 2 half / 8)
-            n.c2 = n.c + 1 < pieces ? n.c + 1 : -1;
+            n.c = LAYOUT == ANYHOW ? i : 2 * i; // (rot is a multiple of 16 where pieces pair up: past the rotation they go on at rot / 8 = 2 half / 8)
+            n.c2 = LAYOUT != ANYHOW && n.c + 1 < pieces ? n.c + 1 : -1;
         }
         n.row = (n.kind == 0 ? a.q + t * a.q_stride : n.kind == 1 ? a.k + t * a.k_stride : a.v + t * a.v_stride) + n.head * a.kv.dim;
         n.x = *(const Eight *)(n.row + 8 * n.c);
@@ -177,7 +178,8 @@ __global__ __launch_bounds__(THREADS) void append_kernel(FqAppendArgs a, int per
 
 hipError_t fq_launch_append(const FqAppendArgs &a, bool interleaved, hipStream_t stream)
 {
-    const int per_head = (a.kv.dim / 8 + 1) / 2;
+    const bool anyhow = !interleaved && a.rot % 16 != 0;
+    const int per_head = anyhow ? a.kv.dim / 8 : (a.kv.dim / 8 + 1) / 2;
     const int units = (a.q_heads + 2 * a.kv.kv_heads) * per_head;
     // a token's rows over as many workgroups as there are steps in them, where the tokens alone do not fill the chip
     const int steps = (units + THREADS - 1) / THREADS;
@@ -185,9 +187,9 @@ hipError_t fq_launch_append(const FqAppendArgs &a, bool interleaved, hipStream_t
     const dim3 grid(a.seqs.tokens, steps < room ? steps : room);
     if (interleaved)
         append_kernel<NEIGHBOURS><<<grid, THREADS, 0, stream>>>(a, per_head, 0);
-    else if (a.rot % 16 == 0)
+    else if (!anyhow)
         append_kernel<PIECES><<<grid, THREADS, 0, stream>>>(a, per_head, 0);
     else
-        append_kernel<ANYHOW><<<grid, THREADS, 0, stream>>>(a, per_head, (a.rot + 15) / 16);
+        append_kernel<ANYHOW><<<grid, THREADS, 0, stream>>>(a, per_head, (a.rot + 7) / 8);
     return hipGetLastError();
 }
