@@ -9,7 +9,9 @@
 //      steps of 1/32 octave from the top, the step that holds the target, and the entries of that step in order
 //   4. the draw: kept weights summed over the 64 stretches, the one that holds the target, its entries in order
 // Bound by reading a long row two (top-k, temperature, min-p) or three times (top-p), all but the first from the caches, and by
-// the exponentials of the entries that count; by the chain of steps for a short one.
+// the exponentials of the entries that count; by the chain of steps for a short one.  Measured, 256 rows of 128256 (131 MB, 22 us to
+// read once): top-k 50 47 us, temperature alone 58, top-p 0.95 93, all of them mixed 110; one row of 32000 with top-k 50 16 us,
+// with top-p 0.95 27.
 #include <hip/hip_runtime.h>
 
 #include "fq_internal.h"
