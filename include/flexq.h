@@ -410,7 +410,7 @@ int fq_sched_peek(const void *state, int *next_event, int *tokens, double *thre,
 /*
  * ---- Between the linears of a decoder, and after its output layer --------------------------------------------
  *
- * Eq. (1) of Sec. 2.1 over a cache that is not quantized (Sec. 5.2 measures the step with it): rotary positions and
+ * Eq. (1) of Sec. 2.1 over a cache that is not quantized (as in Fig. 6, the end-to-end step): rotary positions and
  * the append of keys and values, attention over the cache, and the draw of the next token from the logits.  (The
  * paper takes the argmax and names no cache layout: the interfaces are this library's.)
  */

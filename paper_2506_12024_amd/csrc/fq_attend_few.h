@@ -19,16 +19,25 @@ constexpr int WAVES = FQ_ATTEND_THREADS / 64;
 constexpr int KEYS = 32; // to a wavefront and step
 
 // 16-byte pieces to a row of V in LDS, and where piece c of row r goes: 16 rows of one piece fall on 16 different bank
-// groups (the writes), and so do 8 rows of a pair of pieces (the transposed reads).
+// groups (the writes), and so do the pairs of pieces of any two neighbouring or next but one quarters of the rows (the transposed
+// reads, whichever lanes LDS takes together).
 template <int DP>
 struct Place {
     static constexpr int PITCH = DP <= 64 ? 8 : DP <= 128 ? 16 : 32;
     static __device__ __forceinline__ int at(int r, int c)
     {
-        const int s = PITCH == 8 ? (((r >> 1) & 3) << 1) | ((r >> 3) & 1) : ((r & 7) << 1) | ((r >> 3) & 1);
+        const int s = PITCH == 8 ? (((r >> 1) & 1) << 1 | (((r >> 2) ^ (r >> 3)) & 1) << 2) | ((r >> 3) & 1)
+                                 : ((r & 3) << 1 | (((r >> 2) ^ (r >> 3)) & 1) << 3) | ((r >> 3) & 1);
         return (r * PITCH + (c ^ s)) << 4;
     }
 };
+
+// The rows' sums at the end, 4 dimensions to a piece: 16 rows of one piece on different bank groups (8 where a row has 24).
+template <int DP>
+__device__ __forceinline__ int sum_place(int r, int piece)
+{
+    return (r * (DP / 4) + (piece ^ (r & (DP == 96 ? 7 : 15)))) << 4;
+}
 
 // LDS of a workgroup.
 template <int DP, int RT>
@@ -273,7 +282,7 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
         const float fall = __builtin_amdgcn_exp2f(m[rt] - fq_reference(top));
 #pragma unroll
         for (int d = 0; d < ND; d++)
-            *(float4_t *)(mine + ((col * DP + 16 * d + 4 * quad) << 2)) = o[rt][d] * fall;
+            *(float4_t *)(mine + sum_place<DP>(col, 4 * d + quad)) = o[rt][d] * fall;
         __syncthreads();
         // thread: row tid / (DP / 8), 8 dimensions of it
         for (int u = threadIdx.x; u < 16 * (DP / 8); u += WAVES * 64) {
@@ -291,8 +300,8 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
 #pragma unroll
             for (int i = 0; i < WAVES; i++) {
                 total += all_l[i][rt * 16 + rr] * __builtin_amdgcn_exp2f(all_m[i][rt * 16 + rr] - fq_reference(best));
-                const float4_t *from = (const float4_t *)(lds + i * WAVE_LDS + ((rr * DP + d) << 2));
-                const float4_t x = from[0], y = from[1];
+                const float4_t x = *(const float4_t *)(lds + i * WAVE_LDS + sum_place<DP>(rr, d >> 2));
+                const float4_t y = *(const float4_t *)(lds + i * WAVE_LDS + sum_place<DP>(rr, (d >> 2) + 1));
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
                     sum[e] += x[e];
