@@ -7,6 +7,7 @@ namespace {
 // batch share the prefix besides, and the prefix is a piece of its own.
 struct Plan {
     int n, parts;
+    int most_parts; // for this many keys or any fewer
     FqAttendWork work[2];
     int row_tiles[2]; // 0: the kernel for many rows
 };
@@ -21,7 +22,7 @@ int tiles_of(const FqAttendArgs &a, long long rows)
     return rows > (wide ? 16 : 32) ? 0 : rows > 16 ? 2 : 1;
 }
 
-FqAttendWork work(const FqAttendArgs &a, bool shared, int key0, long long keys, int seqs, int tokens, int row_tiles, int cus)
+FqAttendWork work(const FqAttendArgs &a, bool shared, int key0, long long keys, int seqs, int tokens, int row_tiles, int cus, int &most_parts)
 {
     const long long rows = (long long)tokens * (a.q_heads / a.kv.kv_heads);
     const int step = row_tiles ? 128 : 64; // keys that a workgroup takes at once
@@ -49,6 +50,9 @@ FqAttendWork work(const FqAttendArgs &a, bool shared, int key0, long long keys, 
     }
     if (div_up(steps, take) > MAX_PARTS)
         take = div_up(steps, MAX_PARTS);
+    long long most = row_tiles ? 4 * slots / groups + 1 : slots / groups;
+    most = most > steps ? steps : most < 1 ? 1 : most;
+    most_parts += (int)(most > MAX_PARTS ? MAX_PARTS : most);
     w.chunk = (int)(take < steps ? take : steps) * step;
     w.parts = div_up(keys > 0 ? keys : 1, w.chunk);
     w.blocks_x = (uint32_t)(w.row_blocks * a.kv.kv_heads);
@@ -70,12 +74,12 @@ Plan plan(const FqAttendArgs &a, int cus)
             t0 = t1 = t0 > t1 ? t0 : t1;
         else
             t0 = 0; // (few rows of the batch, many of a sequence: no such batch)
-        pl.work[0] = work(a, true, 0, P, 1, a.seqs.tokens, t0, cus);
-        pl.work[1] = work(a, false, P, a.max_kv, a.seqs.seqs, a.max_q, t1, cus);
+        pl.work[0] = work(a, true, 0, P, 1, a.seqs.tokens, t0, cus, pl.most_parts);
+        pl.work[1] = work(a, false, P, a.max_kv, a.seqs.seqs, a.max_q, t1, cus, pl.most_parts);
         pl.n = 2;
     } else {
         pl.row_tiles[0] = pl.row_tiles[1] = tiles_of(a, a.max_q * group);
-        pl.work[0] = work(a, false, 0, (long long)P + a.max_kv, a.seqs.seqs, a.max_q, pl.row_tiles[0], cus);
+        pl.work[0] = work(a, false, 0, (long long)P + a.max_kv, a.seqs.seqs, a.max_q, pl.row_tiles[0], cus, pl.most_parts);
         pl.n = 1;
     }
     for (int i = 0; i < pl.n; i++) {
@@ -85,12 +89,12 @@ Plan plan(const FqAttendArgs &a, int cus)
     return pl;
 }
 
-size_t bytes(const FqAttendArgs &a, const Plan &pl)
+size_t bytes(const FqAttendArgs &a, int parts)
 {
-    if (pl.parts == 1)
+    if (parts == 1)
         return 256;
     const size_t rows = (size_t)a.seqs.tokens * a.q_heads;
-    return (rows * pl.parts * (a.kv.dim * sizeof(float) + sizeof(float2)) + 255) & ~(size_t)255;
+    return (rows * parts * (a.kv.dim * sizeof(float) + sizeof(float2)) + 255) & ~(size_t)255;
 }
 
 // The parts of a row, added up.  dim / 4 threads take 4 dimensions each of every `lanes`-th part, each with a reference of its own;
@@ -180,7 +184,11 @@ __global__ __launch_bounds__(256) void attend_join_kernel(FqAttendArgs a, FqAtte
 
 } // namespace
 
-size_t fq_attend_bytes(const FqAttendArgs &a, int cus) { return bytes(a, plan(a, cus)); }
+size_t fq_attend_bytes(const FqAttendArgs &a, bool for_fewer_keys, int cus)
+{
+    const Plan pl = plan(a, cus);
+    return bytes(a, for_fewer_keys ? pl.most_parts : pl.parts);
+}
 
 hipError_t fq_launch_attend(const FqAttendArgs &a, void *workspace, hipStream_t stream)
 {

@@ -243,7 +243,8 @@ struct FqAttendArgs {
     int q_heads, max_q, max_kv;
     float scale;
 };
-size_t fq_attend_bytes(const FqAttendArgs &a, int cus);
+// Workspace of a call; for_fewer_keys: of any call with the same rows and no more keys.
+size_t fq_attend_bytes(const FqAttendArgs &a, bool for_fewer_keys, int cus);
 hipError_t fq_launch_attend(const FqAttendArgs &a, void *workspace, hipStream_t stream);
 
 struct FqSampleArgs {

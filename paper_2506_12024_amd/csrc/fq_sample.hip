@@ -6,7 +6,8 @@
 //   2. top-k of at most 1024: the k-th largest of the 1024 threads' own largest is no larger than the k-th of all, so the few
 //      entries from it on go to a list in LDS, which takes the row's place
 //   3. a cut (the entry at which a running count or sum, from the largest logit down, reaches its target): a histogram over 2048
-//      steps of 1/32 octave from the top, the step that holds the target, and the entries of that step in order
+//      steps of 1/32 octave from the top, the step that holds the target, and the entries of that step in order (a step of more than
+//      1024 entries -- flat rows, equal logits -- is parted by standing first, 11 bits at a time)
 //   4. the draw: kept weights summed over the 64 stretches, the one that holds the target, its entries in order
 // Bound by reading a long row two (top-k, temperature, min-p) or three times (top-p), all but the first from the caches, and by
 // the exponentials of the entries that count; by the chain of steps for a short one.  Measured, 256 rows of 128256 (131 MB, 22 us to
@@ -342,38 +343,29 @@ __device__ __forceinline__ bool find_bin(Shared &s, const Target &target_of)
     return true;
 }
 
-// Of entries f(visit) names by visit(key, weight) (weight 0: not among them), from the largest key down: the key at which the running
-// sum of weights reaches `target` (1 <= target <= the sum).  Eight bits at a time: any number of entries and equal keys'
-// prefixes, the way out where a histogram over values does not tell entries apart.
-template <int BITS, class F>
-__device__ __forceinline__ u64 reach(Shared &s, const F &f, u64 target)
-{
-    u64 found = 0;
-    for (int shift = BITS - 8; shift >= 0; shift -= 8) {
-        __syncthreads();
-        if (threadIdx.x < 256)
-            s.bins[threadIdx.x] = 0;
-        __syncthreads();
-        f([&](u64 key, u64 w) {
-            if (w && (shift == BITS - 8 || (key >> (shift + 8)) == (found >> (shift + 8))))
-                atomicAdd(&s.bins[255 - ((key >> shift) & 255)], w);
-        });
-        find_bin<256>(s, [&](u64) { return target; });
-        found |= (255 - s.word[0]) << shift;
-        target = s.word[1];
-    }
-    __syncthreads();
-    return found;
-}
-
-// The entries of the cell, n of them: the same.
+// Of the n entries of the cell, from the largest standing down: the one at which the running sum of weights reaches `target`
+// (1 <= target <= the sum).  More than 256 of them: eight bits of the standing at a time.
 __device__ __forceinline__ u64 reach_cell(Shared &s, int n, u64 target)
 {
-    if (n > 256)
-        return reach<64>(s, [&](const auto &visit) {
-            for (int i = threadIdx.x; i < n; i += THREADS)
-                visit(s.cell_key[i], s.cell_w[i]);
-        }, target);
+    if (n > 256) {
+        u64 found = 0;
+        for (int shift = 56; shift >= 0; shift -= 8) {
+            __syncthreads();
+            if (threadIdx.x < 256)
+                s.bins[threadIdx.x] = 0;
+            __syncthreads();
+            if ((int)threadIdx.x < n) {
+                const u64 key = s.cell_key[threadIdx.x];
+                if (shift == 56 || (key >> (shift + 8)) == (found >> (shift + 8)))
+                    atomicAdd(&s.bins[255 - ((key >> shift) & 255)], s.cell_w[threadIdx.x]);
+            }
+            find_bin<256>(s, [&](u64) { return target; });
+            found |= (255 - s.word[0]) << shift;
+            target = s.word[1];
+        }
+        __syncthreads();
+        return found;
+    }
     // four threads to an entry: what stands before it
     const int mine = threadIdx.x >> 2;
     if (mine < n) {
@@ -390,6 +382,43 @@ __device__ __forceinline__ u64 reach_cell(Shared &s, int n, u64 target)
     const u64 found = s.word[0];
     __syncthreads();
     return found;
+}
+
+// Entries with a weight go to the cell, counted once for a wavefront (all of whose lanes call this).
+__device__ __forceinline__ void put_in_cell(Shared &s, u64 w, u64 key, u64 &lowest, u64 &highest)
+{
+    const u64 who = __ballot(w != 0);
+    if (!who)
+        return;
+    int base = 0;
+    if ((threadIdx.x & 63) == 0)
+        base = atomicAdd(&s.count, __popcll(who));
+    const int at = __builtin_amdgcn_readfirstlane(base) + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+    if (w) {
+        lowest = key < lowest ? key : lowest;
+        highest = key > highest ? key : highest;
+        if (at < CELL) {
+            s.cell_key[at] = key;
+            s.cell_w[at] = w;
+        }
+    }
+}
+
+// The largest of all threads' values.
+__device__ __forceinline__ u64 wg_most(Shared &s, u64 v)
+{
+    for (int o = 32; o; o >>= 1) {
+        const u64 x = __shfl_xor(v, o);
+        v = x > v ? x : v;
+    }
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0)
+        s.wave[threadIdx.x >> 6] = v;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < WAVES; i++)
+        v = s.wave[i] > v ? s.wave[i] : v;
+    return v;
 }
 
 // The entry at which the running sum of weights, from the largest logit down, reaches its target (a function of the whole sum):
@@ -442,19 +471,13 @@ __device__ __forceinline__ bool cut_at(Shared &s, const Source &src, const Weigh
         return false;
     const int cell = (int)s.word[0];
     const u64 left = s.word[1];
+    u64 lowest = ~0ULL, highest = 0; // the standings that went into the cell, this thread's
     auto sort_in = [&](float l, int i) {
         const Depth d = weigh.depth(l);
         const int b = Weigh::bin(d);
         if (b < cell)
             above(l, i, d);
-        if (b == cell) {
-            const u64 w = weight(l, i, d);
-            const int at = w ? atomicAdd(&s.count, 1) : CELL;
-            if (at < CELL) {
-                s.cell_key[at] = standing(l, i);
-                s.cell_w[at] = w;
-            }
-        }
+        put_in_cell(s, b == cell ? weight(l, i, d) : 0, standing(l, i), lowest, highest);
     };
     const float floor = weigh.floor_of(cell + 1);
     if constexpr (VEC == 1 && Source::LIST) {
@@ -497,18 +520,56 @@ __device__ __forceinline__ bool cut_at(Shared &s, const Source &src, const Weigh
     }
     __syncthreads();
     n = s.count;
-    if (n > CELL) {
-        n = -1;
-        cut = cut_of(reach<64>(s, [&](const auto &visit) {
-            src.template each<true>([&](const float (&l)[VEC], int i) {
-#pragma unroll
-                for (int e = 0; e < VEC; e++)
-                    visit(standing(l[e], i + e), weight(l[e], i + e, weigh.depth(l[e])));
-            });
-        }, target));
-    } else {
+    if (n <= CELL) {
         cut = cut_of(reach_cell(s, n, left));
+        return true;
     }
+    // More entries than the cell holds (flat rows, equal logits): the same again over their standings alone, 11 bits closer each
+    // time; equal logits part by index.  The light passes skip what is not between the two ends.
+    u64 low = wg_most(s, ~lowest), high = wg_most(s, highest), rest = left;
+    low = ~low;
+    int held = n;
+    while (held > CELL) {
+        const u64 range = high - low;
+        const int shift = range < BINS ? 0 : 64 - __clzll((long long)range) - 11;
+        __syncthreads();
+        s.bins[threadIdx.x] = s.bins[threadIdx.x + THREADS] = 0;
+        __syncthreads();
+        src.template each<true>([&](const float (&l)[VEC], int i) {
+#pragma unroll
+            for (int e = 0; e < VEC; e++) {
+                const u64 key = standing(l[e], i + e);
+                const bool in = key >= low && key <= high;
+                if (!__any(in))
+                    continue;
+                const u64 w = in ? weight(l[e], i + e, weigh.depth(l[e])) : 0;
+                if (w)
+                    atomicAdd(&s.bins[(high - key) >> shift], w);
+            }
+        });
+        find_bin<BINS>(s, [&](u64) { return rest; });
+        high -= s.word[0] << shift;
+        rest = s.word[1];
+        const u64 width = (1ULL << shift) - 1;
+        low = high - low > width ? high - width : low;
+        if (threadIdx.x == 0)
+            s.count = 0;
+        __syncthreads();
+        src.template each<true>([&](const float (&l)[VEC], int i) {
+#pragma unroll
+            for (int e = 0; e < VEC; e++) {
+                const u64 key = standing(l[e], i + e);
+                const bool in = key >= low && key <= high;
+                if (!__any(in))
+                    continue;
+                put_in_cell(s, in ? weight(l[e], i + e, weigh.depth(l[e])) : 0, key, lowest, highest);
+            }
+        });
+        __syncthreads();
+        held = s.count;
+    }
+    cut = cut_of(reach_cell(s, held, rest));
+    n = -1;
     return true;
 }
 
@@ -623,17 +684,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
                 at = i + e;
             }
     });
-    u64 best = standing(mine, at);
-    for (int o = 32; o; o >>= 1) {
-        const u64 x = __shfl_xor(best, o);
-        best = x > best ? x : best;
-    }
-    if (lane == 0)
-        s.wave[tid >> 6] = best;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < WAVES; i++)
-        best = s.wave[i] > best ? s.wave[i] : best;
+    const u64 best = wg_most(s, standing(mine, at));
     const float top = unordered((uint32_t)(best >> 32));
     if (top == -INFINITY || !(temperature > 0.0f)) {
         if (tid == 0) {

@@ -258,7 +258,7 @@ size_t fq_attend_workspace_bytes(const fq_kv *kv, const fq_seqs *seqs, int token
     FqAttendArgs a;
     if (attend_args("fq_attend_workspace_bytes", kv, seqs, tokens, q_heads, max_q, max_kv, &a))
         return 0;
-    return tokens == 0 ? 256 : fq_attend_bytes(a, fq_device_cus());
+    return tokens == 0 ? 256 : fq_attend_bytes(a, true, fq_device_cus());
 }
 
 int fq_attend(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q, long long q_stride, int q_heads, float scale,
@@ -281,7 +281,7 @@ int fq_attend(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q, l
         return fq_fail(FQ_ERR_ALIGN, "%s: lse needs 4-byte, the workspace 256-byte alignment", who);
     if (!std::isfinite(scale))
         return fq_fail(FQ_ERR_SHAPE, "%s: scale must be finite", who);
-    const size_t need = fq_attend_bytes(a, fq_device_cus());
+    const size_t need = fq_attend_bytes(a, false, fq_device_cus());
     if (workspace_bytes < need)
         return fq_fail(FQ_ERR_SHAPE, "%s: the workspace has %zu bytes, fq_attend_workspace_bytes asks for %zu", who,
                        workspace_bytes, need);

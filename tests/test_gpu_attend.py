@@ -175,6 +175,28 @@ def test_bounds_given_by_the_caller():
     run(Batch([1, 1], [200, 40], 16), 4, 2, 64, torch.float16, max_kv=1, lse=False)
 
 
+@pytest.mark.parametrize("heads,new,prefix", [((32, 32), [1], 0), ((8, 2), [1, 1, 1], 700), ((8, 1), [4, 2], 0), ((4, 4), [130], 0)])
+def test_one_workspace_for_all_lengths(heads, new, prefix):
+    """Sized for the longest, used for every length: the launch asks for no more, and writes no further."""
+    width = 260
+    gen = torch.Generator().manual_seed(31)
+    long = Batch(new, [4100] * len(new), 16, prefix=prefix, width=width)
+    kc, vc = (pool(gen, long.pages, heads[1], 16, 64, torch.float16) for _ in range(2))
+    cache = fq.KVCache(kc, vc)
+    q = torch.randn((long.tokens, heads[0], 64), generator=gen).half().to(DEV)
+    seqs = long.sequences()
+    need = fq.fq_attend_workspace_bytes(cache, seqs, long.tokens, heads[0], max(new), 4100)
+    ws = torch.full((need + 4096,), 77, dtype=torch.uint8, device=DEV)
+    out, lse = torch.empty_like(q), torch.empty((long.tokens, heads[0]), device=DEV)
+    for m in (130, 400, 900, 1500, 2500, 3100, 4100):
+        seqs._keep[1].fill_(m)
+        fq.fq_attend(cache, seqs, q, out, 0.125, max(new), m, ws[:need], lse=lse)
+        torch.cuda.synchronize()
+        long.kv = [m] * len(new)
+        check(long, out, lse, q, kc, vc, 0.125)
+        assert torch.all(ws[need:] == 77)
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.2, 1.0, 30.0])
 def test_scales(scale):
     run(Batch([1, 5], [300, 77], 16), 8, 2, 64, torch.float16, scale=scale)

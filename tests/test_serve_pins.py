@@ -161,6 +161,24 @@ def test_attend_refuses(bad, code):
         fq.lib.fq_kv_destroy(c), fq.lib.fq_seqs_destroy(s)
 
 
+@pytest.mark.parametrize("dim", [64, 80, 128, 256])
+@pytest.mark.parametrize("heads,tokens,max_q,n,prefix", [(2, 1, 1, 1, 0), (16, 4, 1, 4, 0), (2, 4, 1, 4, 300), (64, 40, 1, 40, 5000), (32, 12, 4, 3, 0),
+                                                         (32, 300, 300, 1, 0), (8, 70, 40, 5, 999)])
+def test_a_workspace_serves_every_smaller_length(dim, heads, tokens, max_q, n, prefix):
+    """Parts are not monotonous in the length; what the size call answers is."""
+    _, c = kv(dim=dim, ps=8192, hs=4096, ts=256)
+    _, s = seqs(n=n, width=4000, prefix_table=FAKE if prefix else None, prefix=prefix)
+    try:
+        lengths = list(range(1, 4000, 13)) + list(range(4000, 64000, 997))
+        sizes = [fq.lib.fq_attend_workspace_bytes(c, s, tokens, heads, max_q, m) for m in lengths]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:])) and sizes[0] >= 256
+        for m in lengths[::5]:  # less than the least there is (256 bytes) is refused at every length
+            rc = attend(c, s, T=tokens, qs=heads * dim, os=heads * dim, heads=heads, max_q=max_q, max_kv=m, n=255)
+            assert rc == B.FQ_ERR_SHAPE
+    finally:
+        fq.lib.fq_kv_destroy(c), fq.lib.fq_seqs_destroy(s)
+
+
 def sample(call, logits=FAKE, R=2, V=100, stride=100, u=FAKE, t=None, k=None, p=None, m=None, token=FAKE, prob=None, ws=FAKE, n=1 << 30):
     return call(logits, R, V, stride, u, t, k, p, m, token, prob, ws, n, None)
 
