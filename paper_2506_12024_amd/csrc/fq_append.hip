@@ -5,7 +5,7 @@
 // through registers, 8 values (16 bytes) to a thread and step.  The angle is a binary64 product taken in whole turns: position
 // * freq / 2 pi minus its nearest integer, so a place of 10^6 keeps the accuracy of place 1 (in binary32 it would be off by
 // 0.06 rad); the fraction then goes through a binary32 sincospi.  Bound by the traffic of q, k, v for prompts (2048 tokens of
-// the 70B shapes: 84 MB in 14.7 us, 5.7 TB/s, against 4.8 of a large copy), by one launch for a token (3.5 us on the device, 7.9 a
+// the 70B shapes: 84 MB in 14.7 us, 5.7 TB/s, against 4.8 of a large copy), by one launch for a token (3.5 us on the device, 8.0 a
 // call from Python).
 #include <hip/hip_runtime.h>
 

@@ -1,6 +1,6 @@
 // The attention kernels of one 16-bit type: a launch holds one or two pieces of work, few or many rows to a key head each.  A
 // prefix that a batch shares and the sequences' own keys are one launch, so that neither waits for the other's last workgroup
-// (48 sequences behind 8197 keys: 31 + 19 us as two launches, 41 as one).
+// (48 sequences behind 8197 keys: 31 + 19 us as two launches, 41 as one, 37 with the tiles as they are now).
 #ifndef FQ_ATTEND_KERNELS_H
 #define FQ_ATTEND_KERNELS_H
 

@@ -1,7 +1,7 @@
 // Drawing the next token from a row of logits: temperature, top-k, top-p, min-p and a given random number.
 //
 // Weights are whole numbers (exp in binary64, rounded to a unit under which V of them still fit 62 bits), so sums are exact in any
-// order and atomics give the same bits every time.  One workgroup takes a row, each of its wavefronts four stretches of it:
+// order and atomics give the same bits every time.  One workgroup takes a row, each of its wavefronts four stretches of it, side by side:
 //   1. the largest logit
 //   2. top-k of at most 1024: the k-th largest of the 1024 threads' own largest is no larger than the k-th of all, so the few
 //      entries from it on go to a list in LDS, which takes the row's place
@@ -11,8 +11,8 @@
 //   4. the draw: kept weights summed over the 64 stretches, the one that holds the target, its entries in order
 // Bound by reading a long row two (top-k, temperature, min-p) or three times (top-p), all but the first from the caches, and by
 // the exponentials of the entries that count; by the chain of steps for a short one.  Measured, 256 rows of 128256 (131 MB, 22 us to
-// read once): top-k 50 47 us, temperature alone 58, top-p 0.95 93, all of them mixed 110; one row of 32000 with top-k 50 16 us,
-// with top-p 0.95 27.
+// read once): top-k 50 47 us, temperature alone 58, top-p 0.95 92, all of them mixed 107; one row of 32000 with top-k 50 15 us,
+// with top-p 0.95 26.
 #include <hip/hip_runtime.h>
 
 #include "fq_internal.h"
@@ -230,41 +230,48 @@ struct Row {
                 l[e] = at + e < end ? (float)x[at + e] : -INFINITY;
         }
     }
-    // LIGHT passes ask for 64 bytes a thread at once; the others (exponentials) for the next 32 while the last are worked on.
+    // LIGHT passes ask for 64 bytes a thread at once; the others (exponentials) for the next 32 while the last are worked on.  A
+    // wavefront's stretches lie side by side, and requests run across their ends.
     template <bool LIGHT, class F, class G>
     __device__ __forceinline__ void stretches(const F &f, const G &g) const
     {
         constexpr int AHEAD = (LIGHT ? 64 : 32) / (VEC * (int)sizeof(T)), STEP = AHEAD * 64 * VEC;
         const int lane = threadIdx.x & 63;
-        for (int part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); part < STRETCHES && part * length < V; part += WAVES) {
-            const int end = min((part + 1) * length, V);
-            float l[AHEAD][VEC];
-            auto ask = [&](int first, float (&to)[AHEAD][VEC]) {
+        int part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (STRETCHES / WAVES);
+        const int begin = part * length, end = min(begin + STRETCHES / WAVES * length, V);
+        int part_end = begin + length;
+        float l[AHEAD][VEC];
+        auto ask = [&](int first, float (&to)[AHEAD][VEC]) {
 #pragma unroll
-                for (int b = 0; b < AHEAD; b++)
-                    if (first + b * 64 * VEC < end)
-                        block(first + (b * 64 + lane) * VEC, end, to[b]);
-            };
-            if (!LIGHT)
-                ask(part * length, l);
-            for (int first = part * length; first < end; first += STEP) {
-                float next[AHEAD][VEC];
-                if (LIGHT)
-                    ask(first, l);
-                else if (first + STEP < end)
-                    ask(first + STEP, next);
+            for (int b = 0; b < AHEAD; b++)
+                if (first + b * 64 * VEC < end)
+                    block(first + (b * 64 + lane) * VEC, end, to[b]);
+        };
+        if (!LIGHT)
+            ask(begin, l);
+        for (int first = begin; first < end; first += STEP) {
+            float next[AHEAD][VEC];
+            if (LIGHT)
+                ask(first, l);
+            else if (first + STEP < end)
+                ask(first + STEP, next);
 #pragma unroll
-                for (int b = 0; b < AHEAD; b++)
-                    if (first + b * 64 * VEC < end)
-                        f(l[b], first + (b * 64 + lane) * VEC);
-                if (!LIGHT)
-#pragma unroll
-                    for (int b = 0; b < AHEAD; b++)
-#pragma unroll
-                        for (int e = 0; e < VEC; e++)
-                            l[b][e] = next[b][e];
+            for (int b = 0; b < AHEAD; b++) {
+                const int at = first + b * 64 * VEC;
+                if (at < end) {
+                    f(l[b], at + lane * VEC);
+                    if (at + 64 * VEC >= (part_end < end ? part_end : end)) {
+                        g(part++);
+                        part_end += length;
+                    }
+                }
             }
-            g(part);
+            if (!LIGHT)
+#pragma unroll
+                for (int b = 0; b < AHEAD; b++)
+#pragma unroll
+                    for (int e = 0; e < VEC; e++)
+                        l[b][e] = next[b][e];
         }
     }
     template <bool LIGHT, class F>
