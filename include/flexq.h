@@ -500,7 +500,7 @@ int fq_kv_append(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q
  *   lse        device, f32 [tokens][q_heads], or NULL                                            (written)
  *   max_q      no sequence has more new tokens than this (rows beyond are left alone), 1 <= max_q <= tokens
  *   max_kv     no kv_len is larger than this (keys beyond are not seen; table_width * page_tokens always does); >= 1.  The launch is
- *              shaped by the two: close bounds are faster
+ *              shaped by the two: close bounds are faster, and so are prompts and single tokens in calls of their own
  *   workspace  device, fq_attend_workspace_bytes(...) bytes, 256-byte aligned; calls that may overlap in time need one each.
  *              What is enough for a max_kv is enough for any smaller one
  * q_heads a multiple of kv_heads, at most FQ_MAX_Q_HEADS; scale finite.  tokens >= 0 (0 launches nothing).  Never waits for the

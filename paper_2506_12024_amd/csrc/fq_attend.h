@@ -21,7 +21,7 @@ struct FqAttendWork {
     int key0;
     int chunk;      // keys of one part
     int part0;      // its parts are part0 .. part0 + parts - 1
-    int row_blocks; // of a sequence (shared: of all tokens)
+    int row_blocks; // of a sequence (shared: of all tokens); 0: the sequences' row blocks follow each other, as many as each has
     uint32_t blocks_x, parts, blocks; // its grid: key heads times row blocks, parts, sequences; workgroups in all
     float *part_o;  // [part][token][q_head][dim] not yet divided, or null: one part, the result goes out
     float2 *part_ml; // [part][token][q_head]: largest score (times log2 e), sum
@@ -63,6 +63,32 @@ __device__ __forceinline__ FqAttendRows fq_attend_rows(const FqAttendArgs &a, co
         r.rows = min(s.n, a.max_q) * group;
     }
     return r;
+}
+
+// Row block `at` of those that the sequences have, one after the other: its sequence and its number there, the last one first (its
+// rows see most keys); false past the end.  64 sequences at a time, every lane of the wavefront together.
+__device__ __forceinline__ bool fq_find_row_block(const FqAttendArgs &a, int at, int group, int rows_per_block, int &b, int &block)
+{
+    const int lane = threadIdx.x & 63;
+    for (int b0 = 0; b0 < a.seqs.seqs; b0 += 64) {
+        int mine = 0;
+        if (b0 + lane < a.seqs.seqs)
+            mine = (min(fq_seq(a.seqs, a.kv.page_shift, b0 + lane).n, a.max_q) * group + rows_per_block - 1) / rows_per_block;
+        int to = mine;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(to, o);
+            to += lane >= o ? x : 0;
+        }
+        const uint64_t after = __ballot(to > at);
+        if (after) {
+            const int who = __builtin_ctzll(after);
+            b = b0 + who;
+            block = __shfl(to, who) - 1 - at;
+            return true;
+        }
+        at -= __shfl(to, 63);
+    }
+    return false;
 }
 
 // The page of a key, -1 for one that is not there (past `end`, or a hole).

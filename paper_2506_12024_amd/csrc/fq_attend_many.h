@@ -44,10 +44,13 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
     auto &missing = shared.missing;
 
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
-    const int head = at_block.x % a.kv.kv_heads, b = at_block.z;
-    // the last rows see most keys: they begin first
-    const int row0 = (w.row_blocks - 1 - (int)(at_block.x / a.kv.kv_heads)) * FQ_MANY_ROWS;
     const int group = a.q_heads / a.kv.kv_heads, dim = FULL ? DP : a.kv.dim;
+    const int head = at_block.x % a.kv.kv_heads;
+    int b = at_block.z, block = w.row_blocks - 1 - (int)(at_block.x / a.kv.kv_heads); // the last rows see most keys: they begin first
+    if (w.row_blocks == 0 && !fq_find_row_block(a, (int)(at_block.x / a.kv.kv_heads), group, FQ_MANY_ROWS, b, block))
+        return;
+    b = __builtin_amdgcn_readfirstlane(b);
+    const int row0 = __builtin_amdgcn_readfirstlane(block) * FQ_MANY_ROWS;
     const FqAttendRows rs = fq_attend_rows(a, w, b, group);
     if (row0 >= rs.rows)
         return;

@@ -102,6 +102,20 @@ def test_shared_prefixes(prefix, heads, seqs):
 
 
 @pytest.mark.parametrize("new", [[1, 2, 3], [4, 0, 30], [100, 1, 65]])
+def test_ragged_chunks_behind_a_prefix(new):
+    run(Batch(new, [n + 9 for n in new], 8, prefix=203), 4, 2, 64, torch.float16, lse=False)
+
+
+@pytest.mark.parametrize("dim,heads", [(64, (8, 2)), (128, (4, 4)), (80, (2, 1)), (256, (2, 2))])
+def test_prompts_among_single_tokens(dim, heads):
+    """Row blocks of many sequences follow each other: empty ones, more than 64, prompts first, last and between."""
+    for new in ([150, 1, 1, 40, 0, 0, 7], [0, 0, 1, 300], [1] * 70 + [130, 0, 33] + [2] * 60, [90] * 3):
+        kv = [n + (13 * i) % 50 for i, n in enumerate(new)]
+        run(Batch(new, kv, 16), heads[0], heads[1], dim, torch.float16)
+    run(Batch([150, 1, 0, 40], [160, 300, 0, 40], 16), heads[0], heads[1], dim, torch.bfloat16, max_q=151)
+
+
+@pytest.mark.parametrize("new", [[1, 2, 3], [4, 0, 30], [100, 1, 65]])
 def test_shared_prefixes_of_chunks(new):
     run(Batch(new, [n + 9 for n in new], 8, prefix=203), 4, 2, 128, torch.float16)
     run(Batch(new, new, 8, prefix=64), 8, 2, 64, torch.bfloat16)
