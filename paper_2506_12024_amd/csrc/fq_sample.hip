@@ -209,25 +209,21 @@ template <class T, int VEC_>
 struct Row {
     static constexpr int VEC = VEC_;
     static constexpr bool LIST = false;
-    const T *x;
-    int V, length;
+    const T *x;      // the row
+    int V, skip, length; // skip: entries before it on a 16-byte boundary, which `at` below counts from (rows begin anywhere)
     typedef T Vec __attribute__((ext_vector_type(VEC)));
 
     __device__ __forceinline__ void block(int at, int end, float (&l)[VEC]) const
     {
-        if (at + VEC <= end) {
-            if constexpr (VEC > 1) {
-                const Vec v = *(const Vec *)(x + at);
+        if (at >= skip && at + VEC <= end) {
+            const Vec v = *(const Vec *)(x + (at - skip));
 #pragma unroll
-                for (int e = 0; e < VEC; e++)
-                    l[e] = (float)v[e];
-            } else {
-                l[0] = (float)x[at];
-            }
+            for (int e = 0; e < VEC; e++)
+                l[e] = (float)v[e];
         } else {
 #pragma unroll
             for (int e = 0; e < VEC; e++)
-                l[e] = at + e < end ? (float)x[at + e] : -INFINITY;
+                l[e] = at + e >= skip && at + e < end ? (float)x[at + e - skip] : -INFINITY;
         }
     }
     // LIGHT passes ask for 64 bytes a thread at once; the others (exponentials) for the next 32 while the last are worked on.  A
@@ -238,7 +234,7 @@ struct Row {
         constexpr int AHEAD = (LIGHT ? 64 : 32) / (VEC * (int)sizeof(T)), STEP = AHEAD * 64 * VEC;
         const int lane = threadIdx.x & 63;
         int part = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (STRETCHES / WAVES);
-        const int begin = part * length, end = min(begin + STRETCHES / WAVES * length, V);
+        const int begin = part * length, end = min(begin + STRETCHES / WAVES * length, V + skip);
         int part_end = begin + length;
         float l[AHEAD][VEC];
         auto ask = [&](int first, float (&to)[AHEAD][VEC]) {
@@ -259,7 +255,7 @@ struct Row {
             for (int b = 0; b < AHEAD; b++) {
                 const int at = first + b * 64 * VEC;
                 if (at < end) {
-                    f(l[b], at + lane * VEC);
+                    f(l[b], at + lane * VEC - skip);
                     if (at + 64 * VEC >= (part_end < end ? part_end : end)) {
                         g(part++);
                         part_end += length;
@@ -602,10 +598,10 @@ __device__ __forceinline__ void draw(Shared &s, const Row<T, VEC> &row, const We
     }
     __syncthreads();
     u64 left = s.word[1];
-    const int first = (int)s.word[0] * row.length, end = min(first + row.length, row.V);
+    const int first = (int)s.word[0] * row.length - row.skip, end = min(first + row.length, row.V);
     for (int base = first; base < end; base += THREADS) {
         const int i = base + threadIdx.x;
-        const float l = i < end ? (float)row.x[i] : -INFINITY;
+        const float l = i >= 0 && i < end ? (float)row.x[i] : -INFINITY;
         const u64 w = cut.keeps(l, i) ? weigh.kept(weigh.depth(l)) : 0;
         u64 sum;
         const u64 to = running(s, w, sum);
@@ -676,7 +672,8 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
     const float temperature = a.temperature ? a.temperature[r] : 1.0f, p = a.top_p ? a.top_p[r] : 1.0f;
     const float min_p = a.min_p ? a.min_p[r] : 0.0f, u = a.u[r];
     const int k = a.top_k ? a.top_k[r] : 0;
-    const Row<T, VEC> row{(const T *)a.logits + r * a.row_stride, V, length};
+    const T *const x = (const T *)a.logits + r * a.row_stride;
+    const Row<T, VEC> row{x, V, (int)((uintptr_t)x / sizeof(T) % VEC), length};
     if (tid < ROOTS)
         s.table[tid] = root_of_two(tid) * unit;
     if (tid < STRETCHES)
@@ -768,7 +765,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
             list.template each<true>([&](const float (&l)[1], int i) {
                 const u64 w = cut.keeps(l[0], i) ? weigh.kept(weigh.depth(l[0])) : 0;
                 if (w)
-                    atomicAdd(&s.stretch[i / length], w);
+                    atomicAdd(&s.stretch[(i + row.skip) / length], w);
             });
             draw(s, row, weigh, cut, u, a.token + r, a.prob ? a.prob + r : nullptr);
             return;
@@ -800,7 +797,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
             const Cut c = cut_of(s.cell_key[tid]);
             const u64 w = cut.keeps(c.l, c.i) ? weigh.kept(weigh.depth(c.l)) : 0;
             if (w)
-                atomicAdd(&s.stretch[c.i / length], w);
+                atomicAdd(&s.stretch[(c.i + row.skip) / length], w);
         }
     }
     if (!summed && cut.l == -INFINITY && weigh.least == 0.0)
@@ -829,7 +826,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(FqSampleArgs a, double 
 template <class T, int VEC>
 void launch(const FqSampleArgs &a, double unit, hipStream_t stream)
 {
-    const int blocks = (a.V + STRETCHES * 64 * VEC - 1) / (STRETCHES * 64 * VEC);
+    const int blocks = (a.V + VEC - 1 + STRETCHES * 64 * VEC - 1) / (STRETCHES * 64 * VEC); // (with what a row may skip)
     sample_kernel<T, VEC><<<a.R, THREADS, 0, stream>>>(a, unit, blocks * 64 * VEC);
 }
 
@@ -841,15 +838,9 @@ hipError_t fq_launch_sample(const FqSampleArgs &a, bool half, void *, hipStream_
 {
     const int log_v = a.V > 1 ? 32 - __builtin_clz((unsigned)a.V - 1) : 0;
     const double unit = (double)(1ULL << (log_v > 11 ? 62 - log_v : 51));
-    const int vec = half ? 8 : 4;
-    const bool wide = ((uintptr_t)a.logits & 15) == 0 && (a.R == 1 || a.row_stride % vec == 0);
-    if (half && wide)
+    if (half)
         launch<_Float16, 8>(a, unit, stream);
-    else if (half)
-        launch<_Float16, 1>(a, unit, stream);
-    else if (wide)
-        launch<float, 4>(a, unit, stream);
     else
-        launch<float, 1>(a, unit, stream);
+        launch<float, 4>(a, unit, stream);
     return hipGetLastError();
 }
