@@ -11,8 +11,9 @@
 //   4. the draw: kept weights summed over the 64 stretches, the one that holds the target, its entries in order
 // Bound by reading a long row two (top-k, temperature, min-p) or three times (top-p), all but the first from the caches, and by
 // the exponentials of the entries that count; by the chain of steps for a short one.  Measured, 256 rows of 128256 (131 MB, 22 us to
-// read once): top-k 50 47 us, temperature alone 58, top-p 0.95 92, all of them mixed 107; one row of 32000 with top-k 50 15 us,
-// with top-p 0.95 26.
+// read once): top-k 50 47 us, temperature alone 58, top-p 0.95 92, all of them mixed 107 to 116 (by the settings drawn); one row of
+// 32000 with top-k 50 15 us, with top-p 0.95 26.  Rows count from the 16-byte boundary before them, so that any row is read 16 bytes at a
+// time: 256 of 128255 with top-p 0.95 96 us; it costs aligned rows 0.5 to 2 %.
 #include <hip/hip_runtime.h>
 
 #include "fq_internal.h"
