@@ -194,7 +194,7 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
             float x[8];
 #pragma unroll
             for (int i = 0; i < 8; i++)
-                x[i] = sc[rt][i >> 2][i & 3];
+                x[i] = fq_score(sc[rt][i >> 2][i & 3], c);
             if (masked) {
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
@@ -204,8 +204,8 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
                 }
             }
             float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-            top = fq_over32<false>(fq_over16<false>(top)) * c;
-            if (__any(top > m[rt] + FQ_ATTEND_SLACK)) {
+            top = fq_over32<false>(fq_over16<false>(top));
+            if (__any(top - m[rt] > FQ_ATTEND_SLACK)) {
                 const float now = fmaxf(m[rt], top);
                 const float fall = __builtin_amdgcn_exp2f(m[rt] - fq_reference(now));
                 m[rt] = now;
@@ -218,7 +218,7 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, -ref));
+                x[i] = __builtin_amdgcn_exp2f(x[i] - ref);
                 sum += x[i];
             }
             l[rt] += sum;

@@ -174,12 +174,15 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
                     x[i] = -INFINITY;
             }
         }
+#pragma unroll
+        for (int i = 0; i < 16; i++)
+            x[i] = fq_score(x[i], c);
         float top = x[0];
 #pragma unroll
         for (int i = 1; i < 16; i++)
             top = fmaxf(top, x[i]);
-        top = fq_over32<false>(top) * c;
-        const bool raise = __any(top > m + FQ_ATTEND_SLACK);
+        top = fq_over32<false>(top);
+        const bool raise = __any(top - m > FQ_ATTEND_SLACK);
         const float now = raise ? fmaxf(m, top) : m, ref = fq_reference(now);
         const float fall = __builtin_amdgcn_exp2f(m - ref);
         l *= fall; // (1 where nothing is raised)
@@ -193,7 +196,7 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
                 ring[i % AHEAD] = piece(i + AHEAD, v_last, k_next);
 #pragma unroll
             for (int e = i * 16 / PRODUCTS; e < (i + 1) * 16 / PRODUCTS; e++) {
-                x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], c, -ref));
+                x[e] = __builtin_amdgcn_exp2f(x[e] - ref);
                 if (e > 0)
                     l += x[e - 1]; // (one behind: the exponential takes a while)
                 if (e > 1 && e % 2 == 0)
