@@ -142,8 +142,9 @@ __device__ __forceinline__ uint32_t fq_pack2(float x, float y)
 }
 
 // The factor of the scores in powers of two.  It is never negative -- Q's signs are turned instead (exact), so that the largest
-// product is the largest score -- nor 0, so that a masked -inf stays one (2^-120 of any score is nothing).
-__device__ __forceinline__ float fq_score_factor(float scale) { return fmaxf(fabsf(scale) * FQ_LOG2E, 0x1p-120f); }
+// product is the largest score -- nor 0, so that a masked -inf stays one: at least the smallest binary32 value, which leaves of any score
+// that is finite (under 2^128) 2^-21 at most.
+__device__ __forceinline__ float fq_score_factor(float scale) { return fmaxf(fabsf(scale) * FQ_LOG2E, 0x1p-149f); }
 __device__ __forceinline__ u32x4 fq_signed(u32x4 q, float scale) { return scale < 0.0f ? q ^ 0x80008000u : q; }
 
 // Four consecutive rows (keys) of a 16-column block of LDS, column by column: of 16 lanes, lane t names 8 bytes (row t / 4, columns

@@ -7,7 +7,7 @@ import torch
 
 import paper_2506_12024_amd as fq
 from serve_util import EPS, TYPES, Batch, attend, pool
-from test_gpu_attend import call, f64
+from test_gpu_attend import call, check, f64
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -41,3 +41,18 @@ def test_equal_largest_scores_of_any_size(dtype, dim, new, prefix, scale):
     share = np.abs(f64(out) - want) / tol
     assert np.all(share <= 1), "off by %g of the tolerance at %s" % (share.max(), np.unravel_index(share.argmax(), share.shape))
     assert np.all(np.abs(f64(lse) - want_lse) <= 32 * 2.0 ** -24 * (1 + np.abs(want_lse)))
+
+
+@pytest.mark.parametrize("new", [[1, 1], [3], [40, 1]])
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -121, -(2.0 ** -119), 2.0 ** -126, 2.0 ** -140, -(2.0 ** -149)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_smallest_scales_of_the_largest_products(new, scale, dim):
+    """bfloat16 queries and keys of 2^58: products of 2^120 under scales down to the smallest binary32 value and 0."""
+    batch = Batch(new, [n + 150 for n in new], 16)
+    gen = torch.Generator().manual_seed(43)
+    kc, vc = (pool(gen, batch.pages, 2, 16, dim, torch.bfloat16) for _ in range(2))
+    kc.mul_(2.0 ** 58)
+    q = (2.0 ** 58 * torch.randn((batch.tokens, 4, dim), generator=gen)).bfloat16().to(DEV)
+    out, lse, _ = call(batch, fq.KVCache(kc, vc), q, scale)
+    torch.cuda.synchronize()
+    check(batch, out, lse, q, kc, vc, scale)
