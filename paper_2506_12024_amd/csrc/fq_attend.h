@@ -185,6 +185,16 @@ __device__ __forceinline__ float fq_score(float x, float c)
 // exp2(x - m) for a row whose reference may still be -inf (nothing seen yet: 0)
 __device__ __forceinline__ float fq_reference(float m) { return m == -INFINITY ? 0.0f : m; }
 
+// Adds a step's sum of weights to a row's, with what rounding has taken from it: thousands of small sums beside one large weight lose the
+// same part each time, or all of themselves (16 equal weights of 2^-24.3 at a time to a sum of 1).
+__device__ __forceinline__ void fq_add_weights(float &l, float &lost, float sum)
+{
+#pragma clang fp contract(off)
+    const float add = sum - lost, to = l + add;
+    lost = (to - l) - add;
+    l = to;
+}
+
 // lse in natural logarithms of a row with reference m (times log2 e) and sum l
 __device__ __forceinline__ float fq_lse(float m, float l) { return l == 0.0f ? -INFINITY : fq_reference(m) * FQ_LN2 + logf(l); }
 __device__ __forceinline__ float fq_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
@@ -202,7 +212,7 @@ __device__ __forceinline__ void fq_attend_row_by_row(const FqAttendArgs &a, cons
     for (int r = row0 + (threadIdx.x >> 6); r <= last; r += blockDim.x >> 6) {
         const int j = r / group, h = head * group + r % group, lim = min(rs.limit(j), end);
         const uint16_t *q = a.q + (rs.q0 + j) * a.q_stride + h * dim;
-        float m = -INFINITY, l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        float m = -INFINITY, l = 0.0f, lost = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int k0 = begin; k0 < lim; k0 += 64) {
             const int key = k0 + lane, page = fq_key_page(a, table, key, lim);
             const bool there = page >= 0 && page < a.kv.n_pages;
@@ -219,11 +229,11 @@ __device__ __forceinline__ void fq_attend_row_by_row(const FqAttendArgs &a, cons
             float sum = p;
             for (int o2 = 32; o2; o2 >>= 1)
                 sum += __shfl_xor(sum, o2);
-            l = l * fall + sum;
+            l *= fall;
+            lost *= fall;
+            fq_add_weights(l, lost, sum);
             m = now;
-#pragma unroll
-            for (int e = 0; e < 4; e++)
-                o[e] *= fall;
+            float here[4] = {0.0f, 0.0f, 0.0f, 0.0f}; // (64 keys by themselves: one long sum loses as l would)
             const uint64_t seen = __ballot(there);
             for (int i = 0; i < 64; i++) {
                 const float pi = __shfl(p, i);
@@ -232,8 +242,11 @@ __device__ __forceinline__ void fq_attend_row_by_row(const FqAttendArgs &a, cons
 #pragma unroll
                     for (int e = 0; e < 4; e++)
                         if (lane + 64 * e < dim)
-                            o[e] = fmaf(pi, fq_to_float(a.kv.v[from + lane + 64 * e], BF16), o[e]);
+                            here[e] = fmaf(pi, fq_to_float(a.kv.v[from + lane + 64 * e], BF16), here[e]);
             }
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                o[e] = fmaf(o[e], fall, here[e]);
         }
         const long long t = rs.q0 + j;
         if (w.part_o) {

@@ -94,11 +94,11 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
     }
 
     float4_t o[RT][ND];
-    float m[RT], l[RT];
+    float m[RT], l[RT], lost[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) {
         m[rt] = -INFINITY;
-        l[rt] = 0.0f;
+        l[rt] = lost[rt] = 0.0f;
 #pragma unroll
         for (int d = 0; d < ND; d++)
             o[rt][d] = float4_t{0, 0, 0, 0};
@@ -210,6 +210,7 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
                 const float fall = __builtin_amdgcn_exp2f(m[rt] - fq_reference(now));
                 m[rt] = now;
                 l[rt] *= fall;
+                lost[rt] *= fall;
 #pragma unroll
                 for (int d = 0; d < ND; d++)
                     o[rt][d] *= fall;
@@ -221,7 +222,7 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
                 x[i] = __builtin_amdgcn_exp2f(x[i] - ref);
                 sum += x[i];
             }
-            l[rt] += sum;
+            fq_add_weights(l[rt], lost[rt], sum);
             p[rt] = u32x4{fq_pack2<BF16>(x[0], x[1]), fq_pack2<BF16>(x[2], x[3]), fq_pack2<BF16>(x[4], x[5]),
                           fq_pack2<BF16>(x[6], x[7])};
         }

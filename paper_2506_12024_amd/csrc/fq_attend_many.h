@@ -90,7 +90,7 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
 #pragma unroll
         for (int i = 0; i < 16; i++)
             o[d][i] = 0.0f;
-    float m = -INFINITY, l = 0.0f;
+    float m = -INFINITY, l = 0.0f, lost = 0.0f;
     const float c = fq_score_factor(a.scale);
     const int32_t *table = a.seqs.table + (rs.shared ? 0 : (long long)b * a.seqs.table_width);
 
@@ -186,6 +186,8 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
         const float now = raise ? fmaxf(m, top) : m, ref = fq_reference(now);
         const float fall = __builtin_amdgcn_exp2f(m - ref);
         l *= fall; // (1 where nothing is raised)
+        lost *= fall;
+        float sum = 0.0f;
         m = now;
         u32x4 weights[2];
         __builtin_amdgcn_sched_barrier(0);
@@ -198,13 +200,13 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
             for (int e = i * 16 / PRODUCTS; e < (i + 1) * 16 / PRODUCTS; e++) {
                 x[e] = __builtin_amdgcn_exp2f(x[e] - ref);
                 if (e > 0)
-                    l += x[e - 1]; // (one behind: the exponential takes a while)
+                    sum += x[e - 1]; // (one behind: the exponential takes a while)
                 if (e > 1 && e % 2 == 0)
                     weights[(e - 2) >> 3][((e - 2) & 7) >> 1] = fq_pack2<BF16>(x[e - 2], x[e - 1]);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        l += x[15];
+        fq_add_weights(l, lost, sum + x[15]);
         weights[1][3] = fq_pack2<BF16>(x[14], x[15]);
         pk[0] = weights[0];
         pk[1] = weights[1];

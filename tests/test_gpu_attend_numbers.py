@@ -1,4 +1,5 @@
 """fq_attend at the ends of its arithmetic, against the same 64-bit reference: scores of any size, weights of any size."""
+import copy
 import math
 
 import numpy as np
@@ -6,7 +7,7 @@ import pytest
 import torch
 
 import paper_2506_12024_amd as fq
-from serve_util import EPS, TYPES, Batch, attend, pool
+from serve_util import EPS, TYPES, Batch, attend, attend_tolerance, lse_tolerance, pool
 from test_gpu_attend import call, check, f64
 
 pytestmark = pytest.mark.gpu
@@ -56,3 +57,46 @@ def test_smallest_scales_of_the_largest_products(new, scale, dim):
     out, lse, _ = call(batch, fq.KVCache(kc, vc), q, scale)
     torch.cuda.synchronize()
     check(batch, out, lse, q, kc, vc, scale)
+
+
+def strong_and_weak(dtype, fall, new, kv, odd=False):
+    """The first key of every sequence has a score of 0 and a value of 0, the others -fall (in powers of two) and values about
+    1; odd: the last new token's value is NaN.  For three rows (result, lse, and what serve_util.attend says of it), one at a
+    time: a row's keys, of the first and the last head."""
+    heads, dim = 32, 64
+    batch = Batch(new, kv, 64)
+    gen = torch.Generator().manual_seed(47)
+    shape = (batch.pages, heads, 64, dim)
+    kc = torch.zeros(shape, dtype=dtype, device=DEV)
+    vc = (1.0 + 0.25 * torch.randn((batch.pages, 1, 64, dim), generator=gen)).to(dtype).to(DEV).expand(shape).contiguous()
+    kc[..., 5] = -fall * math.log(2.0) / 8.0
+    first = torch.from_numpy(batch.table[:, 0]).long().to(DEV)
+    kc[first, :, 0], vc[first, :, 0] = 0.0, 0.0
+    q = torch.zeros((batch.tokens, heads, dim), dtype=dtype, device=DEV)
+    q[..., 5] = 8.0
+    some, rows = [0, heads - 1], (0, batch.tokens // 2 + 5, batch.tokens - 1)
+    if odd:
+        rows = [batch.tokens - n for n in (2, 50, 100)]
+        vc[int(batch.table[0, (kv[0] - 1) // 64]), :, (kv[0] - 1) % 64] = float("nan")
+    out, lse, _ = call(batch, fq.KVCache(kc, vc), q, 1.0)
+    torch.cuda.synchronize()
+    k64, v64 = f64(kc[:, some]), f64(vc[:, some])
+    for row in rows:
+        b, place = batch.places()[row]
+        one = copy.copy(batch)
+        one.new, one.kv, one.table, one.q_start = [1], [place + 1], batch.table[b:b + 1], np.array([0, 1])
+        yield f64(out[row:row + 1, some]), f64(lse[row:row + 1, some]), place + 1, attend(one, f64(q[row:row + 1, some]), k64, v64, 1.0)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("fall", [0.0, 5.0, 12.3, 24.3])
+@pytest.mark.parametrize("new,kv,odd", [([1024], [32768], False), ([1024], [32768], True), ([1] * 24, [8192] * 24, False)])
+def test_sums_of_long_rows_lose_nothing(dtype, fall, new, kv, odd):
+    """Tens of thousands of equal weights beside a large one, in every kernel and (odd) on the way round values that are not
+    finite: the sum is as good as one of few."""
+    for out, lse, keys, (want, want_lse, size, steep, mass) in strong_and_weak(TYPES[dtype], fall, new, kv, odd):
+        off = np.abs(lse - want_lse) / lse_tolerance(want_lse, steep, 64, keys)
+        assert np.all(off <= 1), "lse off by %g of the tolerance" % off.max()
+        if odd:
+            off = np.abs(out - want) / attend_tolerance(TYPES[dtype], want, size, steep, mass, 64)
+            assert np.all(off <= 1), "off by %g of the tolerance" % off.max()
