@@ -24,12 +24,17 @@ struct FqAttendWork {
     int row_blocks; // of a sequence (shared: of all tokens); 0: the sequences' row blocks follow each other, as many as each has
     uint32_t blocks_x, parts, blocks; // its grid: key heads times row blocks, parts, sequences; workgroups in all
     float *part_o;  // [part][token][q_head][dim] not yet divided, or null: one part, the result goes out
-    float2 *part_ml; // [part][token][q_head]: largest score (times log2 e), sum
+    float2 *part_ml; // [part][token][q_head]: reference of the row's weights (a score times log2 e), their sum
 };
 
 constexpr float FQ_LOG2E = 1.4426950408889634f, FQ_LN2 = 0.6931471805599453f;
-// Rows are rescaled when a score passes their reference by more than this (in powers of two): p stays under 2^8, which
-// binary16 holds as exactly as 1, and most tiles rescale nothing.
+// A row's weights are 2^(score - its reference), rounded to the 16-bit type where they meet V.  binary16 ends under 2^16 and has fewer
+// bits below 2^-14, so there the reference is set 2^7 below the row's largest score, and the row is rescaled when a score passes that
+// one by more than 2^8 (most tiles rescale nothing): weights lie under 2^15, the largest at 2^7 or above, a key that has 2^-21 of it
+// keeps all its bits and one of 2^-32 still counts.  (With the reference at the largest score those were 2^-14 and 2^-25: 32768 keys
+// of 2^-27.5 beside one of 1 were lost, of 2^-24.3 a quarter too heavy.)  bfloat16 has binary32's range.
+template <bool BF16>
+constexpr float FQ_ATTEND_BELOW = BF16 ? 0.0f : 7.0f;
 constexpr float FQ_ATTEND_SLACK = 8.0f;
 
 // The rows of one workgroup's sequence and what they see.
@@ -195,8 +200,14 @@ __device__ __forceinline__ void fq_add_weights(float &l, float &lost, float sum)
     l = to;
 }
 
-// lse in natural logarithms of a row with reference m (times log2 e) and sum l
-__device__ __forceinline__ float fq_lse(float m, float l) { return l == 0.0f ? -INFINITY : fq_reference(m) * FQ_LN2 + logf(l); }
+// lse in natural logarithms of a row with reference m (times log2 e) and sum l, whose power of two joins the reference: both parts would
+// else be large and cancel where the lse is near 0.
+__device__ __forceinline__ float fq_lse(float m, float l)
+{
+    int power = 0;
+    const float part = frexpf(l, &power);
+    return l == 0.0f ? -INFINITY : (fq_reference(m) + (float)power) * FQ_LN2 + logf(part);
+}
 __device__ __forceinline__ float fq_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 
 // The products sum p v over all keys of a tile, and 0 times an infinity is NaN: a row must not meet a V that it does not see and that is not

@@ -205,8 +205,8 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
             }
             float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
             top = fq_over32<false>(fq_over16<false>(top));
-            if (__any(top - m[rt] > FQ_ATTEND_SLACK)) {
-                const float now = fmaxf(m[rt], top);
+            if (__any(top - m[rt] > FQ_ATTEND_SLACK + FQ_ATTEND_BELOW<BF16>)) {
+                const float now = fmaxf(m[rt], top - FQ_ATTEND_BELOW<BF16>);
                 const float fall = __builtin_amdgcn_exp2f(m[rt] - fq_reference(now));
                 m[rt] = now;
                 l[rt] *= fall;

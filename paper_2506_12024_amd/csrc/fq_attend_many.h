@@ -182,8 +182,8 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
         for (int i = 1; i < 16; i++)
             top = fmaxf(top, x[i]);
         top = fq_over32<false>(top);
-        const bool raise = __any(top - m > FQ_ATTEND_SLACK);
-        const float now = raise ? fmaxf(m, top) : m, ref = fq_reference(now);
+        const bool raise = __any(top - m > FQ_ATTEND_SLACK + FQ_ATTEND_BELOW<BF16>);
+        const float now = raise ? fmaxf(m, top - FQ_ATTEND_BELOW<BF16>) : m, ref = fq_reference(now);
         const float fall = __builtin_amdgcn_exp2f(m - ref);
         l *= fall; // (1 where nothing is raised)
         lost *= fall;

@@ -100,3 +100,14 @@ def test_sums_of_long_rows_lose_nothing(dtype, fall, new, kv, odd):
         if odd:
             off = np.abs(out - want) / attend_tolerance(TYPES[dtype], want, size, steep, mass, 64)
             assert np.all(off <= 1), "off by %g of the tolerance" % off.max()
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("fall", [12.3, 20.4, 24.3, 27.5])
+@pytest.mark.parametrize("new,kv", [([1024], [32768]), ([1] * 24, [8192] * 24)])
+def test_weak_keys_beside_a_strong_one_keep_their_share(dtype, fall, new, kv):
+    """The result is what the weak keys hold, the strong one's value being 0.  A weight errs by half a step of its type, in
+    binary16 by 2^-25 at least, where the largest is 2^7 and more: 2^-32 of the largest, 2^7 less than beside a largest of 1."""
+    for out, _, _, (want, _, size, steep, mass) in strong_and_weak(TYPES[dtype], fall, new, kv):
+        off = np.abs(out - want) / attend_tolerance(TYPES[dtype], want, size, steep, mass / 128, 64)
+        assert np.all(off <= 1), "off by %g of the tolerance" % off.max()
