@@ -231,7 +231,7 @@ __device__ __forceinline__ void fq_attend_row_by_row(const FqAttendArgs &a, cons
             float s = 0.0f;
             for (int d = 0; d < dim; d++)
                 s = fmaf(fq_to_float(q[d], BF16), fq_to_float(a.kv.k[at + d], BF16), s);
-            s = there ? (a.scale < 0.0f ? -s : s) * c : -INFINITY;
+            s = there ? fq_score(a.scale < 0.0f ? -s : s, c) : -INFINITY;
             float top = s;
             for (int o2 = 32; o2; o2 >>= 1)
                 top = fmaxf(top, __shfl_xor(top, o2));

@@ -19,8 +19,19 @@ DEV = "cuda:0"
 @pytest.mark.parametrize("new,prefix", [([1, 1, 1], 0), ([1, 2, 1], 100), ([40], 0), ([150, 9], 70)])
 @pytest.mark.parametrize("scale", [1.0, -0.37, 300.0])
 def test_equal_largest_scores_of_any_size(dtype, dim, new, prefix, scale):
+    equal_largest_scores(dtype, dim, new, prefix, scale, False)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("new,prefix", [([2, 3, 2], 0), ([40], 0), ([150, 9], 70)])
+@pytest.mark.parametrize("scale", [1.0, -0.37, 300.0])
+def test_equal_largest_scores_beside_values_that_are_not_finite(dtype, new, prefix, scale):
+    equal_largest_scores(dtype, 64, new, prefix, scale, True)
+
+
+def equal_largest_scores(dtype, dim, new, prefix, scale, odd):
     """Scores that are exact in binary32 (one product), from 10^5 to 10^12: the largest ones of a row are equal and share
-    its weight, everything else is further down than any weight reaches."""
+    its weight, everything else is further down than any weight reaches.  odd: each last new token's value is NaN."""
     batch = Batch(new, [n + 150 for n in new], 16, prefix=prefix)
     gen = torch.Generator().manual_seed(41)
     vc = pool(gen, batch.pages, 2, 16, dim, TYPES[dtype])
@@ -33,15 +44,22 @@ def test_equal_largest_scores_of_any_size(dtype, dim, new, prefix, scale):
     sizes = np.exp(np.linspace(math.log(4.0), math.log(60000.0), batch.tokens * 4)).reshape(batch.tokens, 4)
     q[..., 3] = torch.from_numpy(sizes).to(TYPES[dtype])
     kc, q = kc.to(DEV), q.to(DEV)
+    if odd:
+        for b, n in enumerate(batch.kv):
+            vc[int(batch.table[b, (n - 1) // 16]), :, (n - 1) % 16] = float("nan")
     out, lse, _ = call(batch, fq.KVCache(kc, vc), q, scale)
     torch.cuda.synchronize()
-    want, want_lse, size, _, _ = attend(batch, f64(q), f64(kc), f64(vc), float(np.float32(scale)))
+    keep = np.ones(batch.tokens, dtype=bool)
+    if odd:
+        keep[batch.q_start[1:] - 1] = False
+    want, want_lse, size, _, _ = (x[keep] for x in attend(batch, f64(q), f64(kc), f64(vc), float(np.float32(scale))))
+    out, lse = f64(out)[keep], f64(lse)[keep]
     # the scores are exact and equal, so are their weights: the roundings of these (binary32, then the type) and of the result
     half = EPS[TYPES[dtype]] / 2
     tol = half * (1 + half) * (np.abs(want) + size) + 2.0 ** -20 * size + 2.0 ** -25
-    share = np.abs(f64(out) - want) / tol
+    share = np.abs(out - want) / tol
     assert np.all(share <= 1), "off by %g of the tolerance at %s" % (share.max(), np.unravel_index(share.argmax(), share.shape))
-    assert np.all(np.abs(f64(lse) - want_lse) <= 32 * 2.0 ** -24 * (1 + np.abs(want_lse)))
+    assert np.all(np.abs(lse - want_lse) <= 32 * 2.0 ** -24 * (1 + np.abs(want_lse)))
 
 
 @pytest.mark.parametrize("new", [[1, 1], [3], [40, 1]])
@@ -111,3 +129,33 @@ def test_weak_keys_beside_a_strong_one_keep_their_share(dtype, fall, new, kv):
     for out, _, _, (want, _, size, steep, mass) in strong_and_weak(TYPES[dtype], fall, new, kv):
         off = np.abs(out - want) / attend_tolerance(TYPES[dtype], want, size, steep, mass / 128, 64)
         assert np.all(off <= 1), "off by %g of the tolerance" % off.max()
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("heads,dim", [((4, 2), 64), ((8, 1), 128), ((2, 2), 80), ((2, 1), 256)])
+@pytest.mark.parametrize("new,own", [([4], 0), ([3, 1], 60), ([40], 90), ([150], 9), ([70, 5], 30)])
+def test_values_that_are_not_finite_behind_a_prefix(dtype, heads, dim, new, own):
+    """A chunk's later tokens hold infinities and NaNs, and it stands behind a prefix with a hole: rows before them see prefix
+    and cache as if they were not there."""
+    batch = Batch(new, [n + own for n in new], 8, prefix=77)
+    batch.prefix_table[3] = -1
+    gen = torch.Generator().manual_seed(51)
+    kc, vc = (pool(gen, batch.pages, heads[1], 8, dim, TYPES[dtype]) for _ in range(2))
+    q = torch.randn((batch.tokens, heads[0], dim), generator=gen).to(TYPES[dtype]).to(DEV)
+    first_bad = [n - n // 2 for n in new]
+    for b, n in enumerate(new):
+        for j in range(first_bad[b], n):
+            p = own + j
+            vc[int(batch.table[b, p // 8]), :, p % 8, j % dim] = [float("nan"), float("inf"), -float("inf")][j % 3]
+            if j % 2:
+                kc[int(batch.table[b, p // 8]), :, p % 8, 3] = float("nan")
+    out, lse, _ = call(batch, fq.KVCache(kc, vc), q, 0.1)
+    torch.cuda.synchronize()
+    keep = np.concatenate([np.arange(n) < f for n, f in zip(new, first_bad)])
+    want, want_lse, size, steep, mass = attend(batch, f64(q), f64(torch.nan_to_num(kc, 0, 0, 0)), f64(torch.nan_to_num(vc, 0, 0, 0)), 0.1)
+    got, tol = f64(out), attend_tolerance(q.dtype, want, size, steep, mass, dim)
+    assert np.all(np.abs(got[keep] - want[keep]) <= tol[keep])
+    assert np.all(np.abs(f64(lse)[keep] - want_lse[keep]) <= lse_tolerance(want_lse[keep], steep[keep], dim, 77 + max(batch.kv)))
+    for b, (n, f) in enumerate(zip(new, first_bad)):
+        for j in range(f, n):
+            assert not np.isfinite(got[batch.q_start[b] + j, :, f % dim]).any()
