@@ -122,10 +122,10 @@ struct Weigh {
     {
         return low_bits(fma(power(d.n), series(d.f), 0x1p52));
     }
-    __device__ __forceinline__ u64 kept(const Depth &d) const // what min-p leaves of it
+    __device__ __forceinline__ u64 kept(const Depth &d) const // what min-p leaves of it: all of the same whole number, or nothing
     {
         const double v = power(d.n) * series(d.f);
-        return v >= least ? low_bits(v + 0x1p52) : 0;
+        return v >= least ? whole(d) : 0;
     }
     static __device__ __forceinline__ int bin(const Depth &d) { return min(max(-d.n, 0) >> 2, BINS - 1); }
     // no entry of the first `bins` bins lies below this
