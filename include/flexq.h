@@ -477,7 +477,7 @@ int fq_seqs_destroy(fq_seqs *seqs);
  * binary32, one rounding to the tensors' type.  The rest of a head is copied.
  *   q, k, v    device, [tokens][heads][head_dim], rows q_stride, k_stride, v_stride elements apart (q, k and v may be parts
  *              of one row), 16-byte aligned, strides multiples of 8                              (read)
- *   q_out      device, rows q_out_stride elements apart; may not overlap q                       (written)
+ *   q_out      device, rows q_out_stride elements apart; may not overlap q, k or v                (written)
  *   freqs      device, f64 [rot_dim / 2]; NULL with rot_dim = 0: nothing is turned
  *   positions  device, int32 [tokens], or NULL: prefix_len + the place in the sequence
  * q and q_out may be NULL with q_heads = 0 (keys and values only).  0 <= rot_dim <= head_dim, even.  tokens >= 0 (0 launches

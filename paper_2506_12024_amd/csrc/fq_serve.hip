@@ -54,6 +54,34 @@ int check_rows(const char *who, const char *name, const void *p, long long strid
     return FQ_OK;
 }
 
+// Whether two sets of as many rows, of width_a and width_b values, share one.  (Rows that lie between each other's share none.)
+bool rows_overlap(const void *a, long long stride_a, long long width_a, const void *b, long long stride_b, long long width_b, int rows)
+{
+    typedef __int128 Place; // of a row in bytes: a stride may be any number
+    Place at_a = (Place)(uintptr_t)a, at_b = (Place)(uintptr_t)b;
+    const Place step_a = (Place)stride_a * 2, step_b = (Place)stride_b * 2, size_a = width_a * 2, size_b = width_b * 2;
+    if (at_a + step_a * (rows - 1) + size_a <= at_b || at_b + step_b * (rows - 1) + size_b <= at_a)
+        return false;
+    if (step_a == step_b) { // (parts of one row) the last of a's rows to begin before a row of b ends, counted from that one's number
+        const Place from = at_b - at_a - size_a, to = at_b - at_a + size_b - 1;
+        Place t = to >= 0 ? to / step_a : -((step_a - 1 - to) / step_a);
+        t = t < rows - 1 ? t : rows - 1;
+        return t > -(Place)rows && t * step_a > from;
+    }
+    for (int i = 0, j = 0; i < rows && j < rows;) { // both ascend: the row that ends first meets nothing further on
+        if (at_a + size_a <= at_b) {
+            at_a += step_a;
+            i++;
+        } else if (at_b + size_b <= at_a) {
+            at_b += step_b;
+            j++;
+        } else {
+            return true;
+        }
+    }
+    return false;
+}
+
 int check_q_heads(const char *who, int q_heads, int kv_heads)
 {
     if (q_heads < 1 || q_heads > FQ_MAX_Q_HEADS || q_heads % kv_heads != 0)
@@ -211,13 +239,18 @@ int fq_kv_append(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q
             return rc;
         if (int rc = check_rows(who, "q_out", q_out, q_out_stride, q_heads, c.dim))
             return rc;
-        if (q == q_out)
-            return fq_fail(FQ_ERR_SHAPE, "%s: q_out may not overlap q", who);
     }
     if (int rc = check_rows(who, "k", k, k_stride, c.kv_heads, c.dim))
         return rc;
     if (int rc = check_rows(who, "v", v, v_stride, c.kv_heads, c.dim))
         return rc;
+    if (q_heads != 0) { // (a thread may read a value after another has written its place)
+        const long long q_width = (long long)q_heads * c.dim, kv_width = (long long)c.kv_heads * c.dim;
+        if (rows_overlap(q_out, q_out_stride, q_width, q, q_stride, q_width, tokens) ||
+            rows_overlap(q_out, q_out_stride, q_width, k, k_stride, kv_width, tokens) ||
+            rows_overlap(q_out, q_out_stride, q_width, v, v_stride, kv_width, tokens))
+            return fq_fail(FQ_ERR_SHAPE, "%s: q_out may not overlap q, k or v", who);
+    }
     if (rot_dim > 0 && !freqs)
         return fq_fail(FQ_ERR_NULL, "%s: freqs is NULL", who);
     if (!std::isfinite(amplitude))
