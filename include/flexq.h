@@ -496,7 +496,7 @@ int fq_kv_append(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q
  * type where it meets v.  A row that sees no key gives 0 and lse = -inf.  What lies in the cache beyond kv_len, in holes and in other pages is not looked
  * at, whatever it holds.
  *   q, out     device, [tokens][q_heads][head_dim], rows q_stride, out_stride elements apart, 16-byte aligned, strides
- *              multiples of 8                                                                    (read / written)
+ *              multiples of 8; out may be q itself, row for row, but not overlap it otherwise    (read / written)
  *   lse        device, f32 [tokens][q_heads], or NULL                                            (written)
  *   max_q      no sequence has more new tokens than this (rows beyond are left alone), 1 <= max_q <= tokens
  *   max_kv     no kv_len is larger than this (keys beyond are not seen; table_width * page_tokens always does); >= 1.  The launch is

@@ -312,12 +312,16 @@ int fq_attend(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q, l
         return fq_fail(FQ_ERR_NULL, "%s: workspace is NULL", who);
     if (!aligned(lse, 4) || !aligned(workspace, 256))
         return fq_fail(FQ_ERR_ALIGN, "%s: lse needs 4-byte, the workspace 256-byte alignment", who);
-    if (!std::isfinite(scale))
-        return fq_fail(FQ_ERR_SHAPE, "%s: scale must be finite", who);
     const size_t need = fq_attend_bytes(a, false, fq_device_cus());
     if (workspace_bytes < need)
         return fq_fail(FQ_ERR_SHAPE, "%s: the workspace has %zu bytes, fq_attend_workspace_bytes asks for %zu", who,
                        workspace_bytes, need);
+    // (a workgroup reads its own rows of q before it writes theirs of out, in any order with others)
+    const long long width = (long long)q_heads * kv->view.dim;
+    if ((q != out || q_stride != out_stride) && rows_overlap(q, q_stride, width, out, out_stride, width, tokens))
+        return fq_fail(FQ_ERR_SHAPE, "%s: out may be q, row for row, but not overlap it otherwise", who);
+    if (!std::isfinite(scale))
+        return fq_fail(FQ_ERR_SHAPE, "%s: scale must be finite", who);
     a.q = (const uint16_t *)q;
     a.q_stride = q_stride;
     a.out = (uint16_t *)out;

@@ -159,3 +159,24 @@ def test_values_that_are_not_finite_behind_a_prefix(dtype, heads, dim, new, own)
     for b, (n, f) in enumerate(zip(new, first_bad)):
         for j in range(f, n):
             assert not np.isfinite(got[batch.q_start[b] + j, :, f % dim]).any()
+
+
+@pytest.mark.parametrize("new,kv,prefix,odd", [([1, 1, 1], [900, 3, 70], 0, False), ([1, 2], [40, 50], 300, False), ([40, 3], [60, 300], 0, False),
+                                               ([300, 0, 5], [999, 0, 5], 70, False), ([4, 130], [30, 400], 0, True)])
+@pytest.mark.parametrize("heads,dim", [((8, 2), 64), ((4, 4), 128), ((2, 1), 256)])
+def test_results_in_the_place_of_the_queries(new, kv, prefix, odd, heads, dim):
+    """The same bits as with a tensor of its own, in rows that lie apart too, and past values that are not finite."""
+    batch = Batch(new, kv, 16, prefix=prefix)
+    gen = torch.Generator().manual_seed(57)
+    kc, vc = (pool(gen, batch.pages, heads[1], 16, dim, torch.float16) for _ in range(2))
+    if odd:
+        for b, n in enumerate(kv):
+            vc[int(batch.table[b, (n - 1) // 16]), :, (n - 1) % 16] = float("nan")
+    wide = torch.randn((batch.tokens, heads[0] + 1, dim), generator=gen).half().to(DEV)
+    kept, q = wide[:, -1].clone(), wide[:, :heads[0]]
+    cache = fq.KVCache(kc, vc)
+    want, want_lse, _ = call(batch, cache, q.contiguous(), 0.2)
+    out, lse, _ = call(batch, cache, q, 0.2, out=q)
+    torch.cuda.synchronize()
+    assert torch.equal(out.nan_to_num(7.0), want.nan_to_num(7.0)) and torch.equal(lse, want_lse)
+    assert torch.equal(wide[:, -1], kept)

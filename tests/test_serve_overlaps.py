@@ -5,7 +5,7 @@ import pytest
 
 import paper_2506_12024_amd as fq
 from paper_2506_12024_amd import binding as B
-from test_serve_pins import append, kv, seqs
+from test_serve_pins import append, attend, kv, seqs
 
 BASE = 0x100000
 
@@ -65,3 +65,15 @@ def test_strides_of_any_size(handles):
     assert code(handles, q=BASE, o=BASE + 512, qs=far, os=far) == B.FQ_ERR_ALIGN
     assert code(handles, q=BASE, o=BASE + 256, qs=far, os=far) == B.FQ_ERR_SHAPE
     assert code(handles, T=0x7fffffff, q=BASE, o=BASE + 512, qs=far, os=far, ks=far, vs=far) == B.FQ_ERR_ALIGN
+
+
+def test_results_may_not_partly_overlap_the_queries(handles):
+    def refused(o, **kw):  # (the scale, looked at last, stops a call that passes)
+        assert attend(*handles, q=BASE, o=o, scale=float("nan"), **kw) == B.FQ_ERR_SHAPE
+        return "overlap" in fq.fq_last_error()
+    for off in (-1520, -1024, -512, -16, 16, 512, 1024, 1520):
+        assert refused(BASE + off)
+    assert refused(BASE, os=264) and refused(BASE + 512, qs=504, os=504) and refused(BASE - 16, qs=1000, os=264)
+    row = dict(qs=768, os=768)
+    assert not any(refused(o, **kw) for o, kw in ((BASE, {}), (BASE + 512, row), (BASE + 1024, row), (BASE - 1536, {}), (BASE + 1536, {})))
+    assert refused(BASE + 496, **row) and refused(BASE + 1040, **row)
