@@ -314,7 +314,7 @@ int fq_attend(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q, l
         return fq_fail(FQ_ERR_ALIGN, "%s: lse needs 4-byte, the workspace 256-byte alignment", who);
     const size_t need = fq_attend_bytes(a, false, fq_device_cus());
     if (workspace_bytes < need)
-        return fq_fail(FQ_ERR_SHAPE, "%s: the workspace has %zu bytes, fq_attend_workspace_bytes asks for %zu", who,
+        return fq_fail(FQ_ERR_SHAPE, "%s: the workspace has %zu bytes, the call needs %zu", who,
                        workspace_bytes, need);
     // (a workgroup reads its own rows of q before it writes theirs of out, in any order with others)
     const long long width = (long long)q_heads * kv->view.dim;
