@@ -529,7 +529,8 @@ int fq_attend(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q, l
  *   temperature, top_k, top_p, min_p   device, f32 / int32 / f32 / f32 [R], or NULL: 1, 0, 1, 0
  *   token        device, int32 [R]                                                               (written)
  *   prob         device, f32 [R], or NULL                                                        (written)
- *   workspace    device, fq_sample_workspace_bytes(R, V) bytes, 256-byte aligned; calls that may overlap need one each
+ *   workspace    device, fq_sample_workspace_bytes(R, V) bytes, 256-byte aligned.  Reserved: it has to be there, but no call
+ *                reads or writes it as yet
  * R >= 0 (R = 0 launches nothing), 1 <= V <= FQ_MAX_SAMPLE_V.  Never waits for the stream.
  */
 #define FQ_MAX_SAMPLE_V (1 << 24)

@@ -256,7 +256,6 @@ struct FqSampleArgs {
     long long row_stride;
     int R, V;
 };
-size_t fq_sample_bytes(int R, int V);
-hipError_t fq_launch_sample(const FqSampleArgs &a, bool half, void *workspace, hipStream_t stream);
+hipError_t fq_launch_sample(const FqSampleArgs &a, bool half, hipStream_t stream);
 
 #endif

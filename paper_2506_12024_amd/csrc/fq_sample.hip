@@ -318,11 +318,6 @@ struct Listed {
             f(l, at < n ? s->list_i[at] : 0);
         }
     }
-    template <bool LIGHT, class F, class G>
-    __device__ __forceinline__ void each(const F &f, const G &) const
-    {
-        each<LIGHT>(f);
-    }
 };
 
 // Among the weights added up in s.bins (bins[0] first): the one at which the running sum reaches `target`; false if it never does.
@@ -833,9 +828,7 @@ void launch(const FqSampleArgs &a, double unit, hipStream_t stream)
 
 } // namespace
 
-size_t fq_sample_bytes(int, int) { return 256; }
-
-hipError_t fq_launch_sample(const FqSampleArgs &a, bool half, void *, hipStream_t stream)
+hipError_t fq_launch_sample(const FqSampleArgs &a, bool half, hipStream_t stream)
 {
     const int log_v = a.V > 1 ? 32 - __builtin_clz((unsigned)a.V - 1) : 0;
     const double unit = (double)(1ULL << (log_v > 11 ? 62 - log_v : 51));

@@ -23,6 +23,7 @@ namespace {
 
 constexpr uint32_t KV_MAGIC = 0x46514B56u;   // "FQKV"
 constexpr uint32_t SEQS_MAGIC = 0x46515351u; // "FQSQ"
+constexpr size_t SAMPLE_BYTES = 256;         // asked of a caller of fq_sample; no kernel uses them (a row is one workgroup's)
 
 inline bool aligned(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
@@ -337,7 +338,7 @@ size_t fq_sample_workspace_bytes(int R, int V)
         fq_fail(FQ_ERR_SHAPE, "fq_sample_workspace_bytes: need R >= 0 and V in 1..%d (got %d and %d)", FQ_MAX_SAMPLE_V, R, V);
         return 0;
     }
-    return fq_sample_bytes(R, V);
+    return SAMPLE_BYTES;
 }
 
 static int sample_any(const char *who, bool half, const void *logits, int R, int V, long long row_stride, const float *u,
@@ -354,11 +355,11 @@ static int sample_any(const char *who, bool half, const void *logits, int R, int
     if (!aligned(logits, half ? 2 : 4) || !aligned(u, 4) || !aligned(temperature, 4) || !aligned(top_k, 4) ||
         !aligned(top_p, 4) || !aligned(min_p, 4) || !aligned(token, 4) || !aligned(prob, 4) || !aligned(workspace, 256))
         return fq_fail(FQ_ERR_ALIGN, "%s: logits need the alignment of their type, the workspace 256 bytes, the rest 4", who);
-    if (workspace_bytes < fq_sample_bytes(R, V))
+    if (workspace_bytes < SAMPLE_BYTES)
         return fq_fail(FQ_ERR_SHAPE, "%s: the workspace has %zu bytes, fq_sample_workspace_bytes asks for %zu", who,
-                       workspace_bytes, fq_sample_bytes(R, V));
+                       workspace_bytes, SAMPLE_BYTES);
     const FqSampleArgs a{logits, u, temperature, top_p, min_p, top_k, token, prob, row_stride, R, V};
-    return launched(fq_launch_sample(a, half, workspace, (hipStream_t)stream), who);
+    return launched(fq_launch_sample(a, half, (hipStream_t)stream), who);
 }
 
 int fq_sample(const float *logits, int R, int V, long long row_stride, const float *u, const float *temperature,
