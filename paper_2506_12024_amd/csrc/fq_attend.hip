@@ -79,12 +79,8 @@ Plan plan(const FqAttendArgs &a, int cus)
     Plan pl{};
     if (P > 0 && a.seqs.seqs > 1 && a.max_q * group < 64) {
         int &t0 = pl.row_tiles[0], &t1 = pl.row_tiles[1];
-        t0 = tiles_of(a, a.seqs.tokens * group);
-        t1 = tiles_of(a, a.max_q * group);
-        if (t0 && t1)
-            t0 = t1 = t0 > t1 ? t0 : t1;
-        else
-            t0 = 0; // (few rows of the batch, many of a sequence: no such batch)
+        t0 = tiles_of(a, a.seqs.tokens * group); // 0 where the batch has more rows than the kernel of few rows takes
+        t1 = t0 ? t0 : tiles_of(a, a.max_q * group); // (a sequence has no more than the batch: the same tiles serve both)
         pl.work[0] = work(a, true, 0, P, 1, a.seqs.tokens, t0, cus, pl.most_parts);
         pl.work[1] = work(a, false, P, a.max_kv, a.seqs.seqs, a.max_q, t1, cus, pl.most_parts);
         pl.n = 2;
