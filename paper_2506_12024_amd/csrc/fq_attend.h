@@ -210,74 +210,24 @@ __device__ __forceinline__ float fq_lse(float m, float l)
 }
 __device__ __forceinline__ float fq_inverse(float l) { return l == 0.0f ? 0.0f : 1.0f / l; }
 
-// The products sum p v over all keys of a tile, and 0 times an infinity is NaN: a row must not meet a V that it does not see and that is not
-// finite.  Keys past the end and holes are zeroed as they arrive.  Where some rows of a workgroup see keys that others do not (among
-// a chunk's own new tokens) a sum that is not finite sends the workgroup here: its rows again, one to a wavefront, key by
-// key, what is not seen left out.  (Also where such a value is seen: the result is the same.)
+// The products sum p v over all keys of a tile, and 0 times an infinity is NaN: a row must not meet a V that it does not see and that is
+// not finite.  Keys past the end and holes are zeroed as they arrive.  So are the values that are not finite of those keys that some rows of
+// a workgroup see and others do not (a chunk's own new tokens); the rows that see them get them back at the end, added to their sums:
+// an infinity stays one whatever its weight, two of them or a NaN give NaN.
+// All bits of those of two values that are not finite: an exponent of ones carries into the sign's place when one is added.
 template <bool BF16>
-__device__ __forceinline__ void fq_attend_row_by_row(const FqAttendArgs &a, const FqAttendWork &w, const FqAttendRows &rs, const int32_t *table,
-                                                     int part, int head, int row0, int last, int begin, int end)
+__device__ __forceinline__ uint32_t fq_odd(uint32_t two)
 {
-    const int lane = threadIdx.x & 63, dim = a.kv.dim, group = a.q_heads / a.kv.kv_heads;
-    const float c = fq_score_factor(a.scale);
-    for (int r = row0 + (threadIdx.x >> 6); r <= last; r += blockDim.x >> 6) {
-        const int j = r / group, h = head * group + r % group, lim = min(rs.limit(j), end);
-        const uint16_t *q = a.q + (rs.q0 + j) * a.q_stride + h * dim;
-        float m = -INFINITY, l = 0.0f, lost = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int k0 = begin; k0 < lim; k0 += 64) {
-            const int key = k0 + lane, page = fq_key_page(a, table, key, lim);
-            const bool there = page >= 0 && page < a.kv.n_pages;
-            const long long at = there ? fq_key_offset(a, page, key, head) : 0;
-            float s = 0.0f;
-            for (int d = 0; d < dim; d++)
-                s = fmaf(fq_to_float(q[d], BF16), fq_to_float(a.kv.k[at + d], BF16), s);
-            s = there ? fq_score(a.scale < 0.0f ? -s : s, c) : -INFINITY;
-            float top = s;
-            for (int o2 = 32; o2; o2 >>= 1)
-                top = fmaxf(top, __shfl_xor(top, o2));
-            const float now = fmaxf(m, top), ref = fq_reference(now), fall = __builtin_amdgcn_exp2f(m - ref);
-            const float p = there ? __builtin_amdgcn_exp2f(s - ref) : 0.0f;
-            float sum = p;
-            for (int o2 = 32; o2; o2 >>= 1)
-                sum += __shfl_xor(sum, o2);
-            l *= fall;
-            lost *= fall;
-            fq_add_weights(l, lost, sum);
-            m = now;
-            float here[4] = {0.0f, 0.0f, 0.0f, 0.0f}; // (64 keys by themselves: one long sum loses as l would)
-            const uint64_t seen = __ballot(there);
-            for (int i = 0; i < 64; i++) {
-                const float pi = __shfl(p, i);
-                const long long from = __shfl(at, i);
-                if ((seen >> i) & 1)
-#pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        if (lane + 64 * e < dim)
-                            here[e] = fmaf(pi, fq_to_float(a.kv.v[from + lane + 64 * e], BF16), here[e]);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; e++)
-                o[e] = fmaf(o[e], fall, here[e]);
-        }
-        const long long t = rs.q0 + j;
-        if (w.part_o) {
-            const long long to = (w.part0 + (long long)part) * a.seqs.tokens * a.q_heads + t * a.q_heads + h;
-#pragma unroll
-            for (int e = 0; e < 4; e++)
-                if (lane + 64 * e < dim)
-                    w.part_o[to * dim + lane + 64 * e] = o[e];
-            if (lane == 0)
-                w.part_ml[to] = float2{m, l};
-        } else {
-            const float inv = fq_inverse(l);
-#pragma unroll
-            for (int e = 0; e < 4; e++)
-                if (lane + 64 * e < dim)
-                    a.out[t * a.out_stride + h * dim + lane + 64 * e] = fq_from_float(o[e] * inv, BF16);
-            if (lane == 0 && a.lse)
-                a.lse[t * a.q_heads + h] = fq_lse(m, l);
-        }
-    }
+    constexpr uint32_t EXPONENTS = BF16 ? 0x7f807f80 : 0x7c007c00, ONES = BF16 ? 0x00800080 : 0x04000400;
+    const uint32_t signs = ((two & EXPONENTS) + ONES) & 0x80008000u;
+    return signs | (signs - (signs >> 15));
+}
+// Value i of four if it is not finite, else 0.
+template <bool BF16>
+__device__ __forceinline__ float fq_odd_value(u32x2 four, int i)
+{
+    const uint32_t two = four[i >> 1] & fq_odd<BF16>(four[i >> 1]);
+    return fq_to_float((uint16_t)(two >> (16 * (i & 1))), BF16);
 }
 
 // rt0, rt1: tiles of 16 rows of a workgroup of each piece, 0 for the kernel of many rows.  A launch of one piece has no workgroups in

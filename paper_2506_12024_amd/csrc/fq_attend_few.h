@@ -16,6 +16,7 @@
 namespace few {
 
 constexpr int WAVES = FQ_ATTEND_THREADS / 64;
+static_assert(WAVES == 4, "the flags of four are read");
 constexpr int KEYS = 32; // to a wavefront and step
 
 // 16-byte pieces to a row of V in LDS, and where piece c of row r goes: 16 rows of one piece fall on 16 different bank
@@ -46,7 +47,7 @@ struct Lds {
     static_assert(WAVE >= 16 * DP * 4, "the rows are added up in the same piece");
     alignas(16) char v[WAVES * WAVE];
     float m[WAVES][RT * 16], l[WAVES][RT * 16];
-    int odd; // some sum is not finite
+    int odd[WAVES]; // values that are not finite were taken out of its keys
 };
 
 // Workgroup `at` of the launch.  DP: dimensions computed; FULL: the head has all of them; RT: tiles of 16 rows.
@@ -135,8 +136,7 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
             }
     };
 
-    if (threadIdx.x == 0)
-        shared.odd = 0;
+    uint32_t odd = 0;
     constexpr int STEP = WAVES * KEYS;
     int key = begin + wave * KEYS;
     if (key < end) {
@@ -175,6 +175,19 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
 #pragma unroll
                     for (int s = 0; s < NS; s++)
                         v[t][s] = u32x4{0, 0, 0, 0};
+        }
+        if (key + KEYS > all_seen) {
+#pragma unroll
+            for (int t = 0; t < 2; t++)
+                if (key + 16 * t + col >= all_seen)
+#pragma unroll
+                    for (int s = 0; s < NS; s++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) {
+                            const uint32_t out = fq_odd<BF16>(v[t][s][e]);
+                            v[t][s][e] &= ~out;
+                            odd |= out;
+                        }
         }
 #pragma unroll
         for (int t = 0; t < 2; t++)
@@ -253,24 +266,9 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
             all_l[wave][rt * 16 + col] = l[rt];
         }
     }
-    if (all_seen < end) { // (the same for all threads)
-        __syncthreads();
-        float z = 0.0f;
-#pragma unroll
-        for (int rt = 0; rt < RT; rt++)
-#pragma unroll
-            for (int d = 0; d < ND; d++)
-#pragma unroll
-                for (int i = 0; i < 4; i++)
-                    z = fmaf(o[rt][d][i], 0.0f, z);
-        if (z != 0.0f) // (a NaN)
-            shared.odd = 1;
-        __syncthreads();
-        if (shared.odd) {
-            fq_attend_row_by_row<BF16>(a, w, rs, table, at_block.y, head, row0, last, begin, end);
-            return;
-        }
-    }
+    const bool wave_odd = __any(odd != 0);
+    if (lane == 0)
+        shared.odd[wave] = wave_odd;
     const long long rows_all = (long long)a.seqs.tokens * a.q_heads;
 #pragma unroll
     for (int rt = 0; rt < RT; rt++) {
@@ -307,6 +305,18 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
                 for (int e = 0; e < 4; e++) {
                     sum[e] += x[e];
                     sum[4 + e] += y[e];
+                }
+            }
+            if (all_seen < end && (shared.odd[0] | shared.odd[1] | shared.odd[2] | shared.odd[3])) {
+                const int sees = min(rs.limit(r / group), end);
+                for (int at = max(all_seen, begin); at < sees; at++) {
+                    const int page_at = fq_key_page(a, table, at, sees);
+                    if (page_at < 0 || page_at >= a.kv.n_pages)
+                        continue;
+                    const u32x4 y = *(const u32x4 *)(a.kv.v + fq_key_offset(a, page_at, at, head) + d);
+#pragma unroll
+                    for (int e = 0; e < 8; e++)
+                        sum[e] += fq_odd_value<BF16>(u32x2{y[e >> 2 << 1], y[(e >> 2 << 1) + 1]}, e & 3);
                 }
             }
             const long long t = rs.q0 + r / group;

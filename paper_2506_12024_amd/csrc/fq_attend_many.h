@@ -31,7 +31,7 @@ struct Lds {
     static constexpr int TILE = KEYS * DP * 2;
     alignas(16) char tiles[4 * TILE]; // K, V; K, V
     uint64_t missing[2][4];           // keys of a tile that are not there, by the wavefront that fetched them
-    int odd;                          // some sum is not finite
+    int odd[4];                       // values that are not finite were taken out of what the wavefront fetched
 };
 
 // Workgroup `at` of the launch.  DP: dimensions computed; FULL: the head has all of them.
@@ -62,8 +62,6 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
     const int begin = begin64 < most ? (int)begin64 : most;
     const int end = (int)(begin64 + w.chunk < most ? begin64 + w.chunk : most);
 
-    if (threadIdx.x == 0)
-        shared.odd = 0;
     const int block_sees = rs.limit(row0 / group); // every row of the workgroup sees the keys before this one
     const int r = row0 + wave * 32 + col;
     const bool real = r <= last;
@@ -111,13 +109,28 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
             vs[i] = *(const u32x4 *)(a.kv.v + at + d);
         }
     };
-    auto put = [&](int half_of_lds) {
+    uint32_t odd = 0;
+    auto put = [&](int half_of_lds, int key) {
         const uint64_t gone = __ballot(!there); // lane 4 k + piece: key 16 wave + k
         if (gone) {
             if (!there)
 #pragma unroll
                 for (int i = 0; i < NC; i++)
                     ks[i] = vs[i] = u32x4{0, 0, 0, 0};
+        }
+        if (key + KEYS > block_sees) {
+            if (key + my_key >= block_sees)
+#pragma unroll
+                for (int i = 0; i < NC; i++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        const uint32_t out = fq_odd<BF16>(vs[i][e]);
+                        vs[i][e] &= ~out;
+                        odd |= out;
+                    }
+            const bool wave_odd = __any(odd != 0);
+            if (lane == 0)
+                shared.odd[wave] = wave_odd;
         }
         char *kt = lds + half_of_lds * 2 * TILE + place<DP>(my_key, my_piece), *vt = kt + TILE;
 #pragma unroll
@@ -226,7 +239,7 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
         find(begin);
         fetch(begin);
         find(begin + KEYS);
-        put(0);
+        put(0, begin);
         if (begin + KEYS < end) {
             fetch(begin + KEYS);
             find(begin + 2 * KEYS);
@@ -251,7 +264,7 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
             step(key, p, 0, v_last, kt + HALF);
         if (more) {
             __syncthreads(); // the other half of LDS is read no more
-            put(p ^ 1);
+            put(p ^ 1, key + KEYS);
             if (key + 2 * KEYS < end) {
                 fetch(key + 2 * KEYS);
                 find(key + 3 * KEYS);
@@ -269,26 +282,30 @@ __device__ __forceinline__ void attend(const FqAttendArgs &a, const FqAttendWork
                 product(i, piece(i, v_last, lds));
     }
 
-    if (block_sees < end) { // (the same for all threads)
-        float z[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int d = 0; d < ND; d++)
-#pragma unroll
-            for (int i = 0; i < 16; i++)
-                z[i & 1] = fmaf(o[d][i], 0.0f, z[i & 1]);
-        if (z[0] + z[1] != 0.0f) // (a NaN)
-            shared.odd = 1;
-        __syncthreads();
-        if (shared.odd) {
-            fq_attend_row_by_row<BF16>(a, w, rs, table, at_block.y, head, row0, last, begin, end);
-            return;
-        }
-    }
     l = fq_over32<true>(l);
     if (!real)
         return;
-    const long long t = rs.q0 + j;
     // register i of tile d holds dimension 32 d + 8 (i / 4) + 4 half + i % 4
+    if (block_sees < end && (shared.odd[0] | shared.odd[1] | shared.odd[2] | shared.odd[3])) // (the last tile's put wrote them all)
+        for (int at = max(block_sees, begin); at < lim; at++) {
+            const int page_at = fq_key_page(a, table, at, lim);
+            if (page_at < 0 || page_at >= a.kv.n_pages)
+                continue;
+            const uint16_t *from = a.kv.v + fq_key_offset(a, page_at, at, head);
+#pragma unroll
+            for (int d = 0; d < ND; d++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int e = 32 * d + 8 * i + 4 * half;
+                    if (FULL || e < dim) {
+                        const u32x2 y = *(const u32x2 *)(from + e);
+#pragma unroll
+                        for (int f = 0; f < 4; f++)
+                            o[d][4 * i + f] += fq_odd_value<BF16>(y, f);
+                    }
+                }
+        }
+    const long long t = rs.q0 + j;
     if (w.part_o) {
         const long long at = (w.part0 + (long long)at_block.y) * a.seqs.tokens * a.q_heads + t * a.q_heads + h;
 #pragma unroll

@@ -180,3 +180,65 @@ def test_results_in_the_place_of_the_queries(new, kv, prefix, odd, heads, dim):
     torch.cuda.synchronize()
     assert torch.equal(out.nan_to_num(7.0), want.nan_to_num(7.0)) and torch.equal(lse, want_lse)
     assert torch.equal(wide[:, -1], kept)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("heads,dim", [((8, 2), 64), ((4, 4), 128), ((2, 2), 80), ((2, 1), 256)])
+@pytest.mark.parametrize("new,own,prefix", [([3], 200, 0), ([2, 3], 40, 90), ([40], 300, 0), ([200, 3], 100, 50)])
+def test_an_old_infinite_value_is_an_infinity_in_every_row_that_sees_it(dtype, heads, dim, new, own, prefix):
+    """In the cache (all rows see it), in the prefix, and in a new token, each in a column of its own; a column with both
+    signs is NaN; all other columns are as if the infinities were not there."""
+    batch = Batch(new, [n + own for n in new], 16, prefix=prefix)
+    gen = torch.Generator().manual_seed(61)
+    kc, vc = (pool(gen, batch.pages, heads[1], 16, dim, TYPES[dtype]) for _ in range(2))
+    inf = float("inf")
+    late = [n + own - 1 - n // 3 for n in new]  # the place of a new token of each sequence
+    for b in range(len(new)):
+        vc[int(batch.table[b, 0]), :, 3, 5] = inf
+        vc[int(batch.table[b, late[b] // 16]), :, late[b] % 16, 6] = -inf
+        vc[int(batch.table[b, 1]), :, 2, 7] = inf
+        vc[int(batch.table[b, late[b] // 16]), :, late[b] % 16, 7] = -inf
+    if prefix:
+        vc[int(batch.prefix_table[0]), :, 0, 4] = -inf
+    q = torch.randn((batch.tokens, heads[0], dim), generator=gen).to(TYPES[dtype]).to(DEV)
+    out, lse, _ = call(batch, fq.KVCache(kc, vc), q, 0.1)
+    torch.cuda.synchronize()
+    got = f64(out)
+    want, want_lse, size, steep, mass = attend(batch, f64(q), f64(kc), f64(torch.nan_to_num(vc, 0, 0, 0)), 0.1)
+    odd = np.zeros(dim, dtype=bool)
+    odd[[5, 6, 7] + ([4] if prefix else [])] = True
+    tol = attend_tolerance(q.dtype, want, size, steep, mass, dim)
+    assert np.all(np.abs(got - want)[..., ~odd] <= tol[..., ~odd])
+    assert np.all(np.abs(f64(lse) - want_lse) <= lse_tolerance(want_lse, steep, dim, prefix + max(batch.kv)))
+    assert np.all(got[..., 5] == inf) and (not prefix or np.all(got[..., 4] == -inf))
+    for t, (b, place) in enumerate(batch.places()):
+        if place >= late[b]:
+            assert np.all(got[t, :, 6] == -inf) and np.all(np.isnan(got[t, :, 7]))
+        else:
+            assert np.all(np.abs(got[t, :, 6] - want[t, :, 6]) <= tol[t, :, 6]) and np.all(got[t, :, 7] == inf)
+
+
+@pytest.mark.parametrize("place", [5, 1500])
+def test_values_that_are_not_finite_take_no_other_time(place):
+    """One infinity among 2048 keys, in an old token and in a new one: a prompt takes a few times what it takes without at most
+    (500 times where such calls were computed row by row)."""
+    batch = Batch([1024], [2048], 16)
+    gen = torch.Generator(device=DEV).manual_seed(63)
+    kc, vc = (torch.randn((batch.pages, 8, 16, 128), generator=gen, device=DEV).half() for _ in range(2))
+    q = torch.randn((1024, 64, 128), generator=gen, device=DEV).half()
+    cache, seqs, out = fq.KVCache(kc, vc), batch.sequences(), torch.empty_like(q)
+    ws = torch.empty(fq.fq_attend_workspace_bytes(cache, seqs, 1024, 64, 1024, 2048), dtype=torch.uint8, device=DEV)
+
+    def least():
+        times = []
+        for _ in range(6):
+            begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            begin.record()
+            fq.fq_attend(cache, seqs, q, out, 0.1, 1024, 2048, ws)
+            end.record()
+            end.synchronize()
+            times.append(begin.elapsed_time(end))
+        return min(times)
+    without = least()
+    vc[int(batch.table[0, place // 16]), :, place % 16, 9] = float("inf")
+    assert least() < 20 * without
