@@ -494,13 +494,15 @@ int fq_kv_append(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q
  *   out[t][h] = sum_i p_i v_i,  p = softmax(scale * q[t][h] . k_i),  lse[t][h] = ln sum_i exp(scale * q[t][h] . k_i)
  * query head h reading key head h / (q_heads / kv_heads).  Scores, statistics and sums in binary32, p rounded to the tensors'
  * type where it meets v.  A row that sees no key gives 0 and lse = -inf.  What lies in the cache beyond kv_len, in holes and in other pages is not looked
- * at, whatever it holds.
+ * at, whatever it holds; a value that is not finite makes infinite or NaN what the rows that see it hold there, and nothing else.
  *   q, out     device, [tokens][q_heads][head_dim], rows q_stride, out_stride elements apart, 16-byte aligned, strides
  *              multiples of 8; out may be q itself, row for row, but not overlap it otherwise    (read / written)
  *   lse        device, f32 [tokens][q_heads], or NULL                                            (written)
  *   max_q      no sequence has more new tokens than this (rows beyond are left alone), 1 <= max_q <= tokens
  *   max_kv     no kv_len is larger than this (keys beyond are not seen; table_width * page_tokens always does); >= 1.  The launch is
- *              shaped by the two: close bounds are faster, and so are prompts and single tokens in calls of their own
+ *              shaped by the two for all sequences alike: close bounds are faster, and prompts and single tokens belong in calls of
+ *              their own.  A shared prefix is read once for 128 rows of a key head (token times query head) while max_q * q_heads /
+ *              kv_heads is under 64 and there is more than one sequence, else by every sequence for itself
  *   workspace  device, fq_attend_workspace_bytes(...) bytes, 256-byte aligned; calls that may overlap in time need one each.
  *              What is enough for a max_kv is enough for any smaller one
  * q_heads a multiple of kv_heads, at most FQ_MAX_Q_HEADS; scale finite.  tokens >= 0 (0 launches nothing).  Never waits for the

@@ -5,7 +5,7 @@
 // through registers, 8 values (16 bytes) to a thread and step.  The angle is a binary64 product taken in whole turns: position
 // * freq / 2 pi minus its nearest integer, so a place of 10^6 keeps the accuracy of place 1 (in binary32 it would be off by
 // 0.06 rad); the fraction then goes through a binary32 sincospi.  Bound by the traffic of q, k, v for prompts (2048 tokens of
-// the 70B shapes: 84 MB in 14.7 us, 5.7 TB/s, against 4.8 of a large copy), by one launch for a token (3.5 us on the device, 8.0 a
+// the 70B shapes: 84 MB in 14.7 to 15.2 us, 5.5 to 5.7 TB/s, against 4.8 of a large copy), by one launch for a token (3.5 us on the device, 8.0 a
 // call from Python).
 #include <hip/hip_runtime.h>
 
@@ -41,7 +41,7 @@ struct alignas(16) Eight {
 enum Layout { NEIGHBOURS, PIECES, ANYHOW };
 
 // A thread's unit is two pieces of a head, which a pair of pieces turns together: what is asked for before any of it is used.
-// (One piece at a time, the partners value by value: 27 us for 2048 tokens of the 70B shapes where this takes 14, 5.8 TB/s.)  Where
+// (One piece at a time, the partners value by value: 27 us for 2048 tokens of the 70B shapes where this takes 15.)  Where
 // partners are fetched value by value a unit is one piece, and those that turn come first, so that other wavefronts do not pass
 // through it.
 template <Layout LAYOUT>

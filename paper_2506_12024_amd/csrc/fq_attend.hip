@@ -43,8 +43,8 @@ FqAttendWork work(const FqAttendArgs &a, bool shared, int key0, long long keys, 
     }
     const long long groups = blocks * a.kv.kv_heads;
     const long long steps = div_up(keys > 0 ? keys : 1, step);
-    // Steps to a part.  Few rows: all workgroups at once where that takes one step each; else four rounds of them (sequences differ
-    // in length), of as many steps that a part's sums (8 bytes to a row and dimension, written and read) are a
+    // Steps to a part.  Few rows: one step each while that makes no more than three workgroups to a compute unit (by their registers three or
+    // four of width 64 fit at once, two of 128, one of more); else four times as many of them (sequences differ in length), of as many steps that a part's sums (8 bytes to a row and dimension, written and read) are a
     // sixteenth of its keys and values at most.  Many rows write 64 KiB of sums a part: one workgroup to a compute unit (48
     // sequences behind a prefix of 8197: 66 us with a quarter as many, 48, 52 with half as many again, 54 with twice), of
     // four steps at least.

@@ -5,9 +5,9 @@
 // dimensions serves if Q has the same), the rows of V pass through a piece of LDS that belongs to the wavefront alone and
 // are read back transposed.  No barrier until the end, where the wavefronts' rows are added up; a lane asks for the next
 // 32 keys as soon as the registers of the last are free, and for the page numbers a step before that.  Measured: 16 sequences of
-// up to 4096 of the 7B shapes 103 us (5.0 TB/s), 32 of up to 16384 of the 70B shapes 245 us (5.4 TB/s); with the registers held to 168
-// so that three workgroups fit a compute unit instead of two, 8 % longer.  One token behind 777 keys takes 8 us on the device,
-// three trips to memory one after the other (lengths, page, keys), and 4 more to join its seven parts.
+// up to 4096 of the 7B shapes 102 us (5.0 TB/s), 32 of up to 16384 of the 70B shapes 251 us (5.3 TB/s); with the registers held to 168
+// so that three workgroups fit a compute unit instead of two, 8 % longer.  One token behind 777 keys takes 7.1 us on the device,
+// three trips to memory one after the other (lengths, page, keys), and 3.7 more to join its seven parts.
 #ifndef FQ_ATTEND_FEW_H
 #define FQ_ATTEND_FEW_H
 

@@ -1,12 +1,12 @@
 // Attention of many rows to a sequence and key head: prompts, chunks of them, and a prefix that a batch shares.
 //
-// Bound by the matrix cores and by the exponentials between the two products.  Four wavefronts take 32 rows each and share
-// tiles of 64 keys in LDS, two of them in turn; a tile's rows come through registers while the one before is computed.  A wavefront
-// works in steps of 32 keys, three of them under way at once: the matrix cores sum V of the last one and score the next one while the
-// vector units take the exponentials of this one.  Measured: 2048 new tokens behind 951 of the 70B shapes 172 us (770 TFLOP/s),
-// 8192 tokens 830 to 870 TFLOP/s, where a library product of 8192^3 reaches 1160 to 1220: the matrix cores are busy 38 % of the cycles
-// (the clock falls to 1.9 GHz under them), the vector units about 45.  Taken one after the other: 187 us, and with heads of 64,
-// where the exponentials weigh more, 49 us where this takes 45.  More pieces read ahead than four changed nothing.
+// Four wavefronts take 32 rows each and share tiles of 64 keys in LDS, two of them in turn; a tile's rows come through
+// registers while the one before is computed.  A wavefront works in steps of 32 keys, three of them under way at once: the matrix cores sum V of the last one and score the next one while the
+// vector units take the exponentials of this one.  Measured: 2048 new tokens behind 951 of the 70B shapes 178 us in fp16 and 171 in bf16
+// (743 and 775 TFLOP/s), 8192 tokens 818 and 863 TFLOP/s, where a library product of 8192^3 reaches 1160 to 1220.  Neither unit is
+// full: the matrix cores are busy 37 % of the cycles (the clock falls to 1.9 GHz under them), the vector units 48 %; two wavefronts to a SIMD
+// have two barriers and a pass through registers to hide in every tile.  With exponentials and products one after the other 9 % longer.
+// More pieces read ahead than four changed nothing.
 #ifndef FQ_ATTEND_MANY_H
 #define FQ_ATTEND_MANY_H
 

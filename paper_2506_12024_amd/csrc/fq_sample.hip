@@ -13,7 +13,8 @@
 // the exponentials of the entries that count; by the chain of steps for a short one.  Measured, 256 rows of 128256 (131 MB, 22 us to
 // read once): top-k 50 47 us, temperature alone 58, top-p 0.95 92, all of them mixed 107 to 116 (by the settings drawn); one row of
 // 32000 with top-k 50 15 us, with top-p 0.95 26.  Rows count from the 16-byte boundary before them, so that any row is read 16 bytes at a
-// time: 256 of 128255 with top-p 0.95 96 us; it costs aligned rows 0.5 to 2 %.
+// time: 256 of 128255 with top-p 0.95 96 us; it costs aligned rows 0.5 to 2 %.  1024 threads have 128 registers each: the fp16 instance
+// keeps 4 of its vector and both 64 of their scalar registers elsewhere (scratch, spare lanes).
 #include <hip/hip_runtime.h>
 
 #include "fq_internal.h"
