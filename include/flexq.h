@@ -544,6 +544,94 @@ int fq_sample_f16(const void *logits, int R, int V, long long row_stride, const 
                   const int32_t *top_k, const float *top_p, const float *min_p, int32_t *token, float *prob, void *workspace,
                   size_t workspace_bytes, void *stream);
 
+/*
+ * ---- What a server adds to the step ---------------------------------------------------------------------------
+ *
+ * Low-rank adapters beside the linears, norms of the heads before the rotary positions, log probabilities of what was
+ * drawn or given.  (The paper serves one model to one user and names none of them: the interfaces are this library's.)
+ */
+
+/*
+ * The low-rank adapters of one linear, for requests that share its weights: slot a holds A_a [rank][K] and B_a [N][rank] in 16
+ * bits, of which the first ranks[a] rows of A_a and columns of B_a count (what lies in the others is not looked at).
+ *   a        device, slot s at a + s * a_stride elements, 16-byte aligned                 (read)
+ *   b        device, slot s at b + s * b_stride elements, 16-byte aligned                 (read)
+ *   ranks    device, int32 [slots], held inside 0 .. rank; NULL: rank for all             (read)
+ *   scales   device, f32 [slots]; NULL: 1 for all                                         (read)
+ * dtype FQ_F16 or FQ_BF16 (of A, B, x, y and out alike); 1 <= slots <= FQ_MAX_ADAPTERS; rank a multiple of 8, at most
+ * FQ_MAX_ADAPTER_RANK; K a multiple of 8, K and N at most 2^24; strides multiples of 8, at least a slot's size where there
+ * is more than one.  The handle borrows the four arrays, which the kernels read at run time (a slot may be filled anew between two
+ * calls or two replays of a graph); creating and destroying it launches nothing.
+ */
+#define FQ_MAX_ADAPTERS 16384
+#define FQ_MAX_ADAPTER_RANK 256
+#define FQ_MAX_ADAPTER_ROWS (1 << 20)
+typedef struct fq_adapters fq_adapters;
+int fq_adapters_create(fq_adapters **out, int dtype, int slots, int rank, int K, int N, const void *a, long long a_stride,
+                       const void *b, long long b_stride, const int32_t *ranks, const float *scales);
+int fq_adapters_destroy(fq_adapters *adapters);
+
+/*
+ * out[m] = y[m] + scales[s] * (x[m] A_s^T) B_s^T with s = adapter[m], row by row; a row whose adapter is outside 0 .. slots - 1
+ * (-1 for a request without one), or has rank 0, is y[m] as it stands.  y is what the shared projection left (fq_linear), x its input.
+ *   x          device, [M][K], rows x_stride elements apart, 16-byte aligned, the stride a multiple of 8   (read)
+ *   adapter    device, int32 [M]                                                                         (read)
+ *   y, out     device, [M][N], rows y_stride, out_stride elements apart, 2-byte aligned; out may be y itself, row for row,
+ *              but not overlap it otherwise, nor x                                                       (read / written)
+ *   workspace  device, fq_adapters_workspace_bytes(adapters, M) bytes (0 on an error), 256-byte aligned; calls that may
+ *              overlap in time need one each.  What is enough for an M is enough for any smaller one
+ * Sums and x A^T in binary32 (x A^T enters the second product as two 16-bit numbers, an error of 2^-17 of a row's largest at
+ * most), one rounding to the type at the end.  M from 0 (launches nothing) to FQ_MAX_ADAPTER_ROWS.  Never waits for the
+ * stream: may be captured into a graph.  Equal calls give equal bits.
+ */
+size_t fq_adapters_workspace_bytes(const fq_adapters *adapters, int M);
+int fq_adapters_add(const fq_adapters *adapters, int M, const void *x, long long x_stride, const int32_t *adapter, const void *y,
+                    long long y_stride, void *out, long long out_stride, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * fq_kv_append with a norm of every head of q and k before it is turned: element d of a head becomes
+ *   x_d / sqrt(mean_i x_i^2 + eps) * (weight[d] + offset)
+ * in binary32, then the pairs are turned, then one rounding to the tensors' type.  v is copied.
+ *   q_weight, k_weight  device, of the cache's type, 16-byte aligned: [head_dim], for all heads (weight_stride 0), or
+ *                       [heads][head_dim], heads weight_stride elements apart (a multiple of 8, >= head_dim)     (read)
+ *   offset              0, or 1 where the weights are kept as their distance from 1; finite.  eps >= 0, finite
+ * Everything else as fq_kv_append (q_weight is not looked at with q_heads = 0).  One launch.
+ */
+int fq_kv_append_normed(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q, long long q_stride, int q_heads,
+                        void *q_out, long long q_out_stride, const void *k, long long k_stride, const void *v,
+                        long long v_stride, const void *q_weight, const void *k_weight, long long weight_stride, float eps,
+                        float offset, const double *freqs, int rot_dim, int interleaved, float amplitude,
+                        const int32_t *positions, void *stream);
+
+/*
+ * Per row of logits, with p = softmax(l): the log probabilities of given tokens, the entropy (as fq_entropy_kl), and the top_n
+ * likeliest tokens with theirs, the larger logit first, the smaller index first on ties.
+ *   given_logprob[r][j] = ln p[given[r][j]];  -inf for a token outside 0 .. V - 1
+ *   top_token[r][i], top_logprob[r][i]: the i-th of the order; -1 and -inf where the row has no more tokens with weight
+ * A NaN logit counts as -inf.  With +inf in a row only the +inf entries have weight, 1 each.  A row of nothing else than -inf gives
+ * -inf, -1 and an entropy of 0.  Exponentials and a thread's sums in binary32, joined in binary64; the largest logit's own weight
+ * stays out of the sums, ln p of a token that is nearly certain keeps its digits (ln p = (l - max) - log1p(sum of the others)).
+ *   logits         device, f32 (or fp16: fq_logprobs_f16) [R][V], rows row_stride elements apart (row_stride >= V; any alignment
+ *                  that the type has)                                                            (read)
+ *   given          device, int32 [R][n_given], or NULL with n_given = 0                          (read)
+ *   given_logprob  device, f32 [R][n_given]                                                      (written)
+ *   top_token      device, int32 [R][top_n], or NULL with top_n = 0; top_logprob device, f32     (written)
+ *   entropy        device, f32 [R], or NULL                                                      (written)
+ *   workspace      device, fq_logprobs_workspace_bytes(R, V) bytes (0 on an error), 256-byte aligned; calls that may overlap in
+ *                  time need one each
+ * R >= 0 (R = 0 launches nothing), 1 <= V <= FQ_MAX_SAMPLE_V, 0 <= n_given <= FQ_MAX_GIVEN, 0 <= top_n <= FQ_MAX_ALTERNATIVES.
+ * Never waits for the stream: may be captured into a graph.  Equal calls give equal bits.
+ */
+#define FQ_MAX_GIVEN 65536
+#define FQ_MAX_ALTERNATIVES 64
+size_t fq_logprobs_workspace_bytes(int R, int V);
+int fq_logprobs(const float *logits, int R, int V, long long row_stride, const int32_t *given, int n_given, float *given_logprob,
+                int top_n, int32_t *top_token, float *top_logprob, float *entropy, void *workspace, size_t workspace_bytes,
+                void *stream);
+int fq_logprobs_f16(const void *logits, int R, int V, long long row_stride, const int32_t *given, int n_given,
+                    float *given_logprob, int top_n, int32_t *top_token, float *top_logprob, float *entropy, void *workspace,
+                    size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

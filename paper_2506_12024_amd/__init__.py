@@ -15,6 +15,9 @@ _EXPORTS = (
     "FQ_MAX_HEAD_DIM", "FQ_MAX_Q_HEADS", "FQ_MAX_SEQS", "FQ_MAX_SAMPLE_V",
     "KVCache", "Sequences", "fq_rope_freqs", "fq_kv_append", "fq_attend", "fq_attend_workspace_bytes",
     "fq_sample", "fq_sample_f16", "fq_sample_workspace_bytes",
+    "FQ_MAX_ADAPTERS", "FQ_MAX_ADAPTER_RANK", "FQ_MAX_ADAPTER_ROWS", "FQ_MAX_GIVEN", "FQ_MAX_ALTERNATIVES",
+    "Adapters", "fq_adapters_add", "fq_adapters_workspace_bytes", "fq_kv_append_normed",
+    "fq_logprobs", "fq_logprobs_f16", "fq_logprobs_workspace_bytes",
     "fq_sched_state_bytes", "fq_sched_step", "fq_sched_threshold_from_prefill", "lib", "lib_path",
 )
 

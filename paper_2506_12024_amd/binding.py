@@ -23,6 +23,11 @@ FQ_MAX_HEAD_DIM = 256
 FQ_MAX_Q_HEADS = 4096
 FQ_MAX_SEQS = 65535
 FQ_MAX_SAMPLE_V = 1 << 24
+FQ_MAX_ADAPTERS = 16384
+FQ_MAX_ADAPTER_RANK = 256
+FQ_MAX_ADAPTER_ROWS = 1 << 20
+FQ_MAX_GIVEN = 65536
+FQ_MAX_ALTERNATIVES = 64
 FQ_OK, FQ_ERR_NULL, FQ_ERR_BITS, FQ_ERR_SHAPE, FQ_ERR_NOT_ATTACHED, FQ_ERR_ALIGN, FQ_ERR_HIP = \
     0, -1, -2, -3, -4, -5, -6
 
@@ -37,6 +42,8 @@ EXPORTS = [
     "fq_stream_read",
     "fq_rope_freqs", "fq_kv_create", "fq_kv_destroy", "fq_seqs_create", "fq_seqs_destroy", "fq_kv_append",
     "fq_attend_workspace_bytes", "fq_attend", "fq_sample_workspace_bytes", "fq_sample", "fq_sample_f16",
+    "fq_adapters_create", "fq_adapters_destroy", "fq_adapters_workspace_bytes", "fq_adapters_add", "fq_kv_append_normed",
+    "fq_logprobs_workspace_bytes", "fq_logprobs", "fq_logprobs_f16",
 ]
 
 
@@ -148,6 +155,21 @@ def _load() -> ctypes.CDLL:
     for name in ("fq_sample", "fq_sample_f16"):
         getattr(L, name).restype = ci
         getattr(L, name).argtypes = [vp, ci, ci, ll, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.fq_adapters_create.restype = ci
+    L.fq_adapters_create.argtypes = [ctypes.POINTER(vp), ci, ci, ci, ci, ci, vp, ll, vp, ll, vp, vp]
+    L.fq_adapters_destroy.restype = ci
+    L.fq_adapters_destroy.argtypes = [vp]
+    L.fq_adapters_workspace_bytes.restype = sz
+    L.fq_adapters_workspace_bytes.argtypes = [vp, ci]
+    L.fq_adapters_add.restype = ci
+    L.fq_adapters_add.argtypes = [vp, ci, vp, ll, vp, vp, ll, vp, ll, vp, sz, vp]
+    L.fq_kv_append_normed.restype = ci
+    L.fq_kv_append_normed.argtypes = [vp, vp, ci, vp, ll, ci, vp, ll, vp, ll, vp, ll, vp, vp, ll, cf, cf, vp, ci, ci, cf, vp, vp]
+    L.fq_logprobs_workspace_bytes.restype = sz
+    L.fq_logprobs_workspace_bytes.argtypes = [ci, ci]
+    for name in ("fq_logprobs", "fq_logprobs_f16"):
+        getattr(L, name).restype = ci
+        getattr(L, name).argtypes = [vp, ci, ci, ll, vp, ci, vp, ci, vp, vp, vp, vp, sz, vp]
     return L
 
 
@@ -544,3 +566,156 @@ def fq_sample_f16(logits, R: int, V: int, u, token, workspace, temperature=None,
                   stream=None):
     """logits: float16 [R][V], rows may lie apart."""
     _sample(lib.fq_sample_f16, _F16, logits, R, V, u, token, workspace, temperature, top_k, top_p, min_p, prob, stream)
+
+
+def _here(*tensors):
+    """The tensors of a call lie on one device, the current one: a kernel runs on the current device's streams."""
+    import torch
+    current = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else 0
+    for t in tensors:
+        if t is not None and not isinstance(t, int) and t.get_device() != current:
+            raise ValueError("a tensor lies on %s, the current device is cuda:%d" % (t.device, current))
+
+
+def _flat(t, name):
+    """(pointer, bytes) of a workspace."""
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def fq_kv_append_normed(cache: KVCache, seqs: Sequences, q, k, v, q_out, freqs, q_weight, k_weight, eps: float = 1e-6,
+                        offset: float = 0.0, interleaved: bool = False, amplitude: float = 1.0, positions=None, stream=None):
+    """As ``fq_kv_append``, every head of q and k divided by its root mean square and multiplied by weight + offset before it is
+    turned.  q_weight, k_weight: of the cache's type, both [dim] (for all heads) or both [heads][dim]."""
+    T, dtype, dim = k.shape[0], cache.dtype, cache.head_dim
+    kp, ks = _rows(k, "k", dtype, T, cache.kv_heads, dim)
+    vp, vs = _rows(v, "v", dtype, T, cache.kv_heads, dim)
+    qp = op = wp = None
+    heads = qs = os_ = 0
+    each = k_weight.dim() == 2
+    if q is not None:
+        heads = q.shape[1]
+        qp, qs = _rows(q, "q", dtype, T, heads, dim)
+        op, os_ = _rows(q_out, "q_out", dtype, T, heads, dim)
+        wp = _weights(q_weight, "q_weight", dtype, heads, dim, each)
+    _here(k, v, q, q_out, freqs, q_weight if q is not None else None, k_weight, positions)
+    _check(lib.fq_kv_append_normed(cache.handle, seqs.handle, T, qp, qs, heads, op, os_, kp, ks, vp, vs, wp,
+                                   _weights(k_weight, "k_weight", dtype, cache.kv_heads, dim, each), dim if each else 0, eps, offset,
+                                   _vector(freqs, _F64, 0, "freqs"), 0 if freqs is None else 2 * freqs.numel(),
+                                   1 if interleaved else 0, amplitude, _vector(positions, _I32, T, "positions"), _stream(stream)))
+
+
+def _weights(t, name, dtype, heads, dim, each):
+    if t.dtype is not dtype or t.shape != ((heads, dim) if each else (dim,)) or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of %s" % (name, dtype, "[%d][%d]" % (heads, dim) if each else "[%d]" % dim))
+    return t.data_ptr()
+
+
+class Adapters:
+    """Owns an ``fq_adapters`` handle and keeps its tensors alive: ``a`` [slots][rank][K] and ``b`` [slots][N][rank] in fp16 or bf16,
+    each slot contiguous; ``ranks`` int32 [slots] and ``scales`` float32 [slots] on the device, or None."""
+
+    def __init__(self, a, b, ranks=None, scales=None):
+        self.handle = None
+        if a.dim() != 3 or b.dim() != 3 or a.shape[0] != b.shape[0] or a.shape[1] != b.shape[2]:
+            raise ValueError("need a [slots][rank][K] and b [slots][N][rank]")
+        if a.dtype not in (_F16, _BF16) or b.dtype is not a.dtype:
+            raise ValueError("a and b must both be float16 or bfloat16 (got %s and %s)" % (a.dtype, b.dtype))
+        self.slots, self.rank, self.K = a.shape
+        self.N, self.dtype = b.shape[1], a.dtype
+        if a.numel() and (not a[0].is_contiguous() or not b[0].is_contiguous()):
+            raise ValueError("the values of a slot of a and b must be contiguous")
+        self._keep = (a, b, ranks, scales)
+        h = ctypes.c_void_p()
+        _check(lib.fq_adapters_create(ctypes.byref(h), FQ_F16 if a.dtype is _F16 else FQ_BF16, self.slots, self.rank, self.K, self.N,
+                                      a.data_ptr(), a.stride(0), b.data_ptr(), b.stride(0),
+                                      _vector(ranks, _I32, self.slots, "ranks"), _vector(scales, _F32, self.slots, "scales")))
+        self.handle = h
+
+    def destroy(self):
+        if self.handle is not None:
+            _check(lib.fq_adapters_destroy(self.handle))
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def fq_adapters_workspace_bytes(adapters: Adapters, M: int) -> int:
+    n = int(lib.fq_adapters_workspace_bytes(adapters.handle, M))
+    if n == 0:
+        raise FlexqError(FQ_ERR_SHAPE, fq_last_error())
+    return n
+
+
+def _matrix(t, name, dtype, M, width):
+    """(pointer, row stride) of [M][width], the values of a row side by side."""
+    if t.dtype is not dtype or t.shape != (M, width):
+        raise ValueError("%s must be [%d][%d] of %s (got %s of %s)" % (name, M, width, dtype, tuple(t.shape), t.dtype))
+    row, one = t.stride()
+    if one != 1 and width > 1:
+        raise ValueError("the values of a row of %s must lie side by side" % name)
+    return t.data_ptr(), row if M > 1 else width
+
+
+def fq_adapters_add(adapters: Adapters, x, adapter, y, out, workspace, stream=None):
+    """out = y + scale * (x A^T) B^T, each row by its own adapter (int32 [M], -1: none).  x: [M][K]; y, out: [M][N] (rows may lie
+    apart), out may be y."""
+    M, dtype = x.shape[0], adapters.dtype
+    xp, xs = _matrix(x, "x", dtype, M, adapters.K)
+    yp, ys = _matrix(y, "y", dtype, M, adapters.N)
+    op, os_ = _matrix(out, "out", dtype, M, adapters.N)
+    _here(x, adapter, y, out, workspace, adapters._keep[0])
+    wp, n = _flat(workspace, "workspace")
+    _check(lib.fq_adapters_add(adapters.handle, M, xp, xs, _vector(adapter, _I32, M, "adapter"), yp, ys, op, os_, wp, n,
+                               _stream(stream)))
+
+
+def fq_logprobs_workspace_bytes(R: int, V: int) -> int:
+    n = int(lib.fq_logprobs_workspace_bytes(R, V))
+    if n == 0:
+        raise FlexqError(FQ_ERR_SHAPE, fq_last_error())
+    return n
+
+
+def _columns(t, dtype, R, name):
+    """(pointer, columns) of a contiguous [R] or [R][n] tensor, or nothing."""
+    if t is None:
+        return None, 0
+    if t.dtype is not dtype or t.dim() not in (1, 2) or t.shape[0] != R or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of [%d] or [%d][n]" % (name, dtype, R, R))
+    return t.data_ptr(), 1 if t.dim() == 1 else t.shape[1]
+
+
+def _logprobs(call, dtype, logits, R, V, workspace, given, given_logprob, top_token, top_logprob, entropy, stream):
+    rows, width = logits.shape
+    row, one = logits.stride()
+    if logits.dtype is not dtype or rows < R or width != V or (one != 1 and V > 1):
+        raise ValueError("logits must be %s [R][V], the logits of a row side by side" % dtype)
+    gp, n = _columns(given, _I32, R, "given")
+    lp, n2 = _columns(given_logprob, _F32, R, "given_logprob")
+    tp, m = _columns(top_token, _I32, R, "top_token")
+    pp, m2 = _columns(top_logprob, _F32, R, "top_logprob")
+    if n != n2 or m != m2:
+        raise ValueError("given and given_logprob, and top_token and top_logprob, must have one shape")
+    _here(logits, workspace, given, given_logprob, top_token, top_logprob, entropy)
+    wp, bytes_ = _flat(workspace, "workspace")
+    _check(call(logits.data_ptr(), R, V, row if R > 1 else V, gp, n, lp, m, tp, pp, _vector(entropy, _F32, R, "entropy"), wp, bytes_,
+                _stream(stream)))
+
+
+def fq_logprobs(logits, R: int, V: int, workspace, given=None, given_logprob=None, top_token=None, top_logprob=None, entropy=None,
+                stream=None):
+    """logits: float32 [R][V], rows may lie apart.  given (int32) and given_logprob: [R] or [R][n]; top_token (int32) and
+    top_logprob: [R][n], the n likeliest; entropy: [R]."""
+    _logprobs(lib.fq_logprobs, _F32, logits, R, V, workspace, given, given_logprob, top_token, top_logprob, entropy, stream)
+
+
+def fq_logprobs_f16(logits, R: int, V: int, workspace, given=None, given_logprob=None, top_token=None, top_logprob=None, entropy=None,
+                    stream=None):
+    """logits: float16 [R][V], rows may lie apart; everything else as ``fq_logprobs``."""
+    _logprobs(lib.fq_logprobs_f16, _F16, logits, R, V, workspace, given, given_logprob, top_token, top_logprob, entropy, stream)

@@ -15,7 +15,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libflexq.so")
 OBJDIR = os.path.join(HERE, "_build")
 SOURCES = ["fq_api.hip", "fq_device.hip", "fq_noalloc.hip", "fq_probe.hip", "fq_quantize.hip", "fq_entropy.hip", "fq_decode.hip", "fq_staged.hip", "fq_skinny.hip", "fq_batch.hip", "fq_stream.hip", "fq_prefill.hip", "fq_prompt.hip", "fq_w8a8.hip", "fq_w8a8_prompt.hip", "fq_sched.hip", "fq_lmhead.hip",
-           "fq_serve.hip", "fq_append.hip", "fq_attend.hip", "fq_attend_f16.hip", "fq_attend_bf16.hip", "fq_sample.hip"]
+           "fq_serve.hip", "fq_append.hip", "fq_attend.hip", "fq_attend_f16.hip", "fq_attend_bf16.hip", "fq_sample.hip",
+           "fq_adapters.hip", "fq_append_normed.hip", "fq_logprobs.hip"]
 HEADERS = [os.path.join(CSRC, "fq_internal.h"), os.path.join(CSRC, "fq_gemv.h"), os.path.join(CSRC, "fq_mfma.h"), os.path.join(CSRC, "fq_div.h"), os.path.join(CSRC, "fq_batch_at.h"),
            os.path.join(CSRC, "fq_staged_src.h"), os.path.join(CSRC, "fq_kv.h"), os.path.join(CSRC, "fq_attend.h"),
            os.path.join(CSRC, "fq_attend_few.h"), os.path.join(CSRC, "fq_attend_many.h"), os.path.join(CSRC, "fq_attend_kernels.h"),

@@ -258,4 +258,42 @@ struct FqSampleArgs {
 };
 hipError_t fq_launch_sample(const FqSampleArgs &a, bool half, hipStream_t stream);
 
+// The same with head norms: q_weight, k_weight of the cache's type, heads weight_stride elements apart (0: one for all).
+struct FqNormArgs {
+    const uint16_t *q_weight, *k_weight;
+    long long weight_stride;
+    float eps, offset;
+};
+hipError_t fq_launch_append_normed(const FqAppendArgs &a, const FqNormArgs &n, bool interleaved, hipStream_t stream);
+
+// Low-rank adapters of one linear (slots of A [rank][K] and B [N][rank], strides in elements) and a call's rows.
+struct FqAdaptersView {
+    const uint16_t *a, *b;
+    long long a_stride, b_stride;
+    const int32_t *ranks; // or null
+    const float *scales;  // or null
+    int slots, rank, K, N, bf16;
+};
+struct FqAdaptersArgs {
+    FqAdaptersView set;
+    const uint16_t *x, *y;
+    uint16_t *out;
+    const int32_t *adapter;
+    long long x_stride, y_stride, out_stride;
+    int M;
+};
+size_t fq_adapters_bytes(const FqAdaptersView &set, int M);
+hipError_t fq_launch_adapters(const FqAdaptersArgs &a, void *workspace, hipStream_t stream);
+
+struct FqLogprobsArgs {
+    const void *logits;
+    const int32_t *given;
+    float *given_logprob, *top_logprob, *entropy;
+    int32_t *top_token;
+    long long row_stride;
+    int R, V, n_given, top_n;
+};
+size_t fq_logprobs_bytes(int R, int V);
+hipError_t fq_launch_logprobs(const FqLogprobsArgs &a, bool half, void *workspace, hipStream_t stream);
+
 #endif

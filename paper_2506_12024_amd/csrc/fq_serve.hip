@@ -19,8 +19,14 @@ struct fq_seqs {
     FqSeqsView view; // tokens: set by each call
 };
 
+struct fq_adapters {
+    uint32_t magic;
+    FqAdaptersView view;
+};
+
 namespace {
 
+constexpr uint32_t ADAPTERS_MAGIC = 0x46514144u; // "FQAD"
 constexpr uint32_t KV_MAGIC = 0x46514B56u;   // "FQKV"
 constexpr uint32_t SEQS_MAGIC = 0x46515351u; // "FQSQ"
 constexpr size_t SAMPLE_BYTES = 256;         // asked of a caller of fq_sample; no kernel uses them (a row is one workgroup's)
@@ -220,12 +226,12 @@ int fq_seqs_destroy(fq_seqs *seqs)
     return FQ_OK;
 }
 
-int fq_kv_append(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q, long long q_stride, int q_heads,
-                 void *q_out, long long q_out_stride, const void *k, long long k_stride, const void *v,
-                 long long v_stride, const double *freqs, int rot_dim, int interleaved, float amplitude,
-                 const int32_t *positions, void *stream)
+// norm: null, or what is done to the heads of q and k before they are turned.
+static int append_any(const char *who, const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q, long long q_stride,
+                      int q_heads, void *q_out, long long q_out_stride, const void *k, long long k_stride, const void *v,
+                      long long v_stride, const FqNormArgs *norm, const double *freqs, int rot_dim, int interleaved,
+                      float amplitude, const int32_t *positions, void *stream)
 {
-    const char *who = "fq_kv_append";
     if (int rc = check_handles(who, kv, seqs, tokens))
         return rc;
     const FqKvView &c = kv->view;
@@ -254,6 +260,18 @@ int fq_kv_append(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q
     }
     if (rot_dim > 0 && !freqs)
         return fq_fail(FQ_ERR_NULL, "%s: freqs is NULL", who);
+    if (norm) {
+        if ((q_heads != 0 && !norm->q_weight) || !norm->k_weight)
+            return fq_fail(FQ_ERR_NULL, "%s: q_weight or k_weight is NULL", who);
+        if (norm->weight_stride != 0 && (norm->weight_stride < c.dim || norm->weight_stride > (1LL << 40)))
+            return fq_fail(FQ_ERR_SHAPE, "%s: weight_stride must be 0 or at least the head's %d (got %lld)", who, c.dim,
+                           norm->weight_stride);
+        if (!(norm->eps >= 0.0f) || !std::isfinite(norm->eps) || !std::isfinite(norm->offset))
+            return fq_fail(FQ_ERR_SHAPE, "%s: eps must be finite and >= 0, offset finite (got %g and %g)", who, norm->eps,
+                           norm->offset);
+        if (!aligned(norm->q_weight, 16) || !aligned(norm->k_weight, 16) || norm->weight_stride % 8 != 0)
+            return fq_fail(FQ_ERR_ALIGN, "%s: weights need 16-byte alignment and a stride that is a multiple of 8", who);
+    }
     if (!std::isfinite(amplitude))
         return fq_fail(FQ_ERR_SHAPE, "%s: amplitude must be finite", who);
     if (!aligned(freqs, 8) || !aligned(positions, 4))
@@ -261,7 +279,28 @@ int fq_kv_append(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q
     FqAppendArgs a{c, seqs->view, (const uint16_t *)q, (const uint16_t *)k, (const uint16_t *)v, (uint16_t *)q_out, q_stride,
                    q_out_stride, k_stride, v_stride, freqs, positions, q_heads, rot_dim, amplitude};
     a.seqs.tokens = tokens;
-    return launched(fq_launch_append(a, interleaved != 0, (hipStream_t)stream), who);
+    return launched(norm ? fq_launch_append_normed(a, *norm, interleaved != 0, (hipStream_t)stream)
+                         : fq_launch_append(a, interleaved != 0, (hipStream_t)stream), who);
+}
+
+int fq_kv_append(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q, long long q_stride, int q_heads,
+                 void *q_out, long long q_out_stride, const void *k, long long k_stride, const void *v,
+                 long long v_stride, const double *freqs, int rot_dim, int interleaved, float amplitude,
+                 const int32_t *positions, void *stream)
+{
+    return append_any("fq_kv_append", kv, seqs, tokens, q, q_stride, q_heads, q_out, q_out_stride, k, k_stride, v, v_stride,
+                      nullptr, freqs, rot_dim, interleaved, amplitude, positions, stream);
+}
+
+int fq_kv_append_normed(const fq_kv *kv, const fq_seqs *seqs, int tokens, const void *q, long long q_stride, int q_heads,
+                        void *q_out, long long q_out_stride, const void *k, long long k_stride, const void *v,
+                        long long v_stride, const void *q_weight, const void *k_weight, long long weight_stride, float eps,
+                        float offset, const double *freqs, int rot_dim, int interleaved, float amplitude,
+                        const int32_t *positions, void *stream)
+{
+    const FqNormArgs norm{(const uint16_t *)q_weight, (const uint16_t *)k_weight, weight_stride, eps, offset};
+    return append_any("fq_kv_append_normed", kv, seqs, tokens, q, q_stride, q_heads, q_out, q_out_stride, k, k_stride, v,
+                      v_stride, &norm, freqs, rot_dim, interleaved, amplitude, positions, stream);
 }
 
 static int attend_args(const char *who, const fq_kv *kv, const fq_seqs *seqs, int tokens, int q_heads, int max_q, int max_kv,
@@ -376,6 +415,142 @@ int fq_sample_f16(const void *logits, int R, int V, long long row_stride, const 
 {
     return sample_any("fq_sample_f16", true, logits, R, V, row_stride, u, temperature, top_k, top_p, min_p, token, prob,
                       workspace, workspace_bytes, stream);
+}
+
+int fq_adapters_create(fq_adapters **out, int dtype, int slots, int rank, int K, int N, const void *a, long long a_stride,
+                       const void *b, long long b_stride, const int32_t *ranks, const float *scales)
+{
+    const char *who = "fq_adapters_create";
+    if (!out)
+        return fq_fail(FQ_ERR_NULL, "%s: out is NULL", who);
+    *out = nullptr;
+    if (dtype != FQ_F16 && dtype != FQ_BF16)
+        return fq_fail(FQ_ERR_BITS, "%s: dtype must be FQ_F16 or FQ_BF16 (got %d)", who, dtype);
+    if (slots < 1 || slots > FQ_MAX_ADAPTERS || rank < 8 || rank > FQ_MAX_ADAPTER_RANK || rank % 8 != 0)
+        return fq_fail(FQ_ERR_SHAPE, "%s: need 1..%d slots of a rank that is a multiple of 8, at most %d (got %d of %d)", who,
+                       FQ_MAX_ADAPTERS, FQ_MAX_ADAPTER_RANK, slots, rank);
+    if (K < 8 || K > (1 << 24) || K % 8 != 0 || N < 1 || N > (1 << 24))
+        return fq_fail(FQ_ERR_SHAPE, "%s: K must be a multiple of 8, K and N at most 2^24 (got %d and %d)", who, K, N);
+    if (!a || !b)
+        return fq_fail(FQ_ERR_NULL, "%s: a or b is NULL", who);
+    // (far below where a slot times a stride could pass 64 bits)
+    if (slots > 1 && (a_stride < (long long)rank * K || b_stride < (long long)rank * N || a_stride > (1LL << 46) / slots ||
+                      b_stride > (1LL << 46) / slots))
+        return fq_fail(FQ_ERR_SHAPE, "%s: slots are %lld and %lld elements apart, A has %lld, B %lld (all within 2^46)", who, a_stride,
+                       b_stride, (long long)rank * K, (long long)rank * N);
+    if (!aligned(a, 16) || !aligned(b, 16) || a_stride % 8 != 0 || b_stride % 8 != 0 || !aligned(ranks, 4) || !aligned(scales, 4))
+        return fq_fail(FQ_ERR_ALIGN, "%s: a and b need 16-byte alignment, strides multiples of 8, ranks and scales 4 bytes", who);
+    fq_adapters *h = new (std::nothrow) fq_adapters();
+    if (!h)
+        return fq_fail(FQ_ERR_HIP, "%s: out of host memory", who);
+    h->magic = ADAPTERS_MAGIC;
+    h->view = FqAdaptersView{(const uint16_t *)a, (const uint16_t *)b, slots > 1 ? a_stride : 0, slots > 1 ? b_stride : 0,
+                             ranks, scales, slots, rank, K, N, dtype == FQ_BF16};
+    *out = h;
+    return FQ_OK;
+}
+
+int fq_adapters_destroy(fq_adapters *adapters)
+{
+    if (!adapters || adapters->magic != ADAPTERS_MAGIC)
+        return fq_fail(FQ_ERR_NULL, "fq_adapters_destroy: NULL or not a valid handle");
+    adapters->magic = 0;
+    delete adapters;
+    return FQ_OK;
+}
+
+static int adapters_args(const char *who, const fq_adapters *adapters, int M)
+{
+    if (!adapters || adapters->magic != ADAPTERS_MAGIC)
+        return fq_fail(FQ_ERR_NULL, "%s: the handle is NULL or not valid (destroyed or corrupted)", who);
+    if (M < 0 || M > FQ_MAX_ADAPTER_ROWS)
+        return fq_fail(FQ_ERR_SHAPE, "%s: M must be 0..%d (got %d)", who, FQ_MAX_ADAPTER_ROWS, M);
+    return FQ_OK;
+}
+
+size_t fq_adapters_workspace_bytes(const fq_adapters *adapters, int M)
+{
+    if (adapters_args("fq_adapters_workspace_bytes", adapters, M))
+        return 0;
+    return fq_adapters_bytes(adapters->view, M);
+}
+
+int fq_adapters_add(const fq_adapters *adapters, int M, const void *x, long long x_stride, const int32_t *adapter, const void *y,
+                    long long y_stride, void *out, long long out_stride, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const char *who = "fq_adapters_add";
+    if (int rc = adapters_args(who, adapters, M))
+        return rc;
+    if (M == 0)
+        return FQ_OK;
+    const FqAdaptersView &set = adapters->view;
+    if (!x || !adapter || !y || !out || !workspace)
+        return fq_fail(FQ_ERR_NULL, "%s: NULL argument", who);
+    const long long most = 1LL << 40;
+    if (x_stride < set.K || y_stride < set.N || out_stride < set.N || x_stride > most || y_stride > most || out_stride > most)
+        return fq_fail(FQ_ERR_SHAPE, "%s: rows of x, y and out are %lld, %lld and %lld elements apart, K = %d and N = %d are needed", who,
+                       x_stride, y_stride, out_stride, set.K, set.N);
+    if (!aligned(x, 16) || x_stride % 8 != 0 || !aligned(y, 2) || !aligned(out, 2) || !aligned(adapter, 4) || !aligned(workspace, 256))
+        return fq_fail(FQ_ERR_ALIGN, "%s: x needs 16-byte alignment and a stride that is a multiple of 8, y and out 2 bytes, adapter 4, "
+                                     "the workspace 256", who);
+    const size_t need = fq_adapters_bytes(set, M);
+    if (workspace_bytes < need)
+        return fq_fail(FQ_ERR_SHAPE, "%s: the workspace has %zu bytes, the call needs %zu", who, workspace_bytes, need);
+    if ((y != out || y_stride != out_stride) && rows_overlap(y, y_stride, set.N, out, out_stride, set.N, M))
+        return fq_fail(FQ_ERR_SHAPE, "%s: out may be y, row for row, but not overlap it otherwise", who);
+    if (rows_overlap(x, x_stride, set.K, out, out_stride, set.N, M))
+        return fq_fail(FQ_ERR_SHAPE, "%s: out may not overlap x", who);
+    const FqAdaptersArgs a{set, (const uint16_t *)x, (const uint16_t *)y, (uint16_t *)out, adapter, x_stride, y_stride, out_stride, M};
+    return launched(fq_launch_adapters(a, workspace, (hipStream_t)stream), who);
+}
+
+size_t fq_logprobs_workspace_bytes(int R, int V)
+{
+    if (R < 0 || V < 1 || V > FQ_MAX_SAMPLE_V) {
+        fq_fail(FQ_ERR_SHAPE, "fq_logprobs_workspace_bytes: need R >= 0 and V in 1..%d (got %d and %d)", FQ_MAX_SAMPLE_V, R, V);
+        return 0;
+    }
+    return fq_logprobs_bytes(R, V);
+}
+
+static int logprobs_any(const char *who, bool half, const void *logits, int R, int V, long long row_stride, const int32_t *given,
+                        int n_given, float *given_logprob, int top_n, int32_t *top_token, float *top_logprob, float *entropy,
+                        void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (R < 0 || V < 1 || V > FQ_MAX_SAMPLE_V || row_stride < V || row_stride > (1LL << 40))
+        return fq_fail(FQ_ERR_SHAPE, "%s: need R >= 0, V in 1..%d and row_stride >= V (got %d, %d, %lld)", who,
+                       FQ_MAX_SAMPLE_V, R, V, row_stride);
+    if (n_given < 0 || n_given > FQ_MAX_GIVEN || top_n < 0 || top_n > FQ_MAX_ALTERNATIVES)
+        return fq_fail(FQ_ERR_SHAPE, "%s: need n_given in 0..%d and top_n in 0..%d (got %d and %d)", who, FQ_MAX_GIVEN,
+                       FQ_MAX_ALTERNATIVES, n_given, top_n);
+    if (R == 0)
+        return FQ_OK;
+    if (!logits || !workspace || (n_given && (!given || !given_logprob)) || (top_n && (!top_token || !top_logprob)))
+        return fq_fail(FQ_ERR_NULL, "%s: NULL argument", who);
+    if (!aligned(logits, half ? 2 : 4) || !aligned(given, 4) || !aligned(given_logprob, 4) || !aligned(top_token, 4) ||
+        !aligned(top_logprob, 4) || !aligned(entropy, 4) || !aligned(workspace, 256))
+        return fq_fail(FQ_ERR_ALIGN, "%s: logits need the alignment of their type, the workspace 256 bytes, the rest 4", who);
+    const size_t need = fq_logprobs_bytes(R, V);
+    if (workspace_bytes < need)
+        return fq_fail(FQ_ERR_SHAPE, "%s: the workspace has %zu bytes, the call needs %zu", who, workspace_bytes, need);
+    const FqLogprobsArgs a{logits, given, given_logprob, top_logprob, entropy, top_token, row_stride, R, V, n_given, top_n};
+    return launched(fq_launch_logprobs(a, half, workspace, (hipStream_t)stream), who);
+}
+
+int fq_logprobs(const float *logits, int R, int V, long long row_stride, const int32_t *given, int n_given, float *given_logprob,
+                int top_n, int32_t *top_token, float *top_logprob, float *entropy, void *workspace, size_t workspace_bytes,
+                void *stream)
+{
+    return logprobs_any("fq_logprobs", false, logits, R, V, row_stride, given, n_given, given_logprob, top_n, top_token, top_logprob,
+                        entropy, workspace, workspace_bytes, stream);
+}
+
+int fq_logprobs_f16(const void *logits, int R, int V, long long row_stride, const int32_t *given, int n_given,
+                    float *given_logprob, int top_n, int32_t *top_token, float *top_logprob, float *entropy, void *workspace,
+                    size_t workspace_bytes, void *stream)
+{
+    return logprobs_any("fq_logprobs_f16", true, logits, R, V, row_stride, given, n_given, given_logprob, top_n, top_token,
+                        top_logprob, entropy, workspace, workspace_bytes, stream);
 }
 
 } // extern "C"
