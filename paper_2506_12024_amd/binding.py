@@ -568,20 +568,28 @@ def fq_sample_f16(logits, R: int, V: int, u, token, workspace, temperature=None,
     _sample(lib.fq_sample_f16, _F16, logits, R, V, u, token, workspace, temperature, top_k, top_p, min_p, prob, stream)
 
 
-def _here(*tensors):
-    """The tensors of a call lie on one device, the current one: a kernel runs on the current device's streams."""
-    import torch
-    current = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else 0
+def _place(stream, *tensors):
+    """The call's stream.  Its tensors have to lie on the current device, whose streams a kernel runs on."""
+    current = _device()
     for t in tensors:
         if t is not None and not isinstance(t, int) and t.get_device() != current:
             raise ValueError("a tensor lies on %s, the current device is cuda:%d" % (t.device, current))
+    return _stream(stream)
+
+
+def _device():
+    import torch
+    if torch.cuda.is_initialized():
+        get = getattr(torch._C, "_cuda_getDevice", None)
+        return get() if get else torch.cuda.current_device()
+    return 0
 
 
 def _flat(t, name):
     """(pointer, bytes) of a workspace."""
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
-    return t.data_ptr(), t.numel() * t.element_size()
+    return t.data_ptr(), t.nbytes
 
 
 def fq_kv_append_normed(cache: KVCache, seqs: Sequences, q, k, v, q_out, freqs, q_weight, k_weight, eps: float = 1e-6,
@@ -599,11 +607,11 @@ def fq_kv_append_normed(cache: KVCache, seqs: Sequences, q, k, v, q_out, freqs, 
         qp, qs = _rows(q, "q", dtype, T, heads, dim)
         op, os_ = _rows(q_out, "q_out", dtype, T, heads, dim)
         wp = _weights(q_weight, "q_weight", dtype, heads, dim, each)
-    _here(k, v, q, q_out, freqs, q_weight if q is not None else None, k_weight, positions)
+    stream = _place(stream, k, v, q, q_out, freqs, q_weight if q is not None else None, k_weight, positions)
     _check(lib.fq_kv_append_normed(cache.handle, seqs.handle, T, qp, qs, heads, op, os_, kp, ks, vp, vs, wp,
                                    _weights(k_weight, "k_weight", dtype, cache.kv_heads, dim, each), dim if each else 0, eps, offset,
                                    _vector(freqs, _F64, 0, "freqs"), 0 if freqs is None else 2 * freqs.numel(),
-                                   1 if interleaved else 0, amplitude, _vector(positions, _I32, T, "positions"), _stream(stream)))
+                                   1 if interleaved else 0, amplitude, _vector(positions, _I32, T, "positions"), stream))
 
 
 def _weights(t, name, dtype, heads, dim, each):
@@ -669,10 +677,10 @@ def fq_adapters_add(adapters: Adapters, x, adapter, y, out, workspace, stream=No
     xp, xs = _matrix(x, "x", dtype, M, adapters.K)
     yp, ys = _matrix(y, "y", dtype, M, adapters.N)
     op, os_ = _matrix(out, "out", dtype, M, adapters.N)
-    _here(x, adapter, y, out, workspace, adapters._keep[0])
+    stream = _place(stream, x, adapter, y, out, workspace, adapters._keep[0])
     wp, n = _flat(workspace, "workspace")
     _check(lib.fq_adapters_add(adapters.handle, M, xp, xs, _vector(adapter, _I32, M, "adapter"), yp, ys, op, os_, wp, n,
-                               _stream(stream)))
+                               stream))
 
 
 def fq_logprobs_workspace_bytes(R: int, V: int) -> int:
@@ -702,10 +710,10 @@ def _logprobs(call, dtype, logits, R, V, workspace, given, given_logprob, top_to
     pp, m2 = _columns(top_logprob, _F32, R, "top_logprob")
     if n != n2 or m != m2:
         raise ValueError("given and given_logprob, and top_token and top_logprob, must have one shape")
-    _here(logits, workspace, given, given_logprob, top_token, top_logprob, entropy)
+    stream = _place(stream, logits, workspace, given, given_logprob, top_token, top_logprob, entropy)
     wp, bytes_ = _flat(workspace, "workspace")
     _check(call(logits.data_ptr(), R, V, row if R > 1 else V, gp, n, lp, m, tp, pp, _vector(entropy, _F32, R, "entropy"), wp, bytes_,
-                _stream(stream)))
+                stream))
 
 
 def fq_logprobs(logits, R: int, V: int, workspace, given=None, given_logprob=None, top_token=None, top_logprob=None, entropy=None,

@@ -1,11 +1,14 @@
 // Low-rank adapters of many requests beside a projection that they share: out = y + scale (x A^T) B^T, row by row.
 //
-// Both products are on the matrix cores, in two launches: `low_kernel` forms u = x A^T, its K split over the wavefronts of a workgroup and over
-// workgroups, whose parts (binary32) lie in the workspace; `out_kernel` adds them up, and B meets them as two 16-bit numbers each, u =
-// hi + lo (binary16: 22 bits of it, a row scaled by a power of two so that its largest fills the range; bfloat16: 17), so that x A^T is
-// nowhere rounded to 16 bits.  A tile is up to 16 or 64 rows of one slot, wherever in the call they stand: a row's sums do not
-// depend on its place in a tile.  Up to SMALL_ROWS rows every workgroup finds its tile itself (the row it is numbered by leads a tile if
-// the rows of its slot before it fill whole ones); for more a launch of one workgroup sorts the rows by slot first.
+// Both products are on the matrix cores.  u = x A^T is a binary32 sum, and meets B as two 16-bit numbers each, u = hi + lo (binary16: 22
+// bits of it, a row scaled by a power of two so that its largest fills the range; bfloat16: 17), so that it is nowhere rounded to
+// 16 bits.  A tile is up to 16 or 64 rows of one slot, wherever in the call they stand: a row's sums do not depend on its place in a
+// tile.  Few rows are one launch (few_kernel), whose workgroups form u for themselves; many are two: low_kernel forms u in parts of K, which lie in
+// the workspace, out_kernel adds them up and multiplies by B.
+//
+// What the operands' registers hold (16 bytes of 16 rows to a quarter of a wavefront) is nowhere loaded from memory in that order: the address unit
+// takes such a quarter a row at a time, 131 KB of A 3.4 us a workgroup as against 0.8 to 1.1 with 128 bytes of a row to eight lanes.
+// It goes through LDS, 16-byte pieces placed so that both sides are free of conflicts.
 #include <hip/hip_runtime.h>
 
 #include "../../include/flexq.h"
@@ -14,11 +17,11 @@
 namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
-constexpr int SMALL_ROWS = 256, SMALL_TILE = 16, TILE = 64;
+constexpr int FEW_ROWS = 64, FEW_TILE = 16, FEW_ELEMENTS = 1 << 18, TILE = 64;
 constexpr int MIDDLE_ROWS = 4096, MIDDLE_SLOTS = 1023;
-constexpr int GROUP_THREADS = 1024, MANY_THREADS = 512;
+constexpr int GROUP_THREADS = 1024, OUT_THREADS = 512;
 constexpr int CHUNK = 256, MAX_PARTS = 16; // of K
-enum Find { ALONE, COUNTED, LISTED }; // how a workgroup finds its tile: of few rows; of MIDDLE_ROWS; in the workspace's list
+enum Find { COUNTED, LISTED }; // how a workgroup of low_kernel finds its tile: by itself, or in the workspace's list
 
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf8_t __attribute__((ext_vector_type(8)));
@@ -45,17 +48,17 @@ struct Work {
     int parts, max_tiles;
 };
 
-int tiles_of(const FqAdaptersView &set, int M) // at most
-{
-    return M <= SMALL_ROWS ? M : M / TILE + (M < set.slots + 1 ? M : set.slots + 1);
-}
+// Whether a call is one launch: every workgroup of a tile reads its slot's A whole, which is less than the second launch and the parts while A
+// is small.
+bool few(const FqAdaptersView &set, int M) { return M <= FEW_ROWS && set.rank <= 64 && (long long)set.rank * set.K <= FEW_ELEMENTS; }
+
+int tiles_of(const FqAdaptersView &set, int M) { return M / TILE + (M < set.slots + 1 ? M : set.slots + 1); } // at most
 
 // Parts of K: workgroups for the whole chip while rows are few, at least a chunk to each.
 int parts_of(const FqAdaptersView &set, int M)
 {
-    const int tiles = M <= SMALL_ROWS ? M : (M + TILE - 1) / TILE, room = 256;
-    int parts = room / tiles;
-    parts = parts > MAX_PARTS ? MAX_PARTS : M <= SMALL_ROWS && parts < 4 ? 4 : parts < 1 ? 1 : parts;
+    int parts = 256 / ((M + TILE - 1) / TILE);
+    parts = parts > MAX_PARTS ? MAX_PARTS : parts < 1 ? 1 : parts;
     const int most = (set.K + CHUNK - 1) / CHUNK;
     return parts < most ? parts : most;
 }
@@ -63,11 +66,18 @@ int parts_of(const FqAdaptersView &set, int M)
 // Rows times parts, from above and never less for more rows: what parts_of gives is at most this.
 size_t low_rows(int M)
 {
-    const size_t m = M, few = M <= SMALL_ROWS ? (4 * m > 256 ? 4 * m : 256) : (m > 256 * TILE ? m : 256 * TILE);
-    return MAX_PARTS * m < few ? MAX_PARTS * m : few;
+    const size_t m = M, most = m > 256 * TILE ? m : 256 * TILE;
+    return MAX_PARTS * m < most ? MAX_PARTS * m : most;
 }
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
+
+// What a wavefront hands to itself through LDS: its operations there are in order, the compiler has to keep them so.
+__device__ __forceinline__ void own_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 
 // A row's adapter, or -1.
 __device__ __forceinline__ int slot_of(const FqAdaptersArgs &a, int m)
@@ -81,36 +91,6 @@ __device__ __forceinline__ int rank_of(const FqAdaptersArgs &a, int slot)
     if (slot < 0)
         return 0;
     return a.set.ranks ? min(max(a.set.ranks[slot], 0), a.set.rank) : a.set.rank;
-}
-
-// The rows of this workgroup's tile into LDS; its slot through `slot`; the number of rows, 0 if there is no tile.
-__device__ __forceinline__ int find_alone(const FqAdaptersArgs &a, int *rows, int &slot)
-{
-    const int tid = threadIdx.x, lane = tid & 63, own = blockIdx.x;
-    int found[SMALL_ROWS / 64];
-    uint64_t mask[SMALL_ROWS / 64];
-    slot = slot_of(a, own);
-#pragma unroll
-    for (int c = 0; c < SMALL_ROWS / 64; c++)
-        found[c] = 64 * c + lane < a.M ? slot_of(a, 64 * c + lane) : -2;
-    int before = 0, seen = 0;
-#pragma unroll
-    for (int c = 0; c < SMALL_ROWS / 64; c++) {
-        mask[c] = __ballot(found[c] == slot);
-        const int upto = own - 64 * c;
-        before += __popcll(upto <= 0 ? 0 : upto >= 64 ? mask[c] : mask[c] & ((1ull << upto) - 1));
-    }
-    if (before % SMALL_TILE != 0)
-        return 0;
-#pragma unroll
-    for (int c = 0; c < SMALL_ROWS / 64; c++) {
-        const int at = seen + __popcll(mask[c] & ((1ull << lane) - 1)) - before;
-        if (tid < 64 && found[c] == slot && at >= 0 && at < SMALL_TILE)
-            rows[at] = 64 * c + lane;
-        seen += __popcll(mask[c]);
-    }
-    __syncthreads();
-    return min(seen - before, SMALL_TILE);
 }
 
 __device__ __forceinline__ Tile find_listed(const Work &w, int *rows)
@@ -309,71 +289,10 @@ __device__ __forceinline__ void join_waves(float4_t (&acc)[TILES], float4_t (*su
     }
 }
 
-// u = x A^T of a tile of few rows: RT * 16 ranks from 16 RT blockIdx.z on, the part blockIdx.y of K.  A step is 64 of K, of which a lane
-// has 16 that follow each other (32 bytes of its row of x and of A): 128 bytes of a row to four lanes.
-template <int RT, bool BF16>
-__global__ __launch_bounds__(THREADS) void low_few_kernel(FqAdaptersArgs a, Work w)
-{
-    __shared__ int rows[SMALL_TILE];
-    __shared__ float4_t sums[WAVES / 2][RT][64];
-    int slot = -1;
-    const int count = find_alone(a, rows, slot);
-    const int rank = count ? rank_of(a, slot) : 0, r0 = 16 * RT * blockIdx.z;
-    leave(a, w, rows, Tile{slot, count, rank, 1.0f});
-    if (r0 >= rank)
-        return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
-    const uint16_t *xp = a.x + rows[col < count ? col : 0] * a.x_stride + 16 * g, *ap[RT];
-#pragma unroll
-    for (int r = 0; r < RT; r++)
-        ap[r] = a.set.a + slot * a.set.a_stride + (size_t)min(r0 + 16 * r + col, rank - 1) * a.set.K + 16 * g;
-    float4_t acc[RT] = {};
-    const int K = a.set.K, steps = (K + 63) / 64;
-    // a workgroup's part is one piece of K, its wavefronts' steps alternate
-    const int part = (steps + gridDim.y - 1) / gridDim.y, end = min(steps, part * ((int)blockIdx.y + 1));
-    struct Step {
-        u32x4 x[2], a[RT][2];
-    };
-    auto ask = [&](Step &s, int step) {
-        const int k = 64 * step;
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const bool in = k + 16 * g + 8 * h < K;
-            s.x[h] = in ? *(const u32x4 *)(xp + k + 8 * h) : u32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int r = 0; r < RT; r++)
-                s.a[r][h] = in ? *(const u32x4 *)(ap[r] + k + 8 * h) : u32x4{0, 0, 0, 0};
-        }
-    };
-    Step now, next;
-    int step = part * blockIdx.y + wave;
-    if (step < end)
-        ask(now, step);
-    for (; step < end; step += WAVES) {
-        if (step + WAVES < end)
-            ask(next, step + WAVES);
-#pragma unroll
-        for (int h = 0; h < 2; h++)
-#pragma unroll
-            for (int r = 0; r < RT; r++)
-                acc[r] = mfma<BF16>(now.a[r][h], now.x[h], acc[r]);
-        now = next;
-    }
-    join_waves(acc, sums);
-    if (wave == 0 && col < count) {
-        float *to = w.low + ((size_t)blockIdx.y * a.M + rows[col]) * a.set.rank + r0 + 4 * g;
-#pragma unroll
-        for (int r = 0; r < RT; r++)
-            if (r0 + 16 * r + 4 * g < a.set.rank)
-                *(float4_t *)(to + 16 * r) = acc[r];
-    }
-}
-
-// The same for tiles of up to 64 rows.  Chunks of 256 of K go through LDS: 32 lanes ask for 512 bytes of a row (the operands' own order asks
-// for 16 bytes of 16 rows at once, which the address unit takes a row at a time), a row's 16-byte piece p lies at place p ^ (row % 16), so that the
-// 16 rows of an operand are read without conflicts.  A wavefront multiplies a quarter of the chunk while the next one is on its way.
+// u = x A^T of a tile of up to 64 rows: 16 RT ranks from 16 RT blockIdx.z on, the part blockIdx.y of K, 256 at a time.  32 lanes ask for 512
+// bytes of a row; a row's piece p lies at place p ^ (row % 16).  A wavefront multiplies a quarter of what is in LDS while the next is on its way.
 template <int RT, bool BF16, Find FIND>
-__global__ __launch_bounds__(THREADS) void low_many_kernel(FqAdaptersArgs a, Work w)
+__global__ __launch_bounds__(THREADS) void low_kernel(FqAdaptersArgs a, Work w)
 {
     constexpr int TT = TILE / 16, PIECES = CHUNK / 8, ROWS_A_TURN = THREADS / PIECES, X_TURNS = TILE / ROWS_A_TURN,
                   A_TURNS = 16 * RT / ROWS_A_TURN;
@@ -463,73 +382,215 @@ __global__ __launch_bounds__(THREADS) void low_many_kernel(FqAdaptersArgs a, Wor
     }
 }
 
-// out = y + scale u B^T of a tile, blocks of 64 outputs to a wavefront.  u lies in LDS as the second operands' registers, 32 ranks
-// to an instruction, hi and lo.  Row i of a first operand is output 16 (i / 4) + 4 j + i % 4 of the block in instruction j of four, so that a lane's results
-// of the four are 16 outputs of its row that follow each other.
-template <int TT, bool BF16, bool VEC>
-__global__ __launch_bounds__(TT == 1 ? THREADS : MANY_THREADS) void out_kernel(FqAdaptersArgs a, Work w)
-{
-    constexpr int THREADS = TT == 1 ? ::THREADS : MANY_THREADS, WAVES = THREADS / 64;
-    __shared__ int rows[TILE];
-    __shared__ float factor[16 * TT];
-    extern __shared__ u32x4 low[]; // [rank / 32][TT][2][64]
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
-    const Tile own = find_listed(w, rows);
-    const int slot = own.slot, count = own.count, rank = own.rank, N = a.set.N;
-    if (count == 0)
-        return;
-    const int first = blockIdx.y * WAVES + wave, stride = gridDim.y * WAVES, blocks = (N + 63) / 64;
-    if (rank == 0) {
-        if (a.out == a.y && a.out_stride == a.y_stride)
-            return;
-        for (int b = first; b < blocks; b += stride)
-            if (64 * b + lane < N)
-                for (int i = 0; i < count; i++)
-                    a.out[rows[i] * a.out_stride + 64 * b + lane] = a.y[rows[i] * a.y_stride + 64 * b + lane];
-        return;
-    }
-    const int chunks = (rank + 31) / 32;
-    const uint16_t *bp = a.set.b + slot * a.set.b_stride;
-    // What a block of 64 outputs needs from memory, asked for a block ahead: B of the first 64 ranks, and y.
-    struct Block {
-        u32x4 b[2][4], y[VEC ? TT : 1][2];
+// The last step: 64 outputs of 16 TT rows to a wavefront and turn, out = y + factor u B^T.  u lies in LDS as the first operands' registers, 32
+// ranks to an instruction, hi and lo: [rank / 32][TT][2][64].  Column c of instruction j of four is output 4 c + j, so that a lane's results of the four
+// are four outputs that follow each other, 128 bytes of a row to sixteen lanes.  B comes 32 ranks of 64 outputs at a time, through 4 KB of
+// LDS of the wavefront's own; that of the first 32 AHEAD ranks, and y, are asked for a turn ahead.
+template <int TT, int AHEAD, bool BF16, bool VEC>
+struct Out {
+    const FqAdaptersArgs &a;
+    const int *rows;
+    const float *factor;
+    const u32x4 *low;
+    u32x4 *mine; // [256]
+    const uint16_t *b;
+    int count, rank, chunks;
+    struct Turn {
+        u32x4 b[AHEAD][4];
+        uint2 y[VEC ? TT : 1][4];
     };
-    auto ask_b = [&](u32x4(&v)[4], int b, int c) {
-        const int r = 32 * c + 8 * g;
+
+    __device__ __forceinline__ void ask_b(u32x4 (&v)[4], int block, int c) const
+    {
+        const int lane = threadIdx.x & 63, r = 32 * c + 8 * (lane & 3);
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const int n = 64 * b + 16 * (col >> 2) + 4 * j + (col & 3);
-            v[j] = n < N && r < rank ? *(const u32x4 *)(bp + (size_t)n * a.set.rank + r) : u32x4{0, 0, 0, 0};
+        for (int i = 0; i < 4; i++) {
+            const int n = 64 * block + 16 * i + (lane >> 2);
+            v[i] = n < a.set.N && r < rank ? *(const u32x4 *)(b + (size_t)n * a.set.rank + r) : u32x4{0, 0, 0, 0};
         }
-    };
-    auto ask = [&](Block &k, int b) {
-        ask_b(k.b[0], b, 0);
-        if (chunks > 1)
-            ask_b(k.b[1], b, 1);
+    }
+
+    __device__ __forceinline__ void ask(Turn &k, int block) const
+    {
+        const int lane = threadIdx.x & 63, n = 64 * block + 4 * (lane & 15);
+        ask_b(k.b[0], block, 0);
+        if (AHEAD > 1 && chunks > 1)
+            ask_b(k.b[AHEAD - 1], block, 1);
         if (VEC) {
 #pragma unroll
             for (int t = 0; t < TT; t++)
 #pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    const int n = 64 * b + 16 * g + 8 * h;
-                    k.y[t][h] = 16 * t + col < count && n < N ? *(const u32x4 *)(a.y + rows[16 * t + col] * a.y_stride + n) : u32x4{0, 0, 0, 0};
+                for (int i = 0; i < 4; i++) {
+                    const int row = 16 * t + 4 * (lane >> 4) + i;
+                    k.y[t][i] = row < count && n < a.set.N ? *(const uint2 *)(a.y + rows[row] * a.y_stride + n) : make_uint2(0, 0);
                 }
         }
-    };
-    Block now, next;
-    if (first < blocks)
-        ask(now, first);
+    }
 
-    // u: as many threads to a row as its ranks take four at a time, up to 16; everything that a turn adds is asked for together
-    const int wide = rank <= 16 ? 4 : rank <= 32 ? 8 : 16, turn = THREADS / wide;
+    __device__ __forceinline__ void multiply(float4_t (&acc)[TT][4], u32x4 (&v)[4], int c) const
+    {
+        const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
+        if (rank & 7) { // (what lies behind a rank may be anything)
+            const int r = 32 * c + 8 * (lane & 3);
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint32_t mask = (r + 2 * i < rank ? 0xffffu : 0u) | (r + 2 * i + 1 < rank ? 0xffff0000u : 0u);
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    v[j][i] &= mask;
+            }
+        }
+        // piece g of output 4 col + j: place 64 j + 16 g + (col ^ (j + 4 g))
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int j = (lane >> 2) & 3, p = lane & 3;
+            mine[64 * j + 16 * p + ((4 * i + (lane >> 4)) ^ (j + 4 * p))] = v[i];
+        }
+        own_fence();
+        u32x4 bv[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+            bv[j] = mine[64 * j + 16 * g + (col ^ (j + 4 * g))];
+        own_fence();
+#pragma unroll
+        for (int t = 0; t < TT; t++) {
+            if (16 * t >= count)
+                break;
+            const u32x4 hi = low[(c * TT + t) * 128 + lane], lo = low[(c * TT + t) * 128 + 64 + lane];
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                acc[t][j] = mfma<BF16>(lo, bv[j], mfma<BF16>(hi, bv[j], acc[t][j]));
+        }
+    }
+
+    __device__ __forceinline__ void finish(const Turn &k, const float4_t (&acc)[TT][4], int block) const
+    {
+        const int lane = threadIdx.x & 63, n = 64 * block + 4 * (lane & 15);
+#pragma unroll
+        for (int t = 0; t < TT; t++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const int row = 16 * t + 4 * (lane >> 4) + i;
+                if (row >= count || n >= a.set.N)
+                    continue;
+                const float f = factor[row];
+                uint16_t *out = a.out + rows[row] * a.out_stride + n;
+                if (VEC) {
+                    const uint2 y = k.y[t][i];
+                    const uint16_t v0 = fq_from_float(fq_to_float((uint16_t)y.x, BF16) + f * acc[t][0][i], BF16);
+                    const uint16_t v1 = fq_from_float(fq_to_float((uint16_t)(y.x >> 16), BF16) + f * acc[t][1][i], BF16);
+                    const uint16_t v2 = fq_from_float(fq_to_float((uint16_t)y.y, BF16) + f * acc[t][2][i], BF16);
+                    const uint16_t v3 = fq_from_float(fq_to_float((uint16_t)(y.y >> 16), BF16) + f * acc[t][3][i], BF16);
+                    *(uint2 *)out = make_uint2(v0 | (uint32_t)v1 << 16, v2 | (uint32_t)v3 << 16);
+                } else {
+                    const uint16_t *y = a.y + rows[row] * a.y_stride + n;
+#pragma unroll
+                    for (int j = 0; j < 4; j++)
+                        if (n + j < a.set.N)
+                            out[j] = fq_from_float(fq_to_float(y[j], BF16) + f * acc[t][j][i], BF16);
+                }
+            }
+    }
+
+    // The blocks first, first + stride ...; `now`: what was asked for the first.
+    __device__ __forceinline__ void run(Turn &now, int first, int stride) const
+    {
+        const int blocks = (a.set.N + 63) / 64;
+        Turn next;
+        for (int block = first; block < blocks; block += stride) {
+            if (block + stride < blocks)
+                ask(next, block + stride);
+            float4_t acc[TT][4] = {};
+            multiply(acc, now.b[0], 0);
+            if (AHEAD > 1 && chunks > 1)
+                multiply(acc, now.b[AHEAD - 1], 1);
+            for (int c = AHEAD; c < chunks; c++) {
+                u32x4 v[4];
+                ask_b(v, block, c);
+                multiply(acc, v, c);
+            }
+            finish(now, acc, block);
+            now = next;
+        }
+    }
+};
+
+// Rows without an adapter: copied, where out is not y.
+__device__ __forceinline__ void copy_rows(const FqAdaptersArgs &a, const int *rows, int count, int first, int stride)
+{
+    if (a.out == a.y && a.out_stride == a.y_stride)
+        return;
+    for (int n = 64 * first + (threadIdx.x & 63); n < a.set.N; n += 64 * stride)
+        for (int i = 0; i < count; i++)
+            a.out[rows[i] * a.out_stride + n] = a.y[rows[i] * a.y_stride + n];
+}
+
+// Four ranks r .. r + 3 of row `row` of u as hi and lo into the operands.  `e`: the row's power of two.
+template <int TT, bool BF16>
+__device__ __forceinline__ void put_low(u32x4 *low, const float4_t u, int e, int row, int r)
+{
+    uint16_t hi[4], lo[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const float v = BF16 ? u[i] : ldexpf(u[i], e);
+        hi[i] = fq_from_float(v, BF16);
+        const float rest = v - fq_to_float(hi[i], BF16);
+        lo[i] = fabsf(rest) < INFINITY ? fq_from_float(rest, BF16) : 0; // (not where hi is infinite or NaN)
+    }
+    // operand: lane row % 16 + 16 (rank % 32 / 8), its 8 ranks
+    uint2 *at = (uint2 *)&low[((r >> 5) * TT + (row >> 4)) * 128 + (row & 15) + 16 * ((r & 31) >> 3)] + ((r & 7) >> 2);
+    at[0] = make_uint2(hi[0] | (uint32_t)hi[1] << 16, hi[2] | (uint32_t)hi[3] << 16);
+    at[128] = make_uint2(lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16);
+}
+
+// binary16: the row's largest finite number becomes 2^13 to 2^14 (a power of two changes no digit)
+template <bool BF16>
+__device__ __forceinline__ int power_of(float most)
+{
+    return BF16 || most == 0.0f ? 0 : min(max(14 - __builtin_amdgcn_frexp_expf(most), -126), 126);
+}
+
+__device__ __forceinline__ float finite(const float4_t v)
+{
+    float most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        most = fmaxf(most, fabsf(v[i]) < INFINITY ? fabsf(v[i]) : 0.0f);
+    return most;
+}
+
+// out = y + scale u B^T of a tile, u in parts.
+template <bool BF16, bool VEC>
+__global__ __launch_bounds__(OUT_THREADS) void out_kernel(FqAdaptersArgs a, Work w)
+{
+    constexpr int TT = TILE / 16, WAVES = OUT_THREADS / 64;
+    __shared__ int rows[TILE];
+    __shared__ float factor[TILE];
+    __shared__ u32x4 b_of[WAVES][256];
+    extern __shared__ u32x4 low[]; // [rank / 32][TT][2][64]
+    const int tid = threadIdx.x, wave = tid >> 6;
+    const Tile own = find_listed(w, rows);
+    const int count = own.count, rank = own.rank;
+    if (count == 0)
+        return;
+    const int first = blockIdx.y * WAVES + wave, stride = gridDim.y * WAVES;
+    if (rank == 0)
+        return copy_rows(a, rows, count, first, stride);
+    const Out<TT, 2, BF16, VEC> o{a, rows, factor, low, b_of[wave], a.set.b + own.slot * a.set.b_stride, count, rank, (rank + 31) / 32};
+    typename Out<TT, 2, BF16, VEC>::Turn now;
+    if (64 * first < a.set.N)
+        o.ask(now, first);
+
+    // as many threads to a row as its ranks, or those of whole instructions, take four at a time, up to 16; what a turn adds is asked for together
+    const int wide = rank <= 32 ? 8 : 16, turn = OUT_THREADS / wide, mine = 4 * (tid & (wide - 1));
     const size_t apart = (size_t)a.M * a.set.rank;
-    for (int row = tid / wide; row < 16 * TT; row += turn) {
+    for (int row = tid / wide; row < TILE; row += turn) {
         const float *from = w.low + (size_t)rows[row < count ? row : 0] * a.set.rank;
         float4_t u[FQ_MAX_ADAPTER_RANK / 64];
         float most = 0.0f;
 #pragma unroll
         for (int c = 0; c < FQ_MAX_ADAPTER_RANK / 64; c++) {
-            const int r = 64 * c + 4 * (tid & (wide - 1));
+            const int r = 64 * c + mine;
             u[c] = float4_t{0, 0, 0, 0};
             if (64 * c < rank && r < rank) {
                 for (int p0 = 0; p0 < w.parts; p0 += 8) {
@@ -543,122 +604,170 @@ __global__ __launch_bounds__(TT == 1 ? THREADS : MANY_THREADS) void out_kernel(F
                             u[c] += part[p];
                 }
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
+                for (int i = 0; i < 4; i++)
                     u[c][i] = r + i < rank ? u[c][i] : 0.0f;
-                    most = fmaxf(most, fabsf(u[c][i]) < INFINITY ? fabsf(u[c][i]) : 0.0f);
-                }
+                most = fmaxf(most, finite(u[c]));
             }
         }
         for (int off = wide / 2; off >= 1; off >>= 1)
             most = fmaxf(most, __shfl_xor(most, off, 64));
-        // binary16: the row's largest becomes 2^13 to 2^14 (a power of two changes no digit)
-        const int e = BF16 || most == 0.0f ? 0 : min(max(14 - __builtin_amdgcn_frexp_expf(most), -126), 126);
-        if ((tid & (wide - 1)) == 0)
+        const int e = power_of<BF16>(most);
+        if (mine == 0)
             factor[row] = ldexpf(own.scale, -e);
 #pragma unroll
-        for (int c = 0; c < FQ_MAX_ADAPTER_RANK / 64; c++) {
-            const int r = 64 * c + 4 * (tid & (wide - 1));
-            if (64 * c < rank && r < 32 * chunks) {
-                uint16_t hi[4], lo[4];
-#pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const float v = BF16 ? u[c][i] : ldexpf(u[c][i], e);
-                    hi[i] = fq_from_float(v, BF16);
-                    const float rest = v - fq_to_float(hi[i], BF16);
-                    lo[i] = fabsf(rest) < INFINITY ? fq_from_float(rest, BF16) : 0; // (not where hi is infinite or NaN)
-                }
-                // operand: lane col + 16 (rank % 32 / 8), its 8 ranks
-                uint2 *at = (uint2 *)&low[((r >> 5) * TT + (row >> 4)) * 128 + (row & 15) + 16 * ((r & 31) >> 3)];
-                at[(r & 7) >> 2] = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
-                at[128 + ((r & 7) >> 2)] = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
-                if (wide == 4 && rank <= 16) { // ranks 16 to 31 of the instruction
-                    at[64 + ((r & 7) >> 2)] = make_uint2(0, 0);
-                    at[128 + 64 + ((r & 7) >> 2)] = make_uint2(0, 0);
-                }
-            }
-        }
+        for (int c = 0; c < FQ_MAX_ADAPTER_RANK / 64; c++)
+            if (64 * c < rank && 64 * c + mine < 32 * o.chunks)
+                put_low<TT, BF16>(low, u[c], e, row, 64 * c + mine);
     }
     __syncthreads();
-    for (int b = first; b < blocks; b += stride) {
-        if (b + stride < blocks)
-            ask(next, b + stride);
-        float4_t acc[TT][4] = {};
-        auto multiply = [&](u32x4(&bv)[4], int c) {
-            if (rank & 7) { // (what lies behind a rank may be anything)
-                const int r = 32 * c + 8 * g;
+    o.run(now, first, stride);
+}
+
+// Few rows, one launch: the tile that row blockIdx.x leads (the rows of its slot before it fill whole tiles), the outputs that are blockIdx.y's.  A
+// wavefront forms u over pieces of K of its own, 128 / RT at a time, two asked for ahead, through LDS of its own (a row's piece p at p ^ row, or p ^ row /
+// 2 where a row is 64 bytes); the sums of the eight meet there.  LDS for two workgroups to a compute unit: rows that lead no tile have one, too.
+template <int RT, bool BF16, bool VEC>
+__global__ __launch_bounds__(OUT_THREADS, 4) void few_kernel(FqAdaptersArgs a)
+{
+    constexpr int WAVES = OUT_THREADS / 64, PIECES = 16 / RT, LANES = 64 / PIECES, A_TURNS = 16 * RT / LANES, X_TURNS = 16 / LANES;
+    constexpr int OWN = (16 + 16 * RT) * PIECES, CHUNKS = (RT + 1) / 2;
+    __shared__ int rows[FEW_TILE];
+    __shared__ float factor[FEW_TILE];
+    __shared__ u32x4 low[CHUNKS * 128];
+    __shared__ u32x4 lds[WAVES][OWN > 256 ? OWN : 256];
+    static_assert(RT * 64 <= OWN, "the sums of a wavefront");
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
+    // (ranks and scales of the first slots beside the rows' slots: one trip to memory fewer)
+    const int some_rank = a.set.ranks ? a.set.ranks[min(lane, a.set.slots - 1)] : 0;
+    const float some_scale = a.set.scales ? a.set.scales[min(lane, a.set.slots - 1)] : 0.0f;
+    const int found = lane < a.M ? slot_of(a, lane) : -2, lead = blockIdx.x;
+    const int slot = __shfl(found, lead, 64);
+    const uint64_t same = __ballot(found == slot);
+    const int before = __popcll(same & ((1ull << lead) - 1)), at = __popcll(same & ((1ull << lane) - 1)) - before;
+    if (before % FEW_TILE != 0)
+        return;
+    const int count = min((int)__popcll(same) - before, FEW_TILE);
+    if (wave == 0 && found == slot && at >= 0 && at < FEW_TILE)
+        rows[at] = lane;
+    int rank = slot < 0 ? 0 : a.set.rank;
+    float scale = 1.0f;
+    if (slot >= 0 && a.set.ranks)
+        rank = min(max(slot < 64 ? __shfl(some_rank, slot, 64) : a.set.ranks[slot], 0), a.set.rank);
+    if (slot >= 0 && a.set.scales)
+        scale = slot < 64 ? __shfl(some_scale, slot, 64) : a.set.scales[slot];
+    __syncthreads();
+    const int first = blockIdx.y * WAVES + wave, stride = gridDim.y * WAVES;
+    if (rank == 0)
+        return copy_rows(a, rows, count, first, stride);
+    const int K = a.set.K, piece = lane % PIECES, row0 = lane / PIECES;
+    const uint16_t *ap = a.set.a + slot * a.set.a_stride + 8 * piece, *xp = a.x + 8 * piece;
+    struct Step {
+        u32x4 x[X_TURNS], a[A_TURNS];
+    };
+    auto ask = [&](Step &s, int k) {
+        const bool in = k + 8 * piece < K;
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const uint32_t mask = (r + 2 * i < rank ? 0xffffu : 0u) | (r + 2 * i + 1 < rank ? 0xffff0000u : 0u);
+        for (int i = 0; i < A_TURNS; i++)
+            s.a[i] = in && row0 + i * LANES < rank ? *(const u32x4 *)(ap + (size_t)(row0 + i * LANES) * K + k) : u32x4{0, 0, 0, 0};
 #pragma unroll
-                    for (int j = 0; j < 4; j++)
-                        bv[j][i] &= mask;
-                }
-            }
+        for (int i = 0; i < X_TURNS; i++)
+            s.x[i] = in && row0 + i * LANES < count ? *(const u32x4 *)(xp + rows[row0 + i * LANES] * a.x_stride + k) : u32x4{0, 0, 0, 0};
+    };
+    auto place = [&](int row, int p) -> u32x4 & {
+        return lds[wave][row * PIECES + (p ^ ((PIECES >= 8 ? row : row >> 1) & (PIECES - 1)))];
+    };
+    float4_t acc[RT] = {};
+    constexpr int STEP = 8 * PIECES, APART = STEP * WAVES;
+    auto use = [&](Step &s, int k) {
 #pragma unroll
-            for (int t = 0; t < TT; t++) {
-                const u32x4 hi = low[(c * TT + t) * 128 + lane], lo = low[(c * TT + t) * 128 + 64 + lane];
+        for (int i = 0; i < A_TURNS; i++)
+            place(16 + row0 + i * LANES, piece) = s.a[i];
 #pragma unroll
-                for (int j = 0; j < 4; j++)
-                    acc[t][j] = mfma<BF16>(bv[j], lo, mfma<BF16>(bv[j], hi, acc[t][j]));
-            }
-        };
-        multiply(now.b[0], 0);
-        if (chunks > 1)
-            multiply(now.b[1], 1);
-        for (int c = 2; c < chunks; c++) {
-            u32x4 bv[4];
-            ask_b(bv, b, c);
-            multiply(bv, c);
+        for (int i = 0; i < X_TURNS; i++)
+            place(row0 + i * LANES, piece) = s.x[i];
+        own_fence();
+        if (k + 2 * APART < K)
+            ask(s, k + 2 * APART);
+#pragma unroll
+        for (int h = 0; h < PIECES / 4; h++) {
+            const u32x4 x = place(col, 4 * h + g);
+#pragma unroll
+            for (int r = 0; r < RT; r++)
+                acc[r] = mfma<BF16>(place(16 + 16 * r + col, 4 * h + g), x, acc[r]);
         }
-        const int n = 64 * b + 16 * g;
-#pragma unroll
-        for (int t = 0; t < TT; t++) {
-            if (16 * t + col >= count)
-                continue;
-            const long long m = rows[16 * t + col];
-            uint16_t *out = a.out + m * a.out_stride + n;
-            const float f = factor[16 * t + col];
-            if (VEC) {
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    if (n + 8 * h >= N)
-                        continue;
-                    u32x4 v = now.y[t][h];
-#pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        const float4_t s = acc[t][2 * h + i / 2];
-                        const uint16_t p = fq_from_float(fq_to_float((uint16_t)v[i], BF16) + f * s[2 * (i & 1)], BF16);
-                        const uint16_t q = fq_from_float(fq_to_float((uint16_t)(v[i] >> 16), BF16) + f * s[2 * (i & 1) + 1], BF16);
-                        v[i] = p | (uint32_t)q << 16;
-                    }
-                    *(u32x4 *)(out + 8 * h) = v;
-                }
-            } else {
-                const uint16_t *y = a.y + m * a.y_stride + n;
-#pragma unroll
-                for (int i = 0; i < 16; i++)
-                    if (n + i < N)
-                        out[i] = fq_from_float(fq_to_float(y[i], BF16) + f * acc[t][i >> 2][i & 3], BF16);
-            }
-        }
-        now = next;
+        own_fence();
+    };
+    Step even, odd;
+    int k = STEP * wave;
+    if (k < K)
+        ask(even, k);
+    if (k + APART < K)
+        ask(odd, k + APART);
+    for (; k < K; k += 2 * APART) {
+        use(even, k);
+        if (k + APART < K)
+            use(odd, k + APART);
     }
+    const Out<1, CHUNKS, BF16, VEC> o{a, rows, factor, low, lds[wave], a.set.b + slot * a.set.b_stride, count, rank, (rank + 31) / 32};
+    typename Out<1, CHUNKS, BF16, VEC>::Turn now;
+    if (64 * first < a.set.N)
+        o.ask(now, first);
+    // u[rank 16 r + 4 g + i][row col] of each wavefront
+#pragma unroll
+    for (int r = 0; r < RT; r++)
+        ((float4_t *)lds[wave])[64 * r + lane] = acc[r];
+    __syncthreads();
+    // four ranks to a thread, 8 RT threads (those of whole instructions) to a row
+    constexpr int WIDE = RT == 1 ? 8 : 4 * RT;
+    const int row = tid / WIDE, r = 4 * (tid % WIDE);
+    if (row < FEW_TILE) {
+        float4_t u = {0, 0, 0, 0};
+        if (r < rank) {
+#pragma unroll
+            for (int v = 0; v < WAVES; v++)
+                u += ((const float4_t *)lds[v])[64 * (r >> 4) + row + 16 * ((r & 15) >> 2)];
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                u[i] = r + i < rank ? u[i] : 0.0f;
+        }
+        float most = finite(u);
+#pragma unroll
+        for (int off = WIDE / 2; off >= 1; off >>= 1)
+            most = fmaxf(most, __shfl_xor(most, off, 64));
+        const int e = power_of<BF16>(most);
+        if (r == 0)
+            factor[row] = ldexpf(scale, -e);
+        put_low<1, BF16>(low, u, e, row, r);
+    }
+    __syncthreads();
+    o.run(now, first, stride);
+}
+
+template <bool BF16, bool VEC>
+hipError_t launch_few(const FqAdaptersArgs &a, hipStream_t stream)
+{
+    // outputs over as many workgroups as fill the chip if every row had a slot of its own, half of that at least
+    const int blocks = (a.set.N + 63) / 64, most = (blocks + OUT_THREADS / 64 - 1) / (OUT_THREADS / 64), room = (256 + a.M - 1) / a.M + 4;
+    const dim3 grid(a.M, most < room ? most : room);
+    if (a.set.rank <= 16)
+        few_kernel<1, BF16, VEC><<<grid, OUT_THREADS, 0, stream>>>(a);
+    else if (a.set.rank <= 32)
+        few_kernel<2, BF16, VEC><<<grid, OUT_THREADS, 0, stream>>>(a);
+    else
+        few_kernel<4, BF16, VEC><<<grid, OUT_THREADS, 0, stream>>>(a);
+    return hipGetLastError();
 }
 
 template <int RT, bool BF16, Find FIND>
 void launch_low(const FqAdaptersArgs &a, const Work &w, hipStream_t stream)
 {
     const dim3 grid(w.max_tiles, w.parts, (a.set.rank + 16 * RT - 1) / (16 * RT));
-    if constexpr (FIND == ALONE)
-        low_few_kernel<RT, BF16><<<grid, THREADS, 0, stream>>>(a, w);
-    else
-        low_many_kernel<RT, BF16, FIND><<<grid, THREADS, 0, stream>>>(a, w);
+    low_kernel<RT, BF16, FIND><<<grid, THREADS, 0, stream>>>(a, w);
 }
 
-template <bool BF16, Find FIND>
-hipError_t launch(const FqAdaptersArgs &a, const Work &w, hipStream_t stream)
+template <bool BF16, bool VEC, Find FIND>
+hipError_t launch_many(const FqAdaptersArgs &a, const Work &w, hipStream_t stream)
 {
-    constexpr int TT = FIND == ALONE ? 1 : TILE / 16, threads = FIND == ALONE ? THREADS : MANY_THREADS;
     if (a.set.rank <= 16)
         launch_low<1, BF16, FIND>(a, w, stream);
     else if (a.set.rank <= 32)
@@ -667,20 +776,42 @@ hipError_t launch(const FqAdaptersArgs &a, const Work &w, hipStream_t stream)
         launch_low<4, BF16, FIND>(a, w, stream);
     if (hipError_t e = hipGetLastError())
         return e;
-    const bool vec = a.set.N % 8 == 0 && a.y_stride % 8 == 0 && a.out_stride % 8 == 0 && ((uintptr_t)a.y & 15) == 0 && ((uintptr_t)a.out & 15) == 0;
     // outputs over as many workgroups as fill the chip
-    const int blocks = (a.set.N + 63) / 64, tiles = TT == 1 ? a.M : (a.M + TILE - 1) / TILE;
-    const int most = (blocks + threads / 64 - 1) / (threads / 64), room = ((TT == 1 ? 512 : 256) + tiles - 1) / tiles;
+    const int blocks = (a.set.N + 63) / 64, tiles = (a.M + TILE - 1) / TILE;
+    const int most = (blocks + OUT_THREADS / 64 - 1) / (OUT_THREADS / 64), room = (256 + tiles - 1) / tiles;
     const dim3 grid(w.max_tiles, most < room ? most : room);
-    const size_t lds = (size_t)(a.set.rank + 31) / 32 * TT * 2 * 64 * sizeof(u32x4);
-    const void *func = vec ? (const void *)out_kernel<TT, BF16, true> : (const void *)out_kernel<TT, BF16, false>;
-    if (hipError_t e = fq_raise_dynamic_lds(func, lds))
-        return e;
-    if (vec)
-        out_kernel<TT, BF16, true><<<grid, threads, lds, stream>>>(a, w);
-    else
-        out_kernel<TT, BF16, false><<<grid, threads, lds, stream>>>(a, w);
+    const size_t lds = (size_t)(a.set.rank + 31) / 32 * (TILE / 16) * 2 * 64 * sizeof(u32x4);
+    if (lds > 16384)
+        if (hipError_t e = fq_raise_dynamic_lds((const void *)out_kernel<BF16, VEC>, lds))
+            return e;
+    out_kernel<BF16, VEC><<<grid, OUT_THREADS, lds, stream>>>(a, w);
     return hipGetLastError();
+}
+
+template <bool BF16, bool VEC>
+hipError_t launch(const FqAdaptersArgs &a, void *workspace, hipStream_t stream)
+{
+    if (few(a.set, a.M))
+        return launch_few<BF16, VEC>(a, stream);
+    Work w{};
+    w.parts = parts_of(a.set, a.M);
+    w.max_tiles = tiles_of(a.set, a.M);
+    char *at = (char *)workspace;
+    w.low = (float *)at;
+    at += up(low_rows(a.M) * a.set.rank * sizeof(float));
+    w.rows = (int *)at;
+    at += up((size_t)w.max_tiles * TILE * sizeof(int));
+    w.tiles = (Tile *)at;
+    if (a.M <= MIDDLE_ROWS && a.set.slots <= MIDDLE_SLOTS)
+        return launch_many<BF16, VEC, COUNTED>(a, w, stream);
+    const size_t lds = (a.set.slots + 1) * sizeof(int);
+    if (lds > 32768)
+        if (hipError_t e = fq_raise_dynamic_lds((const void *)group_kernel, lds))
+            return e;
+    group_kernel<<<1, GROUP_THREADS, lds, stream>>>(a, w);
+    if (hipError_t e = hipGetLastError())
+        return e;
+    return launch_many<BF16, VEC, LISTED>(a, w, stream);
 }
 
 } // namespace
@@ -693,24 +824,9 @@ size_t fq_adapters_bytes(const FqAdaptersView &set, int M)
 
 hipError_t fq_launch_adapters(const FqAdaptersArgs &a, void *workspace, hipStream_t stream)
 {
-    Work w{};
-    w.parts = parts_of(a.set, a.M);
-    w.max_tiles = tiles_of(a.set, a.M);
-    char *at = (char *)workspace;
-    w.low = (float *)at;
-    at += up(low_rows(a.M) * a.set.rank * sizeof(float));
-    w.rows = (int *)at;
-    at += up((size_t)w.max_tiles * TILE * sizeof(int));
-    w.tiles = (Tile *)at;
-    if (a.M <= SMALL_ROWS)
-        return a.set.bf16 ? launch<true, ALONE>(a, w, stream) : launch<false, ALONE>(a, w, stream);
-    if (a.M <= MIDDLE_ROWS && a.set.slots <= MIDDLE_SLOTS)
-        return a.set.bf16 ? launch<true, COUNTED>(a, w, stream) : launch<false, COUNTED>(a, w, stream);
-    const size_t lds = (a.set.slots + 1) * sizeof(int);
-    if (hipError_t e = fq_raise_dynamic_lds((const void *)group_kernel, lds))
-        return e;
-    group_kernel<<<1, GROUP_THREADS, lds, stream>>>(a, w);
-    if (hipError_t e = hipGetLastError())
-        return e;
-    return a.set.bf16 ? launch<true, LISTED>(a, w, stream) : launch<false, LISTED>(a, w, stream);
+    // four outputs of a row at a time
+    const bool vec = a.set.N % 4 == 0 && a.y_stride % 4 == 0 && a.out_stride % 4 == 0 && ((uintptr_t)a.y & 7) == 0 && ((uintptr_t)a.out & 7) == 0;
+    if (a.set.bf16)
+        return vec ? launch<true, true>(a, workspace, stream) : launch<true, false>(a, workspace, stream);
+    return vec ? launch<false, true>(a, workspace, stream) : launch<false, false>(a, workspace, stream);
 }
