@@ -1,6 +1,14 @@
-// Log probabilities of given tokens, the entropy and the likeliest tokens of rows of logits.
+// Log probabilities of given tokens, the entropy and the likeliest tokens of rows of logits, one pass over them.
 //
-// A workgroup takes a row: its largest logit, then the sums beside that one's weight of 1, then one alternative after the other.
+// With m the largest logit, s = sum of e^(l - m) over all others and t = sum of e^(l - m) (l - m):
+//   ln p_i = (l_i - m) - log1p(s),   H = log1p(s) - t / (1 + s)
+// -- the largest one's own 1 stays out of the sums, so that a nearly certain token keeps its digits.  A workgroup takes a row (a piece of one, where few
+// rows are long).  Its wavefronts stream it in 16-byte loads; each keeps a running maximum that all its lanes share, so that a raise is a branch which
+// it takes a few times in a row, and whose new largest logit is taken out of the lane that has it.  On the way the largest logit of every block of 64 goes
+// to LDS.  The n likeliest tokens lie in the n blocks whose largest come first in the order (larger logit, smaller index): any token of another
+// block comes behind the largest of each of them.  So the blocks' maxima are cut at about the n-th by a histogram over their bits, the
+// few blocks above are read again (from a cache), and the tokens there that reach the cut, some more than n, are ranked against each other.  Equal
+// logits by the thousand, or all the best in one place, cost more rounds of the histogram, not another result.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -9,109 +17,547 @@
 
 namespace {
 
-constexpr int THREADS = 256;
+constexpr int BLOCK = 64, MAX_BLOCKS = 2048; // logits; a row of more takes blocks twice, four times ... as large
+constexpr int BINS = 256, LIST = 256, MAX_CHOSEN = 128;
+constexpr int SPLIT_ROWS = 64, MAX_PIECES = 64;
+constexpr uint32_t LOWEST = 0x007fffffu; // the key of -inf
 
-struct Best {
-    float x;
-    int i; // V: none
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// Larger for larger numbers, equal for -0 and 0; a NaN is as -inf.
+__device__ __forceinline__ uint32_t key_of(float x)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, fmaxf(x, -INFINITY) + 0.0f);
+    return (u >> 31) ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float of_key(uint32_t k) { return __builtin_bit_cast(float, (k >> 31) ? k & 0x7fffffffu : ~k); }
+
+template <typename T>
+struct Row {
+    static constexpr int PER = 16 / sizeof(T); // logits to a 16-byte load
+    const T *at;  // the row
+    const T *from; // the 16-byte boundary before it
+    unsigned shift, V;
+
+    __device__ __forceinline__ Row(const FqLogprobsArgs &a, long long r) : at((const T *)a.logits + r * a.row_stride), V(a.V)
+    {
+        shift = (unsigned)((uintptr_t)at & 15) / sizeof(T);
+        from = at - shift;
+    }
+    __device__ __forceinline__ unsigned loads() const { return (shift + V + PER - 1) / PER; }
+    __device__ __forceinline__ float operator[](unsigned i) const { return (float)at[i]; }
 };
 
-__device__ __forceinline__ Best better(Best a, Best b) { return b.x > a.x || (b.x == a.x && b.i < a.i) ? b : a; }
-
-__device__ Best block_best(Best v, Best *s)
+template <typename T>
+__device__ __forceinline__ void widen(const u32x4 v, float (&x)[16 / sizeof(T)])
 {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const uint32_t u = v[i]; // (a bit cast of v[i] itself takes the vector's first element)
+            x[i] = __builtin_bit_cast(float, u);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            x[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)(v[i / 2] >> 16 * (i & 1)));
+    }
+}
+
+// Element e of a load becomes -inf.
+template <typename T>
+__device__ __forceinline__ void blank(u32x4 &v, int e)
+{
+    if constexpr (sizeof(T) == 4)
+        v[e] = 0xff800000u;
+    else
+        v[e / 2] = e & 1 ? (v[e / 2] & 0xffffu) | 0xfc000000u : (v[e / 2] & 0xffff0000u) | 0xfc00u;
+}
+
+// The largest of a group of 8 or 16 lanes, in all of them.
+template <int LANES>
+__device__ __forceinline__ float group_max(float x)
+{
+    auto step = [](float v, auto ctrl) {
+        const int t = __builtin_bit_cast(int, v);
+        return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(t, t, decltype(ctrl)::value, 0xf, 0xf, false)));
+    };
+    x = step(x, std::integral_constant<int, 0xb1>());  // quad_perm 1, 0, 3, 2
+    x = step(x, std::integral_constant<int, 0x4e>());  // quad_perm 2, 3, 0, 1
+    x = step(x, std::integral_constant<int, 0x141>()); // half a row mirrored
+    if (LANES == 16)
+        x = step(x, std::integral_constant<int, 0x140>()); // a row mirrored
+    return x;
+}
+
+__device__ __forceinline__ float lane_of(float x, int lane)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+}
+
+__device__ __forceinline__ double wave_sum(double v)
+{
+#pragma unroll
     for (int off = 32; off >= 1; off >>= 1)
-        v = better(v, Best{__shfl_xor(v.x, off, 64), __shfl_xor(v.i, off, 64)});
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0)
-        s[threadIdx.x >> 6] = v;
-    __syncthreads();
-    for (int w = 0; w < THREADS / 64; w++)
-        v = better(v, s[w]);
+        v += __shfl_xor(v, off, 64);
     return v;
 }
 
-__device__ double block_sum(double v, double *s)
+// A part of a row: its largest logit, the sums beside that one's weight.
+struct Part {
+    float m;
+    double s, t;
+};
+
+struct Work {
+    uint32_t *keys; // [row][MAX_BLOCKS]
+    Part *parts;    // [row][pieces]
+    int pieces, shift; // shift: blocks of BLOCK << shift logits
+    unsigned piece; // loads to a piece
+};
+
+// Parts i = 0 .. n - 1 as one, in every thread, in one order.
+template <typename Get>
+__device__ __forceinline__ Part join(int n, const Get &get)
 {
-    for (int off = 32; off >= 1; off >>= 1)
-        v += __shfl_xor(v, off, 64);
+    Part all{-INFINITY, 0.0, 0.0};
+    for (int i = 0; i < n; i++) {
+        const Part p = get(i);
+        if (!(p.m > -INFINITY))
+            continue;
+        if (p.m > all.m) { // (what was there gets its largest one's 1 back)
+            const double d = (double)all.m - (double)p.m, c = all.m > -INFINITY && p.m < INFINITY ? exp(d) : 0.0;
+            const double s = c > 0.0 ? c * (all.s + 1.0) : 0.0, t = c > 0.0 ? c * (all.t + d * (all.s + 1.0)) : 0.0;
+            all = Part{p.m, p.s + s, p.t + t};
+        } else {
+            const double d = (double)p.m - (double)all.m, c = all.m < INFINITY ? exp(d) : 0.0;
+            all.s += c > 0.0 ? c * (p.s + 1.0) : 0.0;
+            all.t += c > 0.0 ? c * (p.t + d * (p.s + 1.0)) : 0.0;
+        }
+    }
+    return all;
+}
+
+// What a workgroup needs in LDS.
+template <int THREADS>
+struct Shared {
+    uint32_t keys[MAX_BLOCKS];
+    Part parts[THREADS / 64];
+    uint64_t list[LIST];
+    int chosen[MAX_CHOSEN];
+    int bins[BINS];
+    int found[4];
+};
+
+// The loads [begin, end) of a row through the workgroup: parts of the wavefronts and the blocks' maxima, from block `first` on, into `sh`.
+template <typename T, int THREADS, int AHEAD>
+__device__ __forceinline__ void stream(const Row<T> &row, unsigned begin, unsigned end, int block_shift, unsigned first, Shared<THREADS> &sh)
+{
+    constexpr int PER = Row<T>::PER, LANES = BLOCK / PER; // lanes of a block
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const unsigned whole = (row.shift + row.V) / PER; // the loads before are whole, but for the first
+    float m = -INFINITY, s = 0.0f, t = 0.0f;
+    auto turn = [&](unsigned base, auto edge) {
+        constexpr bool EDGE = decltype(edge)::value;
+        u32x4 v[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; j++) {
+            const unsigned g = base + 64 * j + lane;
+            if (!EDGE || g < end)
+                v[j] = __builtin_nontemporal_load((const u32x4 *)row.from + g);
+        }
+        if (EDGE) {
+#pragma unroll
+            for (int j = 0; j < AHEAD; j++) {
+                const unsigned g = base + 64 * j + lane;
+#pragma unroll
+                for (int e = 0; e < PER; e++)
+                    if (g >= end || g * PER + e < row.shift || g * PER + e >= row.shift + row.V)
+                        blank<T>(v[j], e);
+            }
+        }
+        float most[AHEAD], top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < AHEAD; j++) {
+            float x[PER];
+            widen<T>(v[j], x);
+            most[j] = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < PER; e++)
+                most[j] = fmaxf(most[j], x[e]);
+            const float b = group_max<LANES>(most[j]);
+            top = fmaxf(top, b);
+            const unsigned g = base + 64 * j + lane;
+            if ((lane & (LANES - 1)) == 0 && (!EDGE || g < end)) {
+                const unsigned block = (g * PER / BLOCK >> block_shift) - first;
+                if (block_shift == 0)
+                    sh.keys[block] = key_of(b);
+                else
+                    atomicMax(&sh.keys[block], key_of(b));
+            }
+        }
+        top = group_max<16>(top);
+        top = fmaxf(fmaxf(lane_of(top, 0), lane_of(top, 16)), fmaxf(lane_of(top, 32), lane_of(top, 48)));
+        if (top > m) {
+            const float d = m - top, c = __expf(d);
+            t = c > 0.0f ? c * (t + d * s) : 0.0f;
+            s *= c;
+            if (lane == 0 && c > 0.0f) { // the old largest one's 1
+                s += c;
+                t += c * d;
+            }
+            m = top;
+            bool looking = true; // the new one's is left out: one lane's first
+#pragma unroll
+            for (int j = 0; j < AHEAD; j++) {
+                const uint64_t has = __ballot(most[j] == top);
+                if (looking && has) {
+                    looking = false;
+                    if (lane == __ffsll((unsigned long long)has) - 1) {
+                        float x[PER];
+                        widen<T>(v[j], x);
+                        bool mine = true;
+#pragma unroll
+                        for (int e = 0; e < PER; e++)
+                            if (mine && x[e] == top) {
+                                mine = false;
+                                blank<T>(v[j], e);
+                            }
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; j++) {
+            float x[PER], w[PER], turned = 0.0f;
+            widen<T>(v[j], x);
+#pragma unroll
+            for (int e = 0; e < PER; e++) {
+                const float d = fmaxf(x[e] - m, -200.0f); // (-inf, NaN and what is not there: no weight)
+                w[e] = __expf(d);
+                turned += w[e] * d;
+            }
+#pragma unroll
+            for (int e = PER / 2; e >= 1; e /= 2)
+#pragma unroll
+                for (int i = 0; i < e; i++)
+                    w[i] += w[i + e];
+            s += w[0];
+            t += turned;
+        }
+    };
+    constexpr unsigned STEP = 64 * AHEAD, STRIDE = STEP * (THREADS / 64);
+    for (unsigned base = begin + wave * STEP; base < end; base += STRIDE) {
+        if ((base == 0 && row.shift) || base + STEP > whole || base + STEP > end)
+            turn(base, std::true_type());
+        else
+            turn(base, std::false_type());
+    }
+    const double all_s = wave_sum((double)s), all_t = wave_sum((double)t);
+    if (lane == 0)
+        sh.parts[wave] = Part{m, all_s, all_t};
+}
+
+// The cut of items (key, index) at about the n-th of the order (larger key, smaller index): at least n of them, or all, lie at or above it, at most `cap`
+// unless that is n.  each(f) calls f(key, index) for a thread's items.  Keys under `low` do not count.
+struct Cut {
+    uint32_t key, turned; // kept: a larger key, or this one with ~index >= turned
+    __device__ __forceinline__ bool keeps(uint32_t k, uint32_t index) const { return k > key || (k == key && ~index >= turned); }
+};
+
+template <int THREADS, typename Each>
+__device__ __forceinline__ Cut find_cut(int n, int cap, uint32_t low, uint32_t high, uint32_t last_index, Shared<THREADS> &sh, const Each &each)
+{
+    const int tid = threadIdx.x, lane = tid & 63;
+    uint32_t tie = 0;
+    bool tied = false; // by index among equal keys
+    int above = 0;
+    for (;;) {
+        const int bits = 32 - __clz((int)(high - low)), shift = high == low || bits < 8 ? 0 : bits - 8;
+        for (int i = tid; i < BINS; i += THREADS)
+            sh.bins[i] = 0;
+        __syncthreads();
+        each([&](uint32_t key, uint32_t index) {
+            const uint32_t field = tied ? ~index : key;
+            if ((!tied || key == tie) && field >= low && field <= high)
+                atomicAdd(&sh.bins[(field - low) >> shift], 1);
+        });
+        __syncthreads();
+        if (tid < 64) { // the highest bin from which on there are enough
+            int own[4], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                own[i] = sh.bins[4 * (63 - lane) + 3 - i]; // from the top
+                sum += own[i];
+            }
+            int upto = sum;
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) {
+                const int o = __shfl_up(upto, off, 64);
+                upto += lane >= off ? o : 0;
+            }
+            int before = above + upto - sum;
+            const bool here = before < n && above + upto >= n;
+            int bin = 0, count = above + upto, under = before;
+            bool open = true;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                if (open && before + own[i] >= n) {
+                    open = false;
+                    bin = 4 * (63 - lane) + 3 - i;
+                    under = before;
+                    count = before + own[i];
+                }
+                before += own[i];
+            }
+            const uint64_t one = __ballot(here);
+            if (one ? here : lane == 63) { // (fewer than n in all: everything)
+                sh.found[0] = one ? bin : 0;
+                sh.found[1] = count;
+                sh.found[2] = under;
+            }
+        }
+        __syncthreads();
+        const int bin = sh.found[0], count = sh.found[1];
+        const uint32_t edge = low + ((uint32_t)bin << shift);
+        if (count <= cap || count <= n || (shift == 0 && tied))
+            return tied ? Cut{tie, edge} : Cut{edge, 0};
+        above = sh.found[2];
+        if (shift == 0) {
+            tied = true;
+            tie = edge;
+            low = ~last_index;
+            high = ~0u;
+        } else {
+            low = edge;
+            if (high - edge > (1u << shift) - 1)
+                high = edge + ((1u << shift) - 1);
+        }
+        __syncthreads();
+    }
+}
+
+// Everything that comes after a row's logits were streamed.
+template <typename T, int THREADS>
+__device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, const Row<T> &row, Part all, int block_shift, Shared<THREADS> &sh)
+{
+    const int tid = threadIdx.x;
+    const bool none = all.m == -INFINITY, infinite = all.m == INFINITY;
+    if (infinite) { // weights of 1 for these alone
+        int count = 0;
+        for (unsigned i = tid; i < row.V; i += THREADS)
+            count += row[i] == INFINITY;
+        if (tid == 0)
+            sh.found[3] = 0;
+        __syncthreads();
+        if (count)
+            atomicAdd(&sh.found[3], count);
+        __syncthreads();
+        all.s = sh.found[3] - 1.0;
+        all.t = 0.0;
+        __syncthreads();
+    }
+    const double log_sum = none ? 0.0 : log1p(all.s);
+    auto logprob = [&](float x) {
+        if (none || !(x > -INFINITY) || (infinite && x < INFINITY))
+            return -INFINITY;
+        return infinite ? (float)-log_sum : (float)((double)x - (double)all.m - log_sum);
+    };
+    if (a.entropy && tid == 0)
+        a.entropy[r] = none ? 0.0f : (float)(log_sum - all.t / (1.0 + all.s));
+    for (int j = tid; j < a.n_given; j += THREADS) {
+        const int i = a.given[r * a.n_given + j];
+        a.given_logprob[r * a.n_given + j] = i >= 0 && i < a.V ? logprob(row[i]) : -INFINITY;
+    }
+    const int n = a.top_n;
+    if (n == 0)
+        return;
+    const uint32_t high = key_of(all.m), low = infinite ? high : LOWEST + 1;
+    const int blocks = (int)(((row.shift + row.V + BLOCK - 1) / BLOCK + (1u << block_shift) - 1) >> block_shift);
+    const int cap = n > 32 ? MAX_CHOSEN : MAX_CHOSEN / 2;
+    if (tid == 0)
+        sh.found[3] = 0;
+    Cut cut{low - 1, ~0u}; // (nothing has an index of 0 under that key)
+    if (!none && blocks > cap) {
+        auto each = [&](const auto &f) {
+            for (int i = tid; i < blocks; i += THREADS)
+                f(sh.keys[i], (uint32_t)i);
+        };
+        cut = find_cut<THREADS>(n, cap, low, high, (uint32_t)blocks - 1, sh, each);
+    }
     __syncthreads();
-    if ((threadIdx.x & 63) == 0)
-        s[threadIdx.x >> 6] = v;
+    for (int i = tid; i < blocks; i += THREADS) {
+        const uint32_t k = sh.keys[i];
+        if (k >= low && cut.keeps(k, i)) {
+            const int at = atomicAdd(&sh.found[3], 1);
+            if (at < MAX_CHOSEN)
+                sh.chosen[at] = i;
+        }
+    }
     __syncthreads();
-    v = 0.0;
-    for (int w = 0; w < THREADS / 64; w++)
-        v += s[w];
-    return v;
+    const int chosen = none ? 0 : sh.found[3];
+    const uint32_t reach = cut.key > low ? cut.key : low; // (n tokens at least, or all, have such a key)
+    const int size = BLOCK << block_shift;
+    __syncthreads();
+    if (tid == 0)
+        sh.found[3] = 0;
+    __syncthreads();
+    auto each = [&](const auto &f) {
+        for (int i = tid; i < chosen * size; i += THREADS) {
+            const unsigned at = (unsigned)sh.chosen[i / size] * size + i % size;
+            if (at >= row.shift && at < row.shift + row.V)
+                f(key_of((float)row.from[at]), at - row.shift);
+        }
+    };
+    auto collect = [&](uint32_t key, uint32_t index) {
+        const int at = atomicAdd(&sh.found[3], 1);
+        if (at < LIST)
+            sh.list[at] = (uint64_t)key << 32 | (uint32_t)~index;
+    };
+    each([&](uint32_t key, uint32_t index) {
+        if (key >= reach)
+            collect(key, index);
+    });
+    __syncthreads();
+    if (sh.found[3] > LIST) { // more than that reach it: the cut among the tokens
+        __syncthreads();
+        const Cut c = find_cut<THREADS>(n, LIST, reach, high, row.V - 1, sh, each);
+        __syncthreads();
+        if (tid == 0)
+            sh.found[3] = 0;
+        __syncthreads();
+        each([&](uint32_t key, uint32_t index) {
+            if (key >= reach && c.keeps(key, index))
+                collect(key, index);
+        });
+        __syncthreads();
+    }
+    const int listed = min(sh.found[3], LIST);
+    for (int i = tid; i < listed; i += THREADS) {
+        const uint64_t own = sh.list[i];
+        int rank = 0;
+        for (int j = 0; j < listed; j++)
+            rank += sh.list[j] > own;
+        if (rank < n) {
+            a.top_token[r * n + rank] = (int32_t)~(uint32_t)own;
+            a.top_logprob[r * n + rank] = logprob(of_key((uint32_t)(own >> 32)));
+        }
+    }
+    for (int i = listed + tid; i < n; i += THREADS) {
+        a.top_token[r * n + i] = -1;
+        a.top_logprob[r * n + i] = -INFINITY;
+    }
+}
+
+template <typename T, int THREADS, int AHEAD>
+__global__ __launch_bounds__(THREADS) void row_kernel(FqLogprobsArgs a, int block_shift)
+{
+    __shared__ Shared<THREADS> sh;
+    for (long long r = blockIdx.x; r < a.R; r += gridDim.x) {
+        const Row<T> row(a, r);
+        if (block_shift) {
+            for (int i = threadIdx.x; i < MAX_BLOCKS; i += THREADS)
+                sh.keys[i] = 0;
+            __syncthreads();
+        }
+        stream<T, THREADS, AHEAD>(row, 0, row.loads(), block_shift, 0, sh);
+        __syncthreads();
+        const Part all = join(THREADS / 64, [&](int i) { return sh.parts[i]; });
+        finish<T, THREADS>(a, r, row, all, block_shift, sh);
+        __syncthreads();
+    }
+}
+
+// Few long rows: a workgroup takes a piece, a second launch joins them.
+template <typename T, int THREADS, int AHEAD>
+__global__ __launch_bounds__(THREADS) void piece_kernel(FqLogprobsArgs a, Work w)
+{
+    __shared__ Shared<THREADS> sh;
+    const int r = blockIdx.x / w.pieces, p = blockIdx.x % w.pieces;
+    const Row<T> row(a, r);
+    const unsigned begin = p * w.piece, loads = row.loads(), end = min(loads, begin + w.piece);
+    constexpr int PER = Row<T>::PER;
+    const unsigned first = begin * PER / BLOCK >> w.shift;
+    if (w.shift) {
+        for (int i = threadIdx.x; i < MAX_BLOCKS; i += THREADS)
+            sh.keys[i] = 0;
+        __syncthreads();
+    }
+    if (begin < end)
+        stream<T, THREADS, AHEAD>(row, begin, end, w.shift, first, sh);
+    else if ((threadIdx.x & 63) == 0)
+        sh.parts[threadIdx.x >> 6] = Part{-INFINITY, 0.0, 0.0};
+    __syncthreads();
+    if (begin < end) {
+        const unsigned blocks = (((end * PER + BLOCK - 1) / BLOCK + (1u << w.shift) - 1) >> w.shift) - first;
+        for (unsigned i = threadIdx.x; i < blocks; i += THREADS)
+            w.keys[(size_t)r * MAX_BLOCKS + first + i] = sh.keys[i];
+    }
+    const Part all = join(THREADS / 64, [&](int i) { return sh.parts[i]; });
+    if (threadIdx.x == 0)
+        w.parts[r * MAX_PIECES + p] = all;
+}
+
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void join_kernel(FqLogprobsArgs a, Work w)
+{
+    __shared__ Shared<THREADS> sh;
+    __shared__ Part parts[MAX_PIECES];
+    const int r = blockIdx.x;
+    const Row<T> row(a, r);
+    const int blocks = (int)(((row.shift + row.V + BLOCK - 1) / BLOCK + (1u << w.shift) - 1) >> w.shift);
+    for (int i = threadIdx.x; i < blocks; i += THREADS)
+        sh.keys[i] = w.keys[(size_t)r * MAX_BLOCKS + i];
+    if ((int)threadIdx.x < w.pieces)
+        parts[threadIdx.x] = w.parts[r * MAX_PIECES + threadIdx.x];
+    __syncthreads();
+    const Part all = join(w.pieces, [&](int i) { return parts[i]; });
+    finish<T, THREADS>(a, r, row, all, w.shift, sh);
 }
 
 template <typename T>
-__global__ __launch_bounds__(THREADS) void logprobs_kernel(FqLogprobsArgs a)
+hipError_t launch(const FqLogprobsArgs &a, void *workspace, hipStream_t stream)
 {
-    __shared__ Best s_best[THREADS / 64];
-    __shared__ double s_sum[THREADS / 64];
-    const int tid = threadIdx.x;
-    for (long long r = blockIdx.x; r < a.R; r += gridDim.x) {
-        const T *row = (const T *)a.logits + r * a.row_stride;
-        auto at = [&](int i) {
-            const float x = (float)row[i];
-            return x == x ? x : -INFINITY;
-        };
-        Best top{-INFINITY, a.V};
-        for (int i = tid; i < a.V; i += THREADS)
-            top = better(top, Best{at(i), i});
-        top = block_best(top, s_best);
-        const bool none = top.x == -INFINITY, infinite = top.x == INFINITY;
-        double rest = 0.0, turned = 0.0;
-        for (int i = tid; i < a.V; i += THREADS) {
-            const float x = at(i);
-            if (i == top.i || none || (infinite && x < INFINITY))
-                continue;
-            const float t = infinite ? 0.0f : x - top.x, w = expf(t);
-            rest += w;
-            turned += w > 0.0f ? (double)w * t : 0.0;
-        }
-        rest = block_sum(rest, s_sum);
-        turned = block_sum(turned, s_sum);
-        const double log_sum = log1p(rest);
-        auto logprob = [&](float x) {
-            return none || x == -INFINITY || (infinite && x < INFINITY) ? -INFINITY
-                   : infinite ? (float)-log_sum : (float)((double)x - (double)top.x - log_sum);
-        };
-        if (a.entropy && tid == 0)
-            a.entropy[r] = (float)(log_sum - turned / (1.0 + rest));
-        for (int j = tid; j < a.n_given; j += THREADS) {
-            const int i = a.given[r * a.n_given + j];
-            a.given_logprob[r * a.n_given + j] = i >= 0 && i < a.V ? logprob(at(i)) : -INFINITY;
-        }
-        Best last{INFINITY, -1};
-        for (int j = 0; j < a.top_n; j++) {
-            Best next{-INFINITY, a.V};
-            for (int i = tid; i < a.V; i += THREADS) {
-                const float x = at(i);
-                if (x < last.x || (x == last.x && i > last.i))
-                    next = better(next, Best{x, i});
-            }
-            last = block_best(next, s_best);
-            if (tid == 0) {
-                const bool found = last.x > -INFINITY && !(infinite && last.x < INFINITY);
-                a.top_token[r * a.top_n + j] = found ? last.i : -1;
-                a.top_logprob[r * a.top_n + j] = found ? logprob(last.x) : -INFINITY;
-            }
-        }
+    constexpr int PER = Row<T>::PER;
+    int shift = 0;
+    while (((long long)a.V + PER + BLOCK - 1) / BLOCK > (long long)MAX_BLOCKS << shift)
+        shift++;
+    const long long loads = ((long long)a.V + PER - 1) / PER + 1;
+    const int cus = fq_device_cus(), grid = a.R < (1 << 20) ? a.R : 1 << 20;
+    constexpr int AHEAD = 32 / PER, T2 = 512, UNIT = T2 * AHEAD;
+    if (a.R <= SPLIT_ROWS && loads > 8 * UNIT) {
+        Work w{};
+        const long long units = (loads + UNIT - 1) / UNIT;
+        long long pieces = 2 * cus / a.R;
+        pieces = pieces > MAX_PIECES ? MAX_PIECES : pieces < 1 ? 1 : pieces;
+        const long long each = (units + pieces - 1) / pieces;
+        w.pieces = (int)((units + each - 1) / each);
+        w.piece = (unsigned)(each * UNIT);
+        w.shift = shift;
+        w.parts = (Part *)workspace;
+        w.keys = (uint32_t *)((char *)workspace + sizeof(Part) * SPLIT_ROWS * MAX_PIECES);
+        piece_kernel<T, T2, AHEAD><<<a.R * w.pieces, T2, 0, stream>>>(a, w);
+        if (hipError_t e = hipGetLastError())
+            return e;
+        join_kernel<T, T2><<<a.R, T2, 0, stream>>>(a, w);
+        return hipGetLastError();
     }
+    if (loads <= 256)
+        row_kernel<T, 64, 4><<<grid, 64, 0, stream>>>(a, shift);
+    else if (a.R < cus && loads > 4096)
+        row_kernel<T, 1024, AHEAD><<<grid, 1024, 0, stream>>>(a, shift);
+    else if (loads <= 2048)
+        row_kernel<T, 256, 4><<<grid, 256, 0, stream>>>(a, shift);
+    else
+        row_kernel<T, 512, AHEAD><<<grid, 512, 0, stream>>>(a, shift);
+    return hipGetLastError();
 }
 
 } // namespace
 
-size_t fq_logprobs_bytes(int, int) { return 256; }
+size_t fq_logprobs_bytes(int, int) { return sizeof(Part) * SPLIT_ROWS * MAX_PIECES + sizeof(uint32_t) * SPLIT_ROWS * MAX_BLOCKS; }
 
-hipError_t fq_launch_logprobs(const FqLogprobsArgs &a, bool half, void *, hipStream_t stream)
+hipError_t fq_launch_logprobs(const FqLogprobsArgs &a, bool half, void *workspace, hipStream_t stream)
 {
-    const int grid = a.R < 65536 ? a.R : 65536;
-    if (half)
-        logprobs_kernel<_Float16><<<grid, THREADS, 0, stream>>>(a);
-    else
-        logprobs_kernel<float><<<grid, THREADS, 0, stream>>>(a);
-    return hipGetLastError();
+    return half ? launch<_Float16>(a, workspace, stream) : launch<float>(a, workspace, stream);
 }
