@@ -95,6 +95,19 @@ __device__ __forceinline__ float lane_of(float x, int lane)
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
 }
 
+// Sums over the lanes of a wavefront.
+__device__ __forceinline__ double wave_sum(float x)
+{
+    auto step = [](float v, auto ctrl) {
+        const int t = __builtin_bit_cast(int, v);
+        return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(t, t, decltype(ctrl)::value, 0xf, 0xf, false));
+    };
+    x = step(x, std::integral_constant<int, 0xb1>());
+    x = step(x, std::integral_constant<int, 0x4e>());
+    x = step(x, std::integral_constant<int, 0x141>());
+    x = step(x, std::integral_constant<int, 0x140>());
+    return ((double)lane_of(x, 0) + (double)lane_of(x, 16)) + ((double)lane_of(x, 32) + (double)lane_of(x, 48));
+}
 __device__ __forceinline__ double wave_sum(double v)
 {
 #pragma unroll
@@ -116,33 +129,13 @@ struct Work {
     unsigned piece; // loads to a piece
 };
 
-// Parts i = 0 .. n - 1 as one, in every thread, in one order.
-template <typename Get>
-__device__ __forceinline__ Part join(int n, const Get &get)
-{
-    Part all{-INFINITY, 0.0, 0.0};
-    for (int i = 0; i < n; i++) {
-        const Part p = get(i);
-        if (!(p.m > -INFINITY))
-            continue;
-        if (p.m > all.m) { // (what was there gets its largest one's 1 back)
-            const double d = (double)all.m - (double)p.m, c = all.m > -INFINITY && p.m < INFINITY ? exp(d) : 0.0;
-            const double s = c > 0.0 ? c * (all.s + 1.0) : 0.0, t = c > 0.0 ? c * (all.t + d * (all.s + 1.0)) : 0.0;
-            all = Part{p.m, p.s + s, p.t + t};
-        } else {
-            const double d = (double)p.m - (double)all.m, c = all.m < INFINITY ? exp(d) : 0.0;
-            all.s += c > 0.0 ? c * (p.s + 1.0) : 0.0;
-            all.t += c > 0.0 ? c * (p.t + d * (p.s + 1.0)) : 0.0;
-        }
-    }
-    return all;
-}
-
 // What a workgroup needs in LDS.
 template <int THREADS>
 struct Shared {
     uint32_t keys[MAX_BLOCKS];
     Part parts[THREADS / 64];
+    Part all; // of the row
+    double log_sum;
     uint64_t list[LIST];
     int chosen[MAX_CHOSEN];
     int bins[BINS];
@@ -151,7 +144,7 @@ struct Shared {
 
 // The loads [begin, end) of a row through the workgroup: parts of the wavefronts and the blocks' maxima, from block `first` on, into `sh`.
 template <typename T, int THREADS, int AHEAD>
-__device__ __forceinline__ void stream(const Row<T> &row, unsigned begin, unsigned end, int block_shift, unsigned first, Shared<THREADS> &sh)
+__device__ __forceinline__ void stream(const Row<T> &row, unsigned begin, unsigned end, int block_shift, unsigned first, bool top, Shared<THREADS> &sh)
 {
     constexpr int PER = Row<T>::PER, LANES = BLOCK / PER; // lanes of a block
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -176,7 +169,7 @@ __device__ __forceinline__ void stream(const Row<T> &row, unsigned begin, unsign
                         blank<T>(v[j], e);
             }
         }
-        float most[AHEAD], top = -INFINITY;
+        float most[AHEAD], peak = -INFINITY;
 #pragma unroll
         for (int j = 0; j < AHEAD; j++) {
             float x[PER];
@@ -186,9 +179,9 @@ __device__ __forceinline__ void stream(const Row<T> &row, unsigned begin, unsign
             for (int e = 0; e < PER; e++)
                 most[j] = fmaxf(most[j], x[e]);
             const float b = group_max<LANES>(most[j]);
-            top = fmaxf(top, b);
+            peak = fmaxf(peak, b);
             const unsigned g = base + 64 * j + lane;
-            if ((lane & (LANES - 1)) == 0 && (!EDGE || g < end)) {
+            if (top && (lane & (LANES - 1)) == 0 && (!EDGE || g < end)) {
                 const unsigned block = (g * PER / BLOCK >> block_shift) - first;
                 if (block_shift == 0)
                     sh.keys[block] = key_of(b);
@@ -196,21 +189,21 @@ __device__ __forceinline__ void stream(const Row<T> &row, unsigned begin, unsign
                     atomicMax(&sh.keys[block], key_of(b));
             }
         }
-        top = group_max<16>(top);
-        top = fmaxf(fmaxf(lane_of(top, 0), lane_of(top, 16)), fmaxf(lane_of(top, 32), lane_of(top, 48)));
-        if (top > m) {
-            const float d = m - top, c = __expf(d);
+        peak = group_max<16>(peak);
+        peak = fmaxf(fmaxf(lane_of(peak, 0), lane_of(peak, 16)), fmaxf(lane_of(peak, 32), lane_of(peak, 48)));
+        if (peak > m) {
+            const float d = m - peak, c = __expf(d);
             t = c > 0.0f ? c * (t + d * s) : 0.0f;
             s *= c;
             if (lane == 0 && c > 0.0f) { // the old largest one's 1
                 s += c;
                 t += c * d;
             }
-            m = top;
+            m = peak;
             bool looking = true; // the new one's is left out: one lane's first
 #pragma unroll
             for (int j = 0; j < AHEAD; j++) {
-                const uint64_t has = __ballot(most[j] == top);
+                const uint64_t has = __ballot(most[j] == peak);
                 if (looking && has) {
                     looking = false;
                     if (lane == __ffsll((unsigned long long)has) - 1) {
@@ -219,7 +212,7 @@ __device__ __forceinline__ void stream(const Row<T> &row, unsigned begin, unsign
                         bool mine = true;
 #pragma unroll
                         for (int e = 0; e < PER; e++)
-                            if (mine && x[e] == top) {
+                            if (mine && x[e] == peak) {
                                 mine = false;
                                 blank<T>(v[j], e);
                             }
@@ -253,34 +246,76 @@ __device__ __forceinline__ void stream(const Row<T> &row, unsigned begin, unsign
         else
             turn(base, std::false_type());
     }
-    const double all_s = wave_sum((double)s), all_t = wave_sum((double)t);
+    const double all_s = wave_sum(s), all_t = wave_sum(t);
     if (lane == 0)
         sh.parts[wave] = Part{m, all_s, all_t};
 }
 
-// The cut of items (key, index) at about the n-th of the order (larger key, smaller index): at least n of them, or all, lie at or above it, at most `cap`
-// unless that is n.  each(f) calls f(key, index) for a thread's items.  Keys under `low` do not count.
+// The parts' sums as one, by the first wavefront: a lane to a part, up to 64.
+template <int THREADS>
+__device__ __forceinline__ void join(int n, const Part *parts, Shared<THREADS> &sh)
+{
+    const int lane = threadIdx.x;
+    if (lane < 64) {
+        const Part p = lane < n ? parts[lane] : Part{-INFINITY, 0.0, 0.0};
+        float m = group_max<16>(p.m);
+        m = fmaxf(fmaxf(lane_of(m, 0), lane_of(m, 16)), fmaxf(lane_of(m, 32), lane_of(m, 48)));
+        const int first = __ffsll((unsigned long long)__ballot(p.m == m)) - 1; // whose 1 stays out
+        double s = 0.0, t = 0.0;
+        if (p.m > -INFINITY && m < INFINITY) {
+            const double d = (double)p.m - (double)m, c = exp(d);
+            if (c > 0.0) {
+                s = c * (p.s + (lane == first ? 0.0 : 1.0));
+                t = c * (p.t + (lane == first ? 0.0 : d * (p.s + 1.0)));
+            }
+        }
+        if (n > 1) {
+            s = wave_sum(s);
+            t = wave_sum(t);
+        }
+        if (lane == 0) {
+            sh.all = Part{m, s, t};
+            sh.log_sum = log1p(s);
+        }
+    }
+    __syncthreads();
+}
+
+// The cut of items (logit, index) at about the n-th of the order (larger logit, smaller index): at least n of them, or all, lie at or above it, at most
+// `cap` unless that is n.  In eighths of the distance from the row's largest logit m, the last for everything 31.9 and more below; within one of those by the
+// bits of the logit; among equal ones by index.
 struct Cut {
-    uint32_t key, turned; // kept: a larger key, or this one with ~index >= turned
-    __device__ __forceinline__ bool keeps(uint32_t k, uint32_t index) const { return k > key || (k == key && ~index >= turned); }
+    float m;
+    int below; // kept: fewer eighths, or as many and
+    uint32_t key, turned; // a larger key, or this one with ~index >= turned
+    static __device__ __forceinline__ int eighths(float m, float x) { return (int)fminf((m - x) * 8.0f, BINS - 1.0f); }
+    __device__ __forceinline__ bool keeps(uint32_t k, uint32_t index) const
+    {
+        const int e = eighths(m, of_key(k));
+        return e < below || (e == below && (k > key || (k == key && ~index >= turned)));
+    }
 };
 
+// each(f) calls f(key, index) for a thread's items; keys from `low` on count.
 template <int THREADS, typename Each>
-__device__ __forceinline__ Cut find_cut(int n, int cap, uint32_t low, uint32_t high, uint32_t last_index, Shared<THREADS> &sh, const Each &each)
+__device__ __forceinline__ Cut find_cut(int n, int cap, float m, uint32_t low, uint32_t last_index, Shared<THREADS> &sh, const Each &each)
 {
     const int tid = threadIdx.x, lane = tid & 63;
-    uint32_t tie = 0;
-    bool tied = false; // by index among equal keys
+    enum { EIGHTHS, KEYS, INDICES } by = EIGHTHS;
+    Cut cut{m, 0, 0, 0};
+    uint32_t high = BINS - 1; // of the fields that are counted, from `from` on
+    uint32_t from = 0;
     int above = 0;
     for (;;) {
-        const int bits = 32 - __clz((int)(high - low)), shift = high == low || bits < 8 ? 0 : bits - 8;
+        const int bits = 32 - __clz((int)(high - from)), shift = high == from || bits < 8 ? 0 : bits - 8;
         for (int i = tid; i < BINS; i += THREADS)
             sh.bins[i] = 0;
         __syncthreads();
         each([&](uint32_t key, uint32_t index) {
-            const uint32_t field = tied ? ~index : key;
-            if ((!tied || key == tie) && field >= low && field <= high)
-                atomicAdd(&sh.bins[(field - low) >> shift], 1);
+            const int e = Cut::eighths(m, of_key(key));
+            const uint32_t field = by == EIGHTHS ? BINS - 1 - e : by == KEYS ? key : ~index;
+            if (key >= low && (by == EIGHTHS || e == cut.below) && (by != INDICES || key == cut.key) && field >= from && field <= high)
+                atomicAdd(&sh.bins[(field - from) >> shift], 1);
         });
         __syncthreads();
         if (tid < 64) { // the highest bin from which on there are enough
@@ -319,19 +354,30 @@ __device__ __forceinline__ Cut find_cut(int n, int cap, uint32_t low, uint32_t h
         }
         __syncthreads();
         const int bin = sh.found[0], count = sh.found[1];
-        const uint32_t edge = low + ((uint32_t)bin << shift);
-        if (count <= cap || count <= n || (shift == 0 && tied))
-            return tied ? Cut{tie, edge} : Cut{edge, 0};
+        const uint32_t edge = from + ((uint32_t)bin << shift);
+        if (by == EIGHTHS)
+            cut.below = BINS - 1 - (int)edge;
+        else if (by == KEYS)
+            cut.key = edge;
+        else
+            cut.turned = edge;
+        if (count <= cap || count <= n || (by == INDICES && shift == 0))
+            return cut;
         above = sh.found[2];
-        if (shift == 0) {
-            tied = true;
-            tie = edge;
-            low = ~last_index;
-            high = ~0u;
-        } else {
-            low = edge;
+        if (by == EIGHTHS) { // the keys of these eighths, from well below to well above
+            by = KEYS;
+            const float top = m - 0.125f * cut.below;
+            from = cut.below == BINS - 1 ? low : key_of(top - 0.25f - 0x1p-10f * fabsf(top));
+            from = from > low ? from : low;
+            high = key_of(m);
+        } else if (shift > 0) {
+            from = edge;
             if (high - edge > (1u << shift) - 1)
                 high = edge + ((1u << shift) - 1);
+        } else { // all equal
+            by = INDICES;
+            from = ~last_index;
+            high = ~0u;
         }
         __syncthreads();
     }
@@ -339,9 +385,10 @@ __device__ __forceinline__ Cut find_cut(int n, int cap, uint32_t low, uint32_t h
 
 // Everything that comes after a row's logits were streamed.
 template <typename T, int THREADS>
-__device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, const Row<T> &row, Part all, int block_shift, Shared<THREADS> &sh)
+__device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, const Row<T> &row, int block_shift, Shared<THREADS> &sh)
 {
     const int tid = threadIdx.x;
+    Part all = sh.all;
     const bool none = all.m == -INFINITY, infinite = all.m == INFINITY;
     if (infinite) { // weights of 1 for these alone
         int count = 0;
@@ -357,7 +404,7 @@ __device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, con
         all.t = 0.0;
         __syncthreads();
     }
-    const double log_sum = none ? 0.0 : log1p(all.s);
+    const double log_sum = infinite ? log1p(all.s) : sh.log_sum;
     auto logprob = [&](float x) {
         if (none || !(x > -INFINITY) || (infinite && x < INFINITY))
             return -INFINITY;
@@ -372,18 +419,18 @@ __device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, con
     const int n = a.top_n;
     if (n == 0)
         return;
-    const uint32_t high = key_of(all.m), low = infinite ? high : LOWEST + 1;
+    const uint32_t low = infinite ? key_of(INFINITY) : LOWEST + 1; // of what counts
     const int blocks = (int)(((row.shift + row.V + BLOCK - 1) / BLOCK + (1u << block_shift) - 1) >> block_shift);
     const int cap = n > 32 ? MAX_CHOSEN : MAX_CHOSEN / 2;
     if (tid == 0)
         sh.found[3] = 0;
-    Cut cut{low - 1, ~0u}; // (nothing has an index of 0 under that key)
+    Cut cut{all.m, BINS, 0, 0}; // everything
     if (!none && blocks > cap) {
         auto each = [&](const auto &f) {
             for (int i = tid; i < blocks; i += THREADS)
                 f(sh.keys[i], (uint32_t)i);
         };
-        cut = find_cut<THREADS>(n, cap, low, high, (uint32_t)blocks - 1, sh, each);
+        cut = find_cut<THREADS>(n, cap, all.m, low, (uint32_t)blocks - 1, sh, each);
     }
     __syncthreads();
     for (int i = tid; i < blocks; i += THREADS) {
@@ -396,7 +443,7 @@ __device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, con
     }
     __syncthreads();
     const int chosen = none ? 0 : sh.found[3];
-    const uint32_t reach = cut.key > low ? cut.key : low; // (n tokens at least, or all, have such a key)
+    cut.turned = 0; // (n tokens at least, or all, reach the cut by their logits alone)
     const int size = BLOCK << block_shift;
     __syncthreads();
     if (tid == 0)
@@ -415,19 +462,19 @@ __device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, con
             sh.list[at] = (uint64_t)key << 32 | (uint32_t)~index;
     };
     each([&](uint32_t key, uint32_t index) {
-        if (key >= reach)
+        if (key >= low && cut.keeps(key, index))
             collect(key, index);
     });
     __syncthreads();
     if (sh.found[3] > LIST) { // more than that reach it: the cut among the tokens
         __syncthreads();
-        const Cut c = find_cut<THREADS>(n, LIST, reach, high, row.V - 1, sh, each);
+        const Cut c = find_cut<THREADS>(n, LIST, all.m, low, row.V - 1, sh, each);
         __syncthreads();
         if (tid == 0)
             sh.found[3] = 0;
         __syncthreads();
         each([&](uint32_t key, uint32_t index) {
-            if (key >= reach && c.keeps(key, index))
+            if (key >= low && c.keeps(key, index))
                 collect(key, index);
         });
         __syncthreads();
@@ -450,22 +497,20 @@ __device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, con
 }
 
 template <typename T, int THREADS, int AHEAD>
-__global__ __launch_bounds__(THREADS) void row_kernel(FqLogprobsArgs a, int block_shift)
+__global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 6) void row_kernel(FqLogprobsArgs a, int block_shift)
 {
     __shared__ Shared<THREADS> sh;
-    for (long long r = blockIdx.x; r < a.R; r += gridDim.x) {
-        const Row<T> row(a, r);
-        if (block_shift) {
-            for (int i = threadIdx.x; i < MAX_BLOCKS; i += THREADS)
-                sh.keys[i] = 0;
-            __syncthreads();
-        }
-        stream<T, THREADS, AHEAD>(row, 0, row.loads(), block_shift, 0, sh);
-        __syncthreads();
-        const Part all = join(THREADS / 64, [&](int i) { return sh.parts[i]; });
-        finish<T, THREADS>(a, r, row, all, block_shift, sh);
+    const long long r = blockIdx.x;
+    const Row<T> row(a, r);
+    if (block_shift) {
+        for (int i = threadIdx.x; i < MAX_BLOCKS; i += THREADS)
+            sh.keys[i] = 0;
         __syncthreads();
     }
+    stream<T, THREADS, AHEAD>(row, 0, row.loads(), block_shift, 0, a.top_n > 0, sh);
+    __syncthreads();
+    join(THREADS / 64, sh.parts, sh);
+    finish<T, THREADS>(a, r, row, block_shift, sh);
 }
 
 // Few long rows: a workgroup takes a piece, a second launch joins them.
@@ -484,7 +529,7 @@ __global__ __launch_bounds__(THREADS) void piece_kernel(FqLogprobsArgs a, Work w
         __syncthreads();
     }
     if (begin < end)
-        stream<T, THREADS, AHEAD>(row, begin, end, w.shift, first, sh);
+        stream<T, THREADS, AHEAD>(row, begin, end, w.shift, first, a.top_n > 0, sh);
     else if ((threadIdx.x & 63) == 0)
         sh.parts[threadIdx.x >> 6] = Part{-INFINITY, 0.0, 0.0};
     __syncthreads();
@@ -493,9 +538,9 @@ __global__ __launch_bounds__(THREADS) void piece_kernel(FqLogprobsArgs a, Work w
         for (unsigned i = threadIdx.x; i < blocks; i += THREADS)
             w.keys[(size_t)r * MAX_BLOCKS + first + i] = sh.keys[i];
     }
-    const Part all = join(THREADS / 64, [&](int i) { return sh.parts[i]; });
+    join(THREADS / 64, sh.parts, sh);
     if (threadIdx.x == 0)
-        w.parts[r * MAX_PIECES + p] = all;
+        w.parts[r * MAX_PIECES + p] = sh.all;
 }
 
 template <typename T, int THREADS>
@@ -511,8 +556,8 @@ __global__ __launch_bounds__(THREADS) void join_kernel(FqLogprobsArgs a, Work w)
     if ((int)threadIdx.x < w.pieces)
         parts[threadIdx.x] = w.parts[r * MAX_PIECES + threadIdx.x];
     __syncthreads();
-    const Part all = join(w.pieces, [&](int i) { return parts[i]; });
-    finish<T, THREADS>(a, r, row, all, w.shift, sh);
+    join(w.pieces, parts, sh);
+    finish<T, THREADS>(a, r, row, w.shift, sh);
 }
 
 template <typename T>
@@ -523,7 +568,7 @@ hipError_t launch(const FqLogprobsArgs &a, void *workspace, hipStream_t stream)
     while (((long long)a.V + PER + BLOCK - 1) / BLOCK > (long long)MAX_BLOCKS << shift)
         shift++;
     const long long loads = ((long long)a.V + PER - 1) / PER + 1;
-    const int cus = fq_device_cus(), grid = a.R < (1 << 20) ? a.R : 1 << 20;
+    const int cus = fq_device_cus(), grid = a.R;
     constexpr int AHEAD = 32 / PER, T2 = 512, UNIT = T2 * AHEAD;
     if (a.R <= SPLIT_ROWS && loads > 8 * UNIT) {
         Work w{};
@@ -559,5 +604,18 @@ size_t fq_logprobs_bytes(int, int) { return sizeof(Part) * SPLIT_ROWS * MAX_PIEC
 
 hipError_t fq_launch_logprobs(const FqLogprobsArgs &a, bool half, void *workspace, hipStream_t stream)
 {
-    return half ? launch<_Float16>(a, workspace, stream) : launch<float>(a, workspace, stream);
+    constexpr int ROWS = 1 << 20; // to a launch
+    for (long long r = 0; r < a.R; r += ROWS) {
+        FqLogprobsArgs some = a;
+        some.R = a.R - r < ROWS ? (int)(a.R - r) : ROWS;
+        some.logits = (const char *)a.logits + r * a.row_stride * (half ? 2 : 4);
+        some.given = a.n_given ? a.given + r * a.n_given : nullptr;
+        some.given_logprob = a.n_given ? a.given_logprob + r * a.n_given : nullptr;
+        some.top_token = a.top_n ? a.top_token + r * a.top_n : nullptr;
+        some.top_logprob = a.top_n ? a.top_logprob + r * a.top_n : nullptr;
+        some.entropy = a.entropy ? a.entropy + r : nullptr;
+        if (hipError_t e = half ? launch<_Float16>(some, workspace, stream) : launch<float>(some, workspace, stream))
+            return e;
+    }
+    return hipSuccess;
 }
