@@ -19,7 +19,9 @@ namespace {
 
 constexpr int BLOCK = 64, MAX_BLOCKS = 2048; // logits; a row of more takes blocks twice, four times ... as large
 constexpr int BINS = 256, LIST = 256, MAX_CHOSEN = 128;
-constexpr int SPLIT_ROWS = 64, MAX_PIECES = 64;
+// Rows in pieces (a workgroup of 1024 threads to a whole row / pieces and a second launch, us, 20 alternatives): 1 x 32000 in binary32 10.6 / 12.8, 65536
+// 14.1 / 12.5, 128256 21.6 / 14.4, 262144 35.4 / 15.2; 32 x 65536 in binary16 14.1 / 13.2, 128256 21.1 / 15.1; 64 x 65536 14.8 / 15.7, 128256 24.3 / 18.1.
+constexpr int SPLIT_ROWS = 64, SPLIT_LOGITS = 60000, MAX_PIECES = 64;
 constexpr uint32_t LOWEST = 0x007fffffu; // the key of -inf
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -132,7 +134,8 @@ struct Work {
 // What a workgroup needs in LDS.
 template <int THREADS>
 struct Shared {
-    uint32_t keys[MAX_BLOCKS];
+    static constexpr int BLOCKS = THREADS == 64 ? 64 : MAX_BLOCKS;
+    uint32_t keys[BLOCKS];
     Part parts[THREADS / 64];
     Part all; // of the row
     double log_sum;
@@ -383,11 +386,14 @@ __device__ __forceinline__ Cut find_cut(int n, int cap, float m, uint32_t low, u
     }
 }
 
-// Everything that comes after a row's logits were streamed.
+// Everything that comes after a row's logits were streamed.  given: the thread's first given token.
 template <typename T, int THREADS>
-__device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, const Row<T> &row, int block_shift, Shared<THREADS> &sh)
+__device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, const Row<T> &row, int given, int block_shift, Shared<THREADS> &sh)
 {
     const int tid = threadIdx.x;
+    float given_logit = -INFINITY; // (asked for ahead of the next lines)
+    if (given >= 0 && given < a.V)
+        given_logit = row[given];
     Part all = sh.all;
     const bool none = all.m == -INFINITY, infinite = all.m == INFINITY;
     if (infinite) { // weights of 1 for these alone
@@ -410,90 +416,129 @@ __device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, con
             return -INFINITY;
         return infinite ? (float)-log_sum : (float)((double)x - (double)all.m - log_sum);
     };
-    if (a.entropy && tid == 0)
-        a.entropy[r] = none ? 0.0f : (float)(log_sum - all.t / (1.0 + all.s));
-    for (int j = tid; j < a.n_given; j += THREADS) {
-        const int i = a.given[r * a.n_given + j];
-        a.given_logprob[r * a.n_given + j] = i >= 0 && i < a.V ? logprob(row[i]) : -INFINITY;
-    }
     const int n = a.top_n;
-    if (n == 0)
-        return;
-    const uint32_t low = infinite ? key_of(INFINITY) : LOWEST + 1; // of what counts
-    const int blocks = (int)(((row.shift + row.V + BLOCK - 1) / BLOCK + (1u << block_shift) - 1) >> block_shift);
-    const int cap = n > 32 ? MAX_CHOSEN : MAX_CHOSEN / 2;
-    if (tid == 0)
-        sh.found[3] = 0;
-    Cut cut{all.m, BINS, 0, 0}; // everything
-    if (!none && blocks > cap) {
-        auto each = [&](const auto &f) {
+    if (n > 0 && !none) {
+        const uint32_t low = infinite ? key_of(INFINITY) : LOWEST + 1; // of what counts
+        const int size_shift = 6 + block_shift;
+        static_assert(BLOCK == 64, "");
+        const int blocks = (int)((row.shift + row.V + (1u << size_shift) - 1) >> size_shift);
+        uint32_t floor = low; // n tokens at least, or all that count, have such a key
+        Cut cut{all.m, BINS, 0, 0}; // everything
+        bool every = blocks <= n;
+        if (tid == 0)
+            sh.found[3] = 0;
+        if (every) {
             for (int i = tid; i < blocks; i += THREADS)
-                f(sh.keys[i], (uint32_t)i);
-        };
-        cut = find_cut<THREADS>(n, cap, all.m, low, (uint32_t)blocks - 1, sh, each);
-    }
-    __syncthreads();
-    for (int i = tid; i < blocks; i += THREADS) {
-        const uint32_t k = sh.keys[i];
-        if (k >= low && cut.keeps(k, i)) {
-            const int at = atomicAdd(&sh.found[3], 1);
-            if (at < MAX_CHOSEN)
-                sh.chosen[at] = i;
+                sh.chosen[i] = i;
+            if (tid == 0)
+                sh.found[3] = blocks;
+        } else if (blocks <= 64) { // ranked against each other by one wavefront
+            if (tid < 64) {
+                const uint32_t k = tid < blocks ? sh.keys[tid] : 0;
+                int rank = 0;
+                for (int j = 0; j < blocks; j++) {
+                    const uint32_t o = __builtin_amdgcn_readlane(k, j);
+                    rank += o > k || (o == k && j < tid);
+                }
+                if (tid < blocks && rank < n) {
+                    sh.chosen[rank] = tid;
+                    if (rank == n - 1) {
+                        sh.found[0] = (int)k;
+                        sh.found[3] = n;
+                    }
+                }
+            }
+            __syncthreads();
+            floor = (uint32_t)sh.found[0] > low ? (uint32_t)sh.found[0] : low;
+        } else {
+            const int cap = n > 32 ? MAX_CHOSEN : MAX_CHOSEN / 2;
+            cut = find_cut<THREADS>(n, cap, all.m, low, (uint32_t)blocks - 1, sh, [&](const auto &f) {
+                for (int i = tid; i < blocks; i += THREADS)
+                    f(sh.keys[i], (uint32_t)i);
+            });
+            __syncthreads();
+            for (int i = tid; i < blocks; i += THREADS) {
+                const uint32_t k = sh.keys[i];
+                if (k >= low && cut.keeps(k, i)) {
+                    const int at = atomicAdd(&sh.found[3], 1);
+                    if (at < MAX_CHOSEN) // (always)
+                        sh.chosen[at] = i;
+                }
+            }
+            cut.turned = 0; // (the tokens that are wanted reach the cut by their logits alone)
         }
-    }
-    __syncthreads();
-    const int chosen = none ? 0 : sh.found[3];
-    cut.turned = 0; // (n tokens at least, or all, reach the cut by their logits alone)
-    const int size = BLOCK << block_shift;
-    __syncthreads();
-    if (tid == 0)
-        sh.found[3] = 0;
-    __syncthreads();
-    auto each = [&](const auto &f) {
-        for (int i = tid; i < chosen * size; i += THREADS) {
-            const unsigned at = (unsigned)sh.chosen[i / size] * size + i % size;
-            if (at >= row.shift && at < row.shift + row.V)
-                f(key_of((float)row.from[at]), at - row.shift);
-        }
-    };
-    auto collect = [&](uint32_t key, uint32_t index) {
-        const int at = atomicAdd(&sh.found[3], 1);
-        if (at < LIST)
-            sh.list[at] = (uint64_t)key << 32 | (uint32_t)~index;
-    };
-    each([&](uint32_t key, uint32_t index) {
-        if (key >= low && cut.keeps(key, index))
-            collect(key, index);
-    });
-    __syncthreads();
-    if (sh.found[3] > LIST) { // more than that reach it: the cut among the tokens
         __syncthreads();
-        const Cut c = find_cut<THREADS>(n, LIST, all.m, low, row.V - 1, sh, each);
+        const int tokens = min(sh.found[3], MAX_CHOSEN) << size_shift;
         __syncthreads();
         if (tid == 0)
             sh.found[3] = 0;
         __syncthreads();
-        each([&](uint32_t key, uint32_t index) {
-            if (key >= low && c.keeps(key, index))
-                collect(key, index);
-        });
+        auto each = [&](const auto &f) {
+            for (int i = tid; i < tokens; i += THREADS) {
+                const unsigned at = ((unsigned)sh.chosen[i >> size_shift] << size_shift) + (i & ((1 << size_shift) - 1));
+                if (at >= row.shift && at < row.shift + row.V) {
+                    const uint32_t key = key_of((float)row.from[at]);
+                    if (key >= floor)
+                        f(key, at - row.shift);
+                }
+            }
+        };
+        auto collect = [&](uint32_t key, uint32_t index) {
+            if (cut.keeps(key, index)) {
+                const int at = atomicAdd(&sh.found[3], 1);
+                if (at < LIST)
+                    sh.list[at] = (uint64_t)key << 32 | (uint32_t)~index;
+            }
+        };
+        const bool many = every && tokens > LIST;
+        if (!many)
+            each(collect);
         __syncthreads();
-    }
-    const int listed = min(sh.found[3], LIST);
-    for (int i = tid; i < listed; i += THREADS) {
-        const uint64_t own = sh.list[i];
-        int rank = 0;
-        for (int j = 0; j < listed; j++)
-            rank += sh.list[j] > own;
-        if (rank < n) {
-            a.top_token[r * n + rank] = (int32_t)~(uint32_t)own;
-            a.top_logprob[r * n + rank] = logprob(of_key((uint32_t)(own >> 32)));
+        if (many || sh.found[3] > LIST) { // more than that reach the blocks' cut: one among the tokens
+            __syncthreads();
+            cut = find_cut<THREADS>(n, LIST, all.m, floor, row.V - 1, sh, each);
+            __syncthreads();
+            if (tid == 0)
+                sh.found[3] = 0;
+            __syncthreads();
+            each(collect);
+            __syncthreads();
+        }
+        const int listed = min(sh.found[3], LIST);
+        for (int i = tid; i < listed; i += THREADS) {
+            const uint64_t own = sh.list[i];
+            int rank = 0;
+            for (int j = 0; j < listed; j++)
+                rank += sh.list[j] > own;
+            if (rank < n) {
+                a.top_token[r * n + rank] = (int32_t)~(uint32_t)own;
+                a.top_logprob[r * n + rank] = logprob(of_key((uint32_t)(own >> 32)));
+            }
+        }
+        for (int i = listed + tid; i < n; i += THREADS) {
+            a.top_token[r * n + i] = -1;
+            a.top_logprob[r * n + i] = -INFINITY;
+        }
+    } else {
+        for (int i = tid; i < n; i += THREADS) {
+            a.top_token[r * n + i] = -1;
+            a.top_logprob[r * n + i] = -INFINITY;
         }
     }
-    for (int i = listed + tid; i < n; i += THREADS) {
-        a.top_token[r * n + i] = -1;
-        a.top_logprob[r * n + i] = -INFINITY;
+    if (a.entropy && tid == 0)
+        a.entropy[r] = none ? 0.0f : (float)(log_sum - all.t / (1.0 + all.s));
+    for (int j = tid; j < a.n_given; j += THREADS) {
+        if (j != tid) {
+            given = a.given[r * a.n_given + j];
+            given_logit = given >= 0 && given < a.V ? row[given] : -INFINITY;
+        }
+        a.given_logprob[r * a.n_given + j] = logprob(given_logit);
     }
+}
+
+__device__ __forceinline__ int first_given(const FqLogprobsArgs &a, long long r)
+{
+    return (int)threadIdx.x < a.n_given ? a.given[r * a.n_given + threadIdx.x] : -1;
 }
 
 template <typename T, int THREADS, int AHEAD>
@@ -502,15 +547,16 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 6) void row_kernel(F
     __shared__ Shared<THREADS> sh;
     const long long r = blockIdx.x;
     const Row<T> row(a, r);
+    const int given = first_given(a, r);
     if (block_shift) {
-        for (int i = threadIdx.x; i < MAX_BLOCKS; i += THREADS)
+        for (int i = threadIdx.x; i < sh.BLOCKS; i += THREADS)
             sh.keys[i] = 0;
         __syncthreads();
     }
     stream<T, THREADS, AHEAD>(row, 0, row.loads(), block_shift, 0, a.top_n > 0, sh);
     __syncthreads();
     join(THREADS / 64, sh.parts, sh);
-    finish<T, THREADS>(a, r, row, block_shift, sh);
+    finish<T, THREADS>(a, r, row, given, block_shift, sh);
 }
 
 // Few long rows: a workgroup takes a piece, a second launch joins them.
@@ -550,6 +596,7 @@ __global__ __launch_bounds__(THREADS) void join_kernel(FqLogprobsArgs a, Work w)
     __shared__ Part parts[MAX_PIECES];
     const int r = blockIdx.x;
     const Row<T> row(a, r);
+    const int given = first_given(a, r);
     const int blocks = (int)(((row.shift + row.V + BLOCK - 1) / BLOCK + (1u << w.shift) - 1) >> w.shift);
     for (int i = threadIdx.x; i < blocks; i += THREADS)
         sh.keys[i] = w.keys[(size_t)r * MAX_BLOCKS + i];
@@ -557,7 +604,7 @@ __global__ __launch_bounds__(THREADS) void join_kernel(FqLogprobsArgs a, Work w)
         parts[threadIdx.x] = w.parts[r * MAX_PIECES + threadIdx.x];
     __syncthreads();
     join(w.pieces, parts, sh);
-    finish<T, THREADS>(a, r, row, w.shift, sh);
+    finish<T, THREADS>(a, r, row, given, w.shift, sh);
 }
 
 template <typename T>
@@ -570,7 +617,7 @@ hipError_t launch(const FqLogprobsArgs &a, void *workspace, hipStream_t stream)
     const long long loads = ((long long)a.V + PER - 1) / PER + 1;
     const int cus = fq_device_cus(), grid = a.R;
     constexpr int AHEAD = 32 / PER, T2 = 512, UNIT = T2 * AHEAD;
-    if (a.R <= SPLIT_ROWS && loads > 8 * UNIT) {
+    if (a.R <= SPLIT_ROWS && a.V >= SPLIT_LOGITS) {
         Work w{};
         const long long units = (loads + UNIT - 1) / UNIT;
         long long pieces = 2 * cus / a.R;
