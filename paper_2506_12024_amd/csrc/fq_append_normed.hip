@@ -1,8 +1,14 @@
 // Norms of the heads of queries and keys, rotary positions and the append to a paged cache, one launch.
 //
-// A workgroup takes a token, a wavefront a head: its sum of squares, then its values in binary32 through LDS, where a pair's partner
-// is found wherever it lies.
+//   y_d = x_d (w_d + offset) / sqrt(mean_i x_i^2 + eps),  then pairs turn as in fq_append.hip,  one rounding at the end
+//
+// A head lies in the registers of a group of lanes, two 16-byte pieces to a lane: those of a pair of pieces that turn together where a half rotation is
+// whole pieces, else neighbours.  Its sum of squares is a sum over the group's lanes, and a head is read once.  Only where pairs lie anyhow
+// (a half rotation that is no multiple of 8) the normed head goes through LDS for its partners.  A workgroup takes a token, or a share of
+// its heads where there are few tokens; cos and sin of its angles, computed as fq_append.hip does, are in LDS.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "../../include/flexq.h"
 #include "fq_kv.h"
@@ -11,15 +17,84 @@ namespace {
 
 constexpr int THREADS = 256;
 
-__global__ __launch_bounds__(THREADS) void append_normed_kernel(FqAppendArgs a, FqNormArgs norm, int interleaved)
+struct alignas(16) Eight {
+    uint16_t v[8];
+};
+
+// The sequence that owns row t: the last b with q_start[b] <= t, or -1 (64 starts at a time).
+__device__ __forceinline__ int owner(const FqSeqsView &s, int t)
 {
-    __shared__ float cs[FQ_MAX_HEAD_DIM / 2], sn[FQ_MAX_HEAD_DIM / 2], head[THREADS / 64][FQ_MAX_HEAD_DIM];
-    const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const bool bf16 = a.kv.bf16;
-    const int half = a.rot >> 1, dim = a.kv.dim, qk = a.q_heads + a.kv.kv_heads;
-    int b = -1;
-    for (int i = 0; i < a.seqs.seqs && a.seqs.q_start[i] <= t; i++)
-        b = i;
+    const int lane = threadIdx.x & 63;
+    int begun = 0;
+    for (int b0 = 0; b0 < s.seqs; b0 += 64) {
+        const bool in = b0 + lane < s.seqs && s.q_start[b0 + lane] <= t;
+        const int n = __popcll(__ballot(in));
+        begun += n;
+        if (n < 64)
+            break;
+    }
+    return begun - 1;
+}
+
+// The sum over a group of 4, 8 or 16 lanes, in all of them.
+template <int GROUP>
+__device__ __forceinline__ float group_sum(float x)
+{
+    auto step = [](float v, auto ctrl) {
+        const int t = __builtin_bit_cast(int, v);
+        return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(t, t, decltype(ctrl)::value, 0xf, 0xf, false));
+    };
+    x = step(x, std::integral_constant<int, 0xb1>()); // quad_perm 1, 0, 3, 2
+    x = step(x, std::integral_constant<int, 0x4e>()); // quad_perm 2, 3, 0, 1
+    if (GROUP >= 8)
+        x = step(x, std::integral_constant<int, 0x141>()); // half a row mirrored
+    if (GROUP >= 16)
+        x = step(x, std::integral_constant<int, 0x140>()); // a row mirrored
+    return x;
+}
+
+enum Layout { NEIGHBOURS, PIECES, ANYHOW };
+
+// GROUP lanes to a head, a power of two, 2 GROUP pieces at least.
+template <Layout LAYOUT, int GROUP, bool BF16>
+__global__ __launch_bounds__(THREADS) void append_normed_kernel(FqAppendArgs a, FqNormArgs norm)
+{
+    __shared__ float cs[FQ_MAX_HEAD_DIM / 2], sn[FQ_MAX_HEAD_DIM / 2];
+    __shared__ float normed[LAYOUT == ANYHOW ? THREADS * 16 : 1];
+    const int t = blockIdx.x, tid = threadIdx.x;
+    const int half = a.rot >> 1, dim = a.kv.dim, pieces = dim >> 3, qk = a.q_heads + a.kv.kv_heads, heads = qk + a.kv.kv_heads;
+    const int i = tid & (GROUP - 1), c = LAYOUT == PIECES && i < half >> 3 ? i : 2 * i;
+    const int c2 = LAYOUT == PIECES && i < half >> 3 ? i + (half >> 3) : 2 * i + 1; // (past the rotation pieces go on at rot / 8 = 2 half / 8)
+    const bool has = c < pieces, has2 = c2 < pieces;
+    struct Head {
+        Eight x, y, w, w2;
+        int kind, own; // 0, 1, 2: q, k, v
+    };
+    auto ask = [&](int h) {
+        Head n;
+        n.kind = h < a.q_heads ? 0 : h < qk ? 1 : 2;
+        n.own = h - (n.kind == 0 ? 0 : n.kind == 1 ? a.q_heads : qk);
+        const uint16_t *row = (n.kind == 0 ? a.q + t * a.q_stride : n.kind == 1 ? a.k + t * a.k_stride : a.v + t * a.v_stride) + n.own * dim;
+        const uint16_t *w = (n.kind == 0 ? norm.q_weight : norm.k_weight) + n.own * norm.weight_stride;
+        n.x = n.y = n.w = n.w2 = Eight{};
+        if (has) {
+            n.x = *(const Eight *)(row + 8 * c);
+            if (n.kind != 2)
+                n.w = *(const Eight *)(w + 8 * c);
+        }
+        if (has2) {
+            n.y = *(const Eight *)(row + 8 * c2);
+            if (n.kind != 2)
+                n.w2 = *(const Eight *)(w + 8 * c2);
+        }
+        return n;
+    };
+    const int h0 = blockIdx.y * (THREADS / GROUP) + tid / GROUP, stride = gridDim.y * (THREADS / GROUP);
+    Head now;
+    if (h0 < heads)
+        now = ask(h0);
+
+    const int b = owner(a.seqs, t);
     if (b < 0)
         return;
     const FqSeq seq = fq_seq(a.seqs, a.kv.page_shift, b);
@@ -29,69 +104,154 @@ __global__ __launch_bounds__(THREADS) void append_normed_kernel(FqAppendArgs a, 
     int page = -1;
     if (place >= 0)
         page = a.seqs.table[(long long)b * a.seqs.table_width + (place >> a.kv.page_shift)];
-    for (int i = tid; i < half; i += THREADS) {
+    for (int j = tid; j < half; j += THREADS) {
         const int pos = a.positions ? a.positions[t] : a.seqs.prefix_len + place;
-        double turns = (double)pos * (a.freqs[i] * 0.15915494309189533577);
+        double turns = (double)pos * (a.freqs[j] * 0.15915494309189533577);
         turns -= rint(turns);
-        float s, c;
-        sincospif(2.0f * (float)turns, &s, &c);
-        cs[i] = c * a.amplitude;
-        sn[i] = s * a.amplitude;
+        float s, k;
+        sincospif(2.0f * (float)turns, &s, &k);
+        cs[j] = k * a.amplitude;
+        sn[j] = s * a.amplitude;
     }
     const bool stored = page >= 0 && page < a.kv.n_pages;
     const long long at = stored ? page * a.kv.page_stride + (place & ((1 << a.kv.page_shift) - 1)) * a.kv.token_stride : 0;
     __syncthreads();
-    for (int h = wave; h < qk + a.kv.kv_heads; h += THREADS / 64) {
-        const int kind = h < a.q_heads ? 0 : h < qk ? 1 : 2, own = h - (kind == 0 ? 0 : kind == 1 ? a.q_heads : qk);
-        if (kind != 0 && !stored)
-            continue;
-        const uint16_t *row = (kind == 0 ? a.q + t * a.q_stride : kind == 1 ? a.k + t * a.k_stride : a.v + t * a.v_stride) + own * dim;
-        uint16_t *to = kind == 0 ? a.q_out + t * a.q_out_stride + own * dim : (kind == 2 ? a.kv.v : a.kv.k) + at + own * a.kv.head_stride;
-        if (kind == 2) {
-            for (int d = lane; d < dim; d += 64)
-                to[d] = row[d];
-            continue;
-        }
-        // (bfloat16 squares may leave binary32: then the head is taken 2^-70 or 2^70 times as large)
-        float f = 1.0f, mean;
-        for (int again = 0; again < 2; again++) {
-            float sum = 0.0f;
-            for (int d = lane; d < dim; d += 64) {
-                const float v = fq_to_float(row[d], bf16) * f;
-                sum += v * v;
+
+    // (a group's lanes take part in its sums together: heads past the last one are computed on and not written)
+    const int rounds = (heads + stride - 1) / stride;
+    for (int round = 0; round < rounds; round++) {
+        const int h = h0 + round * stride;
+        Head n = now;
+        if (h + stride < heads)
+            now = ask(h + stride);
+        const bool live = h < heads && (n.kind == 0 || stored);
+        if (live && n.kind != 2) {
+            float x[8], y[8], sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                x[e] = fq_to_float(n.x.v[e], BF16);
+                y[e] = fq_to_float(n.y.v[e], BF16);
             }
-            for (int off = 32; off >= 1; off >>= 1)
-                sum += __shfl_xor(sum, off, 64);
-            mean = sum / dim + norm.eps * f * f;
-            if (again || (mean >= 0x1p-100f && mean < 0x1p100f))
-                break;
-            f = mean > 1.0f ? 0x1p-70f : 0x1p70f;
-        }
-        const float inv = 1.0f / sqrtf(mean);
-        const uint16_t *w = (kind == 0 ? norm.q_weight : norm.k_weight) + own * norm.weight_stride;
-        for (int d = lane; d < dim; d += 64)
-            head[wave][d] = fq_to_float(row[d], bf16) * f * inv * (fq_to_float(w[d], bf16) + norm.offset);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        for (int d = lane; d < dim; d += 64) {
-            float v = head[wave][d];
-            if (d < a.rot) {
-                const bool low = interleaved ? (d & 1) == 0 : d < half;
-                const int pair = interleaved ? d >> 1 : low ? d : d - half;
-                const float p = head[wave][interleaved ? d ^ 1 : low ? d + half : d - half];
-                v = low ? v * cs[pair] - p * sn[pair] : v * cs[pair] + p * sn[pair];
+            // (bfloat16 squares may leave binary32: then the head is taken 2^-70 or 2^70 times as large)
+            auto mean_of = [&](float f) {
+                float own = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    own += (x[e] * f) * (x[e] * f) + (y[e] * f) * (y[e] * f);
+                return group_sum<GROUP>(own) / dim + norm.eps * f * f;
+            };
+            float f = 1.0f;
+            sum = mean_of(f);
+            if (BF16 && !(sum >= 0x1p-100f && sum < 0x1p100f)) {
+                f = sum > 1.0f ? 0x1p-70f : 0x1p70f;
+                sum = mean_of(f);
             }
-            to[d] = fq_from_float(v, bf16);
+            const float inv = 1.0f / sqrtf(sum);
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                x[e] = x[e] * f * inv * (fq_to_float(n.w.v[e], BF16) + norm.offset);
+                y[e] = y[e] * f * inv * (fq_to_float(n.w2.v[e], BF16) + norm.offset);
+            }
+            if (LAYOUT == PIECES) {
+                if (c < half >> 3) {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        const float k = cs[8 * c + e], s = sn[8 * c + e], p = x[e], q = y[e];
+                        x[e] = p * k - q * s;
+                        y[e] = q * k + p * s;
+                    }
+                }
+            } else if (LAYOUT == NEIGHBOURS) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    if (8 * c + e < a.rot) {
+                        const float k = cs[4 * c + e / 2], s = sn[4 * c + e / 2], p = x[e], q = x[e + 1];
+                        x[e] = p * k - q * s;
+                        x[e + 1] = q * k + p * s;
+                    }
+                    if (8 * c2 + e < a.rot) {
+                        const float k = cs[4 * c2 + e / 2], s = sn[4 * c2 + e / 2], p = y[e], q = y[e + 1];
+                        y[e] = p * k - q * s;
+                        y[e + 1] = q * k + p * s;
+                    }
+                }
+            } else if (16 * i < a.rot) { // (a lane that turns something; partners of its pieces are among what such lanes put there)
+                float *head = normed + tid / GROUP * (16 * GROUP);
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    head[16 * i + e] = x[e];
+                    head[16 * i + 8 + e] = y[e];
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                auto turned = [&](float p, int d) {
+                    if (d >= a.rot)
+                        return p;
+                    const bool low = d < half;
+                    const int pair = low ? d : d - half;
+                    const float q = head[low ? d + half : pair], k = cs[pair], s = sn[pair];
+                    return low ? p * k - q * s : p * k + q * s;
+                };
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    x[e] = turned(x[e], 16 * i + e);
+                    y[e] = turned(y[e], 16 * i + 8 + e);
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                n.x.v[e] = fq_from_float(x[e], BF16);
+                n.y.v[e] = fq_from_float(y[e], BF16);
+            }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        if (live) {
+            uint16_t *to = n.kind == 0 ? a.q_out + t * a.q_out_stride + n.own * dim
+                                       : (n.kind == 2 ? a.kv.v : a.kv.k) + at + n.own * a.kv.head_stride;
+            if (has)
+                *(Eight *)(to + 8 * c) = n.x;
+            if (has2)
+                *(Eight *)(to + 8 * c2) = n.y;
+        }
     }
+}
+
+template <Layout LAYOUT, bool BF16>
+void launch(const FqAppendArgs &a, const FqNormArgs &n, hipStream_t stream)
+{
+    const int lanes = (a.kv.dim / 8 + 1) / 2, group = lanes <= 4 ? 4 : lanes <= 8 ? 8 : 16;
+    const int heads = a.q_heads + 2 * a.kv.kv_heads;
+    // a token's heads over as many workgroups as there are rounds in them, where the tokens alone do not fill the chip
+    const int rounds = (heads * group + THREADS - 1) / THREADS;
+    const int room = (4 * fq_device_cus() + a.seqs.tokens - 1) / a.seqs.tokens;
+    const dim3 grid(a.seqs.tokens, rounds < room ? rounds : room);
+    if (group == 4)
+        append_normed_kernel<LAYOUT, 4, BF16><<<grid, THREADS, 0, stream>>>(a, n);
+    else if (group == 8)
+        append_normed_kernel<LAYOUT, 8, BF16><<<grid, THREADS, 0, stream>>>(a, n);
+    else
+        append_normed_kernel<LAYOUT, 16, BF16><<<grid, THREADS, 0, stream>>>(a, n);
+}
+
+template <bool BF16>
+void launch(const FqAppendArgs &a, const FqNormArgs &n, bool interleaved, hipStream_t stream)
+{
+    if (interleaved)
+        launch<NEIGHBOURS, BF16>(a, n, stream);
+    else if (a.rot % 16 == 0)
+        launch<PIECES, BF16>(a, n, stream);
+    else
+        launch<ANYHOW, BF16>(a, n, stream);
 }
 
 } // namespace
 
 hipError_t fq_launch_append_normed(const FqAppendArgs &a, const FqNormArgs &n, bool interleaved, hipStream_t stream)
 {
-    append_normed_kernel<<<a.seqs.tokens, THREADS, 0, stream>>>(a, n, interleaved);
+    if (a.kv.bf16)
+        launch<true>(a, n, interleaved, stream);
+    else
+        launch<false>(a, n, interleaved, stream);
     return hipGetLastError();
 }
