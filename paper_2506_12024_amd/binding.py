@@ -409,8 +409,10 @@ def fq_rope_freqs(rot_dim: int, base: float, kind: int = FQ_ROPE_PLAIN, factor: 
 try:
     import torch as _torch
     _F16, _BF16, _F32, _F64, _I32 = _torch.float16, _torch.bfloat16, _torch.float32, _torch.float64, _torch.int32
+    _RAW = hasattr(_torch._C, "_cuda_getDevice") and hasattr(_torch._C, "_cuda_getCurrentRawStream")  # (not public, see _stream)
 except ImportError:  # the host-only calls above work without
     _F16 = _BF16 = _F32 = _F64 = _I32 = None
+    _RAW = False
 
 
 # The calls of a decode step are short: what a small one costs is launch and marshalling, so each argument is looked at once, in
@@ -568,21 +570,22 @@ def fq_sample_f16(logits, R: int, V: int, u, token, workspace, temperature=None,
     _sample(lib.fq_sample_f16, _F16, logits, R, V, u, token, workspace, temperature, top_k, top_p, min_p, prob, stream)
 
 
-def _place(stream, *tensors):
-    """The call's stream.  Its tensors have to lie on the current device, whose streams a kernel runs on."""
-    current = _device()
-    for t in tensors:
-        if t is not None and not isinstance(t, int) and t.get_device() != current:
-            raise ValueError("a tensor lies on %s, the current device is cuda:%d" % (t.device, current))
-    return _stream(stream)
-
-
-def _device():
+def _place(stream, first, *others):
+    """The call's stream.  Its tensors (``first`` is one; the others may be None or raw pointers) have to lie on the current device, whose
+    streams a kernel runs on."""
     import torch
-    if torch.cuda.is_initialized():
-        get = getattr(torch._C, "_cuda_getDevice", None)
-        return get() if get else torch.cuda.current_device()
-    return 0
+    device = first.get_device()
+    for t in others:
+        if t is not None and t.__class__ is not int and t.get_device() != device:
+            raise ValueError("tensors lie on %s and %s" % (first.device, t.device))
+    if device < 0:
+        raise ValueError("a tensor lies on %s" % first.device)
+    current = torch._C._cuda_getDevice() if _RAW else torch.cuda.current_device()
+    if device != current:
+        raise ValueError("the tensors lie on cuda:%d, the current device is cuda:%d" % (device, current))
+    if stream is None and _RAW:
+        return torch._C._cuda_getCurrentRawStream(device)
+    return _stream(stream)
 
 
 def _flat(t, name):

@@ -19,7 +19,7 @@ namespace {
 constexpr int THREADS = 256, WAVES = THREADS / 64;
 constexpr int FEW_ROWS = 64, FEW_TILE = 16, FEW_ELEMENTS = 1 << 18, TILE = 64;
 constexpr int MIDDLE_ROWS = 4096, MIDDLE_SLOTS = 1023;
-constexpr int GROUP_THREADS = 1024, OUT_THREADS = 512;
+constexpr int GROUP_THREADS = 1024, OUT_THREADS = 512, MANY_THREADS = 256, JOIN_THREADS = 256, JOIN_ROWS = JOIN_THREADS / 16;
 constexpr int CHUNK = 256, MAX_PARTS = 16; // of K
 enum Find { COUNTED, LISTED }; // how a workgroup of low_kernel finds its tile: by itself, or in the workspace's list
 
@@ -45,7 +45,9 @@ struct Work {
     float *low;
     int *rows;
     Tile *tiles;
-    int parts, max_tiles;
+    u32x4 *operands; // u as out_kernel's operands, tile_operands to a tile
+    float *factor;   // [tile][TILE]
+    int parts, max_tiles, tile_operands;
 };
 
 // Whether a call is one launch: every workgroup of a tile reads its slot's A whole, which is less than the second launch and the parts while A
@@ -70,6 +72,8 @@ size_t low_rows(int M)
     return MAX_PARTS * m < most ? MAX_PARTS * m : most;
 }
 
+int tile_operands(const FqAdaptersView &set) { return (set.rank + 31) / 32 * (TILE / 16) * 2 * 64; } // 16 bytes each
+
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
 // What a wavefront hands to itself through LDS: its operations there are in order, the compiler has to keep them so.
@@ -77,6 +81,18 @@ __device__ __forceinline__ void own_fence()
 {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+}
+
+// The sum over this lane and those before it.
+__device__ __forceinline__ int sum_upto(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false); // within rows of 16: one, two, four, eight lanes down
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false); // the last lane of rows 0 and 2 to rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false); // lane 31 to rows 2 and 3
+    return x;
 }
 
 // A row's adapter, or -1.
@@ -93,6 +109,31 @@ __device__ __forceinline__ int rank_of(const FqAdaptersArgs &a, int slot)
     return a.set.ranks ? min(max(a.set.ranks[slot], 0), a.set.rank) : a.set.rank;
 }
 
+// Ranks and scales of the first slots, a lane to each, asked for beside the rows' slots: one trip to memory fewer where a slot is among them.
+struct Some {
+    int rank;
+    float scale;
+    __device__ __forceinline__ explicit Some(const FqAdaptersArgs &a)
+    {
+        const int s = min((int)threadIdx.x & 63, a.set.slots - 1);
+        rank = a.set.ranks ? a.set.ranks[s] : a.set.rank;
+        scale = a.set.scales ? a.set.scales[s] : 1.0f;
+    }
+    // (slot is the same in all lanes)
+    __device__ __forceinline__ void of(const FqAdaptersArgs &a, int slot, int &r, float &s) const
+    {
+        r = 0;
+        s = 1.0f;
+        if (slot >= 64) {
+            r = rank_of(a, slot);
+            s = a.set.scales ? a.set.scales[slot] : 1.0f;
+        } else if (slot >= 0) {
+            r = min(max(__builtin_amdgcn_readlane(rank, slot), 0), a.set.rank);
+            s = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scale), slot));
+        }
+    }
+};
+
 __device__ __forceinline__ Tile find_listed(const Work &w, int *rows)
 {
     const Tile t = w.tiles[blockIdx.x];
@@ -103,14 +144,12 @@ __device__ __forceinline__ Tile find_listed(const Work &w, int *rows)
 }
 
 // What one of a tile's workgroups leaves for the second launch.
-__device__ __forceinline__ void leave(const FqAdaptersArgs &a, const Work &w, const int *rows, Tile t)
+__device__ __forceinline__ void leave(const Work &w, const int *rows, const Tile &t)
 {
     if (blockIdx.y != 0 || blockIdx.z != 0)
         return;
-    if (threadIdx.x == 0) {
-        t.scale = t.slot >= 0 && a.set.scales ? a.set.scales[t.slot] : 1.0f;
+    if (threadIdx.x == 0)
         w.tiles[blockIdx.x] = t;
-    }
     if ((int)threadIdx.x < t.count)
         w.rows[TILE * blockIdx.x + threadIdx.x] = rows[threadIdx.x];
 }
@@ -121,7 +160,7 @@ __device__ __forceinline__ int find_counted(const FqAdaptersArgs &a, int *rows, 
 {
     constexpr int PER = MIDDLE_ROWS / THREADS;
     __shared__ int found[2], each[MIDDLE_ROWS / 64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, keys = a.set.slots + 1;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), keys = a.set.slots + 1;
     int key[PER]; // rows i * THREADS + tid
 #pragma unroll
     for (int i = 0; i < PER; i++) {
@@ -153,18 +192,14 @@ __device__ __forceinline__ int find_counted(const FqAdaptersArgs &a, int *rows, 
         int begun = 0;
         for (int k0 = 0; k0 < keys; k0 += 64) {
             const int n = k0 + lane < keys ? (count[k0 + lane] + TILE - 1) / TILE : 0;
-            int upto = n;
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const int t = __shfl_up(upto, off, 64);
-                upto += lane >= off ? t : 0;
-            }
-            const int from = begun + upto - n;
+            const int upto = sum_upto(n), from = begun + upto - n;
             if ((int)blockIdx.x >= from && (int)blockIdx.x < from + n) {
                 found[0] = k0 + lane;
                 found[1] = ((int)blockIdx.x - from) * TILE;
             }
-            begun += __shfl(upto, 63, 64);
+            begun += __builtin_amdgcn_readlane(upto, 63);
+            if (begun > (int)blockIdx.x)
+                break;
         }
     }
     __syncthreads();
@@ -181,18 +216,12 @@ __device__ __forceinline__ int find_counted(const FqAdaptersArgs &a, int *rows, 
     __syncthreads();
     const int total = min(count[mine] - skip, TILE);
     static_assert(MIDDLE_ROWS == 64 * 64, "a lane to 64 rows");
-    int upto = each[lane];
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int t = __shfl_up(upto, off, 64);
-        upto += lane >= off ? t : 0;
-    }
-    upto -= each[lane];
+    const int upto = sum_upto(each[lane]) - each[lane];
 #pragma unroll
     for (int i = 0; i < PER; i++) {
         if (i * THREADS >= a.M)
             break;
-        const int before = __shfl(upto, i * WAVES + wave, 64) - skip;
+        const int before = __builtin_amdgcn_readlane(upto, i * WAVES + wave) - skip;
         const int at = before + (int)__popcll(mask[i] & ((1ull << lane) - 1));
         if (key[i] == mine && at >= 0 && at < TILE)
             rows[at] = i * THREADS + tid;
@@ -233,12 +262,7 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_kernel(FqAdaptersArgs a, 
     int tiles = 0; // of the slots before these
     for (int k0 = 0; k0 < keys; k0 += GROUP_THREADS) {
         const int k = k0 + tid, n = k < keys ? count[k] : 0, t = (n + TILE - 1) / TILE;
-        int tile = t;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int q = __shfl_up(tile, off, 64);
-            tile += lane >= off ? q : 0;
-        }
+        int tile = sum_upto(t);
         if (lane == 63)
             sums[wave] = tile;
         __syncthreads();
@@ -267,47 +291,25 @@ __global__ __launch_bounds__(GROUP_THREADS) void group_kernel(FqAdaptersArgs a, 
     }
 }
 
-// The sums that the wavefronts of a workgroup have of the same u, in one order; the first wavefront's become whole.
-template <int TILES>
-__device__ __forceinline__ void join_waves(float4_t (&acc)[TILES], float4_t (*sums)[TILES][64])
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int half = WAVES / 2; half >= 1; half /= 2) {
-        if (wave >= half && wave < 2 * half) {
-#pragma unroll
-            for (int i = 0; i < TILES; i++)
-                sums[wave - half][i][lane] = acc[i];
-        }
-        __syncthreads();
-        if (wave < half) {
-#pragma unroll
-            for (int i = 0; i < TILES; i++)
-                acc[i] += sums[wave][i][lane];
-        }
-        __syncthreads();
-    }
-}
-
 // u = x A^T of a tile of up to 64 rows: 16 RT ranks from 16 RT blockIdx.z on, the part blockIdx.y of K, 256 at a time.  32 lanes ask for 512
-// bytes of a row; a row's piece p lies at place p ^ (row % 16).  A wavefront multiplies a quarter of what is in LDS while the next is on its way.
+// bytes of a row, two chunks ahead; a row's piece p lies at place p ^ (row % 16).  A wavefront has 16 of the rows.
 template <int RT, bool BF16, Find FIND>
-__global__ __launch_bounds__(THREADS) void low_kernel(FqAdaptersArgs a, Work w)
+__global__ __launch_bounds__(THREADS, 1) void low_kernel(FqAdaptersArgs a, Work w)
 {
-    constexpr int TT = TILE / 16, PIECES = CHUNK / 8, ROWS_A_TURN = THREADS / PIECES, X_TURNS = TILE / ROWS_A_TURN,
-                  A_TURNS = 16 * RT / ROWS_A_TURN;
+    constexpr int PIECES = CHUNK / 8, ROWS_A_TURN = THREADS / PIECES, X_TURNS = TILE / ROWS_A_TURN, A_TURNS = 16 * RT / ROWS_A_TURN;
     __shared__ int rows[TILE];
     __shared__ u32x4 tile[(TILE + 16 * RT) * PIECES];
-    static_assert(sizeof(tile) >= (MIDDLE_SLOTS + 1) * sizeof(int) && sizeof(tile) >= WAVES / 2 * TT * RT * 64 * sizeof(float4_t), "");
-    static_assert(THREADS == WAVES * 64 && CHUNK == 64 * WAVES, "a wavefront to 64 of a chunk");
+    static_assert(sizeof(tile) >= (MIDDLE_SLOTS + 1) * sizeof(int) && TILE == 16 * WAVES, "");
     Tile own;
     if (FIND == LISTED) {
         own = find_listed(w, rows);
     } else {
+        const Some some(a);
         own.slot = -1;
         own.count = find_counted(a, rows, own.slot, (int *)tile);
-        own.rank = own.count ? rank_of(a, own.slot) : 0;
-        leave(a, w, rows, own);
+        own.slot = __builtin_amdgcn_readfirstlane(own.slot);
+        some.of(a, own.count ? own.slot : -1, own.rank, own.scale);
+        leave(w, rows, own);
     }
     const int slot = own.slot, count = own.count, rank = own.rank, r0 = 16 * RT * blockIdx.z;
     if (r0 >= rank)
@@ -319,74 +321,80 @@ __global__ __launch_bounds__(THREADS) void low_kernel(FqAdaptersArgs a, Work w)
     const uint16_t *xp[X_TURNS], *ap = a.set.a + slot * a.set.a_stride;
 #pragma unroll
     for (int i = 0; i < X_TURNS; i++)
-        xp[i] = a.x + rows[min(row0 + i * ROWS_A_TURN, count - 1)] * a.x_stride + 8 * piece;
-    u32x4 xv[X_TURNS], av[A_TURNS];
-    auto ask = [&](int c) {
-        const int k = CHUNK * c + 8 * piece;
-        const bool in = k < K;
+        xp[i] = a.x + rows[min(row0 + i * ROWS_A_TURN, count - 1)] * a.x_stride;
+    struct Step {
+        u32x4 x[X_TURNS], a[A_TURNS];
+    };
+    // (rows beyond the last are the last again, and not used)
+    auto ask = [&](Step &s, int c) {
+        const int k = min(CHUNK * c + 8 * piece, K - 8);
 #pragma unroll
         for (int i = 0; i < X_TURNS; i++)
-            xv[i] = in && row0 + i * ROWS_A_TURN < count ? *(const u32x4 *)(xp[i] + CHUNK * c) : u32x4{0, 0, 0, 0};
+            s.x[i] = *(const u32x4 *)(xp[i] + k);
 #pragma unroll
         for (int i = 0; i < A_TURNS; i++)
-            av[i] = in ? *(const u32x4 *)(ap + (size_t)min(r0 + row0 + i * ROWS_A_TURN, rank - 1) * K + k) : u32x4{0, 0, 0, 0};
+            s.a[i] = *(const u32x4 *)(ap + (size_t)min(r0 + row0 + i * ROWS_A_TURN, rank - 1) * K + k);
     };
-    float4_t acc[TT * RT] = {};
-    if (from < end)
-        ask(from);
-    __syncthreads(); // (the counts lay where the chunk goes)
-    for (int c = from; c < end; c++) {
+    float4_t acc[RT] = {};
+    auto use = [&](Step &s, int c) {
+        if (CHUNK * (c + 1) > K && CHUNK * c + 8 * piece >= K) { // behind the end of K
+#pragma unroll
+            for (int i = 0; i < X_TURNS; i++)
+                s.x[i] = u32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < A_TURNS; i++)
+                s.a[i] = u32x4{0, 0, 0, 0};
+        }
 #pragma unroll
         for (int i = 0; i < X_TURNS; i++) {
             const int row = row0 + i * ROWS_A_TURN;
-            tile[row * PIECES + (piece ^ (row & 15))] = xv[i];
+            tile[row * PIECES + (piece ^ (row & 15))] = s.x[i];
         }
 #pragma unroll
         for (int i = 0; i < A_TURNS; i++) {
             const int row = TILE + row0 + i * ROWS_A_TURN;
-            tile[row * PIECES + (piece ^ (row & 15))] = av[i];
+            tile[row * PIECES + (piece ^ (row & 15))] = s.a[i];
         }
         __syncthreads();
-        if (c + 1 < end)
-            ask(c + 1);
+        if (c + 2 < end)
+            ask(s, c + 2);
+        if (16 * wave < count) {
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const int at = (8 * wave + 4 * h + g) ^ col;
-            u32x4 xf[TT], af[RT];
-#pragma unroll
-            for (int t = 0; t < TT; t++)
-                xf[t] = tile[(16 * t + col) * PIECES + at];
-#pragma unroll
-            for (int r = 0; r < RT; r++)
-                af[r] = tile[(TILE + 16 * r + col) * PIECES + at];
-#pragma unroll
-            for (int t = 0; t < TT; t++)
+            for (int h = 0; h < PIECES / 4; h++) {
+                const int at = (4 * h + g) ^ col;
+                const u32x4 x = tile[(16 * wave + col) * PIECES + at];
 #pragma unroll
                 for (int r = 0; r < RT; r++)
-                    acc[t * RT + r] = mfma<BF16>(af[r], xf[t], acc[t * RT + r]);
+                    acc[r] = mfma<BF16>(tile[(TILE + 16 * r + col) * PIECES + at], x, acc[r]);
+            }
         }
         __syncthreads();
+    };
+    Step even, odd;
+    if (from < end)
+        ask(even, from);
+    if (from + 1 < end)
+        ask(odd, from + 1);
+    __syncthreads(); // (the counts lay where the chunk goes)
+    for (int c = from; c < end; c += 2) {
+        use(even, c);
+        if (c + 1 < end)
+            use(odd, c + 1);
     }
-    join_waves(acc, (float4_t(*)[TT * RT][64])tile);
-    if (wave != 0)
-        return;
-#pragma unroll
-    for (int t = 0; t < TT; t++) {
-        if (16 * t + col >= count)
-            continue;
-        float *to = w.low + ((size_t)blockIdx.y * a.M + rows[16 * t + col]) * a.set.rank + r0 + 4 * g;
+    if (16 * wave + col < count) {
+        float *to = w.low + ((size_t)blockIdx.y * a.M + rows[16 * wave + col]) * a.set.rank + r0 + 4 * g;
 #pragma unroll
         for (int r = 0; r < RT; r++)
             if (r0 + 16 * r + 4 * g < a.set.rank)
-                *(float4_t *)(to + 16 * r) = acc[t * RT + r];
+                *(float4_t *)(to + 16 * r) = acc[r];
     }
 }
 
 // The last step: 64 outputs of 16 TT rows to a wavefront and turn, out = y + factor u B^T.  u lies in LDS as the first operands' registers, 32
-// ranks to an instruction, hi and lo: [rank / 32][TT][2][64].  Column c of instruction j of four is output 4 c + j, so that a lane's results of the four
+// ranks to an instruction, hi and lo: [rank / 32][ALL][2][64].  Column c of instruction j of four is output 4 c + j, so that a lane's results of the four
 // are four outputs that follow each other, 128 bytes of a row to sixteen lanes.  B comes 32 ranks of 64 outputs at a time, through 4 KB of
-// LDS of the wavefront's own; that of the first 32 AHEAD ranks, and y, are asked for a turn ahead.
-template <int TT, int AHEAD, bool BF16, bool VEC>
+// LDS of the wavefront's own; that of the first 32 AHEAD ranks is asked for beside y.
+template <int TT, int ALL, int AHEAD, bool BF16, bool VEC>
 struct Out {
     const FqAdaptersArgs &a;
     const int *rows;
@@ -400,19 +408,18 @@ struct Out {
         uint2 y[VEC ? TT : 1][4];
     };
 
+    // (what lies outside is loaded from inside and not used: a condition around each load is a branch around each)
     __device__ __forceinline__ void ask_b(u32x4 (&v)[4], int block, int c) const
     {
-        const int lane = threadIdx.x & 63, r = 32 * c + 8 * (lane & 3);
+        const int lane = threadIdx.x & 63, r = min(32 * c + 8 * (lane & 3), a.set.rank - 8);
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int n = 64 * block + 16 * i + (lane >> 2);
-            v[i] = n < a.set.N && r < rank ? *(const u32x4 *)(b + (size_t)n * a.set.rank + r) : u32x4{0, 0, 0, 0};
-        }
+        for (int i = 0; i < 4; i++)
+            v[i] = *(const u32x4 *)(b + (size_t)min(64 * block + 16 * i + (lane >> 2), a.set.N - 1) * a.set.rank + r);
     }
 
     __device__ __forceinline__ void ask(Turn &k, int block) const
     {
-        const int lane = threadIdx.x & 63, n = 64 * block + 4 * (lane & 15);
+        const int lane = threadIdx.x & 63, n = min(64 * block + 4 * (lane & 15), a.set.N - 4);
         ask_b(k.b[0], block, 0);
         if (AHEAD > 1 && chunks > 1)
             ask_b(k.b[AHEAD - 1], block, 1);
@@ -420,17 +427,15 @@ struct Out {
 #pragma unroll
             for (int t = 0; t < TT; t++)
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const int row = 16 * t + 4 * (lane >> 4) + i;
-                    k.y[t][i] = row < count && n < a.set.N ? *(const uint2 *)(a.y + rows[row] * a.y_stride + n) : make_uint2(0, 0);
-                }
+                for (int i = 0; i < 4; i++)
+                    k.y[t][i] = *(const uint2 *)(a.y + rows[min(16 * t + 4 * (lane >> 4) + i, count - 1)] * a.y_stride + n);
         }
     }
 
     __device__ __forceinline__ void multiply(float4_t (&acc)[TT][4], u32x4 (&v)[4], int c) const
     {
         const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
-        if (rank & 7) { // (what lies behind a rank may be anything)
+        if (32 * c + 32 > rank) { // (what lies behind a rank may be anything)
             const int r = 32 * c + 8 * (lane & 3);
 #pragma unroll
             for (int i = 0; i < 4; i++) {
@@ -456,7 +461,7 @@ struct Out {
         for (int t = 0; t < TT; t++) {
             if (16 * t >= count)
                 break;
-            const u32x4 hi = low[(c * TT + t) * 128 + lane], lo = low[(c * TT + t) * 128 + 64 + lane];
+            const u32x4 hi = low[(c * ALL + t) * 128 + lane], lo = low[(c * ALL + t) * 128 + 64 + lane];
 #pragma unroll
             for (int j = 0; j < 4; j++)
                 acc[t][j] = mfma<BF16>(lo, bv[j], mfma<BF16>(hi, bv[j], acc[t][j]));
@@ -474,7 +479,8 @@ struct Out {
                 if (row >= count || n >= a.set.N)
                     continue;
                 const float f = factor[row];
-                uint16_t *out = a.out + rows[row] * a.out_stride + n;
+                const int m = rows[row];
+                uint16_t *out = a.out + m * a.out_stride + n;
                 if (VEC) {
                     const uint2 y = k.y[t][i];
                     const uint16_t v0 = fq_from_float(fq_to_float((uint16_t)y.x, BF16) + f * acc[t][0][i], BF16);
@@ -483,7 +489,7 @@ struct Out {
                     const uint16_t v3 = fq_from_float(fq_to_float((uint16_t)(y.y >> 16), BF16) + f * acc[t][3][i], BF16);
                     *(uint2 *)out = make_uint2(v0 | (uint32_t)v1 << 16, v2 | (uint32_t)v3 << 16);
                 } else {
-                    const uint16_t *y = a.y + rows[row] * a.y_stride + n;
+                    const uint16_t *y = a.y + m * a.y_stride + n;
 #pragma unroll
                     for (int j = 0; j < 4; j++)
                         if (n + j < a.set.N)
@@ -492,25 +498,23 @@ struct Out {
             }
     }
 
-    // The blocks first, first + stride ...; `now`: what was asked for the first.
-    __device__ __forceinline__ void run(Turn &now, int first, int stride) const
+    // The blocks first, first + stride ...; k: what was asked for the first.  (A turn ahead in registers would cost half of the wavefronts, which hide more.)
+    __device__ __forceinline__ void run(Turn &k, int first, int stride) const
     {
         const int blocks = (a.set.N + 63) / 64;
-        Turn next;
         for (int block = first; block < blocks; block += stride) {
-            if (block + stride < blocks)
-                ask(next, block + stride);
+            if (block != first)
+                ask(k, block);
             float4_t acc[TT][4] = {};
-            multiply(acc, now.b[0], 0);
+            multiply(acc, k.b[0], 0);
             if (AHEAD > 1 && chunks > 1)
-                multiply(acc, now.b[AHEAD - 1], 1);
+                multiply(acc, k.b[AHEAD - 1], 1);
             for (int c = AHEAD; c < chunks; c++) {
                 u32x4 v[4];
                 ask_b(v, block, c);
                 multiply(acc, v, c);
             }
-            finish(now, acc, block);
-            now = next;
+            finish(k, acc, block);
         }
     }
 };
@@ -559,68 +563,87 @@ __device__ __forceinline__ float finite(const float4_t v)
     return most;
 }
 
-// out = y + scale u B^T of a tile, u in parts.
-template <bool BF16, bool VEC>
-__global__ __launch_bounds__(OUT_THREADS) void out_kernel(FqAdaptersArgs a, Work w)
+// The parts of a tile's u as the operands of the last launch: the tile's piece of `low`, and the rows' factors.  (In the last launch every workgroup of a
+// tile would read all parts, 131 KB for 64 ranks in 8 parts: for a prompt of 2048 40 us, 22 and 3 here.)  64 C ranks at most.
+template <int C, bool BF16>
+__global__ __launch_bounds__(JOIN_THREADS) void join_kernel(FqAdaptersArgs a, Work w)
 {
-    constexpr int TT = TILE / 16, WAVES = OUT_THREADS / 64;
+    constexpr int ALL = TILE / 16;
+    const int tid = threadIdx.x;
+    const Tile own = w.tiles[blockIdx.x];
+    const int count = own.count, rank = own.rank;
+    if (JOIN_ROWS * (int)blockIdx.y >= count || rank == 0)
+        return;
+    // 16 threads to a row, four ranks to a thread and 64
+    const int row = JOIN_ROWS * blockIdx.y + (tid >> 4), mine = 4 * (tid & 15), chunks = (rank + 31) / 32;
+    const size_t apart = (size_t)a.M * a.set.rank;
+    const float *from = w.low + (size_t)w.rows[TILE * blockIdx.x + min(row, count - 1)] * a.set.rank;
+    float4_t u[C];
+    float most = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; c++) {
+        const int r = 64 * c + mine;
+        u[c] = float4_t{0, 0, 0, 0};
+        if (64 * c < rank && r < rank) {
+            for (int p0 = 0; p0 < w.parts; p0 += 8) { // eight asked for together
+                float4_t part[8];
+#pragma unroll
+                for (int p = 0; p < 8; p++)
+                    part[p] = *(const float4_t *)(from + (size_t)min(p0 + p, w.parts - 1) * apart + r);
+#pragma unroll
+                for (int p = 0; p < 8; p++)
+                    if (p0 + p < w.parts)
+                        u[c] += part[p];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                u[c][i] = r + i < rank ? u[c][i] : 0.0f;
+            most = fmaxf(most, finite(u[c]));
+        }
+    }
+#pragma unroll
+    for (int off = 8; off >= 1; off >>= 1)
+        most = fmaxf(most, __shfl_xor(most, off, 64));
+    const int e = power_of<BF16>(most);
+    if (mine == 0)
+        w.factor[TILE * blockIdx.x + row] = ldexpf(own.scale, -e);
+    u32x4 *low = w.operands + (size_t)blockIdx.x * w.tile_operands;
+#pragma unroll
+    for (int c = 0; c < C; c++)
+        if (64 * c < rank && 64 * c + mine < 32 * chunks)
+            put_low<ALL, BF16>(low, u[c], e, row, 64 * c + mine);
+}
+
+// out = y + scale u B^T of a tile.  A wavefront has half of the tile's rows: with all of them 238 registers leave one workgroup to a compute unit.
+template <bool BF16, bool VEC>
+__global__ __launch_bounds__(MANY_THREADS, 3) void out_kernel(FqAdaptersArgs a, Work w)
+{
+    constexpr int ALL = TILE / 16, TT = ALL / 2, COLUMNS = MANY_THREADS / 128;
     __shared__ int rows[TILE];
     __shared__ float factor[TILE];
-    __shared__ u32x4 b_of[WAVES][256];
-    extern __shared__ u32x4 low[]; // [rank / 32][TT][2][64]
-    const int tid = threadIdx.x, wave = tid >> 6;
+    __shared__ u32x4 b_of[MANY_THREADS / 64][256];
+    extern __shared__ u32x4 low[]; // [rank / 32][ALL][2][64]
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row0 = 16 * TT * (wave & 1);
+    if (tid < TILE)
+        factor[tid] = w.factor[TILE * blockIdx.x + tid];
     const Tile own = find_listed(w, rows);
     const int count = own.count, rank = own.rank;
     if (count == 0)
         return;
-    const int first = blockIdx.y * WAVES + wave, stride = gridDim.y * WAVES;
+    const int first = blockIdx.y * COLUMNS + (wave >> 1), stride = gridDim.y * COLUMNS;
     if (rank == 0)
-        return copy_rows(a, rows, count, first, stride);
-    const Out<TT, 2, BF16, VEC> o{a, rows, factor, low, b_of[wave], a.set.b + own.slot * a.set.b_stride, count, rank, (rank + 31) / 32};
-    typename Out<TT, 2, BF16, VEC>::Turn now;
+        return copy_rows(a, rows + row0, min(count - row0, 16 * TT), first, stride);
+    const Out<TT, ALL, 1, BF16, VEC> o{a, rows + row0, factor + row0, low + TT * 128 * (wave & 1), b_of[wave],
+                                       a.set.b + own.slot * a.set.b_stride, count - row0, rank, (rank + 31) / 32};
+    const u32x4 *from = w.operands + (size_t)blockIdx.x * w.tile_operands;
+    for (int i = tid; i < o.chunks * ALL * 128; i += MANY_THREADS)
+        low[i] = from[i];
+    typename Out<TT, ALL, 1, BF16, VEC>::Turn now;
     if (64 * first < a.set.N)
         o.ask(now, first);
-
-    // as many threads to a row as its ranks, or those of whole instructions, take four at a time, up to 16; what a turn adds is asked for together
-    const int wide = rank <= 32 ? 8 : 16, turn = OUT_THREADS / wide, mine = 4 * (tid & (wide - 1));
-    const size_t apart = (size_t)a.M * a.set.rank;
-    for (int row = tid / wide; row < TILE; row += turn) {
-        const float *from = w.low + (size_t)rows[row < count ? row : 0] * a.set.rank;
-        float4_t u[FQ_MAX_ADAPTER_RANK / 64];
-        float most = 0.0f;
-#pragma unroll
-        for (int c = 0; c < FQ_MAX_ADAPTER_RANK / 64; c++) {
-            const int r = 64 * c + mine;
-            u[c] = float4_t{0, 0, 0, 0};
-            if (64 * c < rank && r < rank) {
-                for (int p0 = 0; p0 < w.parts; p0 += 8) {
-                    float4_t part[8];
-#pragma unroll
-                    for (int p = 0; p < 8; p++)
-                        part[p] = *(const float4_t *)(from + (size_t)min(p0 + p, w.parts - 1) * apart + r);
-#pragma unroll
-                    for (int p = 0; p < 8; p++)
-                        if (p0 + p < w.parts)
-                            u[c] += part[p];
-                }
-#pragma unroll
-                for (int i = 0; i < 4; i++)
-                    u[c][i] = r + i < rank ? u[c][i] : 0.0f;
-                most = fmaxf(most, finite(u[c]));
-            }
-        }
-        for (int off = wide / 2; off >= 1; off >>= 1)
-            most = fmaxf(most, __shfl_xor(most, off, 64));
-        const int e = power_of<BF16>(most);
-        if (mine == 0)
-            factor[row] = ldexpf(own.scale, -e);
-#pragma unroll
-        for (int c = 0; c < FQ_MAX_ADAPTER_RANK / 64; c++)
-            if (64 * c < rank && 64 * c + mine < 32 * o.chunks)
-                put_low<TT, BF16>(low, u[c], e, row, 64 * c + mine);
-    }
     __syncthreads();
-    o.run(now, first, stride);
+    if (row0 < count)
+        o.run(now, first, stride);
 }
 
 // Few rows, one launch: the tile that row blockIdx.x leads (the rows of its slot before it fill whole tiles), the outputs that are blockIdx.y's.  A
@@ -637,11 +660,9 @@ __global__ __launch_bounds__(OUT_THREADS, 4) void few_kernel(FqAdaptersArgs a)
     __shared__ u32x4 lds[WAVES][OWN > 256 ? OWN : 256];
     static_assert(RT * 64 <= OWN, "the sums of a wavefront");
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
-    // (ranks and scales of the first slots beside the rows' slots: one trip to memory fewer)
-    const int some_rank = a.set.ranks ? a.set.ranks[min(lane, a.set.slots - 1)] : 0;
-    const float some_scale = a.set.scales ? a.set.scales[min(lane, a.set.slots - 1)] : 0.0f;
+    const Some some(a);
     const int found = lane < a.M ? slot_of(a, lane) : -2, lead = blockIdx.x;
-    const int slot = __shfl(found, lead, 64);
+    const int slot = __builtin_amdgcn_readlane(found, lead);
     const uint64_t same = __ballot(found == slot);
     const int before = __popcll(same & ((1ull << lead) - 1)), at = __popcll(same & ((1ull << lane) - 1)) - before;
     if (before % FEW_TILE != 0)
@@ -649,29 +670,30 @@ __global__ __launch_bounds__(OUT_THREADS, 4) void few_kernel(FqAdaptersArgs a)
     const int count = min((int)__popcll(same) - before, FEW_TILE);
     if (wave == 0 && found == slot && at >= 0 && at < FEW_TILE)
         rows[at] = lane;
-    int rank = slot < 0 ? 0 : a.set.rank;
-    float scale = 1.0f;
-    if (slot >= 0 && a.set.ranks)
-        rank = min(max(slot < 64 ? __shfl(some_rank, slot, 64) : a.set.ranks[slot], 0), a.set.rank);
-    if (slot >= 0 && a.set.scales)
-        scale = slot < 64 ? __shfl(some_scale, slot, 64) : a.set.scales[slot];
+    int rank;
+    float scale;
+    some.of(a, slot, rank, scale);
     __syncthreads();
     const int first = blockIdx.y * WAVES + wave, stride = gridDim.y * WAVES;
     if (rank == 0)
         return copy_rows(a, rows, count, first, stride);
     const int K = a.set.K, piece = lane % PIECES, row0 = lane / PIECES;
-    const uint16_t *ap = a.set.a + slot * a.set.a_stride + 8 * piece, *xp = a.x + 8 * piece;
+    const uint16_t *ap = a.set.a + slot * a.set.a_stride, *xp[X_TURNS];
+#pragma unroll
+    for (int i = 0; i < X_TURNS; i++)
+        xp[i] = a.x + rows[min(row0 + i * LANES, count - 1)] * a.x_stride;
     struct Step {
         u32x4 x[X_TURNS], a[A_TURNS];
     };
+    // (rows beyond the last are the last again, and not used)
     auto ask = [&](Step &s, int k) {
-        const bool in = k + 8 * piece < K;
+        const int at = min(k + 8 * piece, K - 8);
 #pragma unroll
         for (int i = 0; i < A_TURNS; i++)
-            s.a[i] = in && row0 + i * LANES < rank ? *(const u32x4 *)(ap + (size_t)(row0 + i * LANES) * K + k) : u32x4{0, 0, 0, 0};
+            s.a[i] = *(const u32x4 *)(ap + (size_t)min(row0 + i * LANES, rank - 1) * K + at);
 #pragma unroll
         for (int i = 0; i < X_TURNS; i++)
-            s.x[i] = in && row0 + i * LANES < count ? *(const u32x4 *)(xp + rows[row0 + i * LANES] * a.x_stride + k) : u32x4{0, 0, 0, 0};
+            s.x[i] = *(const u32x4 *)(xp[i] + at);
     };
     auto place = [&](int row, int p) -> u32x4 & {
         return lds[wave][row * PIECES + (p ^ ((PIECES >= 8 ? row : row >> 1) & (PIECES - 1)))];
@@ -679,6 +701,14 @@ __global__ __launch_bounds__(OUT_THREADS, 4) void few_kernel(FqAdaptersArgs a)
     float4_t acc[RT] = {};
     constexpr int STEP = 8 * PIECES, APART = STEP * WAVES;
     auto use = [&](Step &s, int k) {
+        if (k + STEP > K && k + 8 * piece >= K) { // behind the end of K
+#pragma unroll
+            for (int i = 0; i < A_TURNS; i++)
+                s.a[i] = u32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < X_TURNS; i++)
+                s.x[i] = u32x4{0, 0, 0, 0};
+        }
 #pragma unroll
         for (int i = 0; i < A_TURNS; i++)
             place(16 + row0 + i * LANES, piece) = s.a[i];
@@ -708,8 +738,8 @@ __global__ __launch_bounds__(OUT_THREADS, 4) void few_kernel(FqAdaptersArgs a)
         if (k + APART < K)
             use(odd, k + APART);
     }
-    const Out<1, CHUNKS, BF16, VEC> o{a, rows, factor, low, lds[wave], a.set.b + slot * a.set.b_stride, count, rank, (rank + 31) / 32};
-    typename Out<1, CHUNKS, BF16, VEC>::Turn now;
+    const Out<1, 1, CHUNKS, BF16, VEC> o{a, rows, factor, low, lds[wave], a.set.b + slot * a.set.b_stride, count, rank, (rank + 31) / 32};
+    typename Out<1, 1, CHUNKS, BF16, VEC>::Turn now;
     if (64 * first < a.set.N)
         o.ask(now, first);
     // u[rank 16 r + 4 g + i][row col] of each wavefront
@@ -776,15 +806,23 @@ hipError_t launch_many(const FqAdaptersArgs &a, const Work &w, hipStream_t strea
         launch_low<4, BF16, FIND>(a, w, stream);
     if (hipError_t e = hipGetLastError())
         return e;
-    // outputs over as many workgroups as fill the chip
-    const int blocks = (a.set.N + 63) / 64, tiles = (a.M + TILE - 1) / TILE;
-    const int most = (blocks + OUT_THREADS / 64 - 1) / (OUT_THREADS / 64), room = (256 + tiles - 1) / tiles;
-    const dim3 grid(w.max_tiles, most < room ? most : room);
-    const size_t lds = (size_t)(a.set.rank + 31) / 32 * (TILE / 16) * 2 * 64 * sizeof(u32x4);
+    const dim3 join_grid(w.max_tiles, TILE / JOIN_ROWS);
+    if (a.set.rank <= 64)
+        join_kernel<1, BF16><<<join_grid, JOIN_THREADS, 0, stream>>>(a, w);
+    else
+        join_kernel<FQ_MAX_ADAPTER_RANK / 64, BF16><<<join_grid, JOIN_THREADS, 0, stream>>>(a, w);
+    if (hipError_t e = hipGetLastError())
+        return e;
+    // outputs over as many workgroups as fill the chip, three to a compute unit
+    const int blocks = (a.set.N + 63) / 64, tiles = (a.M + TILE - 1) / TILE + 1, columns = MANY_THREADS / 128;
+    const int most = (blocks + columns - 1) / columns, room = 768 / tiles > 1 ? 768 / tiles : 1;
+    const int turns = (most + room - 1) / room;
+    const dim3 grid(w.max_tiles, (most + turns - 1) / turns);
+    const size_t lds = (size_t)w.tile_operands * sizeof(u32x4);
     if (lds > 16384)
         if (hipError_t e = fq_raise_dynamic_lds((const void *)out_kernel<BF16, VEC>, lds))
             return e;
-    out_kernel<BF16, VEC><<<grid, OUT_THREADS, lds, stream>>>(a, w);
+    out_kernel<BF16, VEC><<<grid, MANY_THREADS, lds, stream>>>(a, w);
     return hipGetLastError();
 }
 
@@ -802,6 +840,11 @@ hipError_t launch(const FqAdaptersArgs &a, void *workspace, hipStream_t stream)
     w.rows = (int *)at;
     at += up((size_t)w.max_tiles * TILE * sizeof(int));
     w.tiles = (Tile *)at;
+    at += up(w.max_tiles * sizeof(Tile));
+    w.factor = (float *)at;
+    at += up((size_t)w.max_tiles * TILE * sizeof(float));
+    w.operands = (u32x4 *)at;
+    w.tile_operands = tile_operands(a.set);
     if (a.M <= MIDDLE_ROWS && a.set.slots <= MIDDLE_SLOTS)
         return launch_many<BF16, VEC, COUNTED>(a, w, stream);
     const size_t lds = (a.set.slots + 1) * sizeof(int);
@@ -819,7 +862,8 @@ hipError_t launch(const FqAdaptersArgs &a, void *workspace, hipStream_t stream)
 size_t fq_adapters_bytes(const FqAdaptersView &set, int M)
 {
     const size_t tiles = tiles_of(set, M);
-    return up(low_rows(M) * set.rank * sizeof(float)) + up(tiles * TILE * sizeof(int)) + up(tiles * sizeof(Tile)) + 256;
+    return up(low_rows(M) * set.rank * sizeof(float)) + up(tiles * TILE * sizeof(int)) + up(tiles * sizeof(Tile)) + up(tiles * TILE * sizeof(float)) +
+           tiles * tile_operands(set) * sizeof(u32x4) + 256;
 }
 
 hipError_t fq_launch_adapters(const FqAdaptersArgs &a, void *workspace, hipStream_t stream)
