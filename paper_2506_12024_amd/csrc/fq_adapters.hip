@@ -163,13 +163,11 @@ __device__ __forceinline__ int find_counted(const FqAdaptersArgs &a, int *rows, 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), keys = a.set.slots + 1;
     int key[PER]; // rows i * THREADS + tid
 #pragma unroll
-    for (int i = 0; i < PER; i++) {
-        key[i] = -1;
-        if (i * THREADS < a.M && i * THREADS + tid < a.M) {
-            const int s = slot_of(a, i * THREADS + tid);
-            key[i] = s < 0 ? keys - 1 : s;
-        }
-    }
+    for (int i = 0; i < PER; i++)
+        key[i] = a.adapter[min(i * THREADS + tid, a.M - 1)]; // (all asked for together)
+#pragma unroll
+    for (int i = 0; i < PER; i++)
+        key[i] = i * THREADS + tid >= a.M ? -1 : key[i] >= 0 && key[i] < a.set.slots ? key[i] : keys - 1;
     for (int i = tid; i < keys; i += THREADS)
         count[i] = 0;
     if (tid == 0)
@@ -316,7 +314,8 @@ __global__ __launch_bounds__(THREADS, 1) void low_kernel(FqAdaptersArgs a, Work 
         return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
     const int K = a.set.K, chunks = (K + CHUNK - 1) / CHUNK;
-    const int part = (chunks + gridDim.y - 1) / gridDim.y, from = part * blockIdx.y, end = min(chunks, from + part);
+    // (a part's chunks lie among the others': what is read at a time lies together)
+    const int from = blockIdx.y, apart = gridDim.y;
     const int piece = tid % PIECES, row0 = tid / PIECES;
     const uint16_t *xp[X_TURNS], *ap = a.set.a + slot * a.set.a_stride;
 #pragma unroll
@@ -356,8 +355,8 @@ __global__ __launch_bounds__(THREADS, 1) void low_kernel(FqAdaptersArgs a, Work 
             tile[row * PIECES + (piece ^ (row & 15))] = s.a[i];
         }
         __syncthreads();
-        if (c + 2 < end)
-            ask(s, c + 2);
+        if (c + 2 * apart < chunks)
+            ask(s, c + 2 * apart);
         if (16 * wave < count) {
 #pragma unroll
             for (int h = 0; h < PIECES / 4; h++) {
@@ -371,15 +370,14 @@ __global__ __launch_bounds__(THREADS, 1) void low_kernel(FqAdaptersArgs a, Work 
         __syncthreads();
     };
     Step even, odd;
-    if (from < end)
-        ask(even, from);
-    if (from + 1 < end)
-        ask(odd, from + 1);
+    ask(even, from); // (chunks >= parts)
+    if (from + apart < chunks)
+        ask(odd, from + apart);
     __syncthreads(); // (the counts lay where the chunk goes)
-    for (int c = from; c < end; c += 2) {
+    for (int c = from; c < chunks; c += 2 * apart) {
         use(even, c);
-        if (c + 1 < end)
-            use(odd, c + 1);
+        if (c + apart < chunks)
+            use(odd, c + apart);
     }
     if (16 * wave + col < count) {
         float *to = w.low + ((size_t)blockIdx.y * a.M + rows[16 * wave + col]) * a.set.rank + r0 + 4 * g;
