@@ -17,7 +17,7 @@
 namespace {
 
 constexpr int THREADS = 256, WAVES = THREADS / 64;
-constexpr int FEW_ROWS = 64, FEW_TILE = 16, FEW_ELEMENTS = 1 << 18, TILE = 64;
+constexpr int FEW_ROWS = 256, FEW_TILE = 16, TILE = 64;
 constexpr int MIDDLE_ROWS = 4096, MIDDLE_SLOTS = 1023;
 constexpr int GROUP_THREADS = 1024, OUT_THREADS = 512, MANY_THREADS = 256, JOIN_THREADS = 256, JOIN_ROWS = JOIN_THREADS / 16;
 constexpr int CHUNK = 256, MAX_PARTS = 16; // of K
@@ -50,9 +50,15 @@ struct Work {
     int parts, max_tiles, tile_operands;
 };
 
-// Whether a call is one launch: every workgroup of a tile reads its slot's A whole, which is less than the second launch and the parts while A
-// is small.
-bool few(const FqAdaptersView &set, int M) { return M <= FEW_ROWS && set.rank <= 64 && (long long)set.rank * set.K <= FEW_ELEMENTS; }
+// Whether a call is one launch: every workgroup of a tile reads its slot's A whole, which is less than two more launches and the parts while A is
+// small and, beyond 64 rows, B too.  One launch / three (us): 32 rows of 20 slots, 4096 -> 11008, rank 32 11.5 / 18.7; 128 rows of 64 slots, 4096 -> 4096,
+// rank 16 11.2 / 23.2, of 4 slots 11.0 / 16.2; 256 of 64 16.8 / 24.1, of one 17.7 / 14.6; 256 of 8, 4096 -> 11008, rank 32 30.2 / 19.0; 128 of 16, 8192 -> 8192,
+// rank 32 21.5 / 19.2.
+bool few(const FqAdaptersView &set, int M)
+{
+    const long long a = (long long)set.rank * set.K, b = (long long)set.rank * set.N;
+    return set.rank <= 64 && (M <= 64 ? a <= 1 << 18 : M <= FEW_ROWS && a + b <= 1 << 18);
+}
 
 int tiles_of(const FqAdaptersView &set, int M) { return M / TILE + (M < set.slots + 1 ? M : set.slots + 1); } // at most
 
@@ -644,10 +650,10 @@ __global__ __launch_bounds__(MANY_THREADS, 3) void out_kernel(FqAdaptersArgs a, 
         o.run(now, first, stride);
 }
 
-// Few rows, one launch: the tile that row blockIdx.x leads (the rows of its slot before it fill whole tiles), the outputs that are blockIdx.y's.  A
+// Few rows, up to 64 GROUPS, one launch: the tile that row blockIdx.x leads (the rows of its slot before it fill whole tiles), the outputs that are blockIdx.y's.  A
 // wavefront forms u over pieces of K of its own, 128 / RT at a time, two asked for ahead, through LDS of its own (a row's piece p at p ^ row, or p ^ row /
 // 2 where a row is 64 bytes); the sums of the eight meet there.  LDS for two workgroups to a compute unit: rows that lead no tile have one, too.
-template <int RT, bool BF16, bool VEC>
+template <int RT, int GROUPS, bool BF16, bool VEC>
 __global__ __launch_bounds__(OUT_THREADS, 4) void few_kernel(FqAdaptersArgs a)
 {
     constexpr int WAVES = OUT_THREADS / 64, PIECES = 16 / RT, LANES = 64 / PIECES, A_TURNS = 16 * RT / LANES, X_TURNS = 16 / LANES;
@@ -659,15 +665,34 @@ __global__ __launch_bounds__(OUT_THREADS, 4) void few_kernel(FqAdaptersArgs a)
     static_assert(RT * 64 <= OWN, "the sums of a wavefront");
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, g = lane >> 4;
     const Some some(a);
-    const int found = lane < a.M ? slot_of(a, lane) : -2, lead = blockIdx.x;
-    const int slot = __builtin_amdgcn_readlane(found, lead);
-    const uint64_t same = __ballot(found == slot);
-    const int before = __popcll(same & ((1ull << lead) - 1)), at = __popcll(same & ((1ull << lane) - 1)) - before;
+    const int lead = blockIdx.x;
+    int found[GROUPS], slot = -1, before = 0, seen = 0;
+    uint64_t same[GROUPS];
+#pragma unroll
+    for (int i = 0; i < GROUPS; i++)
+        found[i] = a.adapter[min(64 * i + lane, a.M - 1)];
+#pragma unroll
+    for (int i = 0; i < GROUPS; i++) {
+        found[i] = 64 * i + lane >= a.M ? -2 : found[i] >= 0 && found[i] < a.set.slots ? found[i] : -1;
+        if (lead >> 6 == i)
+            slot = __builtin_amdgcn_readlane(found[i], lead & 63);
+    }
+#pragma unroll
+    for (int i = 0; i < GROUPS; i++) {
+        same[i] = __ballot(found[i] == slot);
+        const int upto = lead - 64 * i;
+        before += __popcll(upto <= 0 ? 0 : upto >= 64 ? same[i] : same[i] & ((1ull << upto) - 1));
+    }
     if (before % FEW_TILE != 0)
         return;
-    const int count = min((int)__popcll(same) - before, FEW_TILE);
-    if (wave == 0 && found == slot && at >= 0 && at < FEW_TILE)
-        rows[at] = lane;
+#pragma unroll
+    for (int i = 0; i < GROUPS; i++) {
+        const int at = seen + __popcll(same[i] & ((1ull << lane) - 1)) - before;
+        if (wave == 0 && found[i] == slot && at >= 0 && at < FEW_TILE)
+            rows[at] = 64 * i + lane;
+        seen += __popcll(same[i]);
+    }
+    const int count = min(seen - before, FEW_TILE);
     int rank;
     float scale;
     some.of(a, slot, rank, scale);
@@ -771,18 +796,18 @@ __global__ __launch_bounds__(OUT_THREADS, 4) void few_kernel(FqAdaptersArgs a)
     o.run(now, first, stride);
 }
 
-template <bool BF16, bool VEC>
+template <int GROUPS, bool BF16, bool VEC>
 hipError_t launch_few(const FqAdaptersArgs &a, hipStream_t stream)
 {
-    // outputs over as many workgroups as fill the chip if every row had a slot of its own, half of that at least
-    const int blocks = (a.set.N + 63) / 64, most = (blocks + OUT_THREADS / 64 - 1) / (OUT_THREADS / 64), room = (256 + a.M - 1) / a.M + 4;
+    // outputs over as many workgroups as fill the chip if every row led a tile (32 rows of 20 slots, 4096 -> 11008: 8 of them 11.6 us, 12 15.0, 4 14.0)
+    const int blocks = (a.set.N + 63) / 64, most = (blocks + OUT_THREADS / 64 - 1) / (OUT_THREADS / 64), room = a.M <= 128 ? (256 + a.M - 1) / a.M : 2;
     const dim3 grid(a.M, most < room ? most : room);
     if (a.set.rank <= 16)
-        few_kernel<1, BF16, VEC><<<grid, OUT_THREADS, 0, stream>>>(a);
+        few_kernel<1, GROUPS, BF16, VEC><<<grid, OUT_THREADS, 0, stream>>>(a);
     else if (a.set.rank <= 32)
-        few_kernel<2, BF16, VEC><<<grid, OUT_THREADS, 0, stream>>>(a);
+        few_kernel<2, GROUPS, BF16, VEC><<<grid, OUT_THREADS, 0, stream>>>(a);
     else
-        few_kernel<4, BF16, VEC><<<grid, OUT_THREADS, 0, stream>>>(a);
+        few_kernel<4, GROUPS, BF16, VEC><<<grid, OUT_THREADS, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -828,7 +853,7 @@ template <bool BF16, bool VEC>
 hipError_t launch(const FqAdaptersArgs &a, void *workspace, hipStream_t stream)
 {
     if (few(a.set, a.M))
-        return launch_few<BF16, VEC>(a, stream);
+        return a.M <= 64 ? launch_few<1, BF16, VEC>(a, stream) : launch_few<FEW_ROWS / 64, BF16, VEC>(a, stream);
     Work w{};
     w.parts = parts_of(a.set, a.M);
     w.max_tiles = tiles_of(a.set, a.M);
