@@ -637,6 +637,8 @@ class Adapters:
         self.N, self.dtype = b.shape[1], a.dtype
         if a.numel() and (not a[0].is_contiguous() or not b[0].is_contiguous()):
             raise ValueError("the values of a slot of a and b must be contiguous")
+        if any(t is not None and t.device != a.device for t in (b, ranks, scales)):
+            raise ValueError("a, b, ranks and scales must lie on one device")
         self._keep = (a, b, ranks, scales)
         h = ctypes.c_void_p()
         _check(lib.fq_adapters_create(ctypes.byref(h), FQ_F16 if a.dtype is _F16 else FQ_BF16, self.slots, self.rank, self.K, self.N,

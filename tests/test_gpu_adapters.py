@@ -88,6 +88,53 @@ def test_row_counts(M):
     run(M, 136, 72, 6, 16, torch.float16, seed=M, spare=False)
 
 
+@pytest.mark.parametrize("M,K,N,slots,rank", [(4095, 40, 24, 5, 8), (4097, 40, 24, 5, 8), (5000, 72, 33, 3, 40), (300, 64, 33, 1500, 8), (700, 264, 48, 1023, 16),
+                                              (10, 40, 24, 3000, 72), (257, 8, 5, 16384, 8), (9000, 16, 12, 2, 256), (4200, 24, 8, 1200, 8)])
+def test_many_rows_and_many_slots(M, K, N, slots, rank):
+    run(M, K, N, slots, rank, torch.float16, seed=M)
+
+
+@pytest.mark.parametrize("M,K,rank", [(3, 8192, 32), (40, 8200, 32), (40, 16392, 16), (66, 1000, 136), (70, 12, 8), (400, 2056, 24), (3, 264, 72)])
+def test_long_sums_and_their_ends(M, K, rank):
+    """K at and beside the ends of the pieces that the products take, in one launch and in several."""
+    K = -(-K // 8) * 8
+    run(M, K, 52, 3, rank, torch.bfloat16, seed=K)
+
+
+def test_a_prompt_beside_single_tokens():
+    """Rows of one slot side by side and apart, tiles that end between them, rows of none among them."""
+    a, b, x, y, ranks, scales, _ = data(1000, 136, 72, 6, 24, torch.float16)
+    adapter = np.concatenate([np.full(333, 2), np.full(130, -1), np.full(64, 0), np.arange(473) % 7 - 1]).astype(np.int32)
+    got = add(a.to(DEV), b.to(DEV), x.to(DEV), y.to(DEV), ranks, scales, adapter)
+    check(got, *want(f64(x), f64(y), f64(a), f64(b), adapter, ranks, scales.astype(np.float64)), torch.float16)
+
+
+def test_rows_have_the_same_bits_wherever_they_stand():
+    """A row's sums do not depend on the rows beside it, among calls of one shape."""
+    for M in (40, 150, 700):
+        a, b, x, y, ranks, scales, adapter = data(M, 520, 72, 4, 16, torch.float16)
+        one = add(a.to(DEV), b.to(DEV), x.to(DEV), y.to(DEV), ranks, scales, adapter)
+        order = np.random.default_rng(1).permutation(M)
+        two = add(a.to(DEV), b.to(DEV), x[order].to(DEV), y[order].to(DEV), ranks, scales, adapter[order])
+        assert torch.equal(one[torch.from_numpy(order).to(DEV)], two)
+
+
+def test_two_streams_at_once():
+    sets = [data(M, 264, 136, 4, 16, torch.float16, seed=M) for M in (300, 301)]
+    whole = [add(d[0].to(DEV), d[1].to(DEV), d[2].to(DEV), d[3].to(DEV), *d[4:]) for d in sets]
+    streams, outs, keep = [torch.cuda.Stream() for _ in sets], [], []
+    for d, s in zip(sets, streams):
+        h = fq.Adapters(d[0].to(DEV), d[1].to(DEV), torch.tensor(d[4], dtype=torch.int32).to(DEV), torch.from_numpy(d[5]).to(DEV))
+        keep.append((h, d[2].to(DEV), torch.from_numpy(d[6]).to(DEV), d[3].to(DEV), torch.empty_like(d[3], device=DEV),
+                     torch.empty(fq.fq_adapters_workspace_bytes(h, d[2].shape[0]), dtype=torch.uint8, device=DEV)))
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for k, s in zip(keep, streams):
+            fq.fq_adapters_add(*k, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(k[4], w) for k, w in zip(keep, whole))
+
+
 @pytest.mark.parametrize("ranks", [[16, 1], [1, 15], [0, 0], [7, 9], [-5, 99]])
 def test_ranks_and_what_lies_beyond_them(ranks):
     """Rows of A and columns of B behind a slot's rank, and slots that no row names, hold NaNs."""

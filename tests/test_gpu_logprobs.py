@@ -124,6 +124,37 @@ def test_rows_begin_anywhere(dtype, lead, V):
     check(wide[1:2, lead:lead + V], some(1, V, 1), 7)
 
 
+@pytest.mark.parametrize("dtype", [SINGLE, HALF])
+@pytest.mark.parametrize("R,V", [(1, 59999), (1, 60000), (64, 60001), (65, 60001), (7, 262143), (3, 131072)])
+def test_long_rows_begin_anywhere(dtype, R, V):
+    """Rows of small batches are taken in pieces from 60000 logits on."""
+    gen = torch.Generator(device=DEV).manual_seed(V)
+    for lead in (0, 1, 5):
+        wide = torch.full((R, V + lead + 3), 99.0, dtype=dtype, device=DEV)
+        wide[:, lead:lead + V].normal_(0.0, 3.0, generator=gen)
+        check(wide[:, lead:lead + V], some(R, V, 1), 20, rows=sorted({0, R // 2, R - 1}))
+
+
+def test_more_rows_than_a_launch_takes():
+    R, V = (1 << 20) + 3, 5
+    x = torch.randn((R, V), device=DEV, generator=torch.Generator(device=DEV).manual_seed(1))
+    given = np.ascontiguousarray(np.broadcast_to(np.arange(R, dtype=np.int32)[:, None] % V, (R, 1)))
+    check(x, given, 2, rows=(0, 1, (1 << 20) - 1, 1 << 20, R - 1))
+
+
+def test_two_streams_at_once():
+    xs = [rows_of(3, 128256, SINGLE, seed).to(DEV) for seed in (1, 2)]
+    whole = [call(x, some(3, 128256, 1), 9, 3, 128256) for x in xs]
+    streams, outs = [torch.cuda.Stream() for _ in xs], [{k: None if v is None else v.clone() for k, v in w.items()} for w in whole]
+    spaces = [torch.empty(fq.fq_logprobs_workspace_bytes(3, 128256), dtype=torch.uint8, device=DEV) for _ in xs]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for x, o, ws, s in zip(xs, outs, spaces, streams):
+            fq.fq_logprobs(x, 3, 128256, ws, stream=s, **o)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o[k], w[k]) for o, w in zip(outs, whole) for k in w)
+
+
 ROWS = {"equal": lambda V, g: torch.zeros(V), "ascending": lambda V, g: torch.arange(V) / V * 30, "descending": lambda V, g: -torch.arange(V) / V * 30,
         "few_values": lambda V, g: torch.randint(0, 4, (V,), generator=g).float(),
         "two_values": lambda V, g: (torch.rand(V, generator=g) < 0.01).float() * 5,
