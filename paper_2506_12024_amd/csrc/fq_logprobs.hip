@@ -159,17 +159,21 @@ __device__ __forceinline__ void stream(const Row<T> &row, unsigned begin, unsign
 #pragma unroll
         for (int j = 0; j < AHEAD; j++) {
             const unsigned g = base + 64 * j + lane;
-            if (!EDGE || g < end)
-                v[j] = __builtin_nontemporal_load((const u32x4 *)row.from + g);
+            v[j] = __builtin_nontemporal_load((const u32x4 *)row.from + (EDGE ? min(g, end - 1) : g));
         }
-        if (EDGE) {
+        if (EDGE) { // loads behind the end count as -inf, of the first and the last one what does not belong to the row
 #pragma unroll
             for (int j = 0; j < AHEAD; j++) {
                 const unsigned g = base + 64 * j + lane;
 #pragma unroll
-                for (int e = 0; e < PER; e++)
-                    if (g >= end || g * PER + e < row.shift || g * PER + e >= row.shift + row.V)
-                        blank<T>(v[j], e);
+                for (int i = 0; i < 4; i++)
+                    v[j][i] = g >= end ? sizeof(T) == 4 ? 0xff800000u : 0xfc00fc00u : v[j][i];
+                if ((g == 0 && row.shift) || (g >= whole && g < end)) {
+#pragma unroll
+                    for (int e = 0; e < PER; e++)
+                        if (g * PER + e < row.shift || g * PER + e >= row.shift + row.V)
+                            blank<T>(v[j], e);
+                }
             }
         }
         float most[AHEAD], peak = -INFINITY;
