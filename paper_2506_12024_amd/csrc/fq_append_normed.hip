@@ -4,7 +4,7 @@
 //
 // A head lies in the registers of a group of lanes, two 16-byte pieces to a lane: those of a pair of pieces that turn together where a half rotation is
 // whole pieces, else neighbours.  Its sum of squares is a sum over the group's lanes, and a head is read once.  Only where pairs lie anyhow
-// (a half rotation that is no multiple of 8) the normed head goes through LDS for its partners.  A workgroup takes a token, or a share of
+// (a half rotation that is no multiple of 8) the part of the normed head that turns goes through LDS.  A workgroup takes a token, or a share of
 // its heads where there are few tokens; cos and sin of its angles, computed as fq_append.hip does, are in LDS.
 #include <hip/hip_runtime.h>
 
@@ -51,6 +51,13 @@ __device__ __forceinline__ float group_sum(float x)
     if (GROUP >= 16)
         x = step(x, std::integral_constant<int, 0x140>()); // a row mirrored
     return x;
+}
+
+// What a group's lanes hand each other through LDS: a wavefront's operations there are in order, the compiler has to keep them so.
+__device__ __forceinline__ void own_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
 }
 
 enum Layout { NEIGHBOURS, PIECES, ANYHOW };
@@ -175,30 +182,31 @@ __global__ __launch_bounds__(THREADS) void append_normed_kernel(FqAppendArgs a, 
                         y[e + 1] = q * k + p * s;
                     }
                 }
-            } else if (16 * i < a.rot) { // (a lane that turns something; partners of its pieces are among what such lanes put there)
+            } else { // the part that turns through LDS, its pairs over the group's lanes
                 float *head = normed + tid / GROUP * (16 * GROUP);
+                const bool mine = 16 * i < a.rot;
+                if (mine) {
 #pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    head[16 * i + e] = x[e];
-                    head[16 * i + 8 + e] = y[e];
+                    for (int e = 0; e < 8; e++) {
+                        head[16 * i + e] = x[e];
+                        head[16 * i + 8 + e] = y[e];
+                    }
                 }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-                auto turned = [&](float p, int d) {
-                    if (d >= a.rot)
-                        return p;
-                    const bool low = d < half;
-                    const int pair = low ? d : d - half;
-                    const float q = head[low ? d + half : pair], k = cs[pair], s = sn[pair];
-                    return low ? p * k - q * s : p * k + q * s;
-                };
+                own_fence();
+                for (int pair = i; pair < half; pair += GROUP) {
+                    const float k = cs[pair], s = sn[pair], p = head[pair], q = head[pair + half];
+                    head[pair] = p * k - q * s;
+                    head[pair + half] = q * k + p * s;
+                }
+                own_fence();
+                if (mine) {
 #pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    x[e] = turned(x[e], 16 * i + e);
-                    y[e] = turned(y[e], 16 * i + 8 + e);
+                    for (int e = 0; e < 8; e++) {
+                        x[e] = head[16 * i + e];
+                        y[e] = head[16 * i + 8 + e];
+                    }
                 }
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
+                own_fence();
             }
 #pragma unroll
             for (int e = 0; e < 8; e++) {
