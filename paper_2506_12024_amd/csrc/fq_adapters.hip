@@ -57,7 +57,7 @@ struct Work {
 bool few(const FqAdaptersView &set, int M)
 {
     const long long a = (long long)set.rank * set.K, b = (long long)set.rank * set.N;
-    return set.rank <= 64 && (M <= 64 ? a <= 1 << 18 : M <= FEW_ROWS && a + b <= 1 << 18);
+    return set.rank <= 64 && (M <= 64 ? a <= 1 << 18 : M <= FEW_ROWS && a + b <= 1 << 18 && set.N <= 8192);
 }
 
 int tiles_of(const FqAdaptersView &set, int M) { return M / TILE + (M < set.slots + 1 ? M : set.slots + 1); } // at most
@@ -396,8 +396,9 @@ __global__ __launch_bounds__(THREADS, 1) void low_kernel(FqAdaptersArgs a, Work 
 
 // The last step: 64 outputs of 16 TT rows to a wavefront and turn, out = y + factor u B^T.  u lies in LDS as the first operands' registers, 32
 // ranks to an instruction, hi and lo: [rank / 32][ALL][2][64].  Column c of instruction j of four is output 4 c + j, so that a lane's results of the four
-// are four outputs that follow each other, 128 bytes of a row to sixteen lanes.  B comes 32 ranks of 64 outputs at a time, through 4 KB of
-// LDS of the wavefront's own; that of the first 32 AHEAD ranks is asked for beside y.
+// are four outputs that follow each other, 128 bytes of a row to sixteen lanes; where rows are not aligned to 8 bytes it is output 16 j + c, 32 bytes of a
+// row to an access.  B comes 32 ranks of 64 outputs at a time, through 4 KB of LDS of the wavefront's own; that of the first 32 AHEAD ranks is asked for
+// beside y.
 template <int TT, int ALL, int AHEAD, bool BF16, bool VEC>
 struct Out {
     const FqAdaptersArgs &a;
@@ -410,6 +411,7 @@ struct Out {
     struct Turn {
         u32x4 b[AHEAD][4];
         uint2 y[VEC ? TT : 1][4];
+        uint16_t one[VEC ? 1 : TT][4][4];
     };
 
     // (what lies outside is loaded from inside and not used: a condition around each load is a branch around each)
@@ -423,17 +425,22 @@ struct Out {
 
     __device__ __forceinline__ void ask(Turn &k, int block) const
     {
-        const int lane = threadIdx.x & 63, n = min(64 * block + 4 * (lane & 15), a.set.N - 4);
+        const int lane = threadIdx.x & 63;
         ask_b(k.b[0], block, 0);
         if (AHEAD > 1 && chunks > 1)
             ask_b(k.b[AHEAD - 1], block, 1);
-        if (VEC) {
 #pragma unroll
-            for (int t = 0; t < TT; t++)
+        for (int t = 0; t < TT; t++)
 #pragma unroll
-                for (int i = 0; i < 4; i++)
-                    k.y[t][i] = *(const uint2 *)(a.y + rows[min(16 * t + 4 * (lane >> 4) + i, count - 1)] * a.y_stride + n);
-        }
+            for (int i = 0; i < 4; i++) {
+                const uint16_t *y = a.y + rows[min(16 * t + 4 * (lane >> 4) + i, count - 1)] * a.y_stride;
+                if (VEC)
+                    k.y[VEC ? t : 0][i] = *(const uint2 *)(y + min(64 * block + 4 * (lane & 15), a.set.N - 4));
+                else
+#pragma unroll
+                    for (int j = 0; j < 4; j++)
+                        k.one[VEC ? 0 : t][i][j] = y[min(64 * block + 16 * j + (lane & 15), a.set.N - 1)];
+            }
     }
 
     __device__ __forceinline__ void multiply(float4_t (&acc)[TT][4], u32x4 (&v)[4], int c) const
@@ -449,11 +456,11 @@ struct Out {
                     v[j][i] &= mask;
             }
         }
-        // piece g of output 4 col + j: place 64 j + 16 g + (col ^ (j + 4 g))
+        // piece g of column col of instruction j: place 64 j + 16 g + (col ^ (j + 4 g))
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const int j = (lane >> 2) & 3, p = lane & 3;
-            mine[64 * j + 16 * p + ((4 * i + (lane >> 4)) ^ (j + 4 * p))] = v[i];
+        for (int i = 0; i < 4; i++) { // output 16 i + lane / 4
+            const int j = VEC ? (lane >> 2) & 3 : i, p = lane & 3, c = VEC ? 4 * i + (lane >> 4) : lane >> 2;
+            mine[64 * j + 16 * p + (c ^ (j + 4 * p))] = v[i];
         }
         own_fence();
         u32x4 bv[4];
@@ -474,30 +481,32 @@ struct Out {
 
     __device__ __forceinline__ void finish(const Turn &k, const float4_t (&acc)[TT][4], int block) const
     {
-        const int lane = threadIdx.x & 63, n = 64 * block + 4 * (lane & 15);
+        const int lane = threadIdx.x & 63;
 #pragma unroll
         for (int t = 0; t < TT; t++)
 #pragma unroll
             for (int i = 0; i < 4; i++) {
                 const int row = 16 * t + 4 * (lane >> 4) + i;
-                if (row >= count || n >= a.set.N)
+                if (row >= count)
                     continue;
                 const float f = factor[row];
-                const int m = rows[row];
-                uint16_t *out = a.out + m * a.out_stride + n;
+                uint16_t *out = a.out + rows[row] * a.out_stride;
                 if (VEC) {
-                    const uint2 y = k.y[t][i];
+                    const int n = 64 * block + 4 * (lane & 15);
+                    const uint2 y = k.y[VEC ? t : 0][i];
                     const uint16_t v0 = fq_from_float(fq_to_float((uint16_t)y.x, BF16) + f * acc[t][0][i], BF16);
                     const uint16_t v1 = fq_from_float(fq_to_float((uint16_t)(y.x >> 16), BF16) + f * acc[t][1][i], BF16);
                     const uint16_t v2 = fq_from_float(fq_to_float((uint16_t)y.y, BF16) + f * acc[t][2][i], BF16);
                     const uint16_t v3 = fq_from_float(fq_to_float((uint16_t)(y.y >> 16), BF16) + f * acc[t][3][i], BF16);
-                    *(uint2 *)out = make_uint2(v0 | (uint32_t)v1 << 16, v2 | (uint32_t)v3 << 16);
+                    if (n < a.set.N)
+                        *(uint2 *)(out + n) = make_uint2(v0 | (uint32_t)v1 << 16, v2 | (uint32_t)v3 << 16);
                 } else {
-                    const uint16_t *y = a.y + m * a.y_stride + n;
 #pragma unroll
-                    for (int j = 0; j < 4; j++)
-                        if (n + j < a.set.N)
-                            out[j] = fq_from_float(fq_to_float(y[j], BF16) + f * acc[t][j][i], BF16);
+                    for (int j = 0; j < 4; j++) {
+                        const int n = 64 * block + 16 * j + (lane & 15);
+                        if (n < a.set.N)
+                            out[n] = fq_from_float(fq_to_float(k.one[VEC ? 0 : t][i][j], BF16) + f * acc[t][j][i], BF16);
+                    }
                 }
             }
     }
