@@ -604,8 +604,8 @@ int fq_kv_append_normed(const fq_kv *kv, const fq_seqs *seqs, int tokens, const 
                         const int32_t *positions, void *stream);
 
 /*
- * Per row of logits, with p = softmax(l): the log probabilities of given tokens, the entropy (as fq_entropy_kl), and the top_n
- * likeliest tokens with theirs, the larger logit first, the smaller index first on ties.
+ * Per row of logits, with p = softmax(l) (no temperature, no truncation): the log probabilities of given tokens, the entropy (as
+ * fq_entropy_kl), and the top_n likeliest tokens with theirs, the larger logit first, the smaller index first on ties.
  *   given_logprob[r][j] = ln p[given[r][j]];  -inf for a token outside 0 .. V - 1
  *   top_token[r][i], top_logprob[r][i]: the i-th of the order; -1 and -inf where the row has no more tokens with weight
  * A NaN logit counts as -inf.  With +inf in a row only the +inf entries have weight, 1 each.  A row of nothing else than -inf gives
@@ -617,8 +617,8 @@ int fq_kv_append_normed(const fq_kv *kv, const fq_seqs *seqs, int tokens, const 
  *   given_logprob  device, f32 [R][n_given]                                                      (written)
  *   top_token      device, int32 [R][top_n], or NULL with top_n = 0; top_logprob device, f32     (written)
  *   entropy        device, f32 [R], or NULL                                                      (written)
- *   workspace      device, fq_logprobs_workspace_bytes(R, V) bytes (0 on an error), 256-byte aligned; calls that may overlap in
- *                  time need one each
+ *   workspace      device, fq_logprobs_workspace_bytes(R, V) bytes (0 on an error; what is enough for one R and V is for any),
+ *                  256-byte aligned; calls that may overlap in time need one each
  * R >= 0 (R = 0 launches nothing), 1 <= V <= FQ_MAX_SAMPLE_V, 0 <= n_given <= FQ_MAX_GIVEN, 0 <= top_n <= FQ_MAX_ALTERNATIVES.
  * Never waits for the stream: may be captured into a graph.  Equal calls give equal bits.
  */

@@ -3,8 +3,13 @@
 // Both products are on the matrix cores.  u = x A^T is a binary32 sum, and meets B as two 16-bit numbers each, u = hi + lo (binary16: 22
 // bits of it, a row scaled by a power of two so that its largest fills the range; bfloat16: 17), so that it is nowhere rounded to
 // 16 bits.  A tile is up to 16 or 64 rows of one slot, wherever in the call they stand: a row's sums do not depend on its place in a
-// tile.  Few rows are one launch (few_kernel), whose workgroups form u for themselves; many are two: low_kernel forms u in parts of K, which lie in
-// the workspace, out_kernel adds them up and multiplies by B.
+// tile.  Few rows are one launch (few_kernel), whose workgroups form u for themselves; many are three: low_kernel forms u in parts of K, which lie in
+// the workspace, join_kernel adds them up and parts them into hi and lo, out_kernel multiplies by B.
+//
+// What bounds it: a token (4096 -> 4096, rank 16) 7.1 us a call from Python, of which the host takes 6.6 and the device as much: four trips to memory one
+// after another, launch, the exchange through LDS; 32 rows of 24 slots (4096 -> 11008, rank 32) 11.3 us, A and B once 3.3, A read again by every workgroup
+// of a tile.  A prompt of 2048 rows (8192 -> 8192, rank 64, bfloat16) 42 us, of which low_kernel has 19 (4.6 until it knows its rows, then x at 2/3 of the
+// rate of a large copy), join_kernel 5, out_kernel 19 (67 MB of y and out, 3.5 TB/s); everything once at 5.2 TB/s would be 20.
 //
 // What the operands' registers hold (16 bytes of 16 rows to a quarter of a wavefront) is nowhere loaded from memory in that order: the address unit
 // takes such a quarter a row at a time, 131 KB of A 3.4 us a workgroup as against 0.8 to 1.1 with 128 bytes of a row to eight lanes.
@@ -53,7 +58,7 @@ struct Work {
 // Whether a call is one launch: every workgroup of a tile reads its slot's A whole, which is less than two more launches and the parts while A is
 // small and, beyond 64 rows, B too.  One launch / three (us): 32 rows of 20 slots, 4096 -> 11008, rank 32 11.5 / 18.7; 128 rows of 64 slots, 4096 -> 4096,
 // rank 16 11.2 / 23.2, of 4 slots 11.0 / 16.2; 256 of 64 16.8 / 24.1, of one 17.7 / 14.6; 256 of 8, 4096 -> 11008, rank 32 30.2 / 19.0; 128 of 16, 8192 -> 8192,
-// rank 32 21.5 / 19.2.
+// rank 32 21.5 / 19.2; 117 rows of a few slots, 200 -> 23010, rank 8 65 / 27.
 bool few(const FqAdaptersView &set, int M)
 {
     const long long a = (long long)set.rank * set.K, b = (long long)set.rank * set.N;

@@ -1,5 +1,5 @@
-// Host side of what a decoder does between the linears and after the output layer (include/flexq.h): argument
-// checks, the handles of a paged cache and of a batch's tables, rotary frequencies.  As in fq_api.hip every check comes
+// Host side of what a decoder does between the linears and after the output layer, and of what a server adds to it
+// (include/flexq.h): argument checks, the handles of a paged cache, of a batch's tables and of adapters, rotary frequencies.  As in fq_api.hip every check comes
 // before the first HIP call.
 #include <hip/hip_runtime.h>
 
