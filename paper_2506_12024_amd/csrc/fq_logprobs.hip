@@ -12,7 +12,7 @@
 //
 // What bounds it: many long rows memory (500 x 128256 in binary32 with 20 alternatives 52 us, 4.9 TB/s), in binary16 the vector units too (2048 x 32000
 // without alternatives 31 us, 4.2 TB/s: eleven instructions to a logit, one of them an exponential at a quarter of the rate); short rows what comes
-// after the stream (8000 x 1000 with alternatives 50 us: some 10 steps one after another, 4 to 8 us a row, ten rows to a compute unit at a time);
+// after the stream (8000 x 1000 with alternatives 50 us: some ten steps one after another to a row of 4 KB);
 // one row the same and what one compute unit draws from memory (1 x 32000 in binary32 10.1 us a call: 5.3 until all is there, 1.3 the sums, 2.9 the alternatives).
 #include <hip/hip_runtime.h>
 #include <math.h>
