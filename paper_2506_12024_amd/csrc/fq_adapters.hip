@@ -3,8 +3,9 @@
 // Both products are on the matrix cores.  u = x A^T is a binary32 sum, and meets B as two 16-bit numbers each, u = hi + lo (binary16: 22
 // bits of it, a row scaled by a power of two so that its largest fills the range; bfloat16: 17), so that it is nowhere rounded to
 // 16 bits.  A tile is up to 16 or 64 rows of one slot, wherever in the call they stand: a row's sums do not depend on its place in a
-// tile.  Few rows are one launch (few_kernel), whose workgroups form u for themselves; many are three: low_kernel forms u in parts of K, which lie in
-// the workspace, join_kernel adds them up and parts them into hi and lo, out_kernel multiplies by B.
+// tile.  Few rows are one launch (few_kernel), whose workgroups form u for themselves; many are two or three: low_kernel forms u in parts of K, which lie in
+// the workspace; out_kernel adds them up, parts them into hi and lo and multiplies by B, or join_kernel does the first where each of its workgroups
+// would have much to add.
 //
 // What bounds it: a token (4096 -> 4096, rank 16) 7.1 us a call from Python, of which the host takes 6.6 and the device as much: four trips to memory one
 // after another, launch, the exchange through LDS; 32 rows of 24 slots (4096 -> 11008, rank 32) 11.3 us, A and B once 3.3, A read again by every workgroup
@@ -15,6 +16,9 @@
 // takes such a quarter a row at a time, 131 KB of A 3.4 us a workgroup as against 0.8 to 1.1 with 128 bytes of a row to eight lanes.
 // It goes through LDS, 16-byte pieces placed so that both sides are free of conflicts.
 #include <hip/hip_runtime.h>
+
+#include <math.h>
+#include <type_traits>
 
 #include "../../include/flexq.h"
 #include "fq_kv.h"
@@ -55,17 +59,31 @@ struct Work {
     int parts, max_tiles, tile_operands;
 };
 
-// Whether a call is one launch: every workgroup of a tile reads its slot's A whole, which is less than two more launches and the parts while A is
-// small and, beyond 64 rows, B too.  One launch / three (us): 32 rows of 20 slots, 4096 -> 11008, rank 32 11.5 / 18.7; 128 rows of 64 slots, 4096 -> 4096,
-// rank 16 11.2 / 23.2, of 4 slots 11.0 / 16.2; 256 of 64 16.8 / 24.1, of one 17.7 / 14.6; 256 of 8, 4096 -> 11008, rank 32 30.2 / 19.0; 128 of 16, 8192 -> 8192,
-// rank 32 21.5 / 19.2; 117 rows of a few slots, 200 -> 23010, rank 8 65 / 27.
+// Whether a call is one launch: every workgroup of a tile reads its slot's A whole, which is less than another launch and the parts while A is
+// small, and the tiles of 16 rows suit many slots.  One launch / more (us on the device): 1 row, 4096 -> 4096, rank 16 7.1 / 8.4, rank 64 11.7 / 9.8; 32 rows of
+// 24 slots, 4096 -> 11008, rank 32 10.7 / 17.5, of 2 11.9 / 9.7; 64 of 64, 4096 -> 4096, rank 32 10.9 / 22.6, of 4 10.6 / 9.6, rank 64 17.8 / 28.4 and
+// 17.6 / 10.8; 128 of 64, rank 16 11.7 / 20.7, of 4 12.6 / 10.0, of 4 with 2048 outputs 9.7 / 10.4; 64 of 4, 4096 -> 11008, rank 16 14.6 / 9.7.
 bool few(const FqAdaptersView &set, int M)
 {
-    const long long a = (long long)set.rank * set.K, b = (long long)set.rank * set.N;
-    return set.rank <= 64 && (M <= 64 ? a <= 1 << 18 : M <= FEW_ROWS && a + b <= 1 << 18 && set.N <= 8192);
+    const long long rank = set.rank < 16 ? 16 : set.rank, a = rank * set.K, b = rank * set.N; // (the instructions take 16)
+    if (set.rank > 64 || M > FEW_ROWS)
+        return false;
+    if (8 * (set.slots + 1) <= M) // many rows of a slot
+        return a <= 1 << 17 && M * (a + b) <= 3 << 22;
+    if (M <= 64)
+        return a <= 1 << 17 || (a <= 1 << 18 && M > 32 && set.slots > 32);
+    return a + b <= 1 << 18 && set.N <= 8192;
 }
 
 int tiles_of(const FqAdaptersView &set, int M) { return M / TILE + (M < set.slots + 1 ? M : set.slots + 1); } // at most
+
+// As many as there may well be, between what rows fill and that: the adapters of the rows are not known here.  (Against what rows fill: 300 rows of 200 slots, 4096 ->
+// 11008, rank 64 129 instead of 158 us, 1000 rows of 500 141 instead of 179.)
+int tiles_likely(const FqAdaptersView &set, int M)
+{
+    const int least = (M + TILE - 1) / TILE + 1, mean = (int)(0.5f * sqrtf((float)least * tiles_of(set, M)));
+    return least > mean ? least : mean;
+}
 
 // Parts of K: workgroups for the whole chip while rows are few, at least a chunk to each.
 int parts_of(const FqAdaptersView &set, int M)
@@ -84,6 +102,12 @@ size_t low_rows(int M)
 }
 
 int tile_operands(const FqAdaptersView &set) { return (set.rank + 31) / 32 * (TILE / 16) * 2 * 64; } // 16 bytes each
+
+// Threads to a row where the last launch adds up the parts: four ranks to each.
+__host__ __device__ inline int threads_a_row(const FqAdaptersView &set)
+{
+    return set.rank <= 8 ? 2 : set.rank <= 16 ? 4 : set.rank <= 32 ? 8 : set.rank <= 64 ? 16 : set.rank <= 128 ? 32 : 64;
+}
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -581,8 +605,8 @@ __device__ __forceinline__ float finite(const float4_t v)
     return most;
 }
 
-// The parts of a tile's u as the operands of the last launch: the tile's piece of `low`, and the rows' factors.  (In the last launch every workgroup of a
-// tile would read all parts, 131 KB for 64 ranks in 8 parts: for a prompt of 2048 40 us, 22 and 3 here.)  64 C ranks at most.
+// The parts of a tile's u as the operands of the last launch: the tile's piece of `low`, and the rows' factors.  (By every workgroup of the last launch it would
+// be 131 KB each for 64 ranks in 8 parts: see joined_here.)  64 C ranks at most.
 template <int C, bool BF16>
 __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(FqAdaptersArgs a, Work w)
 {
@@ -632,8 +656,49 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(FqAdaptersArgs a, Wo
             put_low<ALL, BF16>(low, u[c], e, row, 64 * c + mine);
 }
 
+// The same by every workgroup of the last launch, into operands and factors of its own: PARTS parts at most of the rows of PASSES turns, all asked for
+// together (turn by turn, 701 rows of rank 32, 4096 -> 4096, 20.7 us instead of 19.5).
+template <int PARTS, int PASSES, bool BF16>
+__device__ __forceinline__ void join_rows(const FqAdaptersArgs &a, const Work &w, const Tile &own, const int *rows, float *factor, u32x4 *low, int wide)
+{
+    const int step = MANY_THREADS / wide, own_row = threadIdx.x / wide, r = 4 * (threadIdx.x & (wide - 1)), last = own.rank - 1;
+    const size_t apart = (size_t)a.M * a.set.rank;
+    for (int row0 = own_row; row0 < min((own.count + 15) & ~15, TILE); row0 += step * PASSES) { // (a row's threads together)
+        float4_t part[PASSES][PARTS];
+#pragma unroll
+        for (int k = 0; k < PASSES; k++) {
+            const float *from = w.low + (size_t)rows[min(row0 + k * step, own.count - 1)] * a.set.rank + min(r, last & ~3);
+#pragma unroll
+            for (int p = 0; p < PARTS; p++)
+                part[k][p] = *(const float4_t *)(from + (size_t)min(p, w.parts - 1) * apart);
+        }
+#pragma unroll
+        for (int k = 0; k < PASSES; k++) {
+            const int row = row0 + k * step;
+            float4_t u = {0, 0, 0, 0};
+#pragma unroll
+            for (int p = 0; p < PARTS; p++)
+                if (p < w.parts)
+                    u += part[k][p];
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                u[i] = r + i <= last ? u[i] : 0.0f;
+            float most = finite(u);
+            for (int off = wide / 2; off >= 1; off >>= 1)
+                most = fmaxf(most, __shfl_xor(most, off, 64));
+            const int e = power_of<BF16>(most);
+            if (row < TILE) {
+                if (r == 0)
+                    factor[row] = ldexpf(own.scale, -e);
+                if (r < (own.rank + 31) / 32 * 32)
+                    put_low<TILE / 16, BF16>(low, u, e, row, r);
+            }
+        }
+    }
+}
+
 // out = y + scale u B^T of a tile.  A wavefront has half of the tile's rows: with all of them 238 registers leave one workgroup to a compute unit.
-template <bool BF16, bool VEC>
+template <bool BF16, bool VEC, bool JOIN>
 __global__ __launch_bounds__(MANY_THREADS, 3) void out_kernel(FqAdaptersArgs a, Work w)
 {
     constexpr int ALL = TILE / 16, TT = ALL / 2, COLUMNS = MANY_THREADS / 128;
@@ -642,8 +707,13 @@ __global__ __launch_bounds__(MANY_THREADS, 3) void out_kernel(FqAdaptersArgs a, 
     __shared__ u32x4 b_of[MANY_THREADS / 64][256];
     extern __shared__ u32x4 low[]; // [rank / 32][ALL][2][64]
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row0 = 16 * TT * (wave & 1);
-    if (tid < TILE)
+    if ((int)blockIdx.x >= w.max_tiles)
+        return;
+    if (!JOIN && tid < TILE)
         factor[tid] = w.factor[TILE * blockIdx.x + tid];
+    if (JOIN && a.set.rank <= 16)
+        for (int i = tid; i < ALL * 128; i += MANY_THREADS)
+            low[i] = u32x4{0, 0, 0, 0};
     const Tile own = find_listed(w, rows);
     const int count = own.count, rank = own.rank;
     if (count == 0)
@@ -653,12 +723,24 @@ __global__ __launch_bounds__(MANY_THREADS, 3) void out_kernel(FqAdaptersArgs a, 
         return copy_rows(a, rows + row0, min(count - row0, 16 * TT), first, stride);
     const Out<TT, ALL, 1, BF16, VEC> o{a, rows + row0, factor + row0, low + TT * 128 * (wave & 1), b_of[wave],
                                        a.set.b + own.slot * a.set.b_stride, count - row0, rank, (rank + 31) / 32};
-    const u32x4 *from = w.operands + (size_t)blockIdx.x * w.tile_operands;
-    for (int i = tid; i < o.chunks * ALL * 128; i += MANY_THREADS)
-        low[i] = from[i];
     typename Out<TT, ALL, 1, BF16, VEC>::Turn now;
-    if (64 * first < a.set.N)
-        o.ask(now, first);
+    if (JOIN) {
+        if (64 * first < a.set.N)
+            o.ask(now, first);
+        const int wide = threads_a_row(a.set);
+        if (w.parts <= 4)
+            join_rows<4, 4, BF16>(a, w, own, rows, factor, low, wide);
+        else if (w.parts <= 8)
+            join_rows<8, 2, BF16>(a, w, own, rows, factor, low, wide);
+        else
+            join_rows<MAX_PARTS, 1, BF16>(a, w, own, rows, factor, low, wide);
+    } else {
+        const u32x4 *from = w.operands + (size_t)blockIdx.x * w.tile_operands;
+        for (int i = tid; i < o.chunks * ALL * 128; i += MANY_THREADS)
+            low[i] = from[i];
+        if (64 * first < a.set.N)
+            o.ask(now, first);
+    }
     __syncthreads();
     if (row0 < count)
         o.run(now, first, stride);
@@ -832,6 +914,26 @@ void launch_low(const FqAdaptersArgs &a, const Work &w, hipStream_t stream)
     low_kernel<RT, BF16, FIND><<<grid, THREADS, 0, stream>>>(a, w);
 }
 
+// Whether the workgroups of the last launch add up the parts by themselves: a thread's loads, times the workgroups of a compute unit.  By themselves / in a launch
+// (us on the device, those loads): 701 rows, 11008 -> 4096, rank 16 17.5 / 20.1 (24); 3 rows, 9344 -> 634, rank 32 11.1 / 14.1 (16); 2048, 4096 -> 4096, rank 32 24.4 / 25.2
+// (33); 701, rank 32 16.6 / 17.9 (48); 64, 8192 -> 8192, rank 64 16.2 / 16.7 (64); 300, 4096 -> 4096, rank 64 17.8 / 17.2 (64); 2048, 8192 -> 8192, rank 64 51 / 48 (105);
+// 200, 4096 -> 4096, rank 128 21.4 / 18.3 (128).
+bool joined_here(const FqAdaptersArgs &a, const Work &w, int workgroups)
+{
+    const int rows = a.M < TILE ? a.M : TILE, step = MANY_THREADS / threads_a_row(a.set), parts = w.parts <= 4 ? 4 : w.parts <= 8 ? 8 : MAX_PARTS;
+    return (long long)((rows + step - 1) / step) * parts * (workgroups > 256 ? workgroups : 256) <= 64 * 256;
+}
+
+template <bool BF16, bool VEC, bool JOIN>
+hipError_t launch_out(const FqAdaptersArgs &a, const Work &w, dim3 grid, size_t lds, hipStream_t stream)
+{
+    if (lds > 16384)
+        if (hipError_t e = fq_raise_dynamic_lds((const void *)out_kernel<BF16, VEC, JOIN>, lds))
+            return e;
+    out_kernel<BF16, VEC, JOIN><<<grid, MANY_THREADS, lds, stream>>>(a, w);
+    return hipGetLastError();
+}
+
 template <bool BF16, bool VEC, Find FIND>
 hipError_t launch_many(const FqAdaptersArgs &a, const Work &w, hipStream_t stream)
 {
@@ -843,6 +945,16 @@ hipError_t launch_many(const FqAdaptersArgs &a, const Work &w, hipStream_t strea
         launch_low<4, BF16, FIND>(a, w, stream);
     if (hipError_t e = hipGetLastError())
         return e;
+    // outputs over as many workgroups as fill the chip, three to a compute unit
+    const int blocks = (a.set.N + 63) / 64, tiles = tiles_likely(a.set, a.M), columns = MANY_THREADS / 128;
+    const int most = (blocks + columns - 1) / columns, room = 768 / tiles > 1 ? 768 / tiles : 1;
+    const int turns = (most + room - 1) / room;
+    // With a multiple of 8 tiles to a row of the grid all of a tile's workgroups are on one XCD, and find the parts in its L2; but XCDs have unequal shares of y and
+    // out (us with / without: 701 rows of rank 16, N = 4096 17.5 / 18.9, 8192 20.6 / 19.5; 2048 rows, 1024 18.5 / 21.4, 6144 25.3 / 25.9, 8200 31.5 / 30.7, 11008 42 / 37).
+    const dim3 grid(a.set.N <= 6144 ? (w.max_tiles + 7) / 8 * 8 : w.max_tiles, (most + turns - 1) / turns);
+    const size_t lds = (size_t)w.tile_operands * sizeof(u32x4);
+    if (joined_here(a, w, tiles * grid.y))
+        return launch_out<BF16, VEC, true>(a, w, grid, lds, stream);
     const dim3 join_grid(w.max_tiles, TILE / JOIN_ROWS);
     if (a.set.rank <= 64)
         join_kernel<1, BF16><<<join_grid, JOIN_THREADS, 0, stream>>>(a, w);
@@ -850,17 +962,7 @@ hipError_t launch_many(const FqAdaptersArgs &a, const Work &w, hipStream_t strea
         join_kernel<FQ_MAX_ADAPTER_RANK / 64, BF16><<<join_grid, JOIN_THREADS, 0, stream>>>(a, w);
     if (hipError_t e = hipGetLastError())
         return e;
-    // outputs over as many workgroups as fill the chip, three to a compute unit
-    const int blocks = (a.set.N + 63) / 64, tiles = (a.M + TILE - 1) / TILE + 1, columns = MANY_THREADS / 128;
-    const int most = (blocks + columns - 1) / columns, room = 768 / tiles > 1 ? 768 / tiles : 1;
-    const int turns = (most + room - 1) / room;
-    const dim3 grid(w.max_tiles, (most + turns - 1) / turns);
-    const size_t lds = (size_t)w.tile_operands * sizeof(u32x4);
-    if (lds > 16384)
-        if (hipError_t e = fq_raise_dynamic_lds((const void *)out_kernel<BF16, VEC>, lds))
-            return e;
-    out_kernel<BF16, VEC><<<grid, MANY_THREADS, lds, stream>>>(a, w);
-    return hipGetLastError();
+    return launch_out<BF16, VEC, false>(a, w, grid, lds, stream);
 }
 
 template <bool BF16, bool VEC>

@@ -101,6 +101,19 @@ def test_long_sums_and_their_ends(M, K, rank):
     run(M, K, 52, 3, rank, torch.bfloat16, seed=K)
 
 
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("M,K,N,slots,rank", [(300, 4104, 200, 4, 128), (90, 4360, 72, 3, 256), (1500, 2304, 1100, 5, 32), (520, 1544, 6200, 7, 64), (600, 520, 6148, 3, 48),
+                                              (70, 1288, 260, 3, 8), (90, 2056, 132, 20, 40), (1, 2304, 40, 2, 200), (64, 4096, 40, 64, 64), (1100, 768, 66, 3, 16)])
+def test_parts_added_by_one_launch_or_by_all_workgroups(dtype, M, K, N, slots, rank):
+    run(M, K, N, slots, rank, TYPES[dtype], seed=M)
+
+
+@pytest.mark.parametrize("M", [16, 64, 100, 256])
+@pytest.mark.parametrize("slots,K,N", [(1, 8192, 40), (2, 64, 16384), (33, 8200, 36), (70, 256, 8200)])
+def test_sets_of_few_and_of_many_slots(M, slots, K, N):
+    run(M, K, N, slots, 16, torch.float16, seed=M)
+
+
 def test_a_prompt_beside_single_tokens():
     """Rows of one slot side by side and apart, tiles that end between them, rows of none among them."""
     a, b, x, y, ranks, scales, _ = data(1000, 136, 72, 6, 24, torch.float16)
