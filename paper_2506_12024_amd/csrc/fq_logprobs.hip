@@ -31,10 +31,10 @@ constexpr uint32_t LOWEST = 0x007fffffu; // the key of -inf
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// Larger for larger numbers, equal for -0 and 0; a NaN is as -inf.
+// Larger for larger numbers, equal for -0 and 0; a NaN is as -inf (a signalling one only once it is quiet: a maximum with one that is not is a NaN).
 __device__ __forceinline__ uint32_t key_of(float x)
 {
-    const uint32_t u = __builtin_bit_cast(uint32_t, fmaxf(x, -INFINITY) + 0.0f);
+    const uint32_t u = __builtin_bit_cast(uint32_t, fmaxf(__builtin_canonicalizef(x), -INFINITY) + 0.0f);
     return (u >> 31) ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __builtin_bit_cast(float, (k >> 31) ? k & 0x7fffffffu : ~k); }
@@ -189,7 +189,7 @@ __device__ __forceinline__ void stream(const Row<T> &row, unsigned begin, unsign
             most[j] = -INFINITY;
 #pragma unroll
             for (int e = 0; e < PER; e++)
-                most[j] = fmaxf(most[j], x[e]);
+                most[j] = fmaxf(most[j], sizeof(T) == 4 ? __builtin_canonicalizef(x[e]) : x[e]); // (a conversion has made it quiet)
             const float b = group_max<LANES>(most[j]);
             peak = fmaxf(peak, b);
             const unsigned g = base + 64 * j + lane;

@@ -190,6 +190,28 @@ def test_rows_of_all_kinds(dtype, kind, V):
     check(many, np.repeat(given[:1], 300, 0), 5, rows=(0, 1, 2, 298, 299))
 
 
+@pytest.mark.parametrize("dtype,words,ints", [(SINGLE, [0x7f800001, 0x7fc00000, -0x7fffff, -1], torch.int32), (HALF, [0x7c01, 0x7e00, -0x3ff, -1], torch.int16)])
+@pytest.mark.parametrize("R,V", [(1, 777), (3, 32000), (2, 70001)])
+def test_nans_of_all_kinds_are_as_minus_infinity(dtype, words, ints, R, V):
+    """Quiet and signalling, of both signs."""
+    gen = torch.Generator().manual_seed(V)
+    x = torch.randn((R, V), generator=gen).to(dtype)
+    at = torch.rand((R, V), generator=gen) < 0.1
+    which = torch.randint(0, len(words), (R, V), generator=gen)
+    bad = torch.where(at, torch.tensor(words, dtype=ints)[which], x.view(ints)).view(dtype)
+    assert torch.equal(torch.isnan(bad), at)
+    outs = []
+    for logits in (bad.to(DEV), torch.where(at, -torch.inf, x).to(DEV)):
+        token, best = torch.empty((R, 20), dtype=torch.int32, device=DEV), torch.empty((R, 20), device=DEV)
+        given = torch.arange(R * 9, dtype=torch.int32, device=DEV).view(R, 9)
+        lp, h = torch.empty((R, 9), device=DEV), torch.empty(R, device=DEV)
+        ws = torch.empty(fq.fq_logprobs_workspace_bytes(R, V), dtype=torch.uint8, device=DEV)
+        (fq.fq_logprobs if dtype == SINGLE else fq.fq_logprobs_f16)(logits, R, V, ws, given, lp, token, best, h)
+        outs.append((token, best, lp, h))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
 @pytest.mark.parametrize("size", [1e-30, 1e4, 1e30, 3e38])
 def test_magnitudes_of_binary32(size):
     x = torch.rand((2, 5000), generator=torch.Generator().manual_seed(1), dtype=torch.float64) * 2 - 1
