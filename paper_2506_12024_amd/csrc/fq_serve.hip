@@ -496,7 +496,7 @@ int fq_adapters_add(const fq_adapters *adapters, int M, const void *x, long long
     const size_t need = fq_adapters_bytes(set, M);
     if (workspace_bytes < need)
         return fq_fail(FQ_ERR_SHAPE, "%s: the workspace has %zu bytes, the call needs %zu", who, workspace_bytes, need);
-    if ((y != out || y_stride != out_stride) && rows_overlap(y, y_stride, set.N, out, out_stride, set.N, M))
+    if ((y != out || (M > 1 && y_stride != out_stride)) && rows_overlap(y, y_stride, set.N, out, out_stride, set.N, M))
         return fq_fail(FQ_ERR_SHAPE, "%s: out may be y, row for row, but not overlap it otherwise", who);
     if (rows_overlap(x, x_stride, set.K, out, out_stride, set.N, M))
         return fq_fail(FQ_ERR_SHAPE, "%s: out may not overlap x", who);

@@ -200,6 +200,27 @@ def test_rows_that_lie_apart_and_in_place(M, pad, lead):
     assert torch.all(out[:, :lead] == 7.0) and torch.all(out[:, lead + N:] == 7.0)
 
 
+def test_one_row_in_place_has_no_stride():
+    a, b, x, y, ranks, scales, adapter = data(1, 64, 40, 2, 8, torch.float16, spare=False)
+    h = fq.Adapters(a.to(DEV), b.to(DEV), scales=torch.from_numpy(scales).to(DEV))
+    one, who, x, y = torch.empty_like(y, device=DEV), torch.from_numpy(adapter).to(DEV), x.to(DEV), y.to(DEV)
+    ws = torch.empty(fq.fq_adapters_workspace_bytes(h, 1), dtype=torch.uint8, device=DEV)
+    fq.fq_adapters_add(h, x, who, y, one, ws)
+    assert fq.lib.fq_adapters_add(h.handle, 1, x.data_ptr(), 64, who.data_ptr(), y.data_ptr(), 40, y.data_ptr(), 48, ws.data_ptr(), ws.numel(), None) == 0
+    torch.cuda.synchronize()
+    assert torch.equal(one, y)
+
+
+def test_tensors_that_are_not_on_the_device_are_refused():
+    a, b, x, y, ranks, scales, adapter = data(3, 64, 40, 2, 8, torch.float16)
+    h, far = fq.Adapters(a.to(DEV), b.to(DEV)), fq.Adapters(a, b)
+    ws = torch.empty(fq.fq_adapters_workspace_bytes(h, 3), dtype=torch.uint8, device=DEV)
+    good = [h, x.to(DEV), torch.from_numpy(adapter).to(DEV), y.to(DEV), torch.empty_like(y, device=DEV), ws]
+    for i, bad in enumerate([far, x, torch.from_numpy(adapter), y, y, ws.cpu()]):
+        with pytest.raises(ValueError):
+            fq.fq_adapters_add(*good[:i], bad, *good[i + 1:])
+
+
 def test_slots_that_lie_apart():
     dtype = torch.bfloat16
     a, b, x, y, ranks, scales, adapter = data(30, 64, 40, 3, 16, dtype)
