@@ -610,7 +610,8 @@ def fq_kv_append_normed(cache: KVCache, seqs: Sequences, q, k, v, q_out, freqs, 
         qp, qs = _rows(q, "q", dtype, T, heads, dim)
         op, os_ = _rows(q_out, "q_out", dtype, T, heads, dim)
         wp = _weights(q_weight, "q_weight", dtype, heads, dim, each)
-    stream = _place(stream, k, v, q, q_out, freqs, q_weight if q is not None else None, k_weight, positions)
+    stream = _place(stream, k, v, q, q_out, freqs, q_weight if q is not None else None, k_weight, positions, cache._keep[0],
+                    seqs._keep[2])
     _check(lib.fq_kv_append_normed(cache.handle, seqs.handle, T, qp, qs, heads, op, os_, kp, ks, vp, vs, wp,
                                    _weights(k_weight, "k_weight", dtype, cache.kv_heads, dim, each), dim if each else 0, eps, offset,
                                    _vector(freqs, _F64, 0, "freqs"), 0 if freqs is None else 2 * freqs.numel(),

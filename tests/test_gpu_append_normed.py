@@ -152,6 +152,17 @@ def test_bad_pages_are_not_written(bad):
     run(batch, 4, 2, 64, 64, False, torch.float16)
 
 
+def test_tables_and_caches_that_are_not_on_the_device_are_refused():
+    dtype, gen = torch.float16, torch.Generator().manual_seed(1)
+    kc, vc = (pool(gen, 4, 2, 8, 64, dtype) for _ in range(2))
+    k, w = torch.randn((3, 2, 64), generator=gen).to(dtype).to(DEV), torch.ones(64, dtype=dtype, device=DEV)
+    tables = [torch.tensor(v, dtype=torch.int32) for v in ([0, 3], [3], [[0, 1]])]
+    near, far = fq.Sequences(*(t.to(DEV) for t in tables)), fq.Sequences(*tables)
+    for cache, seqs, weight in ((fq.KVCache(kc.cpu(), vc.cpu()), near, w), (fq.KVCache(kc, vc), far, w), (fq.KVCache(kc, vc), near, w.cpu())):
+        with pytest.raises(ValueError):
+            fq.fq_kv_append_normed(cache, seqs, None, k, k, None, None, None, weight)
+
+
 def test_more_new_tokens_than_length_have_no_place():
     run(Batch([6], [4], 4), 4, 2, 64, 64, False, torch.float16)
 
