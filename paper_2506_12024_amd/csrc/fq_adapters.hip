@@ -9,7 +9,8 @@
 //
 // What bounds it: a token (4096 -> 4096, rank 16) 7.1 us a call from Python, of which the host takes 6.6 and the device as much: four trips to memory one
 // after another, launch, the exchange through LDS; 32 rows of 24 slots (4096 -> 11008, rank 32) 11.3 us, A and B once 3.3, A read again by every workgroup
-// of a tile.  A prompt of 2048 rows (8192 -> 8192, rank 64, bfloat16) 42 us, of which low_kernel has 19 (4.6 until it knows its rows, then x at 2/3 of the
+// of a tile.  701 rows, chunks and single tokens (11008 -> 4096, rank 16) 17.8 us, low_kernel 9.2 (3.5 until it knows its rows), out_kernel 9.5, everything once 6.0.
+// A prompt of 2048 rows (8192 -> 8192, rank 64, bfloat16) 42 us, of which low_kernel has 19 (4.6 until it knows its rows, then x at 2/3 of the
 // rate of a large copy), join_kernel 5, out_kernel 19 (67 MB of y and out, 3.5 TB/s); everything once at 5.2 TB/s would be 20.
 //
 // What the operands' registers hold (16 bytes of 16 rows to a quarter of a wavefront) is nowhere loaded from memory in that order: the address unit
