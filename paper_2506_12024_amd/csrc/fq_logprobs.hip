@@ -115,12 +115,37 @@ __device__ __forceinline__ double wave_sum(float x)
     x = step(x, std::integral_constant<int, 0x140>());
     return ((double)lane_of(x, 0) + (double)lane_of(x, 16)) + ((double)lane_of(x, 32) + (double)lane_of(x, 48));
 }
-__device__ __forceinline__ double wave_sum(double v)
+__device__ __forceinline__ double lane_of(double x, int lane)
 {
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1)
-        v += __shfl_xor(v, off, 64);
-    return v;
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t low = __builtin_amdgcn_readlane((int)u, lane), high = __builtin_amdgcn_readlane((int)(u >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)high << 32 | low);
+}
+__device__ __forceinline__ double wave_sum(double x)
+{
+    auto step = [](double v, auto ctrl) {
+        const uint64_t t = __builtin_bit_cast(uint64_t, v);
+        const uint32_t low = __builtin_amdgcn_update_dpp((int)t, (int)t, decltype(ctrl)::value, 0xf, 0xf, false);
+        const uint32_t high = __builtin_amdgcn_update_dpp((int)(t >> 32), (int)(t >> 32), decltype(ctrl)::value, 0xf, 0xf, false);
+        return v + __builtin_bit_cast(double, (uint64_t)high << 32 | low);
+    };
+    x = step(x, std::integral_constant<int, 0xb1>());
+    x = step(x, std::integral_constant<int, 0x4e>());
+    x = step(x, std::integral_constant<int, 0x141>());
+    x = step(x, std::integral_constant<int, 0x140>());
+    return (lane_of(x, 0) + lane_of(x, 16)) + (lane_of(x, 32) + lane_of(x, 48));
+}
+
+// The sum over this lane and those before it.
+__device__ __forceinline__ int sum_upto(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false); // within rows of 16: one, two, four, eight lanes down
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false); // the last lane of rows 0 and 2 to rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false); // lane 31 to rows 2 and 3
+    return x;
 }
 
 // A part of a row: its largest logit, the sums beside that one's weight.
@@ -337,12 +362,7 @@ __device__ __forceinline__ Cut find_cut(int n, int cap, float m, uint32_t low, u
                 own[i] = sh.bins[4 * (63 - lane) + 3 - i]; // from the top
                 sum += own[i];
             }
-            int upto = sum;
-#pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const int o = __shfl_up(upto, off, 64);
-                upto += lane >= off ? o : 0;
-            }
+            const int upto = sum_upto(sum);
             int before = above + upto - sum;
             const bool here = before < n && above + upto >= n;
             int bin = 0, count = above + upto, under = before;
