@@ -172,7 +172,7 @@ struct Shared {
     uint64_t list[LIST];
     int chosen[MAX_CHOSEN];
     int bins[BINS];
-    int found[4];
+    int found[5];
 };
 
 // The loads [begin, end) of a row through the workgroup: parts of the wavefronts and the blocks' maxima, from block `first` on, into `sh`.
@@ -288,9 +288,24 @@ __device__ __forceinline__ void stream(const Row<T> &row, unsigned begin, unsign
         sh.parts[wave] = Part{m, all_s, all_t};
 }
 
+// The blocks of a row.
+template <typename T>
+__device__ __forceinline__ int blocks_of(const Row<T> &row, int block_shift)
+{
+    static_assert(BLOCK == 64, "");
+    return (int)((row.shift + row.V + (1u << (6 + block_shift)) - 1) >> (6 + block_shift));
+}
+
+// Whether the second wavefront takes the logarithm while the first is alone at work on the cut.
+template <int THREADS, typename T>
+__device__ __forceinline__ bool later(const FqLogprobsArgs &a, const Row<T> &row, int block_shift)
+{
+    return THREADS > 64 && a.top_n > 0 && blocks_of(row, block_shift) > a.top_n;
+}
+
 // The parts' sums as one, by the first wavefront: a lane to a part, up to 64.
 template <int THREADS>
-__device__ __forceinline__ void join(int n, const Part *parts, Shared<THREADS> &sh)
+__device__ __forceinline__ void join(int n, const Part *parts, bool log_later, Shared<THREADS> &sh)
 {
     const int lane = threadIdx.x;
     if (lane < 64) {
@@ -312,7 +327,8 @@ __device__ __forceinline__ void join(int n, const Part *parts, Shared<THREADS> &
         }
         if (lane == 0) {
             sh.all = Part{m, s, t};
-            sh.log_sum = log1p(s);
+            if (!log_later)
+                sh.log_sum = log1p(s);
         }
     }
     __syncthreads();
@@ -333,9 +349,10 @@ struct Cut {
     }
 };
 
-// each(f) calls f(key, index) for a thread's items; keys from `low` on count.
-template <int THREADS, typename Each>
-__device__ __forceinline__ Cut find_cut(int n, int cap, float m, uint32_t low, uint32_t last_index, Shared<THREADS> &sh, const Each &each)
+// each(f) calls f(key, index) for a thread's items; keys from `low` on count.  meanwhile(): once, by a thread of the second wavefront.
+template <int THREADS, typename Each, typename Meanwhile>
+__device__ __forceinline__ Cut find_cut(int n, int cap, float m, uint32_t low, uint32_t last_index, Shared<THREADS> &sh, const Each &each,
+                                        const Meanwhile &meanwhile)
 {
     const int tid = threadIdx.x, lane = tid & 63;
     enum { EIGHTHS, KEYS, INDICES } by = EIGHTHS;
@@ -355,6 +372,8 @@ __device__ __forceinline__ Cut find_cut(int n, int cap, float m, uint32_t low, u
                 atomicAdd(&sh.bins[(field - from) >> shift], 1);
         });
         __syncthreads();
+        if (by == EIGHTHS && tid == 64)
+            meanwhile();
         if (tid < 64) { // the highest bin from which on there are enough
             int own[4], sum = 0;
 #pragma unroll
@@ -439,29 +458,31 @@ __device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, con
         all.t = 0.0;
         __syncthreads();
     }
-    const double log_sum = infinite ? log1p(all.s) : sh.log_sum;
+    const double log_infinite = infinite ? log1p(all.s) : 0.0;
     auto logprob = [&](float x) {
         if (none || !(x > -INFINITY) || (infinite && x < INFINITY))
             return -INFINITY;
-        return infinite ? (float)-log_sum : (float)((double)x - (double)all.m - log_sum);
+        return infinite ? (float)-log_infinite : (float)((double)x - (double)all.m - sh.log_sum);
     };
+    auto log_now = [&]() { sh.log_sum = log1p(sh.all.s); };
     const int n = a.top_n;
     if (n > 0 && !none) {
         const uint32_t low = infinite ? key_of(INFINITY) : LOWEST + 1; // of what counts
         const int size_shift = 6 + block_shift;
-        static_assert(BLOCK == 64, "");
-        const int blocks = (int)((row.shift + row.V + (1u << size_shift) - 1) >> size_shift);
+        const int blocks = blocks_of(row, block_shift);
         uint32_t floor = low; // n tokens at least, or all that count, have such a key
         Cut cut{all.m, BINS, 0, 0}; // everything
         bool every = blocks <= n;
         if (tid == 0)
-            sh.found[3] = 0;
+            sh.found[3] = sh.found[4] = 0;
         if (every) {
             for (int i = tid; i < blocks; i += THREADS)
                 sh.chosen[i] = i;
             if (tid == 0)
                 sh.found[3] = blocks;
         } else if (blocks <= 64) { // ranked against each other by one wavefront
+            if (THREADS > 64 && tid == 64)
+                log_now();
             if (tid < 64) {
                 const uint32_t k = tid < blocks ? sh.keys[tid] : 0;
                 int rank = 0;
@@ -484,7 +505,7 @@ __device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, con
             cut = find_cut<THREADS>(n, cap, all.m, low, (uint32_t)blocks - 1, sh, [&](const auto &f) {
                 for (int i = tid; i < blocks; i += THREADS)
                     f(sh.keys[i], (uint32_t)i);
-            });
+            }, log_now);
             __syncthreads();
             for (int i = tid; i < blocks; i += THREADS) {
                 const uint32_t k = sh.keys[i];
@@ -498,10 +519,6 @@ __device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, con
         }
         __syncthreads();
         const int tokens = min(sh.found[3], MAX_CHOSEN) << size_shift;
-        __syncthreads();
-        if (tid == 0)
-            sh.found[3] = 0;
-        __syncthreads();
         auto each = [&](const auto &f) {
             for (int i = tid; i < tokens; i += THREADS) {
                 const unsigned at = ((unsigned)sh.chosen[i >> size_shift] << size_shift) + (i & ((1 << size_shift) - 1));
@@ -514,7 +531,7 @@ __device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, con
         };
         auto collect = [&](uint32_t key, uint32_t index) {
             if (cut.keeps(key, index)) {
-                const int at = atomicAdd(&sh.found[3], 1);
+                const int at = atomicAdd(&sh.found[4], 1);
                 if (at < LIST)
                     sh.list[at] = (uint64_t)key << 32 | (uint32_t)~index;
             }
@@ -523,17 +540,17 @@ __device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, con
         if (!many)
             each(collect);
         __syncthreads();
-        if (many || sh.found[3] > LIST) { // more than that reach the blocks' cut: one among the tokens
+        if (many || sh.found[4] > LIST) { // more than that reach the blocks' cut: one among the tokens
             __syncthreads();
-            cut = find_cut<THREADS>(n, LIST, all.m, floor, row.V - 1, sh, each);
+            cut = find_cut<THREADS>(n, LIST, all.m, floor, row.V - 1, sh, each, [] {});
             __syncthreads();
             if (tid == 0)
-                sh.found[3] = 0;
+                sh.found[4] = 0;
             __syncthreads();
             each(collect);
             __syncthreads();
         }
-        const int listed = min(sh.found[3], LIST);
+        const int listed = min(sh.found[4], LIST);
         for (int i = tid; i < listed; i += THREADS) {
             const uint64_t own = sh.list[i];
             int rank = 0;
@@ -555,7 +572,7 @@ __device__ __forceinline__ void finish(const FqLogprobsArgs &a, long long r, con
         }
     }
     if (a.entropy && tid == 0)
-        a.entropy[r] = none ? 0.0f : (float)(log_sum - all.t / (1.0 + all.s));
+        a.entropy[r] = none ? 0.0f : (float)((infinite ? log_infinite : sh.log_sum) - all.t / (1.0 + all.s));
     for (int j = tid; j < a.n_given; j += THREADS) {
         if (j != tid) {
             given = a.given[r * a.n_given + j];
@@ -584,7 +601,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 1024 ? 4 : 6) void row_kernel(F
     }
     stream<T, THREADS, AHEAD>(row, 0, row.loads(), block_shift, 0, a.top_n > 0, sh);
     __syncthreads();
-    join(THREADS / 64, sh.parts, sh);
+    join(THREADS / 64, sh.parts, later<THREADS>(a, row, block_shift), sh);
     finish<T, THREADS>(a, r, row, given, block_shift, sh);
 }
 
@@ -613,7 +630,7 @@ __global__ __launch_bounds__(THREADS) void piece_kernel(FqLogprobsArgs a, Work w
         for (unsigned i = threadIdx.x; i < blocks; i += THREADS)
             w.keys[(size_t)r * MAX_BLOCKS + first + i] = sh.keys[i];
     }
-    join(THREADS / 64, sh.parts, sh);
+    join(THREADS / 64, sh.parts, true, sh);
     if (threadIdx.x == 0)
         w.parts[r * MAX_PIECES + p] = sh.all;
 }
@@ -632,7 +649,7 @@ __global__ __launch_bounds__(THREADS) void join_kernel(FqLogprobsArgs a, Work w)
     if ((int)threadIdx.x < w.pieces)
         parts[threadIdx.x] = w.parts[r * MAX_PIECES + threadIdx.x];
     __syncthreads();
-    join(w.pieces, parts, sh);
+    join(w.pieces, parts, later<THREADS>(a, row, w.shift), sh);
     finish<T, THREADS>(a, r, row, given, w.shift, sh);
 }
 
