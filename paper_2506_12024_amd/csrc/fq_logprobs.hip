@@ -12,8 +12,8 @@
 //
 // What bounds it: many long rows memory (500 x 128256 in binary32 with 20 alternatives 52 us, 4.9 TB/s), in binary16 the vector units too (2048 x 32000
 // without alternatives 31 us, 4.2 TB/s: eleven instructions to a logit, one of them an exponential at a quarter of the rate); short rows what comes
-// after the stream (8000 x 1000 with alternatives 50 us: some ten steps one after another to a row of 4 KB);
-// one row the same and what one compute unit draws from memory (1 x 32000 in binary32 10.1 us a call: 5.3 until all is there, 1.3 the sums, 2.9 the alternatives).
+// after the stream (8000 x 1000 with alternatives 49 us: some ten steps one after another to a row of 4 KB);
+// one row the same and what one compute unit draws from memory (1 x 32000 in binary32 9.6 us a call: 5.3 until all is there, 1 the sums, 2.7 the alternatives).
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -24,8 +24,8 @@ namespace {
 
 constexpr int BLOCK = 64, MAX_BLOCKS = 2048; // logits; a row of more takes blocks twice, four times ... as large
 constexpr int BINS = 256, LIST = 256, MAX_CHOSEN = 128;
-// Rows in pieces (a workgroup of 1024 threads to a whole row / pieces and a second launch, us, 20 alternatives): 1 x 32000 in binary32 10.6 / 12.8, 65536
-// 14.1 / 12.5, 128256 21.6 / 14.4, 262144 35.4 / 15.2; 32 x 65536 in binary16 14.1 / 13.2, 128256 21.1 / 15.1; 64 x 65536 14.8 / 15.7, 128256 24.3 / 18.1.
+// Rows in pieces (a workgroup of 1024 threads to a whole row / pieces and a second launch, us, 20 alternatives): 1 x 32000 in binary32 10.1 / 11.5, 65536
+// 14.2 / 11.8, 128256 21.9 / 13.2, 262144 37.6 / 14.6; 32 x 65536 in binary16 13.5 / 12.4, 128256 20.8 / 13.8; 64 x 65536 13.8 / 14.5, 128256 21.1 / 16.1.
 constexpr int SPLIT_ROWS = 64, SPLIT_LOGITS = 60000, MAX_PIECES = 64;
 constexpr uint32_t LOWEST = 0x007fffffu; // the key of -inf
 
@@ -296,7 +296,8 @@ __device__ __forceinline__ int blocks_of(const Row<T> &row, int block_shift)
     return (int)((row.shift + row.V + (1u << (6 + block_shift)) - 1) >> (6 + block_shift));
 }
 
-// Whether the second wavefront takes the logarithm while the first is alone at work on the cut.
+// Whether the second wavefront takes the logarithm while the first is alone at work on the cut (32 x 128256 in binary16 14.2 to 13.7 us; the sums there, too, won
+// nothing).
 template <int THREADS, typename T>
 __device__ __forceinline__ bool later(const FqLogprobsArgs &a, const Row<T> &row, int block_shift)
 {
