@@ -473,6 +473,12 @@ struct Out {
             }
     }
 
+    // Infinities of B meet hi alone, whose product has u's sign: lo may be 0 or of the other sign, and would make NaN of them.  (A u that is 2^-38 of its row's
+    // largest or less has a hi of 0 in binary16.)  What other calls pay for it: with TILE rows a look at B while it lies in LDS (a prompt of 2048, 8192 -> 8192, rank
+    // 64 42.5 to 43.1 us, others nothing); with FEW_TILE, where that is 0.2 to 0.6 us, a look at the sums, and where they are not all numbers a second walk (0 to
+    // 0.2 us; in out_kernel 2 %).
+    enum Infinities { SOUGHT, IGNORED, APART };
+    template <Infinities B>
     __device__ __forceinline__ void multiply(float4_t (&acc)[TT][4], u32x4 (&v)[4], int c) const
     {
         const int lane = threadIdx.x & 63, col = lane & 15, g = lane >> 4;
@@ -492,21 +498,62 @@ struct Out {
             const int j = VEC ? (lane >> 2) & 3 : i, p = lane & 3, c = VEC ? 4 * i + (lane >> 4) : lane >> 2;
             mine[64 * j + 16 * p + (c ^ (j + 4 * p))] = v[i];
         }
+        const bool infinite = B == APART || (B == SOUGHT && __ballot(has_infinity(v)));
         own_fence();
         u32x4 bv[4];
 #pragma unroll
         for (int j = 0; j < 4; j++)
             bv[j] = mine[64 * j + 16 * g + (col ^ (j + 4 * g))];
         own_fence();
+        u32x4 lo[TT];
 #pragma unroll
         for (int t = 0; t < TT; t++) {
             if (16 * t >= count)
                 break;
-            const u32x4 hi = low[(c * ALL + t) * 128 + lane], lo = low[(c * ALL + t) * 128 + 64 + lane];
+            const u32x4 hi = low[(c * ALL + t) * 128 + lane];
+            lo[t] = low[(c * ALL + t) * 128 + 64 + lane];
 #pragma unroll
             for (int j = 0; j < 4; j++)
-                acc[t][j] = mfma<BF16>(lo, bv[j], mfma<BF16>(hi, bv[j], acc[t][j]));
+                acc[t][j] = mfma<BF16>(hi, bv[j], acc[t][j]);
         }
+        if (__builtin_expect(infinite, B == APART))
+            without_infinities(bv);
+#pragma unroll
+        for (int t = 0; t < TT; t++) {
+            if (16 * t >= count)
+                break;
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+                acc[t][j] = mfma<BF16>(lo[t], bv[j], acc[t][j]);
+        }
+    }
+
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    static constexpr uint32_t ONES = BF16 ? 0x7f807f80u : 0x7c007c00u; // the exponents of infinities and NaNs
+
+    static __device__ __forceinline__ bool has_infinity(const u32x4 (&v)[4]) // or a NaN
+    {
+        u16x2 most = {0, 0};
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint32_t u = v[j][i] & 0x7fff7fffu;
+                most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, u));
+            }
+        return max(most[0], most[1]) >= (ONES & 0xffffu);
+    }
+
+    static __device__ __forceinline__ void without_infinities(u32x4 (&v)[4])
+    {
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) { // times 0 where exponent and fraction are an infinity's, else 1
+                const uint32_t u = v[j][i], apart = (u & 0x7fff7fffu) ^ ONES;
+                const u16x2 kept = __builtin_bit_cast(u16x2, u) * __builtin_elementwise_min(__builtin_bit_cast(u16x2, apart), u16x2{1, 1});
+                v[j][i] = __builtin_bit_cast(uint32_t, kept);
+            }
     }
 
     __device__ __forceinline__ void finish(const Turn &k, const float4_t (&acc)[TT][4], int block) const
@@ -541,23 +588,53 @@ struct Out {
             }
     }
 
-    // The blocks first, first + stride ...; k: what was asked for the first.  (A turn ahead in registers would cost half of the wavefronts, which hide more.)
-    __device__ __forceinline__ void run(Turn &k, int first, int stride) const
+    static __device__ __forceinline__ bool all_numbers(const float4_t (&acc)[TT][4])
+    {
+        float zero[4] = {};
+#pragma unroll
+        for (int t = 0; t < TT; t++)
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    zero[i] = fmaf(acc[t][j][i], 0.0f, zero[i]);
+        return (zero[0] + zero[1]) + (zero[2] + zero[3]) == 0.0f;
+    }
+
+    // The blocks first, first + stride ...; k: what was asked for the first, if it was.  (A turn ahead in registers would cost half of the wavefronts, which hide
+    // more.)  IGNORED: ends before a block whose sums are not all numbers, and returns it.
+    template <Infinities B>
+    __device__ __forceinline__ int walk(Turn &k, int first, int stride) const
     {
         const int blocks = (a.set.N + 63) / 64;
-        for (int block = first; block < blocks; block += stride) {
-            if (block != first)
+        int block = first;
+        for (; block < blocks; block += stride) {
+            if (B == APART || block != first)
                 ask(k, block);
             float4_t acc[TT][4] = {};
-            multiply(acc, k.b[0], 0);
+            multiply<B>(acc, k.b[0], 0);
             if (AHEAD > 1 && chunks > 1)
-                multiply(acc, k.b[AHEAD - 1], 1);
+                multiply<B>(acc, k.b[AHEAD - 1], 1);
             for (int c = AHEAD; c < chunks; c++) {
                 u32x4 v[4];
                 ask_b(v, block, c);
-                multiply(acc, v, c);
+                multiply<B>(acc, v, c);
             }
+            if (B == IGNORED && __ballot(!all_numbers(acc)))
+                break;
             finish(k, acc, block);
+        }
+        return block;
+    }
+
+    __device__ __forceinline__ void run(Turn &k, int first, int stride) const
+    {
+        if (TT > 1) {
+            walk<SOUGHT>(k, first, stride);
+        } else {
+            const int block = walk<IGNORED>(k, first, stride);
+            if (64 * block < a.set.N)
+                walk<APART>(k, block, stride);
         }
     }
 };

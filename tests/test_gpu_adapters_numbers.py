@@ -1,0 +1,41 @@
+"""fq_adapters_add at the ends of its numbers: infinities of B."""
+import numpy as np
+import pytest
+import torch
+
+from serve_util import TYPES
+from test_gpu_adapters import DEV, add
+
+pytestmark = pytest.mark.gpu
+
+
+def device(*tensors):
+    return [t.to(DEV) for t in tensors]
+
+
+@pytest.mark.parametrize("M,rank", [(5, 8), (5, 32), (5, 64), (300, 8), (300, 64), (300, 136)])
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("N", [40, 41])
+def test_an_infinity_of_b_is_one_of_the_result(M, rank, dtype, N):
+    """u B with an infinite value of B is the infinity of the product's sign, whatever digits u has; beside 0 or the other infinity NaN."""
+    dtype = TYPES[dtype]
+    gen = torch.Generator().manual_seed(3)
+    a, b = torch.rand((1, rank, 16), generator=gen).to(dtype) + 0.25, torch.randn((1, N, rank), generator=gen).to(dtype)
+    x, y = torch.rand((M, 16), generator=gen).to(dtype) + 0.25, torch.randn((M, N), generator=gen).to(dtype)
+    a[0, 1], x[1] = 1.0, 1.0  # (row 1, rank 1: 16 exactly)
+    x[2] = -x[2]
+    x[3] = 0.0
+    clean = add(*device(a, b, x, y), None, None, np.zeros(M, np.int32))
+    inf = float("inf")
+    b[0, 5, rank - 1], b[0, 17, 1], b[0, 30, 0] = inf, -inf, float("nan")
+    b[0, 39, 0], b[0, 39, 1] = inf, -inf
+    got, here = add(*device(a, b, x, y), None, None, np.zeros(M, np.int32)), y.to(DEV)
+    add(*device(a, b, x), here, None, None, np.zeros(M, np.int32), out=here)
+    assert torch.equal(here.view(torch.int16), got.view(torch.int16))
+    sign = torch.ones(M, device=DEV)
+    sign[2] = -1.0
+    rows = [m for m in range(M) if m != 3]
+    assert torch.equal(got[rows, 5].float(), (inf * sign)[rows]) and torch.equal(got[rows, 17].float(), (-inf * sign)[rows])
+    assert torch.all(torch.isnan(got[:, [30, 39]])) and torch.all(torch.isnan(got[3, [5, 17]]))
+    other = [n for n in range(N) if n not in (5, 17, 30, 39)]
+    assert torch.equal(got[:, other], clean[:, other])
