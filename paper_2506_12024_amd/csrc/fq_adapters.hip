@@ -658,6 +658,8 @@ __device__ __forceinline__ void put_low(u32x4 *low, const float4_t u, int e, int
     for (int i = 0; i < 4; i++) {
         const float v = BF16 ? u[i] : ldexpf(u[i], e);
         hi[i] = fq_from_float(v, BF16);
+        if (BF16 && (hi[i] & 0x7fff) == 0x7f80 && fabsf(v) < INFINITY)
+            hi[i]--; // a number beyond bfloat16's largest: that one, and the rest in lo
         const float rest = v - fq_to_float(hi[i], BF16);
         lo[i] = fabsf(rest) < INFINITY ? fq_from_float(rest, BF16) : 0; // (not where hi is infinite or NaN)
     }

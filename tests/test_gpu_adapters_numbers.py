@@ -1,10 +1,10 @@
-"""fq_adapters_add at the ends of its numbers: infinities of B."""
+"""fq_adapters_add at the ends of its numbers: infinities of B, sums beyond the types."""
 import numpy as np
 import pytest
 import torch
 
 from serve_util import TYPES
-from test_gpu_adapters import DEV, add
+from test_gpu_adapters import DEV, add, check, f64, want
 
 pytestmark = pytest.mark.gpu
 
@@ -39,3 +39,18 @@ def test_an_infinity_of_b_is_one_of_the_result(M, rank, dtype, N):
     assert torch.all(torch.isnan(got[:, [30, 39]])) and torch.all(torch.isnan(got[3, [5, 17]]))
     other = [n for n in range(N) if n not in (5, 17, 30, 39)]
     assert torch.equal(got[:, other], clean[:, other])
+
+
+@pytest.mark.parametrize("M", [2, 300])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_sums_beyond_the_largest_bfloat16_are_numbers(M, sign):
+    """x A^T between the largest bfloat16 and the largest binary32, and a scale that brings it back."""
+    dtype = torch.bfloat16
+    a, b, x = torch.zeros((1, 8, 8)), torch.zeros((1, 12, 8)), torch.zeros((M, 8))
+    x[:, 0], a[0, 0, 0] = sign * 1.9921875 * 2.0 ** 64, 2.0 ** 63
+    x[:, 1], a[0, 0, 1] = sign * 1.5 * 2.0 ** 60, 2.0 ** 59  # u = 2^127 (255 / 128 + 3 / 512)
+    b[0, :, 0] = 1.0
+    scales, y, adapter = np.array([2.0 ** -120], dtype=np.float32), torch.zeros((M, 12)), np.zeros(M, np.int32)
+    a, b, x, y = (t.to(dtype) for t in (a, b, x, y))
+    got = add(*device(a, b, x, y), None, scales, adapter)
+    check(got, *want(f64(x), f64(y), f64(a), f64(b), adapter, [8], scales.astype(np.float64)), dtype)
