@@ -676,6 +676,15 @@ __device__ __forceinline__ int power_of(float most)
     return BF16 || most == 0.0f ? 0 : min(max(14 - __builtin_amdgcn_frexp_expf(most), -126), 126);
 }
 
+// What a row's sums are multiplied by.  A finite scale stays inside binary32: an infinity would make NaN of a sum of 0 (other sums pass binary16 either way: they are
+// 2^-48 at least).
+template <bool BF16>
+__device__ __forceinline__ float factor_of(float scale, int e)
+{
+    const float f = BF16 ? scale : ldexpf(scale, -e);
+    return !BF16 && fabsf(scale) < INFINITY ? fminf(fmaxf(f, -0x1.fffffep127f), 0x1.fffffep127f) : f;
+}
+
 __device__ __forceinline__ float finite(const float4_t v)
 {
     float most = 0.0f;
@@ -728,7 +737,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(FqAdaptersArgs a, Wo
         most = fmaxf(most, __shfl_xor(most, off, 64));
     const int e = power_of<BF16>(most);
     if (mine == 0)
-        w.factor[TILE * blockIdx.x + row] = ldexpf(own.scale, -e);
+        w.factor[TILE * blockIdx.x + row] = factor_of<BF16>(own.scale, e);
     u32x4 *low = w.operands + (size_t)blockIdx.x * w.tile_operands;
 #pragma unroll
     for (int c = 0; c < C; c++)
@@ -769,7 +778,7 @@ __device__ __forceinline__ void join_rows(const FqAdaptersArgs &a, const Work &w
             const int e = power_of<BF16>(most);
             if (row < TILE) {
                 if (r == 0)
-                    factor[row] = ldexpf(own.scale, -e);
+                    factor[row] = factor_of<BF16>(own.scale, e);
                 if (r < (own.rank + 31) / 32 * 32)
                     put_low<TILE / 16, BF16>(low, u, e, row, r);
             }
@@ -965,7 +974,7 @@ __global__ __launch_bounds__(OUT_THREADS, 4) void few_kernel(FqAdaptersArgs a)
             most = fmaxf(most, __shfl_xor(most, off, 64));
         const int e = power_of<BF16>(most);
         if (r == 0)
-            factor[row] = ldexpf(scale, -e);
+            factor[row] = factor_of<BF16>(scale, e);
         put_low<1, BF16>(low, u, e, row, r);
     }
     __syncthreads();

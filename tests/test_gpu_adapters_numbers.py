@@ -1,4 +1,4 @@
-"""fq_adapters_add at the ends of its numbers: infinities of B, sums beyond the types."""
+"""fq_adapters_add at the ends of its numbers: infinities of B, sums beyond the types, scales of any size."""
 import numpy as np
 import pytest
 import torch
@@ -54,3 +54,16 @@ def test_sums_beyond_the_largest_bfloat16_are_numbers(M, sign):
     a, b, x, y = (t.to(dtype) for t in (a, b, x, y))
     got = add(*device(a, b, x, y), None, scales, adapter)
     check(got, *want(f64(x), f64(y), f64(a), f64(b), adapter, [8], scales.astype(np.float64)), dtype)
+
+
+@pytest.mark.parametrize("M", [2, 300])
+@pytest.mark.parametrize("scale", [2.0 ** 100, -2.0 ** 127, 2.0 ** -140])
+def test_scales_of_any_size_beside_sums_of_any_size(M, scale):
+    """The power of two that a row's x A^T is held by does not take a finite scale out of binary32: a product of 0 stays 0."""
+    a, b, x = torch.full((1, 8, 512), 2.0 ** 15), torch.zeros((1, 12, 8)), torch.full((M, 512), 2.0 ** 15)
+    b[0, 6:] = 1.0
+    y = torch.randn((M, 12), generator=torch.Generator().manual_seed(1))
+    a, b, x, y = (t.half() for t in (a, b, x, y))
+    got = add(*device(a, b, x, y), None, np.array([scale], dtype=np.float32), np.zeros(M, np.int32)).cpu()
+    assert torch.equal(got[:, :6], y[:, :6])
+    assert torch.equal(got[:, 6:], y[:, 6:]) if abs(scale) < 1.0 else torch.all(got[:, 6:] == scale * float("inf"))
