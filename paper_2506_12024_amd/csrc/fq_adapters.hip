@@ -76,6 +76,16 @@ bool few(const FqAdaptersView &set, int M)
     return a + b <= 1 << 18 && set.N <= 8192;
 }
 
+// Workgroups to a row of that launch: outputs over as many as fill the chip if every row led a tile (32 rows of 20 slots, 4096 -> 11008, rank 32: 8 of them 11.6 us,
+// 12 15.0, 4 14.0).  Up to 64 rows not one more than there are compute units: a unit that has two takes twice as long (40 rows of 40 slots, 4096 -> 4096, rank 16
+// 7 11.5 us, 6 9.0; 48 of 48, 4096 -> 11008, rank 32 6 19.1, 5 15.9).
+int few_shares(const FqAdaptersView &set, int M)
+{
+    const int blocks = (set.N + 63) / 64, most = (blocks + OUT_THREADS / 64 - 1) / (OUT_THREADS / 64);
+    const int room = M <= 64 ? 256 / M : M <= 128 ? (256 + M - 1) / M : 2;
+    return most < room ? most : room;
+}
+
 int tiles_of(const FqAdaptersView &set, int M) { return M / TILE + (M < set.slots + 1 ? M : set.slots + 1); } // at most
 
 // As many as there may well be, between what rows fill and that: the adapters of the rows are not known here.  (Against what rows fill: 300 rows of 200 slots, 4096 ->
@@ -109,6 +119,9 @@ __host__ __device__ inline int threads_a_row(const FqAdaptersView &set)
 {
     return set.rank <= 8 ? 2 : set.rank <= 16 ? 4 : set.rank <= 32 ? 8 : set.rank <= 64 ? 16 : set.rank <= 128 ? 32 : 64;
 }
+
+// Ranks to a workgroup of low_kernel.
+int low_ranks(const FqAdaptersView &set) { return set.rank <= 16 ? 16 : set.rank <= 32 ? 32 : 64; }
 
 size_t up(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -984,9 +997,7 @@ __global__ __launch_bounds__(OUT_THREADS, 4) void few_kernel(FqAdaptersArgs a)
 template <int GROUPS, bool BF16, bool VEC>
 hipError_t launch_few(const FqAdaptersArgs &a, hipStream_t stream)
 {
-    // outputs over as many workgroups as fill the chip if every row led a tile (32 rows of 20 slots, 4096 -> 11008: 8 of them 11.6 us, 12 15.0, 4 14.0)
-    const int blocks = (a.set.N + 63) / 64, most = (blocks + OUT_THREADS / 64 - 1) / (OUT_THREADS / 64), room = a.M <= 128 ? (256 + a.M - 1) / a.M : 2;
-    const dim3 grid(a.M, most < room ? most : room);
+    const dim3 grid(a.M, few_shares(a.set, a.M));
     if (a.set.rank <= 16)
         few_kernel<1, GROUPS, BF16, VEC><<<grid, OUT_THREADS, 0, stream>>>(a);
     else if (a.set.rank <= 32)
@@ -999,7 +1010,7 @@ hipError_t launch_few(const FqAdaptersArgs &a, hipStream_t stream)
 template <int RT, bool BF16, Find FIND>
 void launch_low(const FqAdaptersArgs &a, const Work &w, hipStream_t stream)
 {
-    const dim3 grid(w.max_tiles, w.parts, (a.set.rank + 16 * RT - 1) / (16 * RT));
+    const dim3 grid(w.max_tiles, w.parts, (a.set.rank + 16 * RT - 1) / (16 * RT)); // (16 RT = low_ranks)
     low_kernel<RT, BF16, FIND><<<grid, THREADS, 0, stream>>>(a, w);
 }
 
@@ -1026,9 +1037,10 @@ hipError_t launch_out(const FqAdaptersArgs &a, const Work &w, dim3 grid, size_t 
 template <bool BF16, bool VEC, Find FIND>
 hipError_t launch_many(const FqAdaptersArgs &a, const Work &w, hipStream_t stream)
 {
-    if (a.set.rank <= 16)
+    const int ranks = low_ranks(a.set);
+    if (ranks == 16)
         launch_low<1, BF16, FIND>(a, w, stream);
-    else if (a.set.rank <= 32)
+    else if (ranks == 32)
         launch_low<2, BF16, FIND>(a, w, stream);
     else
         launch_low<4, BF16, FIND>(a, w, stream);
@@ -1057,7 +1069,8 @@ hipError_t launch_many(const FqAdaptersArgs &a, const Work &w, hipStream_t strea
 template <bool BF16, bool VEC>
 hipError_t launch(const FqAdaptersArgs &a, void *workspace, hipStream_t stream)
 {
-    if (few(a.set, a.M))
+    const FqAdaptersRoute route = fq_adapters_route(a.set, a.M);
+    if (route.few)
         return a.M <= 64 ? launch_few<1, BF16, VEC>(a, stream) : launch_few<FEW_ROWS / 64, BF16, VEC>(a, stream);
     Work w{};
     w.parts = parts_of(a.set, a.M);
@@ -1073,7 +1086,7 @@ hipError_t launch(const FqAdaptersArgs &a, void *workspace, hipStream_t stream)
     at += up((size_t)w.max_tiles * TILE * sizeof(float));
     w.operands = (u32x4 *)at;
     w.tile_operands = tile_operands(a.set);
-    if (a.M <= MIDDLE_ROWS && a.set.slots <= MIDDLE_SLOTS)
+    if (!route.listed)
         return launch_many<BF16, VEC, COUNTED>(a, w, stream);
     const size_t lds = (a.set.slots + 1) * sizeof(int);
     if (lds > 32768)
@@ -1086,6 +1099,13 @@ hipError_t launch(const FqAdaptersArgs &a, void *workspace, hipStream_t stream)
 }
 
 } // namespace
+
+FqAdaptersRoute fq_adapters_route(const FqAdaptersView &set, int M)
+{
+    if (few(set, M))
+        return {1, 0, M * few_shares(set, M)};
+    return {0, M > MIDDLE_ROWS || set.slots > MIDDLE_SLOTS, tiles_of(set, M) * parts_of(set, M) * ((set.rank + low_ranks(set) - 1) / low_ranks(set))};
+}
 
 size_t fq_adapters_bytes(const FqAdaptersView &set, int M)
 {

@@ -282,6 +282,11 @@ struct FqAdaptersArgs {
     long long x_stride, y_stride, out_stride;
     int M;
 };
+// How a call of M rows runs: one launch, or several, behind one that sorts its rows by slot; workgroups of the one, or of the one that forms x A^T.
+struct FqAdaptersRoute {
+    int few, listed, workgroups;
+};
+FqAdaptersRoute fq_adapters_route(const FqAdaptersView &set, int M);
 size_t fq_adapters_bytes(const FqAdaptersView &set, int M);
 hipError_t fq_launch_adapters(const FqAdaptersArgs &a, void *workspace, hipStream_t stream);
 

@@ -1,0 +1,34 @@
+"""Which launches fq_adapters_add takes, a choice of the host that needs no device."""
+import ctypes
+
+import pytest
+
+import paper_2506_12024_amd as fq
+
+
+class _View(ctypes.Structure):  # FqAdaptersView
+    _fields_ = ([("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("a_stride", ctypes.c_longlong), ("b_stride", ctypes.c_longlong),
+                 ("ranks", ctypes.c_void_p), ("scales", ctypes.c_void_p)] + [(n, ctypes.c_int) for n in ("slots", "rank", "K", "N", "bf16")])
+
+
+class _Route(ctypes.Structure):  # FqAdaptersRoute
+    _fields_ = [(n, ctypes.c_int) for n in ("few", "listed", "workgroups")]
+
+
+_route = fq.lib["_Z17fq_adapters_routeRK14FqAdaptersViewi"]
+_route.restype, _route.argtypes = _Route, [ctypes.c_void_p, ctypes.c_int]
+
+
+def route(M, K, N, slots, rank):
+    v = _View(slots=slots, rank=rank, K=K, N=N)
+    r = _route(ctypes.byref(v), M)
+    return r.few, r.listed, r.workgroups
+
+
+@pytest.mark.parametrize("rank", [16, 32, 64])
+def test_few_rows_take_no_more_workgroups_than_compute_units(rank):
+    """A unit that has two workgroups takes twice as long."""
+    for M in range(1, 65):
+        for N in (64, 4096, 11008, 28672):
+            few, _, groups = route(M, (1 << 17) // rank, N, 64, rank)
+            assert few and M <= groups <= 256, (M, N)
