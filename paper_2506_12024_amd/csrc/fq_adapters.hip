@@ -88,6 +88,13 @@ int few_shares(const FqAdaptersView &set, int M)
 
 int tiles_of(const FqAdaptersView &set, int M) { return M / TILE + (M < set.slots + 1 ? M : set.slots + 1); } // at most
 
+// Tiles to a row of the last launch's grid.  With a multiple of 8 all of a tile's workgroups are on one XCD, and find the parts in its L2; but XCDs have unequal shares
+// of y and out, and one has all where a call names one slot; with an odd number they are on all XCDs.  (us with a multiple of 8 / odd: 701 rows of rank 16, N =
+// 4096 17.5 / 18.9, 8192 20.6 / 19.5; 2048 rows, 1024 18.5 / 21.4, 6144 25.3 / 25.9, 8200 31.5 / 30.7, 11008 42 / 37; 511 rows of 12 slots, 4096 -> 2048 12.2 / 12.6, of
+// one of them 11.0 / 12.6; 64 rows of one of 8 slots, 4096 -> 5120, rank 64 20.1 / 14.9, of all 13.6 / 12.9; 32 rows of one of 64 slots, 4096 -> 11008, rank 64
+// 32.3 / 14.6, of 32 27.9 / 28.1.)
+int out_tiles(const FqAdaptersView &set, int M) { return set.N <= 6144 && M > 64 ? (tiles_of(set, M) + 7) / 8 * 8 : tiles_of(set, M) | 1; }
+
 // As many as there may well be, between what rows fill and that: the adapters of the rows are not known here.  (Against what rows fill: 300 rows of 200 slots, 4096 ->
 // 11008, rank 64 129 instead of 158 us, 1000 rows of 500 141 instead of 179.)
 int tiles_likely(const FqAdaptersView &set, int M)
@@ -1050,9 +1057,7 @@ hipError_t launch_many(const FqAdaptersArgs &a, const Work &w, hipStream_t strea
     const int blocks = (a.set.N + 63) / 64, tiles = tiles_likely(a.set, a.M), columns = MANY_THREADS / 128;
     const int most = (blocks + columns - 1) / columns, room = 768 / tiles > 1 ? 768 / tiles : 1;
     const int turns = (most + room - 1) / room;
-    // With a multiple of 8 tiles to a row of the grid all of a tile's workgroups are on one XCD, and find the parts in its L2; but XCDs have unequal shares of y and
-    // out (us with / without: 701 rows of rank 16, N = 4096 17.5 / 18.9, 8192 20.6 / 19.5; 2048 rows, 1024 18.5 / 21.4, 6144 25.3 / 25.9, 8200 31.5 / 30.7, 11008 42 / 37).
-    const dim3 grid(a.set.N <= 6144 ? (w.max_tiles + 7) / 8 * 8 : w.max_tiles, (most + turns - 1) / turns);
+    const dim3 grid(out_tiles(a.set, a.M), (most + turns - 1) / turns);
     const size_t lds = (size_t)w.tile_operands * sizeof(u32x4);
     if (joined_here(a, w, tiles * grid.y))
         return launch_out<BF16, VEC, true>(a, w, grid, lds, stream);
@@ -1103,8 +1108,8 @@ hipError_t launch(const FqAdaptersArgs &a, void *workspace, hipStream_t stream)
 FqAdaptersRoute fq_adapters_route(const FqAdaptersView &set, int M)
 {
     if (few(set, M))
-        return {1, 0, M * few_shares(set, M)};
-    return {0, M > MIDDLE_ROWS || set.slots > MIDDLE_SLOTS, tiles_of(set, M) * parts_of(set, M) * ((set.rank + low_ranks(set) - 1) / low_ranks(set))};
+        return {1, 0, M * few_shares(set, M), 0};
+    return {0, M > MIDDLE_ROWS || set.slots > MIDDLE_SLOTS, tiles_of(set, M) * parts_of(set, M) * ((set.rank + low_ranks(set) - 1) / low_ranks(set)), out_tiles(set, M)};
 }
 
 size_t fq_adapters_bytes(const FqAdaptersView &set, int M)

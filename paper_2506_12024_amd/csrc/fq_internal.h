@@ -282,9 +282,10 @@ struct FqAdaptersArgs {
     long long x_stride, y_stride, out_stride;
     int M;
 };
-// How a call of M rows runs: one launch, or several, behind one that sorts its rows by slot; workgroups of the one, or of the one that forms x A^T.
+// How a call of M rows runs: one launch, or several, behind one that sorts its rows by slot; workgroups of the one, or of the one that forms x A^T; tiles to a
+// row of the last one's grid.
 struct FqAdaptersRoute {
-    int few, listed, workgroups;
+    int few, listed, workgroups, out_tiles;
 };
 FqAdaptersRoute fq_adapters_route(const FqAdaptersView &set, int M);
 size_t fq_adapters_bytes(const FqAdaptersView &set, int M);
