@@ -88,12 +88,11 @@ int few_shares(const FqAdaptersView &set, int M)
 
 int tiles_of(const FqAdaptersView &set, int M) { return M / TILE + (M < set.slots + 1 ? M : set.slots + 1); } // at most
 
-// Tiles to a row of the last launch's grid.  With a multiple of 8 all of a tile's workgroups are on one XCD, and find the parts in its L2; but XCDs have unequal shares
-// of y and out, and one has all where a call names one slot; with an odd number they are on all XCDs.  (us with a multiple of 8 / odd: 701 rows of rank 16, N =
-// 4096 17.5 / 18.9, 8192 20.6 / 19.5; 2048 rows, 1024 18.5 / 21.4, 6144 25.3 / 25.9, 8200 31.5 / 30.7, 11008 42 / 37; 511 rows of 12 slots, 4096 -> 2048 12.2 / 12.6, of
-// one of them 11.0 / 12.6; 64 rows of one of 8 slots, 4096 -> 5120, rank 64 20.1 / 14.9, of all 13.6 / 12.9; 32 rows of one of 64 slots, 4096 -> 11008, rank 64
-// 32.3 / 14.6, of 32 27.9 / 28.1.)
-int out_tiles(const FqAdaptersView &set, int M) { return set.N <= 6144 && M > 64 ? (tiles_of(set, M) + 7) / 8 * 8 : tiles_of(set, M) | 1; }
+// Tiles to a row of the last launch's grid.  With a multiple of 8 all of a tile's workgroups are on one XCD, and find B and the parts in its L2; but XCDs have unequal
+// shares of y and out, and one has all where a call names one slot; with an odd number they are on all XCDs.  (us with a multiple of 8 / odd: 701 rows of rank 16, N =
+// 4096 17.5 / 18.9, 8192 20.6 / 19.5; 2048 rows, 1024 18.5 / 21.4, 6144 25.3 / 25.9, 8200 31.5 / 30.7, 11008 42 / 37; 24 rows of 24 slots of rank 128, 4096 -> 4096 23.6 / 27.0,
+// 64 of one of 64 25.2 / 23.1; 32 rows of one of 64 slots of rank 64, 4096 -> 11008 32.3 / 14.6, of 32 27.9 / 28.1, 4096 -> 5120 19.6 / 13.5 and 18.9 / 19.2.)
+int out_tiles(const FqAdaptersView &set, int M) { return set.N <= 6144 ? (tiles_of(set, M) + 7) / 8 * 8 : tiles_of(set, M) | 1; }
 
 // As many as there may well be, between what rows fill and that: the adapters of the rows are not known here.  (Against what rows fill: 300 rows of 200 slots, 4096 ->
 // 11008, rank 64 129 instead of 158 us, 1000 rows of 500 141 instead of 179.)
