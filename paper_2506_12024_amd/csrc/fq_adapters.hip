@@ -62,8 +62,14 @@ struct Work {
 
 // Whether a call is one launch: every workgroup of a tile reads its slot's A whole, which is less than another launch and the parts while A is
 // small, and the tiles of 16 rows suit many slots.  One launch / more (us on the device): 1 row, 4096 -> 4096, rank 16 7.1 / 8.4, rank 64 11.7 / 9.8; 32 rows of
-// 24 slots, 4096 -> 11008, rank 32 10.7 / 17.5, of 2 11.9 / 9.7; 64 of 64, 4096 -> 4096, rank 32 10.9 / 22.6, of 4 10.6 / 9.6, rank 64 17.8 / 28.4 and
-// 17.6 / 10.8; 128 of 64, rank 16 11.7 / 20.7, of 4 12.6 / 10.0, of 4 with 2048 outputs 9.7 / 10.4; 64 of 4, 4096 -> 11008, rank 16 14.6 / 9.7.
+// 24 slots, 4096 -> 11008, rank 32 10.7 / 17.5, of 2 11.9 / 9.7; 64 of 64, 4096 -> 4096, rank 32 10.9 / 22.6, of 4 10.6 / 9.6; 128 of 64, rank 16 11.7 / 20.7, of 4
+// 12.6 / 10.0, of 4 with 2048 outputs 9.7 / 10.4; 64 of 4, 4096 -> 11008, rank 16 14.6 / 9.7.  An A above 2^17 pays where many slots may be in the call, whose tiles, empty
+// or not, cost more launches most (all of a set's slots named, or one of them): with a tile's x up to 2^18 in rank 32, 5120 -> 5120, 16 rows of 16 slots 10.5 / 12.3,
+// 10.3 / 11.5, 32 of 32 11.8 / 15.0, 11.6 / 15.8, of 8 12.0 / 12.1, 11.4 / 12.7, 64 of 64 13.9 / 26.3, of 32 13.2 / 16.5, 12.9 / 15.5, of 16 14.0 / 13.1, 12.9 / 14.7; beyond
+// of nearly as many slots as rows: rank 16, 11008 -> 4096, 16 of 16 11.9 / 11.2, 11.5 / 10.2, 32 of 32 12.3 / 14.5, 12.0 / 14.6, 64 of 32 13.7 / 15.9, 13.7 / 13.4; rank 64,
+// 4096 -> 4096, 24 of 24 14.2 / 14.7, 13.5 / 12.4, 32 of 32 15.0 / 16.9, 14.0 / 17.9, 64 of 64 24.3 / 32.7, 15.7 / 19.7; with more than 6144 outputs (out_tiles) later:
+// rank 32, 8192 -> 8192, 32 of 32 15.3 / 20.4, 14.8 / 13.2, 48 of 64 19.6 / 31.4, 17.0 / 16.3, 64 of 64 21.3 / 39.5, 17.2 / 15.7, of 32 17.1 / 20.7, 17.2 / 14.1; rank 64,
+// 4096 -> 11008, 32 of 32 26.9 / 29.9, 18.1 / 15.1, 64 of 64 37.9 / 52.6, 24.1 / 18.2.
 bool few(const FqAdaptersView &set, int M)
 {
     const long long rank = set.rank < 16 ? 16 : set.rank, a = rank * set.K, b = rank * set.N; // (the instructions take 16)
@@ -71,8 +77,10 @@ bool few(const FqAdaptersView &set, int M)
         return false;
     if (8 * (set.slots + 1) <= M) // many rows of a slot
         return a <= 1 << 17 && M * (a + b) <= 3 << 22;
+    const int named = M < set.slots ? M : set.slots; // slots that the call may name
     if (M <= 64)
-        return a <= 1 << 17 || (a <= 1 << 18 && M > 32 && set.slots > 32);
+        return a <= 1 << 17 || (a + 16 * set.K <= 1 << 18 && named >= 16 && 2 * named >= M) ||
+               (a <= 1 << 18 && named >= (set.N <= 6144 ? 28 : 40) && 5 * named >= 4 * M);
     return a + b <= 1 << 18 && set.N <= 8192;
 }
 

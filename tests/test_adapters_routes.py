@@ -44,3 +44,30 @@ def test_a_tile_is_on_one_chiplet_only_where_that_pays(rank):
                 most = M // 64 + min(M, slots + 1)
                 assert not few and most <= tiles < most + 8
                 assert tiles % 8 == 0 if N <= 6144 else tiles % 2 == 1, (M, slots, N)
+
+
+@pytest.mark.parametrize("K,N,rank", [(5120, 5120, 32), (5120, 13824, 32), (3200, 4096, 64)])
+def test_decode_batches_of_many_slots_are_one_launch(K, N, rank):
+    """A and a tile's x together up to 2^18 values: sets whose slots may give most rows a tile of their own."""
+    for M, slots in ((16, 16), (24, 64), (32, 16), (32, 32), (32, 64), (40, 1000), (64, 32), (64, 64)):
+        assert route(M, K, N, slots, rank)[0], (M, slots)
+    for M, slots in ((1, 64), (8, 64), (32, 8), (64, 8), (64, 31)):
+        assert not route(M, K, N, slots, rank)[0], (M, slots)
+
+
+@pytest.mark.parametrize("K,rank", [(11008, 16), (14336, 16), (8192, 32), (4096, 64)])
+def test_decode_batches_of_nearly_as_many_slots_as_rows_are_one_launch(K, rank):
+    """Up to 2^18 values of A."""
+    for M, slots in ((28, 28), (32, 32), (32, 1000), (40, 32), (64, 52), (64, 64)):
+        assert route(M, K, 4096, slots, rank)[0], (M, slots)
+        assert route(M, K, 8192, slots, rank)[0] == (min(M, slots) >= 40), (M, slots)
+    for M, slots in ((1, 64), (16, 64), (27, 64), (32, 16), (64, 32), (64, 51)):
+        assert not route(M, K, 4096, slots, rank)[0], (M, slots)
+
+
+@pytest.mark.parametrize("M,K,N,rank,slots,few", [
+    (16, 5456, 4096, 32, 16, 1), (16, 5464, 4096, 32, 16, 0), (32, 5456, 9000, 32, 16, 1), (33, 5456, 4096, 32, 16, 0), (15, 5456, 9000, 32, 64, 0),
+    (28, 8192, 6144, 32, 28, 1), (39, 8192, 6145, 32, 64, 0), (40, 8192, 6145, 32, 40, 1), (64, 8200, 4096, 32, 64, 0),
+    (1, 8192, 4096, 16, 1, 1), (64, 4096, 4096, 32, 8, 1), (256, 4096, 4096, 16, 64, 1), (257, 4096, 4096, 16, 64, 0), (1, 64, 4096, 72, 1, 0)])
+def test_where_one_launch_ends(M, K, N, rank, slots, few):
+    assert route(M, K, N, slots, rank)[0] == few
