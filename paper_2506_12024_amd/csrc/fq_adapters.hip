@@ -501,9 +501,8 @@ struct Out {
     }
 
     // Infinities of B meet hi alone, whose product has u's sign: lo may be 0 or of the other sign, and would make NaN of them.  (A u that is 2^-38 of its row's
-    // largest or less has a hi of 0 in binary16.)  What other calls pay for it: with TILE rows a look at B while it lies in LDS (a prompt of 2048, 8192 -> 8192, rank
-    // 64 42.5 to 43.1 us, others nothing); with FEW_TILE, where that is 0.2 to 0.6 us, a look at the sums, and where they are not all numbers a second walk (0 to
-    // 0.2 us; in out_kernel 2 %).
+    // largest or less has a hi of 0 in binary16.)  SOUGHT: B is looked at while it lies in LDS, which costs out_kernel nothing, few_kernel 0.1 to 0.3 us of 5 to 10;
+    // IGNORED: its sums are looked at, and where they are not all numbers the rest is walked APART (few_kernel up to rank 32 0 to 0.1 us, of rank 64 0.1 to 2 of 30).
     enum Infinities { SOUGHT, IGNORED, APART };
     template <Infinities B>
     __device__ __forceinline__ void multiply(float4_t (&acc)[TT][4], u32x4 (&v)[4], int c) const
@@ -542,7 +541,13 @@ struct Out {
 #pragma unroll
             for (int j = 0; j < 4; j++)
                 acc[t][j] = mfma<BF16>(hi, bv[j], acc[t][j]);
+            if (B == IGNORED)
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    acc[t][j] = mfma<BF16>(lo[t], bv[j], acc[t][j]);
         }
+        if (B == IGNORED)
+            return;
         if (__builtin_expect(infinite, B == APART))
             without_infinities(bv);
 #pragma unroll
@@ -617,15 +622,15 @@ struct Out {
 
     static __device__ __forceinline__ bool all_numbers(const float4_t (&acc)[TT][4])
     {
-        float zero[4] = {};
+        float most[2] = {}; // (a maximum that is NaN where one of its operands is)
 #pragma unroll
         for (int t = 0; t < TT; t++)
 #pragma unroll
             for (int j = 0; j < 4; j++)
 #pragma unroll
                 for (int i = 0; i < 4; i++)
-                    zero[i] = fmaf(acc[t][j][i], 0.0f, zero[i]);
-        return (zero[0] + zero[1]) + (zero[2] + zero[3]) == 0.0f;
+                    most[j & 1] = __builtin_elementwise_maximum(most[j & 1], fabsf(acc[t][j][i]));
+        return __builtin_elementwise_maximum(most[0], most[1]) < INFINITY;
     }
 
     // The blocks first, first + stride ...; k: what was asked for the first, if it was.  (A turn ahead in registers would cost half of the wavefronts, which hide
@@ -647,6 +652,9 @@ struct Out {
                 ask_b(v, block, c);
                 multiply<B>(acc, v, c);
             }
+            // vmcnt(0): y is here before the first store, behind which a wait for the rest of it would be one for the store (64 rows of 8 slots, 1024 -> 28672, rank
+            // 16 25.6 to 22.9 us; the 2048 rows 43.8 to 43.3)
+            __builtin_amdgcn_s_waitcnt(0x0f70);
             if (B == IGNORED && __ballot(!all_numbers(acc)))
                 break;
             finish(k, acc, block);
@@ -656,7 +664,7 @@ struct Out {
 
     __device__ __forceinline__ void run(Turn &k, int first, int stride) const
     {
-        if (TT > 1) {
+        if (TT > 1 || AHEAD > 1) {
             walk<SOUGHT>(k, first, stride);
         } else {
             const int block = walk<IGNORED>(k, first, stride);
