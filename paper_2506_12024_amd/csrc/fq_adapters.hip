@@ -29,6 +29,11 @@ namespace {
 constexpr int THREADS = 256, WAVES = THREADS / 64;
 constexpr int FEW_ROWS = 256, FEW_TILE = 16, TILE = 64;
 constexpr int MIDDLE_ROWS = 4096, MIDDLE_SLOTS = 1023;
+// With more workgroups of the first launch than these, one that sorts the rows goes ahead of it: each that counts the rows for itself, those without a tile, too, takes 3.5
+// to 5 us for that, behind a list one read.  (4 slots named, us counted / sorted: 257 rows, 4096 -> 4096, rank 16, of a set of 32 13.4 / 14.4, of 300 27.0 / 18.8; 700 of 50
+// 20.4 / 20.7, of 100 20.6 / 19.0, of 1000 74 / 27; 2048 of 100 22.9 / 24.8, of 300 30.2 / 26.9; 257 rows, 4096 -> 1024, rank 256, of 1000 141 / 39.  Over 2300 shapes this choice
+// is 0.3 % from the better, 1500 0.7, 512 0.9.)
+constexpr int COUNTING = 1024;
 constexpr int GROUP_THREADS = 1024, OUT_THREADS = 512, MANY_THREADS = 256, JOIN_THREADS = 256, JOIN_ROWS = JOIN_THREADS / 16;
 constexpr int CHUNK = 256, MAX_PARTS = 16; // of K
 enum Find { COUNTED, LISTED }; // how a workgroup of low_kernel finds its tile: by itself, or in the workspace's list
@@ -1124,7 +1129,8 @@ FqAdaptersRoute fq_adapters_route(const FqAdaptersView &set, int M)
 {
     if (few(set, M))
         return {1, 0, M * few_shares(set, M), 0};
-    return {0, M > MIDDLE_ROWS || set.slots > MIDDLE_SLOTS, tiles_of(set, M) * parts_of(set, M) * ((set.rank + low_ranks(set) - 1) / low_ranks(set)), out_tiles(set, M)};
+    const int groups = tiles_of(set, M) * parts_of(set, M) * ((set.rank + low_ranks(set) - 1) / low_ranks(set));
+    return {0, M > MIDDLE_ROWS || set.slots > MIDDLE_SLOTS || groups > COUNTING, groups, out_tiles(set, M)};
 }
 
 size_t fq_adapters_bytes(const FqAdaptersView &set, int M)

@@ -71,3 +71,12 @@ def test_decode_batches_of_nearly_as_many_slots_as_rows_are_one_launch(K, rank):
     (1, 8192, 4096, 16, 1, 1), (64, 4096, 4096, 32, 8, 1), (256, 4096, 4096, 16, 64, 1), (257, 4096, 4096, 16, 64, 0), (1, 64, 4096, 72, 1, 0)])
 def test_where_one_launch_ends(M, K, N, rank, slots, few):
     assert route(M, K, N, slots, rank)[0] == few
+
+
+@pytest.mark.parametrize("M,K,N,slots,rank,listed", [
+    (701, 11008, 4096, 12, 16, 0), (2048, 8192, 8192, 4, 64, 0), (300, 4096, 4096, 32, 16, 0), (4096, 4096, 4096, 64, 16, 0), (10, 4096, 4096, 1000, 128, 0),
+    # sets of many slots, of which a call may name a few: most workgroups have no tile
+    (701, 4096, 4096, 1000, 16, 1), (257, 4096, 4096, 300, 16, 1), (257, 4096, 1024, 300, 256, 1), (4096, 4096, 4096, 1000, 16, 1), (100, 4096, 4096, 64, 256, 1),
+    (2048, 4096, 4096, 300, 16, 1), (64, 4096, 4096, 1000, 128, 1), (4097, 64, 64, 1, 16, 1), (300, 64, 64, 1024, 16, 1)])
+def test_many_workgroups_find_their_rows_in_a_list(M, K, N, slots, rank, listed):
+    assert route(M, K, N, slots, rank)[:2] == (0, listed)

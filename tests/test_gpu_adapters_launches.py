@@ -11,9 +11,11 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 F16 = torch.float16
 # M, K, N, slots, rank: rows counted by every workgroup, parts of x A^T added by every workgroup of the last launch; the same where rows of y are not
-# aligned to 8 bytes; parts added by a launch of their own, for ranks up to 64 and beyond; rows sorted by a launch of their own
+# aligned to 8 bytes; parts added by a launch of their own, for ranks up to 64 and beyond; rows sorted by a launch of their own, of sets of many slots and in calls
+# whose set and rank give many workgroups
 ROUTES = {"all_add": (300, 136, 72, 4, 16), "odd": (300, 264, 61, 5, 24), "join_64": (300, 4096, 5504, 4, 64), "join_136": (300, 2056, 72, 4, 136),
-          "sorted": (300, 136, 72, 1100, 16), "many_rows": (4200, 72, 40, 6, 32)}
+          "sorted": (300, 136, 72, 1100, 16), "many_rows": (4200, 72, 40, 6, 32),
+          "sorted_few": (64, 4096, 72, 64, 128)}
 routes = pytest.mark.parametrize("route", sorted(ROUTES))
 
 
