@@ -609,8 +609,9 @@ int fq_kv_append_normed(const fq_kv *kv, const fq_seqs *seqs, int tokens, const 
  *   given_logprob[r][j] = ln p[given[r][j]];  -inf for a token outside 0 .. V - 1
  *   top_token[r][i], top_logprob[r][i]: the i-th of the order; -1 and -inf where the row has no more tokens with weight
  * A NaN logit counts as -inf.  With +inf in a row only the +inf entries have weight, 1 each.  A row of nothing else than -inf gives
- * -inf, -1 and an entropy of 0.  Exponentials and a thread's sums in binary32, joined in binary64; the largest logit's own weight
- * stays out of the sums, ln p of a token that is nearly certain keeps its digits (ln p = (l - max) - log1p(sum of the others)).
+ * -inf, -1 and an entropy of 0.  Exponentials, a thread's sums and those of sixteen threads in binary32, joined in binary64; the
+ * largest logit's own weight stays out of the sums, ln p of a token that is nearly certain keeps its digits (ln p = (l - max) -
+ * log1p(sum of the others)).
  *   logits         device, f32 (or fp16: fq_logprobs_f16) [R][V], rows row_stride elements apart (row_stride >= V; any alignment
  *                  that the type has)                                                            (read)
  *   given          device, int32 [R][n_given], or NULL with n_given = 0                          (read)

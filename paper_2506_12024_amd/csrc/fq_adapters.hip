@@ -995,7 +995,7 @@ __global__ __launch_bounds__(OUT_THREADS, 4) void few_kernel(FqAdaptersArgs a)
     for (int r = 0; r < RT; r++)
         ((float4_t *)lds[wave])[64 * r + lane] = acc[r];
     __syncthreads();
-    // four ranks to a thread, 8 RT threads (those of whole instructions) to a row
+    // four ranks to a thread, the threads of whole instructions (32 ranks) to a row
     constexpr int WIDE = RT == 1 ? 8 : 4 * RT;
     const int row = tid / WIDE, r = 4 * (tid % WIDE);
     if (row < FEW_TILE) {

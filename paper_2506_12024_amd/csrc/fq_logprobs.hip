@@ -102,7 +102,7 @@ __device__ __forceinline__ float lane_of(float x, int lane)
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
 }
 
-// Sums over the lanes of a wavefront.
+// Sums over the lanes of a wavefront; of binary32 numbers those of sixteen lanes in binary32 (four roundings, as a thread's own sums have more), the four in binary64.
 __device__ __forceinline__ double wave_sum(float x)
 {
     auto step = [](float v, auto ctrl) {
