@@ -3,13 +3,13 @@
 // Both products are on the matrix cores.  u = x A^T is a binary32 sum, and meets B as two 16-bit numbers each, u = hi + lo (binary16: 22
 // bits of it, a row scaled by a power of two so that its largest fills the range; bfloat16: 17), so that it is nowhere rounded to
 // 16 bits.  A tile is up to 16 or 64 rows of one slot, wherever in the call they stand: a row's sums do not depend on its place in a
-// tile.  Few rows are one launch (few_kernel), whose workgroups form u for themselves; many are two or three: low_kernel forms u in parts of K, which lie in
+// tile.  Few rows are one launch (few_kernel), whose workgroups form u for themselves; many are two to four: low_kernel forms u in parts of K, which lie in
 // the workspace; out_kernel adds them up, parts them into hi and lo and multiplies by B, or join_kernel does the first where each of its workgroups
-// would have much to add.
+// would have much to add; group_kernel sorts the rows ahead of them where the workgroups of low_kernel are too many to count them each.
 //
-// What bounds it: a token (4096 -> 4096, rank 16) 7.1 us a call from Python, of which the host takes 6.6 and the device as much: four trips to memory one
+// What bounds it: a token (4096 -> 4096, rank 16) 7.2 us a call from Python, of which the host takes 6.7 and the device as much: four trips to memory one
 // after another, launch, the exchange through LDS; 32 rows of 24 slots (4096 -> 11008, rank 32) 11.3 us, A and B once 3.3, A read again by every workgroup
-// of a tile.  701 rows, chunks and single tokens (11008 -> 4096, rank 16) 17.8 us, low_kernel 9.2 (3.5 until it knows its rows), out_kernel 9.5, everything once 6.0.
+// of a tile.  701 rows, chunks and single tokens (11008 -> 4096, rank 16) 17.8 us, low_kernel 9.6 (3.5 until it knows its rows), out_kernel 9.1, everything once 6.0.
 // A prompt of 2048 rows (8192 -> 8192, rank 64, bfloat16) 42 us, of which low_kernel has 19 (4.6 until it knows its rows, then x at 2/3 of the
 // rate of a large copy), join_kernel 5, out_kernel 19 (67 MB of y and out, 3.5 TB/s); everything once at 5.2 TB/s would be 20.
 //
